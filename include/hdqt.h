@@ -370,6 +370,94 @@ typedef struct hdqt_ws_layout {
 hdqt_status_t hdqt_workspace_layout(const hdqt_gemm_desc_t* desc /*host*/, int64_t M,
                                     int64_t N, int64_t K, hdqt_ws_layout_t* out /*host*/);
 
+/* ------------------------------------------------------------------------ */
+/* The rest of a training step: operators around the quantized products       */
+/* (Section 3 quantizes the inputs and accumulators of matrix products only:   */
+/* normalisation, loss and gradient clipping stay in floating point)           */
+/* ------------------------------------------------------------------------ */
+
+/* element types of the operators below; statistics, sums and scales are fp32 or wider whatever the type */
+typedef enum {
+  HDQT_DTYPE_F32 = 0,
+  HDQT_DTYPE_BF16 = 1,
+  HDQT_DTYPE_F16 = 2
+} hdqt_dtype_t;
+
+/* One tensor of a list: `numel` elements of `dtype` (hdqt_dtype_t) at src, read; written to dst, which may equal src
+ * but must not overlap any source otherwise.  Elements are dense; the base needs the element's own alignment only
+ * (16 bytes, the same for both, selects the vector path).  numel may be 0 (the pointers are then not looked at). */
+typedef struct hdqt_tensor {
+  const void* src;
+  void* dst;
+  int64_t numel;
+  int64_t dtype;
+} hdqt_tensor_t;
+
+#define HDQT_NORM_L2 2
+#define HDQT_NORM_INF 0
+
+/*
+ * Global norm over all elements of `count` tensors, and clipping by it:
+ *
+ *   norm = sqrt(sum x^2)  (HDQT_NORM_L2)   or   max |x|  (HDQT_NORM_INF)
+ *   dst  = src * min(1, max_norm / (norm + 1e-6)),   rounded once to the tensor's type
+ *
+ * norm_out: device fp32 scalar.  Per-thread sums are fp32, everything above fp64, joined in a fixed order (the result does not
+ * depend on scheduling).  A NaN anywhere makes the norm NaN and, for the clipping call, every element NaN; an infinity makes
+ * the factor 0.  With a factor of 1 tensors whose dst equals src are left untouched (x * 1 = x).
+ * `tensors` is a HOST array, read before the call returns.  max_norm >= 0.  count may be 0 (norm 0).
+ * workspace: hdqt_grad_norm_workspace_bytes(count) bytes, 128-byte aligned.
+ */
+hdqt_status_t hdqt_grad_norm(const hdqt_tensor_t* tensors /*host*/, int64_t count, int32_t norm_type, float* norm_out,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+hdqt_status_t hdqt_clip_grad_norm(const hdqt_tensor_t* tensors /*host*/, int64_t count, int32_t norm_type,
+                                  float max_norm, float* norm_out, void* workspace, size_t workspace_bytes,
+                                  void* stream);
+
+size_t hdqt_grad_norm_workspace_bytes(int64_t count);
+
+/*
+ * Group norm with an activation on channels-last activations x[batch, pixels, channels] (the layout of hdqt_conv2d_*;
+ * pixels = height * width):
+ *
+ *   mu, rs = mean and 1/sqrt(variance + eps) over the pixels and the channels/groups channels of a group
+ *   z = gamma[c] * (x - mu) * rs + beta[c],   y = act(z)
+ *
+ * backward, dz = dy * act'(z) (ReLU's derivative at 0 is 0):
+ *   dgamma[c] = sum dz * xhat,  dbeta[c] = sum dz   over batch and pixels
+ *   dx = rs * (gamma dz - mean(gamma dz) - xhat * mean(gamma dz * xhat)),   means over the group
+ *
+ * Pixel p of image b of x starts at x + b*x_batch_stride + p*x_pixel_stride (elements; pixel stride >= channels,
+ * batch stride >= pixels*pixel stride unless batch is 1): a channel slice of a wider tensor needs no copy.  y, dy and
+ * dx have the strides y_batch_stride, y_pixel_stride.  16-byte alignment of bases and strides selects wider accesses.
+ * gamma, beta (and dgamma, dbeta): [channels] of param_dtype, which is fp32 or x's type; NULL gamma/beta = ones/zeros.
+ * mean, rstd: fp32 [batch, groups], written by the forward call and read by the backward call.
+ * batch or pixels may be 0: nothing but zero dgamma/dbeta is written then (mean and rstd of images without pixels are NaN).
+ * workspace: hdqt_group_norm_workspace_bytes(desc, backward) bytes, 256-byte aligned.
+ */
+typedef enum { HDQT_ACT_NONE = 0, HDQT_ACT_RELU = 1, HDQT_ACT_SILU = 2 } hdqt_act_t;
+
+typedef struct hdqt_group_norm_desc {
+  int64_t batch, pixels, channels, groups;
+  int64_t x_batch_stride, x_pixel_stride; /* of x          */
+  int64_t y_batch_stride, y_pixel_stride; /* of y, dy, dx  */
+  int32_t dtype, param_dtype; /* hdqt_dtype_t */
+  int32_t act;                /* hdqt_act_t   */
+  float eps;                  /* >= 0         */
+} hdqt_group_norm_desc_t;
+
+hdqt_status_t hdqt_group_norm_fwd(const hdqt_group_norm_desc_t* desc /*host*/, const void* x, const void* gamma,
+                                  const void* beta, void* y, float* mean, float* rstd, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
+/* dgamma and dbeta may be NULL (not needed); dx may be NULL as well. */
+hdqt_status_t hdqt_group_norm_bwd(const hdqt_group_norm_desc_t* desc /*host*/, const void* dy, const void* x,
+                                  const void* gamma, const void* beta, const float* mean, const float* rstd, void* dx,
+                                  void* dgamma, void* dbeta, void* workspace, size_t workspace_bytes, void* stream);
+
+size_t hdqt_group_norm_workspace_bytes(const hdqt_group_norm_desc_t* desc /*host*/, int32_t backward);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,7 +11,7 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libhdqt.so")
-SOURCES = ["hdqt_api.cu", "hdqt_quant.cu", "hdqt_gemm.cu"]
+SOURCES = ["hdqt_api.cu", "hdqt_quant.cu", "hdqt_gemm.cu", "hdqt_clip.cu", "hdqt_norm.cu"]
 
 
 def nvcc_path() -> str:
@@ -53,7 +53,7 @@ def needs_rebuild() -> bool:
 
 def _compile(out_path: str, defines=(), verbose: bool = False) -> None:
     cmd = [nvcc_path(), "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++20", "-lineinfo",
-           "-Xcompiler", "-fPIC", "-shared", "-cudart", "static",
+           "-Xcompiler", "-fPIC", "-shared", "-cudart", "static", "--threads", "0",
            "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     cmd += [f"-D{d}" for d in defines]
     if verbose:

@@ -1,0 +1,53 @@
+// Element types of the floating-point operators: conversions to and from fp32 and vector accesses.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "hdqt_common.cuh"
+
+namespace hdqt {
+
+template <typename T>
+__device__ __forceinline__ float to_f32(T v);
+template <>
+__device__ __forceinline__ float to_f32<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <>
+__device__ __forceinline__ float to_f32<__half>(__half v) { return __half2float(v); }
+
+// one rounding, ties to even
+template <typename T>
+__device__ __forceinline__ T from_f32(float v);
+template <>
+__device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <>
+__device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+
+// N elements of T as one access; the address must be aligned to sizeof(Vec)
+template <typename T, int N>
+struct alignas(sizeof(T) * N) Vec {
+  T v[N];
+};
+
+// Element i of a parameter vector whose type is known at run time only.  Plain loads: the 16-bit forms of __ldg are
+// inline assembly that the compiler may execute ahead of the test that guards it, and a pointer may be null behind such a test.
+__device__ __forceinline__ float load_param(const void* p, int32_t dtype, int64_t i) {
+  if (dtype == HDQT_DTYPE_F32) return reinterpret_cast<const float*>(p)[i];
+  if (dtype == HDQT_DTYPE_BF16) return to_f32(reinterpret_cast<const __nv_bfloat16*>(p)[i]);
+  return to_f32(reinterpret_cast<const __half*>(p)[i]);
+}
+__device__ __forceinline__ void store_param(void* p, int32_t dtype, int64_t i, float v) {
+  if (dtype == HDQT_DTYPE_F32) reinterpret_cast<float*>(p)[i] = v;
+  else if (dtype == HDQT_DTYPE_BF16) reinterpret_cast<__nv_bfloat16*>(p)[i] = from_f32<__nv_bfloat16>(v);
+  else reinterpret_cast<__half*>(p)[i] = from_f32<__half>(v);
+}
+
+inline int dtype_size(int64_t dtype) {   // 0 = unknown type
+  return dtype == HDQT_DTYPE_F32 ? 4 : (dtype == HDQT_DTYPE_BF16 || dtype == HDQT_DTYPE_F16) ? 2 : 0;
+}
+
+}  // namespace hdqt

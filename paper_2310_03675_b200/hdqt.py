@@ -20,6 +20,9 @@ FLAG_NO_MERGE = 1
 FLAG_NO_SPLIT_K = 2
 FLAG_RELU = 4
 AMAX_HISTORY_WORDS = 1024
+DTYPE_CODES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # hdqt_dtype_t
+ACT_CODES = {"none": 0, "relu": 1, "silu": 2}                           # hdqt_act_t
+NORM_CODES = {2.0: 2, float("inf"): 0}                                  # HDQT_NORM_*
 
 STATUS_NAMES = ["OK", "INVALID_ARG", "UNSUPPORTED", "ALIGNMENT", "WORKSPACE", "NONFINITE", "TIMEOUT", "CUDA",
                 "STATIC_SCRATCH"]
@@ -30,6 +33,8 @@ EXPORTED = [
     "hdqt_gemm_i8_workspace_bytes", "hdqt_calibrate_acc_shift", "hdqt_gemm_fwd", "hdqt_gemm_dgrad",
     "hdqt_gemm_wgrad", "hdqt_workspace_bytes", "hdqt_workspace_layout", "hdqt_quantize_hadamard_static",
     "hdqt_selftest_bounded_wait", "hdqt_conv2d_fwd", "hdqt_conv2d_wgrad", "hdqt_selftest_mma_rate",
+    "hdqt_grad_norm", "hdqt_clip_grad_norm", "hdqt_grad_norm_workspace_bytes",
+    "hdqt_group_norm_fwd", "hdqt_group_norm_bwd", "hdqt_group_norm_workspace_bytes",
 ]
 
 
@@ -51,6 +56,13 @@ class Conv2dGeom(C.Structure):
     """Mirror of hdqt_conv2d_geom_t."""
     _fields_ = [("batch", C.c_int64), ("height", C.c_int64), ("width", C.c_int64), ("channels", C.c_int64),
                 ("kernel_h", C.c_int32), ("kernel_w", C.c_int32), ("stride", C.c_int32), ("padding", C.c_int32)]
+
+
+class GroupNormDesc(C.Structure):
+    """Mirror of hdqt_group_norm_desc_t."""
+    _fields_ = [(n, C.c_int64) for n in ("batch", "pixels", "channels", "groups", "x_batch_stride", "x_pixel_stride",
+                                         "y_batch_stride", "y_pixel_stride")] + \
+               [("dtype", C.c_int32), ("param_dtype", C.c_int32), ("act", C.c_int32), ("eps", C.c_float)]
 
 
 class WsLayout(C.Structure):
@@ -100,6 +112,16 @@ def _load() -> C.CDLL:
     lib.hdqt_selftest_bounded_wait.restype = C.c_int
     for name in ("hdqt_conv2d_fwd", "hdqt_conv2d_wgrad"):
         getattr(lib, name).argtypes = [C.POINTER(GemmDesc), C.POINTER(Conv2dGeom), vp, vp, vp, i64, vp, sz, vp, vp]
+        getattr(lib, name).restype = C.c_int
+    lib.hdqt_grad_norm.argtypes = [vp, i64, i32, vp, vp, sz, vp]
+    lib.hdqt_clip_grad_norm.argtypes = [vp, i64, i32, f32, vp, vp, sz, vp]
+    lib.hdqt_grad_norm_workspace_bytes.argtypes = [i64]
+    lib.hdqt_grad_norm_workspace_bytes.restype = sz
+    lib.hdqt_group_norm_fwd.argtypes = [C.POINTER(GroupNormDesc), vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.hdqt_group_norm_bwd.argtypes = [C.POINTER(GroupNormDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.hdqt_group_norm_workspace_bytes.argtypes = [C.POINTER(GroupNormDesc), i32]
+    lib.hdqt_group_norm_workspace_bytes.restype = sz
+    for name in ("hdqt_grad_norm", "hdqt_clip_grad_norm", "hdqt_group_norm_fwd", "hdqt_group_norm_bwd"):
         getattr(lib, name).restype = C.c_int
     lib.hdqt_workspace_bytes.argtypes = [C.POINTER(GemmDesc), i64, i64, i64]
     lib.hdqt_workspace_bytes.restype = sz
@@ -433,3 +455,147 @@ def mma_rate_tops(iters: int = 20000, repeats: int = 3, dev_status=None) -> floa
         torch.cuda.synchronize()
         best = max(best, ops.value / (e0.elapsed_time(e1) * 1e-3) / 1e12)
     return best
+
+
+# ---- the rest of a training step: gradient clipping, group norm --------------------------------------
+
+def _tensor_table(tensors, out):
+    """hdqt_tensor_t[len(tensors)] as a flat int64 array (source, destination, elements, type)."""
+    flat = []
+    dev = None
+    for i, t in enumerate(tensors):
+        code = DTYPE_CODES.get(t.dtype)
+        if code is None or not t.is_cuda or not t.is_contiguous():
+            raise ValueError(f"tensor {i}: expected a dense fp32, bf16 or fp16 CUDA tensor")
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            raise ValueError("the tensors must be on one device")
+        at = t.data_ptr()
+        flat += (at, at, t.numel(), code)
+    if out is not None:
+        if len(out) != len(tensors):
+            raise ValueError("out must hold one tensor per input")
+        for i, (t, o) in enumerate(zip(tensors, out)):
+            if o.dtype != t.dtype or o.shape != t.shape or o.device != t.device or not o.is_contiguous():
+                raise ValueError(f"out[{i}] must be a dense tensor of the type and shape of its input")
+            flat[4 * i + 1] = o.data_ptr()
+    return (C.c_int64 * len(flat))(*flat), dev
+
+
+def _norm_code(norm_type) -> int:
+    code = NORM_CODES.get(float(norm_type))
+    if code is None:
+        raise ValueError("norm_type must be 2 or inf")
+    return code
+
+
+def grad_norm(tensors, norm_type: float = 2.0, device=None) -> torch.Tensor:
+    """Norm over all elements of a list of dense fp32 / bf16 / fp16 tensors (types may be mixed), as an fp32 scalar
+    tensor: 2 = Euclidean, inf = largest magnitude.  `device` is needed for an empty list only."""
+    tensors = list(tensors)
+    code = _norm_code(norm_type)
+    table, dev = _tensor_table(tensors, None)
+    norm = torch.empty((), dtype=torch.float32, device=dev if dev is not None else device or "cuda")
+    ws = torch.empty(lib.hdqt_grad_norm_workspace_bytes(len(tensors)), dtype=torch.uint8, device=norm.device)
+    _check(lib.hdqt_grad_norm(C.addressof(table), len(tensors), code, norm.data_ptr(), ws.data_ptr(), ws.numel(),
+                              _stream()), "hdqt_grad_norm")
+    return norm
+
+
+def clip_grad_norm(tensors, max_norm: float, norm_type: float = 2.0, out=None, device=None) -> torch.Tensor:
+    """Scales the tensors by min(1, max_norm / (norm + 1e-6)), in place or into the tensors of `out`, and returns the
+    norm they had (see grad_norm).  Nothing synchronises the host; the call can be recorded into a CUDA graph."""
+    tensors = list(tensors)
+    code = _norm_code(norm_type)
+    table, dev = _tensor_table(tensors, None if out is None else list(out))
+    norm = torch.empty((), dtype=torch.float32, device=dev if dev is not None else device or "cuda")
+    ws = torch.empty(lib.hdqt_grad_norm_workspace_bytes(len(tensors)), dtype=torch.uint8, device=norm.device)
+    _check(lib.hdqt_clip_grad_norm(C.addressof(table), len(tensors), code, max_norm, norm.data_ptr(), ws.data_ptr(),
+                                   ws.numel(), _stream()), "hdqt_clip_grad_norm")
+    return norm
+
+
+def _pixel_strides(t: torch.Tensor, name: str):
+    """(batch stride, pixel stride) of a [batch, ..., channels] tensor whose inner dimensions step evenly."""
+    shape, st = t.shape, t.stride()
+    if len(shape) < 2:
+        raise ValueError(f"{name} must be [batch, ..., channels]")
+    if st[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"{name} must have its channels contiguous")
+    pixel, step = None, 0
+    for size, stride in zip(shape[-2:0:-1], st[-2:0:-1]):      # pixel dimensions, innermost first
+        if size == 1:
+            continue
+        if pixel is None:
+            pixel = stride
+        elif stride != step:
+            raise ValueError(f"the pixels of {name} must be evenly spaced")
+        step = stride * size
+    if pixel is None:
+        pixel = shape[-1]
+        step = pixel
+    batch = st[0] if shape[0] > 1 else step
+    return batch, pixel
+
+
+def _group_norm_desc(x, gamma, beta, groups: int, eps: float, act: str):
+    code = DTYPE_CODES.get(x.dtype)
+    if code is None or not x.is_cuda:
+        raise ValueError("expected an fp32, bf16 or fp16 CUDA tensor")
+    if act not in ACT_CODES:
+        raise ValueError(f"act must be one of {sorted(ACT_CODES)}")
+    channels = x.shape[-1]
+    pdt = x.dtype
+    for t in (gamma, beta):
+        if t is None:
+            continue
+        if t.shape != (channels,) or not t.is_contiguous() or t.device != x.device:
+            raise ValueError("gamma and beta must be dense [channels] tensors on x's device")
+        pdt = t.dtype
+    if gamma is not None and beta is not None and gamma.dtype != beta.dtype:
+        raise ValueError("gamma and beta must have one type")
+    if pdt not in (torch.float32, x.dtype):
+        raise ValueError("gamma and beta must be fp32 or of x's type")
+    pixels = 1
+    for n in x.shape[1:-1]:
+        pixels *= n
+    d = GroupNormDesc(x.shape[0], pixels, channels, groups, 0, 0, pixels * channels, channels, code, DTYPE_CODES[pdt],
+                      ACT_CODES[act], eps)
+    d.x_batch_stride, d.x_pixel_stride = _pixel_strides(x, "x")
+    return d
+
+
+def group_norm_fwd(x, gamma, beta, groups: int, eps: float = 1e-5, act: str = "none"):
+    """act(group norm) of x[batch, ..., channels] (channels last, evenly spaced pixels: a channel slice is fine).
+    gamma, beta: [channels], fp32 or x's type, or None.  act: "none", "relu" or "silu".
+    Returns (y dense, mean fp32 [batch, groups], rstd fp32 [batch, groups])."""
+    d = _group_norm_desc(x, gamma, beta, groups, eps, act)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    stats = torch.empty((2, d.batch, max(groups, 0)), dtype=torch.float32, device=x.device)
+    mean, rstd = stats[0], stats[1]
+    ws = torch.empty(max(256, lib.hdqt_group_norm_workspace_bytes(C.byref(d), 0)), dtype=torch.uint8, device=x.device)
+    _check(lib.hdqt_group_norm_fwd(C.byref(d), x.data_ptr(), _ptr(gamma), _ptr(beta), y.data_ptr(),
+                                   stats.data_ptr(), stats.data_ptr() + 4 * mean.numel(), ws.data_ptr(), ws.numel(),
+                                   _stream()), "hdqt_group_norm_fwd")
+    return y, mean, rstd
+
+
+def group_norm_bwd(dy, x, gamma, beta, mean, rstd, groups: int, act: str = "none", want_dx: bool = True,
+                   want_params: bool = True):
+    """Gradients of group_norm_fwd: (dx dense or None, dgamma or None, dbeta or None)."""
+    d = _group_norm_desc(x, gamma, beta, groups, 0.0, act)
+    if dy.shape != x.shape or dy.dtype != x.dtype or dy.device != x.device:
+        raise ValueError("dy must have x's shape, type and device")
+    if tuple(mean.shape) != (d.batch, groups) or mean.shape != rstd.shape or mean.dtype != torch.float32 \
+            or rstd.dtype != torch.float32 or not (mean.is_contiguous() and rstd.is_contiguous()):
+        raise ValueError("mean and rstd must be the dense fp32 [batch, groups] tensors of the forward call")
+    dy = dy.contiguous()
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_dx else None
+    dgamma = torch.empty_like(gamma) if want_params and gamma is not None else None
+    dbeta = torch.empty_like(beta) if want_params and beta is not None else None
+    ws = torch.empty(max(256, lib.hdqt_group_norm_workspace_bytes(C.byref(d), 1)), dtype=torch.uint8, device=x.device)
+    _check(lib.hdqt_group_norm_bwd(C.byref(d), dy.data_ptr(), x.data_ptr(), _ptr(gamma), _ptr(beta), mean.data_ptr(),
+                                   rstd.data_ptr(), _ptr(dx), _ptr(dgamma), _ptr(dbeta), ws.data_ptr(), ws.numel(),
+                                   _stream()), "hdqt_group_norm_bwd")
+    return dx, dgamma, dbeta
