@@ -458,6 +458,61 @@ hdqt_status_t hdqt_group_norm_bwd(const hdqt_group_norm_desc_t* desc /*host*/, c
 
 size_t hdqt_group_norm_workspace_bytes(const hdqt_group_norm_desc_t* desc /*host*/, int32_t backward);
 
+/*
+ * Linear layer + softmax cross entropy over a large vocabulary, without the logits in memory.
+ *
+ *   z[t, v] = sum_d X[t, d] W[v, d],   lse[t] = log sum_v exp z[t, v],   loss[t] = lse[t] - z[t, label[t]]
+ *   dz[t, v] = g[t] (exp(z[t, v] - lse[t]) - [v == label[t]]),   dX = dz W,   dW = dz^T X
+ *
+ * X [tokens, features], W [classes, features] (w_is_cd != 0) or [features, classes] (w_is_cd == 0), rows ld_* elements apart,
+ * dX and dW in the layout of X and W; bf16 or fp32 (all four the same).  Products are formed on the tensor cores from bf16
+ * operands with fp32 sums; an fp32 operand is split into three bf16 planes, which keeps fp32 precision (infinite inputs then
+ * give NaN).  For bf16, dz is rounded to bf16 once before the gradient products; dX and dW are rounded once.
+ * labels: int64 [tokens]; ignore_index rows have loss 0 and gradient 0.  A label outside [0, classes) makes its loss
+ * NaN, its gradient 0, and sets HDQT_ERR_INVALID_ARG in *dev_status.
+ * reduction: HDQT_REDUCE_NONE loss[tokens]; HDQT_REDUCE_MEAN one value, the mean over the rows that are not ignored (NaN
+ * if there are none); HDQT_REDUCE_SUM one value.  lse: [tokens], always written.
+ *
+ *   _fwd    loss and lse.  The logits exist as 256 x 256 blocks in tensor memory only.
+ *   _bwd    dX and dW from lse, the logits formed again.  g (device fp32): [tokens] for HDQT_REDUCE_NONE, else one value, the
+ *           gradient of the loss (NULL = 1).  Works through the vocabulary in pieces.
+ *   _train  all of them in one call, for a loss whose gradient's weights are known beforehand: the logits are formed once
+ *           and held as 16-bit softmax codes (fp32: as logits) for a piece of the tokens at a time.  g as in _bwd.
+ *           Two thirds of _fwd + _bwd's tensor work at the price of a larger workspace.
+ *
+ * dX or dW may be NULL (not needed).  tokens may be 0 (mean loss NaN, dW = 0).
+ * Alignment: bf16 X and W 16 bytes; every other pointer its element's; workspace 256 bytes.  bf16 leading dimensions that are multiples
+ * of 8 are read in place, others are copied first.
+ * workspace: hdqt_linear_xent_workspace_bytes(desc, kind) bytes, kind = HDQT_XENT_FWD, _BWD or _TRAIN.
+ */
+enum { HDQT_REDUCE_NONE = 0, HDQT_REDUCE_MEAN = 1, HDQT_REDUCE_SUM = 2 };
+enum { HDQT_XENT_FWD = 0, HDQT_XENT_BWD = 1, HDQT_XENT_TRAIN = 2 };
+
+typedef struct hdqt_xent_desc {
+  int64_t tokens, features, classes;
+  int64_t ld_x, ld_w, ld_dx, ld_dw;
+  int64_t ignore_index;
+  int64_t piece_bytes; /* most bytes of the buffer that holds a piece's dz (or codes); 0 = chosen by the library */
+  int32_t dtype;       /* HDQT_DTYPE_F32 or HDQT_DTYPE_BF16 */
+  int32_t w_is_cd;
+  int32_t reduction;
+  int32_t reserved;    /* 0 */
+} hdqt_xent_desc_t;
+
+hdqt_status_t hdqt_linear_xent_fwd(const hdqt_xent_desc_t* desc /*host*/, const void* X, const void* W,
+                                   const int64_t* labels, float* loss, float* lse, void* workspace,
+                                   size_t workspace_bytes, int32_t* dev_status, void* stream);
+
+hdqt_status_t hdqt_linear_xent_bwd(const hdqt_xent_desc_t* desc /*host*/, const void* X, const void* W,
+                                   const int64_t* labels, const float* lse, const float* g, void* dX, void* dW,
+                                   void* workspace, size_t workspace_bytes, int32_t* dev_status, void* stream);
+
+hdqt_status_t hdqt_linear_xent_train(const hdqt_xent_desc_t* desc /*host*/, const void* X, const void* W,
+                                     const int64_t* labels, const float* g, float* loss, float* lse, void* dX, void* dW,
+                                     void* workspace, size_t workspace_bytes, int32_t* dev_status, void* stream);
+
+size_t hdqt_linear_xent_workspace_bytes(const hdqt_xent_desc_t* desc /*host*/, int32_t kind);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,7 +11,7 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libhdqt.so")
-SOURCES = ["hdqt_api.cu", "hdqt_quant.cu", "hdqt_gemm.cu", "hdqt_clip.cu", "hdqt_norm.cu"]
+SOURCES = ["hdqt_api.cu", "hdqt_quant.cu", "hdqt_gemm.cu", "hdqt_clip.cu", "hdqt_norm.cu", "hdqt_xent.cu"]
 
 
 def nvcc_path() -> str:

@@ -1,11 +1,10 @@
-// Device-side building blocks of the tiled integer GEMM kernels: tile constants, kernel parameters, PTX
-// wrappers (mbarrier, TMA, tcgen05), and the epilogue of one output block (accumulator quantisation, packed
+// Device-side building blocks of the tiled integer GEMM kernels: tile constants, kernel parameters, the
+// MMA wrappers, and the epilogue of one output block (accumulator quantisation, packed
 // 16-bit-lane sums, staged stores).  Included by hdqt_gemm.cu only (one translation unit).
 #pragma once
 
-#include <cuda.h>
-
 #include "hdqt_common.cuh"
+#include "hdqt_ptx.cuh"
 
 namespace hdqt {
 
@@ -101,119 +100,7 @@ struct GemmParams {
   const int32_t* block_count;
 };
 
-// ---- PTX wrappers ---------------------------------------------------------------------------
-
-__device__ __forceinline__ uint32_t smem_u32(const void* p) {
-  return (uint32_t)__cvta_generic_to_shared(p);
-}
-
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
-}
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-
-__device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-
-// Bounded waits: each gives up after ~1 s, or as soon as another role has given up.
-//
-// mbar_wait: for the two single-thread roles (TMA producer, MMA issuer), whose waits are on the
-// critical path of every K tile: polls without suspending first, then backs off.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag,
-                                          int slow_polls = 1 << 20) {
-  for (int i = 0; i < (1 << 12); ++i) {
-    if (mbar_test_wait(bar, parity)) return true;
-  }
-  for (int i = 0; i < slow_polls; ++i) {
-    if (mbar_try_wait(bar, parity)) return true;
-    if (*abort_flag) return false;
-    __nanosleep(512);
-  }
-  *abort_flag = 1;
-  return false;
-}
-
-// mbar_wait_suspend: for waits that are usually long (the TMA producer far ahead of the MMAs, the MMA issuer
-// behind a slower epilogue): try_wait parks the thread in hardware until the phase completes or a short time
-// limit passes, so the waiting warp takes no issue slots from the warps of its scheduler that have work.
-__device__ __forceinline__ bool mbar_wait_suspend(uint32_t bar, uint32_t parity, volatile int* abort_flag,
-                                                  long long limit_clk = 2000000000ll) {
-  if (mbar_try_wait(bar, parity)) return true;
-  const long long start = clock64();
-  while (true) {
-    if (mbar_try_wait(bar, parity)) return true;
-    if (*abort_flag) return false;
-    if (clock64() - start > limit_clk) break;
-  }
-  *abort_flag = 1;
-  return false;
-}
-// mbar_wait_yield: for the epilogue warps. A warp that spins steals issue slots from the MMA issuer
-// and from the warps that have work, so these waits suspend in hardware (try_wait) and sleep between
-// polls; kSleepNs is the poll period (short for the per-tile handshake, long for the one wait on the
-// merged accumulator that spans the whole main loop).
-template <int kSleepNs>
-__device__ __forceinline__ bool mbar_wait_yield(uint32_t bar, uint32_t parity, volatile int* abort_flag,
-                                                int polls = (kSleepNs >= 512) ? (1 << 21) : (1 << 24)) {
-  if (mbar_try_wait(bar, parity)) return true;
-  for (int i = 0; i < polls; ++i) {
-    __nanosleep(kSleepNs);
-    if (mbar_try_wait(bar, parity)) return true;
-    if ((i & 63) == 63 && *abort_flag) return false;
-  }
-  *abort_flag = 1;
-  return false;
-}
-
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y,
-                                            uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
-      : "memory");
-}
-
-template <int kRegs>
-__device__ __forceinline__ void warpgroup_reg_dec() {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs));
-}
-template <int kRegs>
-__device__ __forceinline__ void warpgroup_reg_inc() {
-  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs));
-}
-
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-
-__device__ __forceinline__ void tc_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
-               : "memory");
-}
+// ---- MMAs of the integer GEMM ----------------------------------------------------------------
 
 __device__ __forceinline__ void tc_mma_i8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t accumulate) {
   asm volatile(
@@ -241,43 +128,6 @@ __device__ __forceinline__ void tc_mma_i8_acc(uint32_t d_tmem, uint64_t a_desc, 
       ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(IDESC)
       : "memory");
 }
-
-// K-major operand tile with 128-byte swizzle: 8-row groups are 1024 bytes apart.
-__device__ __forceinline__ uint64_t make_smem_desc(uint32_t addr) {
-  uint64_t d = 0;
-  d |= (uint64_t)((addr & 0x3FFFFu) >> 4);        // start address
-  d |= (uint64_t)1 << 16;                         // leading byte offset (unused for swizzled K-major)
-  d |= (uint64_t)(1024 >> 4) << 32;               // stride byte offset between 8-row groups
-  d |= (uint64_t)1 << 46;                         // descriptor version of this architecture
-  d |= (uint64_t)2 << 61;                         // SWIZZLE_128B
-  return d;
-}
-
-// K-major operand tile without swizzle: 8 rows x 16 bytes are contiguous (128 bytes); `lbo` = distance between
-// the two 16-byte K chunks of a 32-byte K slice, `sbo` = distance between 8-row groups.
-__device__ __forceinline__ uint64_t make_smem_desc_plain(uint32_t addr, uint32_t lbo, uint32_t sbo) {
-  uint64_t d = 0;
-  d |= (uint64_t)((addr & 0x3FFFFu) >> 4);
-  d |= (uint64_t)(lbo >> 4) << 16;
-  d |= (uint64_t)(sbo >> 4) << 32;
-  d |= (uint64_t)1 << 46;
-  return d;
-}
-
-#define HDQT_TMEM_LD32(taddr, v)                                                                        \
-  asm volatile(                                                                                         \
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "                                                         \
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "                         \
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"         \
-      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), \
-        "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]),        \
-        "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]),      \
-        "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]),      \
-        "=r"(v[29]), "=r"(v[30]), "=r"(v[31])                                                           \
-      : "r"(taddr)                                                                                      \
-      : "memory")
-
-__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 #define HDQT_TMEM_LD32_PACK16(taddr, v)                                                                 \
   asm volatile(                                                                                         \
@@ -314,36 +164,6 @@ __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.
 #define HDQT_TMEM_LD16_PACK16(taddr, v)                                                                 \
   asm volatile(                                                                                         \
       "tcgen05.ld.sync.aligned.32x32b.x16.pack::16b.b32 "                                               \
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"                  \
-      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), \
-        "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]),        \
-        "=r"(v[15])                                                                                     \
-      : "r"(taddr)                                                                                      \
-      : "memory")
-
-// tcgen05.wait::ld tied to the registers of the load it completes, so that the compiler cannot move
-// their first use above the wait
-#define HDQT_TMEM_WAIT16(v)                                                                             \
-  asm volatile("tcgen05.wait::ld.sync.aligned;"                                                         \
-               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]),    \
-                 "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), \
-                 "+r"(v[14]), "+r"(v[15])                                                               \
-               :                                                                                        \
-               : "memory")
-
-#define HDQT_TMEM_WAIT32(v)                                                                             \
-  asm volatile("tcgen05.wait::ld.sync.aligned;"                                                         \
-               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]),    \
-                 "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), \
-                 "+r"(v[14]), "+r"(v[15]), "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]),          \
-                 "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]), "+r"(v[25]),          \
-                 "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])           \
-               :                                                                                        \
-               : "memory")
-
-#define HDQT_TMEM_LD16(taddr, v)                                                                        \
-  asm volatile(                                                                                         \
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "                                                         \
       "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"                  \
       : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), \
         "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]),        \

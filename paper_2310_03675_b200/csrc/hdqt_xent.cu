@@ -1,0 +1,724 @@
+// Linear layer + softmax cross entropy over a large vocabulary, without the logits in memory.
+//
+//   z = X W^T,  lse = log sum exp z,  loss = lse - z[label],  dz = g (exp(z - lse) - [label]),  dX = dz W,  dW = dz^T X
+//
+// Everything large is a matrix product on the tensor cores (hdqt_xent_gemm.cuh); this file holds the row kernels between
+// them and the host side.  The logits product's epilogue leaves, per row and 128 columns, the maximum and the sum of
+// exponentials, so the softmax statistics never need the logits again; a row is joined from these parts.
+//
+//   forward  : logits product (statistics) -> rows
+//   training : per piece of the tokens: logits product (statistics + 16-bit codes) -> rows, codes to dz in place ->
+//              dX and dW products in one launch
+//   backward : per piece of the vocabulary: logits product (dz from lse) -> dX (fp32 sums over the pieces) and dW
+#include <math.h>
+
+#include "hdqt_xent_gemm.cuh"
+
+namespace hdqt {
+
+namespace {
+
+constexpr int kRowThreads = 256;
+
+// ---- labels ------------------------------------------------------------------------------------------------
+
+// label[t] = class, -1 (ignored) or -2 (outside [0, classes)); scale[0] = weight of a row's loss in the reduced loss: 1 / kept rows
+// (mean) or 1; one block
+__global__ void __launch_bounds__(1024) xent_labels_kernel(const int64_t* __restrict__ labels, int64_t tokens, int64_t classes,
+                                                           int64_t ignore, int32_t mean, int32_t* __restrict__ label,
+                                                           float* __restrict__ scale, int32_t* dev_status) {
+  __shared__ int s_kept;
+  if (threadIdx.x == 0) s_kept = 0;
+  __syncthreads();
+  int kept = 0;
+  bool bad = false;
+  for (int64_t t = threadIdx.x; t < tokens; t += blockDim.x) {
+    const int64_t l = labels[t];
+    int32_t v = -1;
+    if (l != ignore) {
+      ++kept;
+      if (l >= 0 && l < classes) v = (int32_t)l;
+      else { v = -2; bad = true; }
+    }
+    label[t] = v;
+  }
+  atomicAdd(&s_kept, kept);
+  if (bad) report_status(dev_status, HDQT_ERR_INVALID_ARG);
+  __syncthreads();
+  if (threadIdx.x == 0) scale[0] = mean ? 1.0f / (float)s_kept : 1.0f;
+}
+
+// ---- rows: joining the parts of the softmax statistics -------------------------------------------------------
+
+struct MaxSum {
+  float m, s;    // sum of exp(z - m)
+};
+__device__ __forceinline__ MaxSum join(const MaxSum& a, const MaxSum& b) {
+  MaxSum r;
+  r.m = fmaxf(a.m, b.m);
+  r.s = a.s * ex2((a.m - r.m) * kLog2e) + b.s * ex2((b.m - r.m) * kLog2e);
+  return r;
+}
+__device__ __forceinline__ MaxSum warp_join(MaxSum v) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    MaxSum o;
+    o.m = __shfl_xor_sync(0xFFFFFFFFu, v.m, d);
+    o.s = __shfl_xor_sync(0xFFFFFFFFu, v.s, d);
+    v = join(v, o);
+  }
+  return v;
+}
+
+__device__ __forceinline__ float row_loss(int32_t label, float lse, float label_logit) {
+  return label >= 0 ? lse - label_logit : label == -1 ? 0.0f : NAN;
+}
+
+// one warp per row
+__global__ void __launch_bounds__(kRowThreads) xent_rows_kernel(const float2* __restrict__ part, int parts, int64_t parts_ld,
+                                                                const int32_t* __restrict__ label,
+                                                                const float* __restrict__ label_logit, int64_t rows,
+                                                                float* __restrict__ lse, float* __restrict__ loss) {
+  const int64_t row = (int64_t)blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
+  if (row >= rows) return;
+  const int lane = threadIdx.x & 31;
+  MaxSum v = {kLowest, 0.0f};
+  for (int i = lane; i < parts; i += 32) {
+    const float2 q = part[row * parts_ld + i];
+    v = join(v, MaxSum{q.x, q.y});
+  }
+  v = warp_join(v);
+  if (lane == 0) {
+    const float l = v.m + logf(v.s);
+    lse[row] = l;
+    loss[row] = row_loss(label[row], l, label_logit[row]);
+  }
+}
+
+// one block: loss = scale * sum of the rows' losses
+__global__ void __launch_bounds__(1024) xent_loss_kernel(const float* __restrict__ rows, int64_t n, const float* __restrict__ scale,
+                                                         float* __restrict__ loss) {
+  __shared__ double s_part[32];
+  double s = 0.0;
+  for (int64_t i = threadIdx.x; i < n; i += blockDim.x) s += (double)rows[i];
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+  if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s = 0.0;
+    for (int w = 0; w < 32; ++w) s += s_part[w];
+    loss[0] = (float)(s * (double)scale[0]);
+  }
+}
+
+// weights of the rows' losses: g[row] or g[0] (or 1), times scale[0]
+__global__ void xent_weights_kernel(const float* __restrict__ g, int g_rows, const float* __restrict__ scale, int64_t n,
+                                    float* __restrict__ w) {
+  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  if (i < n) w[i] = (g != nullptr ? g[g_rows ? i : 0] : 1.0f) * scale[0];
+}
+
+// Training: one block per row joins the row's parts, writes lse and the loss, and turns the row's codes (or fp32
+// logits) into dz = w (softmax - [label]): bf16 in place of the codes, or three bf16 planes.
+template <int kPlanes>
+__global__ void __launch_bounds__(kRowThreads)
+xent_dz_kernel(const float2* __restrict__ part, int parts, int64_t parts_ld, const int32_t* __restrict__ label,
+               const float* __restrict__ label_logit, const float* __restrict__ weight, int64_t classes, void* z, int64_t ld,
+               uint16_t* planes, int64_t plane, float* __restrict__ lse, float* __restrict__ loss) {
+  __shared__ float s_m[kRowThreads / 32], s_s[kRowThreads / 32];
+  const int64_t row = blockIdx.x;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const float2* pr = part + row * parts_ld;
+  MaxSum v = {kLowest, 0.0f};
+  for (int i = threadIdx.x; i < parts; i += kRowThreads) {
+    const float2 q = pr[i];
+    v = join(v, MaxSum{q.x, q.y});
+  }
+  v = warp_join(v);
+  if (lane == 0) { s_m[warp] = v.m; s_s[warp] = v.s; }
+  __syncthreads();
+  v = MaxSum{s_m[0], s_s[0]};
+#pragma unroll
+  for (int w = 1; w < kRowThreads / 32; ++w) v = join(v, MaxSum{s_m[w], s_s[w]});
+  const int32_t lab = label[row];
+  if (threadIdx.x == 0) {
+    const float l = v.m + logf(v.s);
+    lse[row] = l;
+    loss[row] = row_loss(lab, l, label_logit[row]);
+  }
+  const bool keep = lab >= 0;
+  const float w = keep ? weight[row] : 0.0f;
+  const float scale = w / v.s;
+  if (kPlanes == 1) {
+    uint4* codes = reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(z) + row * ld);
+#pragma unroll 2
+    for (int j = threadIdx.x; j * 8 < classes; j += kRowThreads) {
+      uint4 c = codes[j];
+      uint32_t* cw = reinterpret_cast<uint32_t*>(&c);
+      const float f = keep ? ex2((pr[j >> 4].x - v.m) * kLog2e) * scale : 0.0f;   // NaN where the row has one
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t ca = cw[k] & 0xFFFFu, cb = cw[k] >> 16;
+        float a = (ca == kCodeZero ? 0.0f : ex2((float)ca * (-1.0f / kCodeScale))) * f;
+        float b = (cb == kCodeZero ? 0.0f : ex2((float)cb * (-1.0f / kCodeScale))) * f;
+        if (lab == j * 8 + 2 * k) a -= w;
+        if (lab == j * 8 + 2 * k + 1) b -= w;
+        cw[k] = pack_bf16(a, b);
+      }
+      codes[j] = c;
+    }
+  } else {
+    const float4* logits = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(z) + row * ld);
+    uint2* o = reinterpret_cast<uint2*>(planes + row * ld);
+#pragma unroll 2
+    for (int j = threadIdx.x; j * 4 < classes; j += kRowThreads) {
+      const float4 q = logits[j];
+      float a[4] = {q.x, q.y, q.z, q.w}, p0[4], p1[4], p2[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float e = keep ? ex2((a[k] - v.m) * kLog2e) * scale : 0.0f;
+        if (lab == j * 4 + k) e -= w;
+        split3(e, p0[k], p1[k], p2[k]);
+      }
+      o[j] = make_uint2(pack_bf16(p0[0], p0[1]), pack_bf16(p0[2], p0[3]));
+      reinterpret_cast<uint2*>(planes + plane + row * ld)[j] = make_uint2(pack_bf16(p1[0], p1[1]), pack_bf16(p1[2], p1[3]));
+      reinterpret_cast<uint2*>(planes + 2 * plane + row * ld)[j] = make_uint2(pack_bf16(p2[0], p2[1]), pack_bf16(p2[2], p2[3]));
+    }
+  }
+}
+
+// ---- operands that cannot be read in place ---------------------------------------------------------------------
+
+// fp32 -> three bf16 planes, or bf16 -> a copy with rows that start on 16 bytes; two columns per thread
+template <typename T>
+__global__ void __launch_bounds__(256) xent_stage_kernel(const T* __restrict__ src, int64_t ld, int64_t rows, int64_t cols,
+                                                         uint16_t* __restrict__ dst, int64_t ld_dst, int64_t plane) {
+  const int64_t c = 2 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
+  if (c >= cols) return;
+  for (int64_t r = blockIdx.y; r < rows; r += gridDim.y) {
+    const T* s = src + r * ld + c;
+    const float a = to_f32(s[0]), b = c + 1 < cols ? to_f32(s[1]) : 0.0f;
+    uint16_t* d = dst + r * ld_dst + c;
+    if (sizeof(T) == 2) {
+      *reinterpret_cast<uint32_t*>(d) = pack_bf16(a, b);
+    } else {
+      float a0, a1, a2, b0, b1, b2;
+      split3(a, a0, a1, a2);
+      split3(b, b0, b1, b2);
+      *reinterpret_cast<uint32_t*>(d) = pack_bf16(a0, b0);
+      *reinterpret_cast<uint32_t*>(d + plane) = pack_bf16(a1, b1);
+      *reinterpret_cast<uint32_t*>(d + 2 * plane) = pack_bf16(a2, b2);
+    }
+  }
+}
+
+// sum of the splits' partial outputs, in order
+template <typename T>
+__global__ void __launch_bounds__(256) xent_join_splits_kernel(const float* __restrict__ part, int splits, int64_t rows,
+                                                               int64_t cols, T* __restrict__ out, int64_t ld) {
+  const int64_t n = rows * cols;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    float s = part[i];
+    for (int k = 1; k < splits; ++k) s += part[k * n + i];
+    const int64_t r = i / cols;
+    out[r * ld + (i - r * cols)] = from_f32<T>(s);
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) xent_zero_kernel(T* out, int64_t rows, int64_t cols, int64_t ld) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * cols; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / cols;
+    out[r * ld + (i - r * cols)] = from_f32<T>(0.0f);
+  }
+}
+
+// ---- host side ---------------------------------------------------------------------------------------------
+
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// A bf16 operand (or its three planes) as the product kernels read it.
+struct Operand {
+  const void* base;
+  int64_t inner, outer;     // contiguous extent, and the number of rows that far apart
+  int64_t ld, plane;        // elements
+  int planes;
+};
+
+bool make_map(CUtensorMap* map, const Operand& o, bool mn_major) {
+  EncodeTiledFn enc = get_encode_fn();
+  if (enc == nullptr) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)o.inner, (cuuint64_t)o.outer, (cuuint64_t)o.planes};
+  const cuuint64_t strides[2] = {(cuuint64_t)o.ld * 2, (cuuint64_t)(o.planes > 1 ? o.plane : o.ld) * 2};
+  const cuuint32_t box[3] = {64, mn_major ? 64u : 128u, 1};
+  const cuuint32_t elem_strides[3] = {1, 1, 1};
+  const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(o.base), dims, strides, box,
+                         elem_strides, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS;
+}
+
+struct Product {     // out[M, N] = A B^T with the operands stored as they are
+  Operand a, b;
+  bool a_mn, b_mn;
+  int64_t M, N, K;
+};
+
+XProblem make_problem(const Product& g, int splits) {
+  XProblem r{};
+  r.M = (int32_t)g.M;
+  r.N = (int32_t)g.N;
+  r.tiles_m = (int32_t)ceil_div(g.M, XM);
+  r.tiles_n = (int32_t)ceil_div(g.N, XN);
+  r.group_m = 16;
+  r.kblocks = (int32_t)ceil_div(g.K, XK);
+  r.kblocks_split = (int32_t)ceil_div(r.kblocks, splits);
+  r.splits = (int32_t)ceil_div(r.kblocks, r.kblocks_split);
+  r.a_mn = g.a_mn;
+  r.b_mn = g.b_mn;
+  r.items = r.tiles_m * r.tiles_n * r.splits;
+  return r;
+}
+
+template <int kEpi>
+hdqt_status_t launch(XParams& p, const Product* g, int n, cudaStream_t s) {
+  CUtensorMap maps[4];
+  for (int i = 0; i < n; ++i) {
+    if (!make_map(&maps[2 * i], g[i].a, g[i].a_mn) || !make_map(&maps[2 * i + 1], g[i].b, g[i].b_mn)) return HDQT_ERR_CUDA;
+  }
+  if (n == 1) { maps[2] = maps[0]; maps[3] = maps[1]; }
+  p.num_problems = n;
+  const int sms = sm_count();
+  if (sms < 2) return HDQT_ERR_CUDA;
+  const int items = p.pr[0].items + (n > 1 ? p.pr[1].items : 0);
+  const int pairs = items < sms / 2 ? items : sms / 2;
+  cudaError_t e = cudaFuncSetAttribute(xent_gemm_kernel<kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, X_SMEM);
+  if (e != cudaSuccess) return cuda_failure(e, "cross entropy product");
+  xent_gemm_kernel<kEpi><<<2 * pairs, X_THREADS, X_SMEM, s>>>(maps[0], maps[1], maps[2], maps[3], p);
+  e = cudaGetLastError();
+  return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy product");
+}
+
+// Sizes and workspace of a call.
+struct Plan {
+  int planes;
+  bool stage_x, stage_w;
+  int64_t ld_xs, ld_ws;                 // of the staged copies
+  int64_t w_rows, w_cols;
+  int64_t rows_piece, cols_piece;       // tokens x classes of a piece
+  int64_t ld_z;
+  int64_t parts_ld;
+  int splits_dx, splits_dw;
+  bool acc_dx, acc_dw;                  // fp32 sums over several pieces
+  // workspace offsets
+  size_t label, scale, label_logit, loss_rows, weight, part, xs, ws, z, dz, dx_f32, dw_f32, total;
+};
+
+constexpr int64_t kPieceBytes = 1ll << 30;
+
+int choose_splits(int64_t kblocks, int64_t per_pair) {
+  // An item longer than half of what a pair has to do in all leaves the others waiting at the end; a split below 16 stages
+  // costs more to join than it saves.
+  const int64_t most = per_pair / 2 > 16 ? per_pair / 2 : 16;
+  const int64_t s = ceil_div(kblocks, most);
+  return (int)(s < 16 ? s : 16);
+}
+
+hdqt_status_t make_plan(const hdqt_xent_desc_t* d, int kind, Plan* pl) {
+  if (!d || kind < HDQT_XENT_FWD || kind > HDQT_XENT_TRAIN) return HDQT_ERR_INVALID_ARG;
+  if (d->tokens < 0 || d->features <= 0 || d->classes <= 0 || d->piece_bytes < 0) return HDQT_ERR_INVALID_ARG;
+  if (d->dtype != HDQT_DTYPE_F32 && d->dtype != HDQT_DTYPE_BF16)
+    return dtype_size(d->dtype) ? HDQT_ERR_UNSUPPORTED : HDQT_ERR_INVALID_ARG;
+  if (d->reduction < HDQT_REDUCE_NONE || d->reduction > HDQT_REDUCE_SUM) return HDQT_ERR_INVALID_ARG;
+  pl->w_rows = d->w_is_cd ? d->classes : d->features;
+  pl->w_cols = d->w_is_cd ? d->features : d->classes;
+  if (d->ld_x < d->features || d->ld_w < pl->w_cols) return HDQT_ERR_INVALID_ARG;
+  if (kind != HDQT_XENT_FWD && (d->ld_dx < d->features || d->ld_dw < pl->w_cols)) return HDQT_ERR_INVALID_ARG;
+  if (d->tokens > (1 << 30) || d->features > (1 << 24) || d->classes > (1 << 30)) return HDQT_ERR_UNSUPPORTED;
+  if (ceil_div(d->tokens, XM) * ceil_div(d->classes, XN) > (1 << 26) ||
+      ceil_div(d->tokens > d->classes ? d->tokens : d->classes, XM) * ceil_div(d->features, XN) > (1 << 26))
+    return HDQT_ERR_UNSUPPORTED;
+  const bool f32 = d->dtype == HDQT_DTYPE_F32;
+  pl->planes = f32 ? 3 : 1;
+  pl->stage_x = f32 || d->ld_x % 8 != 0;
+  pl->stage_w = f32 || d->ld_w % 8 != 0;
+  pl->ld_xs = ceil_div(d->features, 8) * 8;
+  pl->ld_ws = ceil_div(pl->w_cols, 8) * 8;
+  const int64_t T = d->tokens > 0 ? d->tokens : 1, V = d->classes, D = d->features;
+  // a piece: all classes of some tokens (forward, training) or all tokens of some classes (backward)
+  const int64_t elem = f32 ? (kind == HDQT_XENT_TRAIN ? 10 : 6) : 2;
+  int64_t budget = d->piece_bytes;
+  if (budget == 0) {
+    // a second piece needs fp32 sums of dW (dX): splitting below that size would save no memory
+    const int64_t sums = 4 * D * (kind == HDQT_XENT_BWD ? T : V);
+    budget = kPieceBytes > sums ? kPieceBytes : sums;
+  }
+  pl->rows_piece = T;
+  pl->cols_piece = V;
+  if (kind == HDQT_XENT_BWD) {
+    const int64_t fit = budget / (T * elem) / 256 * 256;
+    if (fit < V) pl->cols_piece = fit > 256 ? fit : 256;
+  } else {
+    const int64_t ldv = ceil_div(V, 256) * 256;
+    // the forward call only holds the parts, 8 bytes per 128 columns
+    const int64_t row = kind == HDQT_XENT_TRAIN ? ldv * elem : ldv / 128 * 8;
+    const int64_t fit = budget / row / 256 * 256;
+    if (fit < T) pl->rows_piece = fit > 256 ? fit : 256;
+  }
+  if (pl->cols_piece > V) pl->cols_piece = V;
+  if (pl->rows_piece > T) pl->rows_piece = T;
+  pl->ld_z = ceil_div(pl->cols_piece, 256) * 256;
+  pl->parts_ld = ceil_div(V, XN) * 2;
+  pl->acc_dw = kind == HDQT_XENT_TRAIN && pl->rows_piece < T;
+  pl->acc_dx = kind == HDQT_XENT_BWD && pl->cols_piece < V;
+  const int64_t sms = 148;
+  const int64_t dx_blocks = ceil_div(pl->rows_piece, XM) * ceil_div(D, XN), dx_k = ceil_div(pl->cols_piece, XK);
+  const int64_t dw_blocks = ceil_div(pl->cols_piece, XM) * ceil_div(D, XN), dw_k = ceil_div(pl->rows_piece, XK);
+  const int64_t per_pair = (dx_blocks * dx_k + dw_blocks * dw_k) / (sms / 2);
+  const bool whole = !pl->acc_dx && !pl->acc_dw;
+  pl->splits_dx = whole ? choose_splits(dx_k, per_pair) : 1;
+  pl->splits_dw = whole ? choose_splits(dw_k, per_pair) : 1;
+
+  size_t o = 0;
+  auto take = [&](size_t bytes) { const size_t at = o; o += up256(bytes); return at; };
+  pl->label = take(4 * T);
+  pl->scale = take(256);
+  pl->label_logit = take(4 * T);
+  pl->loss_rows = take(4 * T);
+  pl->weight = take(4 * T);
+  pl->part = kind == HDQT_XENT_BWD ? o : take(8 * pl->rows_piece * pl->parts_ld);
+  pl->xs = pl->stage_x ? take(2 * pl->planes * T * pl->ld_xs) : o;
+  pl->ws = pl->stage_w ? take(2 * pl->planes * pl->w_rows * pl->ld_ws) : o;
+  pl->z = pl->dz = o;
+  if (kind == HDQT_XENT_TRAIN) {
+    pl->z = take((f32 ? 4 : 2) * pl->rows_piece * pl->ld_z);
+    pl->dz = f32 ? take(6 * pl->rows_piece * pl->ld_z) : pl->z;
+  } else if (kind == HDQT_XENT_BWD) {
+    pl->dz = take(2 * pl->planes * pl->rows_piece * pl->ld_z);
+  }
+  pl->dx_f32 = pl->dw_f32 = o;
+  if (kind != HDQT_XENT_FWD) {
+    if (pl->splits_dx > 1) pl->dx_f32 = take(4 * pl->splits_dx * T * D);
+    else if (pl->acc_dx && !f32) pl->dx_f32 = take(4 * T * D);
+    if (pl->splits_dw > 1) pl->dw_f32 = take(4 * pl->splits_dw * V * D);
+    else if (pl->acc_dw && !f32) pl->dw_f32 = take(4 * V * D);
+  }
+  pl->total = o;
+  return HDQT_OK;
+}
+
+struct Call {
+  const hdqt_xent_desc_t* d;
+  Plan pl;
+  uint8_t* ws;
+  int32_t* dev_status;
+  cudaStream_t s;
+  Operand x, w;          // as stored: x [tokens, features], w [w_rows, w_cols]
+
+  template <typename T>
+  T* at(size_t off) const { return reinterpret_cast<T*>(ws + off); }
+
+  Operand x_rows(int64_t t0, int64_t n) const {
+    Operand o = x;
+    o.base = reinterpret_cast<const uint16_t*>(x.base) + t0 * x.ld;
+    o.outer = n;
+    return o;
+  }
+  // the columns [v0, v0 + n) of the vocabulary
+  Operand w_classes(int64_t v0, int64_t n) const {
+    Operand o = w;
+    o.base = reinterpret_cast<const uint16_t*>(w.base) + (d->w_is_cd ? v0 * w.ld : v0);
+    (d->w_is_cd ? o.outer : o.inner) = n;
+    return o;
+  }
+  Operand dz(int64_t rows, int64_t cols) const {
+    Operand o;
+    o.base = at<uint16_t>(pl.dz);
+    o.inner = cols;
+    o.outer = rows;
+    o.ld = pl.ld_z;
+    o.plane = pl.rows_piece * pl.ld_z;
+    o.planes = pl.planes;
+    return o;
+  }
+};
+
+void fill_common(const Call& c, XParams* p) {
+  memset(p, 0, sizeof(*p));
+  p->planes = c.pl.planes;
+  // stages per part: 1024 additions of 16 products for bf16 results, 64 where fp32 precision is to be kept
+  p->part_iters = c.pl.planes == 1 ? 256 : 16;
+  p->dev_status = c.dev_status;
+}
+
+// checks, staged operands and labels: what all three calls begin with
+hdqt_status_t begin(Call* c, const hdqt_xent_desc_t* d, int kind, const void* X, const void* W, const int64_t* labels,
+                    void* workspace, size_t workspace_bytes, int32_t* dev_status, void* stream) {
+  const hdqt_status_t st = make_plan(d, kind, &c->pl);
+  if (st != HDQT_OK) return st;
+  const bool empty = d->tokens == 0;
+  if (!W || !workspace || (!empty && (!X || !labels))) return HDQT_ERR_INVALID_ARG;
+  const uintptr_t need = d->dtype == HDQT_DTYPE_BF16 ? 15 : 3;
+  if (((reinterpret_cast<uintptr_t>(X) | reinterpret_cast<uintptr_t>(W)) & need) || (reinterpret_cast<uintptr_t>(labels) & 7) ||
+      (reinterpret_cast<uintptr_t>(workspace) & 255))
+    return HDQT_ERR_ALIGNMENT;
+  if (workspace_bytes < c->pl.total) return HDQT_ERR_WORKSPACE;
+  c->d = d;
+  c->ws = reinterpret_cast<uint8_t*>(workspace);
+  c->dev_status = dev_status;
+  c->s = reinterpret_cast<cudaStream_t>(stream);
+  return HDQT_OK;
+}
+
+hdqt_status_t stage(const Call& c, const void* src, int64_t ld, int64_t rows, int64_t cols, size_t off, int64_t ld_dst,
+                    Operand* o) {
+  uint16_t* dst = c.at<uint16_t>(off);
+  o->base = dst;
+  o->ld = ld_dst;
+  o->plane = rows * ld_dst;
+  if (rows == 0) return HDQT_OK;
+  const dim3 grid((unsigned)ceil_div(cols, 512), (unsigned)(rows < 16384 ? rows : 16384));
+  if (c.d->dtype == HDQT_DTYPE_F32)
+    xent_stage_kernel<<<grid, 256, 0, c.s>>>(reinterpret_cast<const float*>(src), ld, rows, cols, dst, ld_dst, rows * ld_dst);
+  else
+    xent_stage_kernel<<<grid, 256, 0, c.s>>>(reinterpret_cast<const __nv_bfloat16*>(src), ld, rows, cols, dst, ld_dst, 0);
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy operands");
+}
+
+hdqt_status_t prepare(Call* c, const void* X, const void* W, const int64_t* labels, bool mean) {
+  const hdqt_xent_desc_t& d = *c->d;
+  const Plan& pl = c->pl;
+  c->x = Operand{X, d.features, d.tokens, d.ld_x, 0, pl.planes};
+  c->w = Operand{W, pl.w_cols, pl.w_rows, d.ld_w, 0, pl.planes};
+  hdqt_status_t st = HDQT_OK;
+  if (pl.stage_x) st = stage(*c, X, d.ld_x, d.tokens, d.features, pl.xs, pl.ld_xs, &c->x);
+  if (st == HDQT_OK && pl.stage_w) st = stage(*c, W, d.ld_w, pl.w_rows, pl.w_cols, pl.ws, pl.ld_ws, &c->w);
+  if (st != HDQT_OK) return st;
+  xent_labels_kernel<<<1, 1024, 0, c->s>>>(labels, d.tokens, d.classes, d.ignore_index, mean, c->at<int32_t>(pl.label),
+                                           c->at<float>(pl.scale), c->dev_status);
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy labels");
+}
+
+Product logits_product(const Call& c, int64_t t0, int64_t nt, int64_t v0, int64_t nv) {
+  return Product{c.x_rows(t0, nt), c.w_classes(v0, nv), false, c.d->w_is_cd == 0, nt, nv, c.d->features};
+}
+
+// dX and dW of a piece whose dz lies in the workspace: one launch
+hdqt_status_t gradient_products(const Call& c, int64_t t0, int64_t nt, int64_t v0, int64_t nv, void* dX, void* dW,
+                                bool first, bool last) {
+  const hdqt_xent_desc_t& d = *c.d;
+  const Plan& pl = c.pl;
+  const bool bf16 = d.dtype == HDQT_DTYPE_BF16;
+  const int64_t D = d.features;
+  XParams p;
+  fill_common(c, &p);
+  Product g[2];
+  int n = 0;
+  const Operand dz = c.dz(nt, nv);
+  // where a product goes: partial sums of its splits, the result itself, or fp32 sums over the pieces
+  auto target = [&](XProblem& r, void* out, int64_t ld, int64_t offset, bool acc, size_t f32_off, int64_t f32_ld) {
+    float* f32 = c.at<float>(f32_off);
+    if (r.splits > 1) {
+      r.out = f32;
+      r.ld_out = f32_ld;
+      r.split_stride = (int64_t)r.M * f32_ld;
+    } else if (!acc || !bf16) {
+      r.out = reinterpret_cast<uint8_t*>(out) + offset * (bf16 ? 2 : 4);
+      r.ld_out = ld;
+      r.out_bf16 = bf16;
+      if (acc && !first) { r.add = reinterpret_cast<const float*>(r.out); r.ld_add = ld; }
+    } else {
+      if (!first) { r.add = f32; r.ld_add = f32_ld; }
+      r.out = last ? out : static_cast<void*>(f32);
+      r.ld_out = last ? ld : f32_ld;
+      r.out_bf16 = last;
+    }
+  };
+  if (dX) {
+    // dX[t, d] = sum_v dz[t, v] W[v, d]
+    g[n] = Product{dz, c.w_classes(v0, nv), false, d.w_is_cd != 0, nt, D, nv};
+    p.pr[n] = make_problem(g[n], pl.splits_dx);
+    target(p.pr[n], dX, d.ld_dx, t0 * d.ld_dx, pl.acc_dx, pl.dx_f32, D);
+    ++n;
+  }
+  if (dW) {
+    // dW[v, d] = sum_t dz[t, v] X[t, d], or its transpose
+    if (d.w_is_cd) {
+      g[n] = Product{dz, c.x_rows(t0, nt), true, true, nv, D, nt};
+    } else {
+      g[n] = Product{c.x_rows(t0, nt), dz, true, true, D, nv, nt};
+    }
+    p.pr[n] = make_problem(g[n], pl.splits_dw);
+    target(p.pr[n], dW, d.ld_dw, d.w_is_cd ? v0 * d.ld_dw : v0, pl.acc_dw, pl.dw_f32, pl.w_cols);
+    ++n;
+  }
+  if (n == 0) return HDQT_OK;
+  hdqt_status_t st = launch<X_OUT>(p, g, n, c.s);
+  if (st != HDQT_OK) return st;
+  int i = 0;
+  auto join = [&](const XProblem& r, void* out, int64_t ld, size_t off) {
+    if (r.splits <= 1) return;
+    const int64_t blocks = ceil_div((int64_t)r.M * r.N, 256);
+    const unsigned grid = (unsigned)(blocks < 148 * 16 ? blocks : 148 * 16);
+    if (bf16) xent_join_splits_kernel<<<grid, 256, 0, c.s>>>(c.at<float>(off), r.splits, r.M, r.N, reinterpret_cast<__nv_bfloat16*>(out), ld);
+    else xent_join_splits_kernel<<<grid, 256, 0, c.s>>>(c.at<float>(off), r.splits, r.M, r.N, reinterpret_cast<float*>(out), ld);
+  };
+  if (dX) join(p.pr[i++], dX, d.ld_dx, pl.dx_f32);
+  if (dW) join(p.pr[i], dW, d.ld_dw, pl.dw_f32);
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy gradients");
+}
+
+hdqt_status_t zero_out(const Call& c, void* out, int64_t rows, int64_t cols, int64_t ld) {
+  if (c.d->dtype == HDQT_DTYPE_BF16) xent_zero_kernel<<<148 * 4, 256, 0, c.s>>>(reinterpret_cast<__nv_bfloat16*>(out), rows, cols, ld);
+  else xent_zero_kernel<<<148 * 4, 256, 0, c.s>>>(reinterpret_cast<float*>(out), rows, cols, ld);
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy gradients");
+}
+
+// reduced loss from the rows' losses (which are the result themselves without a reduction)
+hdqt_status_t reduce_loss(const Call& c, float* loss) {
+  if (c.d->reduction != HDQT_REDUCE_NONE)
+    xent_loss_kernel<<<1, 1024, 0, c.s>>>(c.at<float>(c.pl.loss_rows), c.d->tokens, c.at<float>(c.pl.scale), loss);
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy loss");
+}
+
+// weights of the rows' losses in the workspace
+void weights(const Call& c, const float* g) {
+  xent_weights_kernel<<<(unsigned)ceil_div(c.d->tokens, 256), 256, 0, c.s>>>(
+      g, c.d->reduction == HDQT_REDUCE_NONE, c.at<float>(c.pl.scale), c.d->tokens, c.at<float>(c.pl.weight));
+}
+
+bool outputs_misaligned(const hdqt_xent_desc_t* d, const void* a, const void* b) {
+  return ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) & (uintptr_t)(dtype_size(d->dtype) - 1)) != 0;
+}
+bool floats_misaligned(const void* a, const void* b, const void* c) {
+  return ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b) | reinterpret_cast<uintptr_t>(c)) & 3) != 0;
+}
+
+}  // namespace
+
+}  // namespace hdqt
+
+using namespace hdqt;
+
+extern "C" size_t hdqt_linear_xent_workspace_bytes(const hdqt_xent_desc_t* d, int32_t kind) {
+  Plan pl;
+  return make_plan(d, kind, &pl) == HDQT_OK ? pl.total : 0;
+}
+
+extern "C" hdqt_status_t hdqt_linear_xent_fwd(const hdqt_xent_desc_t* d, const void* X, const void* W,
+                                              const int64_t* labels, float* loss, float* lse, void* workspace,
+                                              size_t workspace_bytes, int32_t* dev_status, void* stream) {
+  Call c;
+  hdqt_status_t st = begin(&c, d, HDQT_XENT_FWD, X, W, labels, workspace, workspace_bytes, dev_status, stream);
+  if (st != HDQT_OK) return st;
+  if ((d->tokens > 0 && !lse) || (!loss && (d->tokens > 0 || d->reduction != HDQT_REDUCE_NONE))) return HDQT_ERR_INVALID_ARG;
+  if (floats_misaligned(loss, lse, nullptr)) return HDQT_ERR_ALIGNMENT;
+  st = prepare(&c, X, W, labels, d->reduction == HDQT_REDUCE_MEAN);
+  if (st != HDQT_OK) return st;
+  float* rows = d->reduction == HDQT_REDUCE_NONE ? loss : c.at<float>(c.pl.loss_rows);
+  for (int64_t t0 = 0; t0 < d->tokens; t0 += c.pl.rows_piece) {
+    const int64_t nt = d->tokens - t0 < c.pl.rows_piece ? d->tokens - t0 : c.pl.rows_piece;
+    const Product g = logits_product(c, t0, nt, 0, d->classes);
+    XParams p;
+    fill_common(c, &p);
+    p.pr[0] = make_problem(g, 1);
+    p.label = c.at<int32_t>(c.pl.label) + t0;
+    p.part = c.at<float2>(c.pl.part);
+    p.parts_ld = c.pl.parts_ld;
+    p.label_logit = c.at<float>(c.pl.label_logit) + t0;
+    st = launch<X_STATS>(p, &g, 1, c.s);
+    if (st != HDQT_OK) return st;
+    xent_rows_kernel<<<(unsigned)ceil_div(nt, kRowThreads / 32), kRowThreads, 0, c.s>>>(
+        p.part, (int)p.parts_ld, p.parts_ld, p.label, p.label_logit, nt, lse + t0, rows + t0);
+  }
+  return reduce_loss(c, loss);
+}
+
+extern "C" hdqt_status_t hdqt_linear_xent_bwd(const hdqt_xent_desc_t* d, const void* X, const void* W,
+                                              const int64_t* labels, const float* lse, const float* gr, void* dX, void* dW,
+                                              void* workspace, size_t workspace_bytes, int32_t* dev_status, void* stream) {
+  Call c;
+  hdqt_status_t st = begin(&c, d, HDQT_XENT_BWD, X, W, labels, workspace, workspace_bytes, dev_status, stream);
+  if (st != HDQT_OK) return st;
+  if (d->tokens > 0 && (!lse || (d->reduction == HDQT_REDUCE_NONE && !gr))) return HDQT_ERR_INVALID_ARG;
+  if (floats_misaligned(lse, gr, nullptr) || outputs_misaligned(d, dX, dW)) return HDQT_ERR_ALIGNMENT;
+  if (!dX && !dW) return HDQT_OK;
+  if (d->tokens == 0) return dW ? zero_out(c, dW, c.pl.w_rows, c.pl.w_cols, d->ld_dw) : HDQT_OK;
+  st = prepare(&c, X, W, labels, d->reduction == HDQT_REDUCE_MEAN);
+  if (st != HDQT_OK) return st;
+  weights(c, gr);
+  for (int64_t v0 = 0; v0 < d->classes; v0 += c.pl.cols_piece) {
+    const int64_t nv = d->classes - v0 < c.pl.cols_piece ? d->classes - v0 : c.pl.cols_piece;
+    const Product g = logits_product(c, 0, d->tokens, v0, nv);
+    XParams p;
+    fill_common(c, &p);
+    p.pr[0] = make_problem(g, 1);
+    p.label = c.at<int32_t>(c.pl.label);
+    p.n0 = (int32_t)v0;
+    p.z = c.at<void>(c.pl.dz);
+    p.ld_z = c.pl.ld_z;
+    p.plane_z = c.pl.rows_piece * c.pl.ld_z;
+    p.lse = lse;
+    p.g = c.at<float>(c.pl.weight);
+    p.g_rows = 1;
+    st = launch<X_DZ>(p, &g, 1, c.s);
+    if (st != HDQT_OK) return st;
+    st = gradient_products(c, 0, d->tokens, v0, nv, dX, dW, v0 == 0, v0 + nv == d->classes);
+    if (st != HDQT_OK) return st;
+  }
+  return HDQT_OK;
+}
+
+extern "C" hdqt_status_t hdqt_linear_xent_train(const hdqt_xent_desc_t* d, const void* X, const void* W,
+                                                const int64_t* labels, const float* gr, float* loss, float* lse, void* dX,
+                                                void* dW, void* workspace, size_t workspace_bytes, int32_t* dev_status,
+                                                void* stream) {
+  Call c;
+  hdqt_status_t st = begin(&c, d, HDQT_XENT_TRAIN, X, W, labels, workspace, workspace_bytes, dev_status, stream);
+  if (st != HDQT_OK) return st;
+  if ((d->tokens > 0 && !lse) || (!loss && (d->tokens > 0 || d->reduction != HDQT_REDUCE_NONE))) return HDQT_ERR_INVALID_ARG;
+  if (d->tokens > 0 && d->reduction == HDQT_REDUCE_NONE && !gr) return HDQT_ERR_INVALID_ARG;
+  if (floats_misaligned(loss, lse, gr) || outputs_misaligned(d, dX, dW)) return HDQT_ERR_ALIGNMENT;
+  st = prepare(&c, X, W, labels, d->reduction == HDQT_REDUCE_MEAN);
+  if (st != HDQT_OK) return st;
+  if (d->tokens == 0) {
+    if (dW) st = zero_out(c, dW, c.pl.w_rows, c.pl.w_cols, d->ld_dw);
+    return st == HDQT_OK ? reduce_loss(c, loss) : st;
+  }
+  weights(c, gr);
+  float* rows = d->reduction == HDQT_REDUCE_NONE ? loss : c.at<float>(c.pl.loss_rows);
+  for (int64_t t0 = 0; t0 < d->tokens; t0 += c.pl.rows_piece) {
+    const int64_t nt = d->tokens - t0 < c.pl.rows_piece ? d->tokens - t0 : c.pl.rows_piece;
+    const Product g = logits_product(c, t0, nt, 0, d->classes);
+    XParams p;
+    fill_common(c, &p);
+    p.pr[0] = make_problem(g, 1);
+    p.label = c.at<int32_t>(c.pl.label) + t0;
+    p.part = c.at<float2>(c.pl.part);
+    p.parts_ld = c.pl.parts_ld;
+    p.label_logit = c.at<float>(c.pl.label_logit) + t0;
+    p.z = c.at<void>(c.pl.z);
+    p.ld_z = c.pl.ld_z;
+    st = c.pl.planes == 1 ? launch<X_CODES>(p, &g, 1, c.s) : launch<X_LOGITS>(p, &g, 1, c.s);
+    if (st != HDQT_OK) return st;
+    if (c.pl.planes == 1)
+      xent_dz_kernel<1><<<(unsigned)nt, kRowThreads, 0, c.s>>>(p.part, (int)p.parts_ld, p.parts_ld, p.label, p.label_logit,
+                                                               c.at<float>(c.pl.weight) + t0, d->classes, p.z, c.pl.ld_z,
+                                                               nullptr, 0, lse + t0, rows + t0);
+    else
+      xent_dz_kernel<3><<<(unsigned)nt, kRowThreads, 0, c.s>>>(p.part, (int)p.parts_ld, p.parts_ld, p.label, p.label_logit,
+                                                               c.at<float>(c.pl.weight) + t0, d->classes, p.z, c.pl.ld_z,
+                                                               c.at<uint16_t>(c.pl.dz), c.pl.rows_piece * c.pl.ld_z,
+                                                               lse + t0, rows + t0);
+    st = gradient_products(c, t0, nt, 0, d->classes, dX, dW, t0 == 0, t0 + nt == d->tokens);
+    if (st != HDQT_OK) return st;
+  }
+  return reduce_loss(c, loss);
+}

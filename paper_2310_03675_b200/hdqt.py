@@ -22,6 +22,8 @@ FLAG_RELU = 4
 AMAX_HISTORY_WORDS = 1024
 DTYPE_CODES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # hdqt_dtype_t
 ACT_CODES = {"none": 0, "relu": 1, "silu": 2}                           # hdqt_act_t
+REDUCE_CODES = {"none": 0, "mean": 1, "sum": 2}                         # HDQT_REDUCE_*
+XENT_FWD, XENT_BWD, XENT_TRAIN = 0, 1, 2
 NORM_CODES = {2.0: 2, float("inf"): 0}                                  # HDQT_NORM_*
 
 STATUS_NAMES = ["OK", "INVALID_ARG", "UNSUPPORTED", "ALIGNMENT", "WORKSPACE", "NONFINITE", "TIMEOUT", "CUDA",
@@ -35,6 +37,7 @@ EXPORTED = [
     "hdqt_selftest_bounded_wait", "hdqt_conv2d_fwd", "hdqt_conv2d_wgrad", "hdqt_selftest_mma_rate",
     "hdqt_grad_norm", "hdqt_clip_grad_norm", "hdqt_grad_norm_workspace_bytes",
     "hdqt_group_norm_fwd", "hdqt_group_norm_bwd", "hdqt_group_norm_workspace_bytes",
+    "hdqt_linear_xent_fwd", "hdqt_linear_xent_bwd", "hdqt_linear_xent_train", "hdqt_linear_xent_workspace_bytes",
 ]
 
 
@@ -63,6 +66,13 @@ class GroupNormDesc(C.Structure):
     _fields_ = [(n, C.c_int64) for n in ("batch", "pixels", "channels", "groups", "x_batch_stride", "x_pixel_stride",
                                          "y_batch_stride", "y_pixel_stride")] + \
                [("dtype", C.c_int32), ("param_dtype", C.c_int32), ("act", C.c_int32), ("eps", C.c_float)]
+
+
+class XentDesc(C.Structure):
+    """Mirror of hdqt_xent_desc_t."""
+    _fields_ = [(n, C.c_int64) for n in ("tokens", "features", "classes", "ld_x", "ld_w", "ld_dx", "ld_dw",
+                                         "ignore_index", "piece_bytes")] + \
+               [(n, C.c_int32) for n in ("dtype", "w_is_cd", "reduction", "reserved")]
 
 
 class WsLayout(C.Structure):
@@ -121,6 +131,13 @@ def _load() -> C.CDLL:
     lib.hdqt_group_norm_bwd.argtypes = [C.POINTER(GroupNormDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.hdqt_group_norm_workspace_bytes.argtypes = [C.POINTER(GroupNormDesc), i32]
     lib.hdqt_group_norm_workspace_bytes.restype = sz
+    lib.hdqt_linear_xent_fwd.argtypes = [C.POINTER(XentDesc), vp, vp, vp, vp, vp, vp, sz, vp, vp]
+    lib.hdqt_linear_xent_bwd.argtypes = [C.POINTER(XentDesc), vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp]
+    lib.hdqt_linear_xent_train.argtypes = [C.POINTER(XentDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp]
+    lib.hdqt_linear_xent_workspace_bytes.argtypes = [C.POINTER(XentDesc), i32]
+    lib.hdqt_linear_xent_workspace_bytes.restype = sz
+    for name in ("hdqt_linear_xent_fwd", "hdqt_linear_xent_bwd", "hdqt_linear_xent_train"):
+        getattr(lib, name).restype = C.c_int
     for name in ("hdqt_grad_norm", "hdqt_clip_grad_norm", "hdqt_group_norm_fwd", "hdqt_group_norm_bwd"):
         getattr(lib, name).restype = C.c_int
     lib.hdqt_workspace_bytes.argtypes = [C.POINTER(GemmDesc), i64, i64, i64]
@@ -599,3 +616,99 @@ def group_norm_bwd(dy, x, gamma, beta, mean, rstd, groups: int, act: str = "none
                                    rstd.data_ptr(), _ptr(dx), _ptr(dgamma), _ptr(dbeta), ws.data_ptr(), ws.numel(),
                                    _stream()), "hdqt_group_norm_bwd")
     return dx, dgamma, dbeta
+
+
+# ---- linear layer + softmax cross entropy over a large vocabulary ------------------------------------
+
+def _rows(t, name: str, shape=None):
+    """A 2-D bf16 / fp32 CUDA tensor with contiguous rows that the library can read in place (bf16: rows from 16-byte
+    boundaries on; a tensor that starts elsewhere is copied)."""
+    if t.dim() != 2 or t.dtype not in (torch.float32, torch.bfloat16) or not t.is_cuda:
+        raise ValueError(f"{name} must be a 2-D fp32 or bf16 CUDA tensor")
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{name} must have shape {shape}")
+    if (t.stride(1) != 1 and t.shape[1] > 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError(f"the rows of {name} must be contiguous")
+    if t.dtype == torch.bfloat16 and t.data_ptr() % 16:
+        t = t.clone(memory_format=torch.contiguous_format)
+    return t
+
+
+def _ld(t) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _xent_call(X, W, labels, ignore_index, reduction, w_is_cd, piece_bytes, kind):
+    X, W = _rows(X, "X"), _rows(W, "W")
+    if reduction not in REDUCE_CODES:
+        raise ValueError(f"reduction must be one of {sorted(REDUCE_CODES)}")
+    T, D = X.shape
+    V = W.shape[0] if w_is_cd else W.shape[1]
+    if W.shape[1 if w_is_cd else 0] != D or W.dtype != X.dtype or W.device != X.device:
+        raise ValueError("X [tokens, features] and W must agree in features, type and device")
+    if labels.shape != (T,) or labels.dtype != torch.int64 or labels.device != X.device:
+        raise ValueError("labels must be an int64 [tokens] tensor on X's device")
+    labels = labels.contiguous()
+    d = XentDesc(T, D, V, max(_ld(X), D), max(_ld(W), W.shape[1]), D, W.shape[1], ignore_index, piece_bytes,
+                 DTYPE_CODES[X.dtype], int(w_is_cd), REDUCE_CODES[reduction], 0)
+    nbytes = lib.hdqt_linear_xent_workspace_bytes(C.byref(d), kind)
+    ws = torch.empty(max(256, nbytes), dtype=torch.uint8, device=X.device)
+    return X, W, labels, d, ws
+
+
+def _loss_weight(g, reduction, T, device):
+    shape = (T,) if reduction == "none" else ()
+    if g is None:
+        if reduction == "none":
+            raise ValueError("reduction 'none' needs the weight of each token's loss (g)")
+        return None
+    if tuple(g.shape) != shape or g.dtype != torch.float32 or g.device != device:
+        raise ValueError(f"g must be an fp32 tensor of shape {shape} on X's device")
+    return g.contiguous()
+
+
+def linear_xent_fwd(X, W, labels, ignore_index: int = -100, reduction: str = "mean", w_is_cd: bool = False,
+                    dev_status=None):
+    """Softmax cross entropy of X[tokens, features] times W ([features, classes], or [classes, features] with w_is_cd)
+    against int64 labels; the logits are never stored.  bf16 or fp32.  Returns (loss: scalar, or [tokens] with reduction
+    "none"; lse fp32 [tokens])."""
+    X, W, labels, d, ws = _xent_call(X, W, labels, ignore_index, reduction, w_is_cd, 0, XENT_FWD)
+    lse = torch.empty(d.tokens, dtype=torch.float32, device=X.device)
+    loss = torch.empty((d.tokens,) if reduction == "none" else (), dtype=torch.float32, device=X.device)
+    _check(lib.hdqt_linear_xent_fwd(C.byref(d), X.data_ptr(), W.data_ptr(), labels.data_ptr(), loss.data_ptr(),
+                                    lse.data_ptr(), ws.data_ptr(), ws.numel(), _ptr(dev_status), _stream()),
+           "hdqt_linear_xent_fwd")
+    return loss, lse
+
+
+def linear_xent_bwd(X, W, labels, lse, g=None, ignore_index: int = -100, reduction: str = "mean", w_is_cd: bool = False,
+                    want_dx: bool = True, want_dw: bool = True, piece_bytes: int = 0, dev_status=None):
+    """Gradients (dX, dW; None if not wanted) of linear_xent_fwd's loss from its lse.  g: gradient of the loss, an fp32
+    scalar (None = 1) or [tokens] with reduction "none".  Works through the vocabulary in pieces of piece_bytes (0 = chosen by
+    the library)."""
+    X, W, labels, d, ws = _xent_call(X, W, labels, ignore_index, reduction, w_is_cd, piece_bytes, XENT_BWD)
+    g = _loss_weight(g, reduction, d.tokens, X.device)
+    if tuple(lse.shape) != (d.tokens,) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != X.device:
+        raise ValueError("lse must be the dense fp32 [tokens] tensor of the forward call")
+    dX = torch.empty(X.shape, dtype=X.dtype, device=X.device) if want_dx else None
+    dW = torch.empty(W.shape, dtype=W.dtype, device=W.device) if want_dw else None
+    _check(lib.hdqt_linear_xent_bwd(C.byref(d), X.data_ptr(), W.data_ptr(), labels.data_ptr(), lse.data_ptr(), _ptr(g),
+                                    _ptr(dX), _ptr(dW), ws.data_ptr(), ws.numel(), _ptr(dev_status), _stream()),
+           "hdqt_linear_xent_bwd")
+    return dX, dW
+
+
+def linear_xent_train(X, W, labels, g=None, ignore_index: int = -100, reduction: str = "mean", w_is_cd: bool = False,
+                      want_dx: bool = True, want_dw: bool = True, piece_bytes: int = 0, dev_status=None):
+    """Loss and gradients in one call (two thirds of the tensor work of linear_xent_fwd + linear_xent_bwd), for a loss whose
+    gradient is known beforehand: g as in linear_xent_bwd.  Returns (loss, lse, dX, dW)."""
+    X, W, labels, d, ws = _xent_call(X, W, labels, ignore_index, reduction, w_is_cd, piece_bytes, XENT_TRAIN)
+    g = _loss_weight(g, reduction, d.tokens, X.device)
+    lse = torch.empty(d.tokens, dtype=torch.float32, device=X.device)
+    loss = torch.empty((d.tokens,) if reduction == "none" else (), dtype=torch.float32, device=X.device)
+    dX = torch.empty(X.shape, dtype=X.dtype, device=X.device) if want_dx else None
+    dW = torch.empty(W.shape, dtype=W.dtype, device=W.device) if want_dw else None
+    _check(lib.hdqt_linear_xent_train(C.byref(d), X.data_ptr(), W.data_ptr(), labels.data_ptr(), _ptr(g),
+                                      loss.data_ptr(), lse.data_ptr(), _ptr(dX), _ptr(dW), ws.data_ptr(), ws.numel(),
+                                      _ptr(dev_status), _stream()), "hdqt_linear_xent_train")
+    return loss, lse, dX, dW
