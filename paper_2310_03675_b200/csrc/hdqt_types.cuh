@@ -4,6 +4,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "hdqt_common.cuh"
 
 namespace hdqt {
@@ -32,6 +34,56 @@ template <typename T, int N>
 struct alignas(sizeof(T) * N) Vec {
   T v[N];
 };
+
+// all N elements to and from fp32, two at a time where there are two
+template <typename T, int N>
+__device__ __forceinline__ void unpack(const Vec<T, N>& v, float (&f)[N]) {
+  if constexpr (sizeof(T) == 2 && N % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(&v.v[i]);   // bf16 is the upper half of an fp32
+        f[i] = __uint_as_float(w << 16);
+        f[i + 1] = __uint_as_float(w & 0xFFFF0000u);
+      } else {
+        const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&v.v[i]));
+        f[i] = t.x;
+        f[i + 1] = t.y;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = to_f32(v.v[i]);
+  }
+}
+template <typename T, int N>
+__device__ __forceinline__ Vec<T, N> pack(const float (&f)[N]) {
+  Vec<T, N> v;
+  if constexpr (sizeof(T) == 2 && N % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      if constexpr (std::is_same_v<T, __nv_bfloat16>) *reinterpret_cast<__nv_bfloat162*>(&v.v[i]) = __floats2bfloat162_rn(f[i], f[i + 1]);
+      else *reinterpret_cast<__half2*>(&v.v[i]) = __floats2half2_rn(f[i], f[i + 1]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v.v[i] = from_f32<T>(f[i]);
+  }
+  return v;
+}
+
+// hardware approximations (2 units in the last place or better; results below 2^-126 become 0)
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float rcp(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+constexpr float kLog2e = 1.4426950408889634f;
 
 // Element i of a parameter vector whose type is known at run time only.  Plain loads: the 16-bit forms of __ldg are
 // inline assembly that the compiler may execute ahead of the test that guards it, and a pointer may be null behind such a test.

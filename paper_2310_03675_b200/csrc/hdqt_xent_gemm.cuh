@@ -36,7 +36,6 @@ constexpr int X_SMEM = X_STAGES * X_STAGE_BYTES + 256;
 constexpr int X_TMEM_COLS = 512;
 static_assert(X_SMEM <= 232448, "exceeds the 227 KB of shared memory a CTA may use");
 
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.402823466e38f;
 // Softmax codes: 16 bits of log2(max / value) with 2^-11 resolution.  The rounding is at most 2^-12 in log2, 1.7e-4
 // relative, a twelfth of the bf16 rounding that follows.  A value below 2^-32 of the largest of its 128 columns is held as 0:
@@ -123,12 +122,6 @@ __device__ __forceinline__ void st256(void* p, const uint32_t (&v)[8]) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]),
                "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
                : "memory");
-}
-
-__device__ __forceinline__ float ex2(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
