@@ -12,6 +12,8 @@
 //   backward : per piece of the vocabulary: logits product (dz from lse) -> dX (fp32 sums over the pieces) and dW
 #include <math.h>
 
+#include <atomic>
+
 #include "hdqt_xent_gemm.cuh"
 
 namespace hdqt {
@@ -22,16 +24,18 @@ constexpr int kRowThreads = 256;
 
 // ---- labels ------------------------------------------------------------------------------------------------
 
-// label[t] = class, -1 (ignored) or -2 (outside [0, classes)); scale[0] = weight of a row's loss in the reduced loss: 1 / kept rows
-// (mean) or 1; one block
-__global__ void __launch_bounds__(1024) xent_labels_kernel(const int64_t* __restrict__ labels, int64_t tokens, int64_t classes,
-                                                           int64_t ignore, int32_t mean, int32_t* __restrict__ label,
-                                                           float* __restrict__ scale, int32_t* dev_status) {
+// label[t] = class, -1 (ignored) or -2 (outside [0, classes)); scale[0] = 1 / kept rows (mean) or 1;
+// weight[t] = scale[0] times g[t] or g[0] (or 1 without g), the weight of a row's loss.  One block.
+__global__ void __launch_bounds__(1024)
+xent_labels_kernel(const int64_t* __restrict__ labels, int64_t tokens, int64_t classes, int64_t ignore, int32_t mean,
+                   const float* __restrict__ g, int32_t g_rows, int32_t* __restrict__ label, float* __restrict__ weight,
+                   float* __restrict__ scale, int32_t* dev_status) {
   __shared__ int s_kept;
   if (threadIdx.x == 0) s_kept = 0;
   __syncthreads();
   int kept = 0;
   bool bad = false;
+#pragma unroll 4
   for (int64_t t = threadIdx.x; t < tokens; t += blockDim.x) {
     const int64_t l = labels[t];
     int32_t v = -1;
@@ -42,10 +46,18 @@ __global__ void __launch_bounds__(1024) xent_labels_kernel(const int64_t* __rest
     }
     label[t] = v;
   }
-  atomicAdd(&s_kept, kept);
+  if (mean) {
+    kept = __reduce_add_sync(0xFFFFFFFFu, kept);
+    if ((threadIdx.x & 31) == 0) atomicAdd(&s_kept, kept);
+  }
   if (bad) report_status(dev_status, HDQT_ERR_INVALID_ARG);
   __syncthreads();
-  if (threadIdx.x == 0) scale[0] = mean ? 1.0f / (float)s_kept : 1.0f;
+  const float sc = mean ? 1.0f / (float)s_kept : 1.0f;
+  if (threadIdx.x == 0) scale[0] = sc;
+  if (weight != nullptr) {
+#pragma unroll 4
+    for (int64_t t = threadIdx.x; t < tokens; t += blockDim.x) weight[t] = (g != nullptr ? g[g_rows ? t : 0] : 1.0f) * sc;
+  }
 }
 
 // ---- rows: joining the parts of the softmax statistics -------------------------------------------------------
@@ -110,13 +122,6 @@ __global__ void __launch_bounds__(1024) xent_loss_kernel(const float* __restrict
     for (int w = 0; w < 32; ++w) s += s_part[w];
     loss[0] = (float)(s * (double)scale[0]);
   }
-}
-
-// weights of the rows' losses: g[row] or g[0] (or 1), times scale[0]
-__global__ void xent_weights_kernel(const float* __restrict__ g, int g_rows, const float* __restrict__ scale, int64_t n,
-                                    float* __restrict__ w) {
-  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  if (i < n) w[i] = (g != nullptr ? g[g_rows ? i : 0] : 1.0f) * scale[0];
 }
 
 // Training: one block per row joins the row's parts, writes lse and the loss, and turns the row's codes (or fp32
@@ -294,7 +299,14 @@ hdqt_status_t launch(XParams& p, const Product* g, int n, cudaStream_t s) {
   if (sms < 2) return HDQT_ERR_CUDA;
   const int items = p.pr[0].items + (n > 1 ? p.pr[1].items : 0);
   const int pairs = items < sms / 2 ? items : sms / 2;
-  cudaError_t e = cudaFuncSetAttribute(xent_gemm_kernel<kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, X_SMEM);
+  // the attribute holds per device for as long as the library is loaded: set at the kernel's first launch there
+  static std::atomic<uint64_t> ready{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && (dev > 63 || !((ready.load(std::memory_order_relaxed) >> dev) & 1))) {
+    e = cudaFuncSetAttribute(xent_gemm_kernel<kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, X_SMEM);
+    if (e == cudaSuccess && dev <= 63) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
   if (e != cudaSuccess) return cuda_failure(e, "cross entropy product");
   xent_gemm_kernel<kEpi><<<2 * pairs, X_THREADS, X_SMEM, s>>>(maps[0], maps[1], maps[2], maps[3], p);
   e = cudaGetLastError();
@@ -448,8 +460,8 @@ struct Call {
 void fill_common(const Call& c, XParams* p) {
   memset(p, 0, sizeof(*p));
   p->planes = c.pl.planes;
-  // stages per part: 1024 additions of 16 products for bf16 results, 64 where fp32 precision is to be kept
-  p->part_iters = c.pl.planes == 1 ? 256 : 16;
+  // stages per part: 1024 additions of 16 products for bf16 results, 32 where fp32 precision is to be kept
+  p->part_iters = c.pl.planes == 1 ? 256 : 8;
   p->dev_status = c.dev_status;
 }
 
@@ -488,7 +500,7 @@ hdqt_status_t stage(const Call& c, const void* src, int64_t ld, int64_t rows, in
   return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy operands");
 }
 
-hdqt_status_t prepare(Call* c, const void* X, const void* W, const int64_t* labels, bool mean) {
+hdqt_status_t prepare(Call* c, const void* X, const void* W, const int64_t* labels, const float* g, bool gradients) {
   const hdqt_xent_desc_t& d = *c->d;
   const Plan& pl = c->pl;
   c->x = Operand{X, d.features, d.tokens, d.ld_x, 0, pl.planes};
@@ -497,8 +509,9 @@ hdqt_status_t prepare(Call* c, const void* X, const void* W, const int64_t* labe
   if (pl.stage_x) st = stage(*c, X, d.ld_x, d.tokens, d.features, pl.xs, pl.ld_xs, &c->x);
   if (st == HDQT_OK && pl.stage_w) st = stage(*c, W, d.ld_w, pl.w_rows, pl.w_cols, pl.ws, pl.ld_ws, &c->w);
   if (st != HDQT_OK) return st;
-  xent_labels_kernel<<<1, 1024, 0, c->s>>>(labels, d.tokens, d.classes, d.ignore_index, mean, c->at<int32_t>(pl.label),
-                                           c->at<float>(pl.scale), c->dev_status);
+  xent_labels_kernel<<<1, d.tokens > 512 ? 1024 : 256, 0, c->s>>>(
+      labels, d.tokens, d.classes, d.ignore_index, d.reduction == HDQT_REDUCE_MEAN, g, d.reduction == HDQT_REDUCE_NONE,
+      c->at<int32_t>(pl.label), gradients ? c->at<float>(pl.weight) : nullptr, c->at<float>(pl.scale), c->dev_status);
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy labels");
 }
@@ -588,12 +601,6 @@ hdqt_status_t reduce_loss(const Call& c, float* loss) {
   return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy loss");
 }
 
-// weights of the rows' losses in the workspace
-void weights(const Call& c, const float* g) {
-  xent_weights_kernel<<<(unsigned)ceil_div(c.d->tokens, 256), 256, 0, c.s>>>(
-      g, c.d->reduction == HDQT_REDUCE_NONE, c.at<float>(c.pl.scale), c.d->tokens, c.at<float>(c.pl.weight));
-}
-
 bool outputs_misaligned(const hdqt_xent_desc_t* d, const void* a, const void* b) {
   return ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) & (uintptr_t)(dtype_size(d->dtype) - 1)) != 0;
 }
@@ -620,7 +627,7 @@ extern "C" hdqt_status_t hdqt_linear_xent_fwd(const hdqt_xent_desc_t* d, const v
   if (st != HDQT_OK) return st;
   if ((d->tokens > 0 && !lse) || (!loss && (d->tokens > 0 || d->reduction != HDQT_REDUCE_NONE))) return HDQT_ERR_INVALID_ARG;
   if (floats_misaligned(loss, lse, nullptr)) return HDQT_ERR_ALIGNMENT;
-  st = prepare(&c, X, W, labels, d->reduction == HDQT_REDUCE_MEAN);
+  st = prepare(&c, X, W, labels, nullptr, false);
   if (st != HDQT_OK) return st;
   float* rows = d->reduction == HDQT_REDUCE_NONE ? loss : c.at<float>(c.pl.loss_rows);
   for (int64_t t0 = 0; t0 < d->tokens; t0 += c.pl.rows_piece) {
@@ -651,9 +658,8 @@ extern "C" hdqt_status_t hdqt_linear_xent_bwd(const hdqt_xent_desc_t* d, const v
   if (floats_misaligned(lse, gr, nullptr) || outputs_misaligned(d, dX, dW)) return HDQT_ERR_ALIGNMENT;
   if (!dX && !dW) return HDQT_OK;
   if (d->tokens == 0) return dW ? zero_out(c, dW, c.pl.w_rows, c.pl.w_cols, d->ld_dw) : HDQT_OK;
-  st = prepare(&c, X, W, labels, d->reduction == HDQT_REDUCE_MEAN);
+  st = prepare(&c, X, W, labels, gr, true);
   if (st != HDQT_OK) return st;
-  weights(c, gr);
   for (int64_t v0 = 0; v0 < d->classes; v0 += c.pl.cols_piece) {
     const int64_t nv = d->classes - v0 < c.pl.cols_piece ? d->classes - v0 : c.pl.cols_piece;
     const Product g = logits_product(c, 0, d->tokens, v0, nv);
@@ -686,13 +692,12 @@ extern "C" hdqt_status_t hdqt_linear_xent_train(const hdqt_xent_desc_t* d, const
   if ((d->tokens > 0 && !lse) || (!loss && (d->tokens > 0 || d->reduction != HDQT_REDUCE_NONE))) return HDQT_ERR_INVALID_ARG;
   if (d->tokens > 0 && d->reduction == HDQT_REDUCE_NONE && !gr) return HDQT_ERR_INVALID_ARG;
   if (floats_misaligned(loss, lse, gr) || outputs_misaligned(d, dX, dW)) return HDQT_ERR_ALIGNMENT;
-  st = prepare(&c, X, W, labels, d->reduction == HDQT_REDUCE_MEAN);
+  st = prepare(&c, X, W, labels, gr, true);
   if (st != HDQT_OK) return st;
   if (d->tokens == 0) {
     if (dW) st = zero_out(c, dW, c.pl.w_rows, c.pl.w_cols, d->ld_dw);
     return st == HDQT_OK ? reduce_loss(c, loss) : st;
   }
-  weights(c, gr);
   float* rows = d->reduction == HDQT_REDUCE_NONE ? loss : c.at<float>(c.pl.loss_rows);
   for (int64_t t0 = 0; t0 < d->tokens; t0 += c.pl.rows_piece) {
     const int64_t nt = d->tokens - t0 < c.pl.rows_piece ? d->tokens - t0 : c.pl.rows_piece;

@@ -6,6 +6,7 @@ CPU fallback: if the library cannot be loaded, importing this module fails.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import os
 from typing import Optional
@@ -163,7 +164,14 @@ def _check(status: int, where: str) -> None:
         raise HdqtError(status, where)
 
 
+# the raw handle of the current stream without a Stream object around it (0.2 us instead of 3 per call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream() -> int:
+    if _raw_stream is not None and _raw_device is not None:
+        return _raw_stream(_raw_device())
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -477,27 +485,30 @@ def mma_rate_tops(iters: int = 20000, repeats: int = 3, dev_status=None) -> floa
 # ---- the rest of a training step: gradient clipping, group norm --------------------------------------
 
 def _tensor_table(tensors, out):
-    """hdqt_tensor_t[len(tensors)] as a flat int64 array (source, destination, elements, type)."""
-    flat = []
-    dev = None
-    for i, t in enumerate(tensors):
-        code = DTYPE_CODES.get(t.dtype)
-        if code is None or not t.is_cuda or not t.is_contiguous():
-            raise ValueError(f"tensor {i}: expected a dense fp32, bf16 or fp16 CUDA tensor")
-        if dev is None:
-            dev = t.device
-        elif t.device != dev:
-            raise ValueError("the tensors must be on one device")
-        at = t.data_ptr()
-        flat += (at, at, t.numel(), code)
+    """hdqt_tensor_t[len(tensors)] as a flat int64 array (source, destination, elements, type), and the device.  One pass
+    per property: a model has hundreds of tensors, and this is most of the call's host time."""
+    n = len(tensors)
+    codes = [DTYPE_CODES.get(t.dtype) for t in tensors]
+    sizes = [t.numel() for t in tensors]
+    at = [t.data_ptr() for t in tensors]
+    devices = {t.get_device() for t in tensors}
+    if None in codes or -1 in devices or not all([t.is_contiguous() for t in tensors]):
+        raise ValueError("expected dense fp32, bf16 or fp16 CUDA tensors")
+    to = at
     if out is not None:
-        if len(out) != len(tensors):
-            raise ValueError("out must hold one tensor per input")
-        for i, (t, o) in enumerate(zip(tensors, out)):
-            if o.dtype != t.dtype or o.shape != t.shape or o.device != t.device or not o.is_contiguous():
-                raise ValueError(f"out[{i}] must be a dense tensor of the type and shape of its input")
-            flat[4 * i + 1] = o.data_ptr()
-    return (C.c_int64 * len(flat))(*flat), dev
+        if len(out) != n or [t.numel() for t in out] != sizes or [DTYPE_CODES.get(t.dtype) for t in out] != codes \
+                or not all([t.is_contiguous() for t in out]):
+            raise ValueError("out must hold a dense tensor of the type and size of each input")
+        devices.update([t.get_device() for t in out])
+        to = [t.data_ptr() for t in out]
+    if len(devices) > 1:
+        raise ValueError("the tensors must be on one device")
+    table = array.array("q", bytes(32 * n))
+    table[0::4] = array.array("q", at)
+    table[1::4] = array.array("q", to)
+    table[2::4] = array.array("q", sizes)
+    table[3::4] = array.array("q", codes)
+    return table, torch.device("cuda", devices.pop()) if devices else None
 
 
 def _norm_code(norm_type) -> int:
@@ -513,9 +524,11 @@ def grad_norm(tensors, norm_type: float = 2.0, device=None) -> torch.Tensor:
     tensors = list(tensors)
     code = _norm_code(norm_type)
     table, dev = _tensor_table(tensors, None)
-    norm = torch.empty((), dtype=torch.float32, device=dev if dev is not None else device or "cuda")
-    ws = torch.empty(lib.hdqt_grad_norm_workspace_bytes(len(tensors)), dtype=torch.uint8, device=norm.device)
-    _check(lib.hdqt_grad_norm(C.addressof(table), len(tensors), code, norm.data_ptr(), ws.data_ptr(), ws.numel(),
+    dev = dev if dev is not None else torch.device(device or "cuda")
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    nbytes = lib.hdqt_grad_norm_workspace_bytes(len(tensors))
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    _check(lib.hdqt_grad_norm(table.buffer_info()[0], len(tensors), code, norm.data_ptr(), ws.data_ptr(), nbytes,
                               _stream()), "hdqt_grad_norm")
     return norm
 
@@ -526,10 +539,12 @@ def clip_grad_norm(tensors, max_norm: float, norm_type: float = 2.0, out=None, d
     tensors = list(tensors)
     code = _norm_code(norm_type)
     table, dev = _tensor_table(tensors, None if out is None else list(out))
-    norm = torch.empty((), dtype=torch.float32, device=dev if dev is not None else device or "cuda")
-    ws = torch.empty(lib.hdqt_grad_norm_workspace_bytes(len(tensors)), dtype=torch.uint8, device=norm.device)
-    _check(lib.hdqt_clip_grad_norm(C.addressof(table), len(tensors), code, max_norm, norm.data_ptr(), ws.data_ptr(),
-                                   ws.numel(), _stream()), "hdqt_clip_grad_norm")
+    dev = dev if dev is not None else torch.device(device or "cuda")
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    nbytes = lib.hdqt_grad_norm_workspace_bytes(len(tensors))
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    _check(lib.hdqt_clip_grad_norm(table.buffer_info()[0], len(tensors), code, max_norm, norm.data_ptr(), ws.data_ptr(),
+                                   nbytes, _stream()), "hdqt_clip_grad_norm")
     return norm
 
 
@@ -557,6 +572,7 @@ def _pixel_strides(t: torch.Tensor, name: str):
 
 
 def _group_norm_desc(x, gamma, beta, groups: int, eps: float, act: str):
+    """Checks, descriptor and workspace sizes of a call."""
     code = DTYPE_CODES.get(x.dtype)
     if code is None or not x.is_cuda:
         raise ValueError("expected an fp32, bf16 or fp16 CUDA tensor")
@@ -567,8 +583,8 @@ def _group_norm_desc(x, gamma, beta, groups: int, eps: float, act: str):
     for t in (gamma, beta):
         if t is None:
             continue
-        if t.shape != (channels,) or not t.is_contiguous() or t.device != x.device:
-            raise ValueError("gamma and beta must be dense [channels] tensors on x's device")
+        if t.shape != (channels,) or not t.is_contiguous():
+            raise ValueError("gamma and beta must be dense [channels] tensors")
         pdt = t.dtype
     if gamma is not None and beta is not None and gamma.dtype != beta.dtype:
         raise ValueError("gamma and beta must have one type")
@@ -580,40 +596,59 @@ def _group_norm_desc(x, gamma, beta, groups: int, eps: float, act: str):
     d = GroupNormDesc(x.shape[0], pixels, channels, groups, 0, 0, pixels * channels, channels, code, DTYPE_CODES[pdt],
                       ACT_CODES[act], eps)
     d.x_batch_stride, d.x_pixel_stride = _pixel_strides(x, "x")
-    return d
+    sizes = [max(256, lib.hdqt_group_norm_workspace_bytes(C.byref(d), i)) for i in (0, 1)]
+    return d, sizes
+
+
+_GROUP_NORM_PLANS = {}     # descriptor and workspace sizes by shapes, strides and types
+
+
+def _group_norm_plan(x, gamma, beta, groups, eps, act):
+    key = (x.shape, x.stride(), x.dtype, x.is_cuda, groups, eps, act,
+           None if gamma is None else (gamma.shape, gamma.dtype, gamma.is_contiguous()),
+           None if beta is None else (beta.shape, beta.dtype, beta.is_contiguous()))
+    plan = _GROUP_NORM_PLANS.get(key)
+    if plan is None:
+        if len(_GROUP_NORM_PLANS) >= 1024:
+            _GROUP_NORM_PLANS.clear()
+        plan = _GROUP_NORM_PLANS[key] = _group_norm_desc(x, gamma, beta, groups, eps, act)
+    dev = x.device
+    if (gamma is not None and gamma.device != dev) or (beta is not None and beta.device != dev):
+        raise ValueError("gamma and beta must be on x's device")
+    return plan
 
 
 def group_norm_fwd(x, gamma, beta, groups: int, eps: float = 1e-5, act: str = "none"):
     """act(group norm) of x[batch, ..., channels] (channels last, evenly spaced pixels: a channel slice is fine).
     gamma, beta: [channels], fp32 or x's type, or None.  act: "none", "relu" or "silu".
     Returns (y dense, mean fp32 [batch, groups], rstd fp32 [batch, groups])."""
-    d = _group_norm_desc(x, gamma, beta, groups, eps, act)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    stats = torch.empty((2, d.batch, max(groups, 0)), dtype=torch.float32, device=x.device)
-    mean, rstd = stats[0], stats[1]
-    ws = torch.empty(max(256, lib.hdqt_group_norm_workspace_bytes(C.byref(d), 0)), dtype=torch.uint8, device=x.device)
-    _check(lib.hdqt_group_norm_fwd(C.byref(d), x.data_ptr(), _ptr(gamma), _ptr(beta), y.data_ptr(),
-                                   stats.data_ptr(), stats.data_ptr() + 4 * mean.numel(), ws.data_ptr(), ws.numel(),
-                                   _stream()), "hdqt_group_norm_fwd")
+    d, (nbytes, _) = _group_norm_plan(x, gamma, beta, groups, eps, act)
+    y = torch.empty_like(x, memory_format=torch.contiguous_format)
+    stats = x.new_empty((2, d.batch, max(groups, 0)), dtype=torch.float32)
+    mean, rstd = stats.unbind(0)
+    ws = x.new_empty(nbytes, dtype=torch.uint8)
+    _check(lib.hdqt_group_norm_fwd(C.byref(d), x.data_ptr(), _ptr(gamma), _ptr(beta), y.data_ptr(), mean.data_ptr(),
+                                   rstd.data_ptr(), ws.data_ptr(), nbytes, _stream()), "hdqt_group_norm_fwd")
     return y, mean, rstd
 
 
 def group_norm_bwd(dy, x, gamma, beta, mean, rstd, groups: int, act: str = "none", want_dx: bool = True,
                    want_params: bool = True):
     """Gradients of group_norm_fwd: (dx dense or None, dgamma or None, dbeta or None)."""
-    d = _group_norm_desc(x, gamma, beta, groups, 0.0, act)
+    d, (_, nbytes) = _group_norm_plan(x, gamma, beta, groups, 0.0, act)
     if dy.shape != x.shape or dy.dtype != x.dtype or dy.device != x.device:
         raise ValueError("dy must have x's shape, type and device")
-    if tuple(mean.shape) != (d.batch, groups) or mean.shape != rstd.shape or mean.dtype != torch.float32 \
+    if mean.shape != (d.batch, groups) or mean.shape != rstd.shape or mean.dtype != torch.float32 \
             or rstd.dtype != torch.float32 or not (mean.is_contiguous() and rstd.is_contiguous()):
         raise ValueError("mean and rstd must be the dense fp32 [batch, groups] tensors of the forward call")
-    dy = dy.contiguous()
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if want_dx else None
+    if not dy.is_contiguous():
+        dy = dy.contiguous()
+    dx = torch.empty_like(x, memory_format=torch.contiguous_format) if want_dx else None
     dgamma = torch.empty_like(gamma) if want_params and gamma is not None else None
     dbeta = torch.empty_like(beta) if want_params and beta is not None else None
-    ws = torch.empty(max(256, lib.hdqt_group_norm_workspace_bytes(C.byref(d), 1)), dtype=torch.uint8, device=x.device)
+    ws = x.new_empty(nbytes, dtype=torch.uint8)
     _check(lib.hdqt_group_norm_bwd(C.byref(d), dy.data_ptr(), x.data_ptr(), _ptr(gamma), _ptr(beta), mean.data_ptr(),
-                                   rstd.data_ptr(), _ptr(dx), _ptr(dgamma), _ptr(dbeta), ws.data_ptr(), ws.numel(),
+                                   rstd.data_ptr(), _ptr(dx), _ptr(dgamma), _ptr(dbeta), ws.data_ptr(), nbytes,
                                    _stream()), "hdqt_group_norm_bwd")
     return dx, dgamma, dbeta
 
@@ -638,22 +673,33 @@ def _ld(t) -> int:
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
+_XENT_PLANS = {}     # descriptor and workspace size by sizes, strides, types and options
+
+
 def _xent_call(X, W, labels, ignore_index, reduction, w_is_cd, piece_bytes, kind):
     X, W = _rows(X, "X"), _rows(W, "W")
-    if reduction not in REDUCE_CODES:
-        raise ValueError(f"reduction must be one of {sorted(REDUCE_CODES)}")
-    T, D = X.shape
-    V = W.shape[0] if w_is_cd else W.shape[1]
-    if W.shape[1 if w_is_cd else 0] != D or W.dtype != X.dtype or W.device != X.device:
-        raise ValueError("X [tokens, features] and W must agree in features, type and device")
-    if labels.shape != (T,) or labels.dtype != torch.int64 or labels.device != X.device:
-        raise ValueError("labels must be an int64 [tokens] tensor on X's device")
-    labels = labels.contiguous()
-    d = XentDesc(T, D, V, max(_ld(X), D), max(_ld(W), W.shape[1]), D, W.shape[1], ignore_index, piece_bytes,
-                 DTYPE_CODES[X.dtype], int(w_is_cd), REDUCE_CODES[reduction], 0)
-    nbytes = lib.hdqt_linear_xent_workspace_bytes(C.byref(d), kind)
-    ws = torch.empty(max(256, nbytes), dtype=torch.uint8, device=X.device)
-    return X, W, labels, d, ws
+    key = (X.shape, X.stride(), X.dtype, W.shape, W.stride(), W.dtype, ignore_index, reduction, w_is_cd, piece_bytes, kind)
+    plan = _XENT_PLANS.get(key)
+    if plan is None:
+        if reduction not in REDUCE_CODES:
+            raise ValueError(f"reduction must be one of {sorted(REDUCE_CODES)}")
+        T, D = X.shape
+        V = W.shape[0] if w_is_cd else W.shape[1]
+        if W.shape[1 if w_is_cd else 0] != D or W.dtype != X.dtype:
+            raise ValueError("X [tokens, features] and W must agree in features and type")
+        d = XentDesc(T, D, V, max(_ld(X), D), max(_ld(W), W.shape[1]), D, W.shape[1], ignore_index, piece_bytes,
+                     DTYPE_CODES[X.dtype], int(w_is_cd), REDUCE_CODES[reduction], 0)
+        if len(_XENT_PLANS) >= 1024:
+            _XENT_PLANS.clear()
+        plan = _XENT_PLANS[key] = (d, max(256, lib.hdqt_linear_xent_workspace_bytes(C.byref(d), kind)))
+    if W.device != X.device or labels.device != X.device:
+        raise ValueError("X, W and labels must be on one device")
+    if labels.dim() != 1 or labels.shape[0] != X.shape[0] or labels.dtype != torch.int64:
+        raise ValueError("labels must be an int64 [tokens] tensor")
+    if not labels.is_contiguous():
+        labels = labels.contiguous()
+    d, nbytes = plan
+    return X, W, labels, d, X.new_empty(nbytes, dtype=torch.uint8), nbytes
 
 
 def _loss_weight(g, reduction, T, device):
@@ -672,11 +718,11 @@ def linear_xent_fwd(X, W, labels, ignore_index: int = -100, reduction: str = "me
     """Softmax cross entropy of X[tokens, features] times W ([features, classes], or [classes, features] with w_is_cd)
     against int64 labels; the logits are never stored.  bf16 or fp32.  Returns (loss: scalar, or [tokens] with reduction
     "none"; lse fp32 [tokens])."""
-    X, W, labels, d, ws = _xent_call(X, W, labels, ignore_index, reduction, w_is_cd, 0, XENT_FWD)
-    lse = torch.empty(d.tokens, dtype=torch.float32, device=X.device)
-    loss = torch.empty((d.tokens,) if reduction == "none" else (), dtype=torch.float32, device=X.device)
+    X, W, labels, d, ws, nbytes = _xent_call(X, W, labels, ignore_index, reduction, w_is_cd, 0, XENT_FWD)
+    lse = X.new_empty(d.tokens, dtype=torch.float32)
+    loss = X.new_empty((d.tokens,) if reduction == "none" else (), dtype=torch.float32)
     _check(lib.hdqt_linear_xent_fwd(C.byref(d), X.data_ptr(), W.data_ptr(), labels.data_ptr(), loss.data_ptr(),
-                                    lse.data_ptr(), ws.data_ptr(), ws.numel(), _ptr(dev_status), _stream()),
+                                    lse.data_ptr(), ws.data_ptr(), nbytes, _ptr(dev_status), _stream()),
            "hdqt_linear_xent_fwd")
     return loss, lse
 
@@ -686,14 +732,14 @@ def linear_xent_bwd(X, W, labels, lse, g=None, ignore_index: int = -100, reducti
     """Gradients (dX, dW; None if not wanted) of linear_xent_fwd's loss from its lse.  g: gradient of the loss, an fp32
     scalar (None = 1) or [tokens] with reduction "none".  Works through the vocabulary in pieces of piece_bytes (0 = chosen by
     the library)."""
-    X, W, labels, d, ws = _xent_call(X, W, labels, ignore_index, reduction, w_is_cd, piece_bytes, XENT_BWD)
+    X, W, labels, d, ws, nbytes = _xent_call(X, W, labels, ignore_index, reduction, w_is_cd, piece_bytes, XENT_BWD)
     g = _loss_weight(g, reduction, d.tokens, X.device)
     if tuple(lse.shape) != (d.tokens,) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != X.device:
         raise ValueError("lse must be the dense fp32 [tokens] tensor of the forward call")
-    dX = torch.empty(X.shape, dtype=X.dtype, device=X.device) if want_dx else None
-    dW = torch.empty(W.shape, dtype=W.dtype, device=W.device) if want_dw else None
+    dX = torch.empty_like(X, memory_format=torch.contiguous_format) if want_dx else None
+    dW = torch.empty_like(W, memory_format=torch.contiguous_format) if want_dw else None
     _check(lib.hdqt_linear_xent_bwd(C.byref(d), X.data_ptr(), W.data_ptr(), labels.data_ptr(), lse.data_ptr(), _ptr(g),
-                                    _ptr(dX), _ptr(dW), ws.data_ptr(), ws.numel(), _ptr(dev_status), _stream()),
+                                    _ptr(dX), _ptr(dW), ws.data_ptr(), nbytes, _ptr(dev_status), _stream()),
            "hdqt_linear_xent_bwd")
     return dX, dW
 
@@ -702,13 +748,13 @@ def linear_xent_train(X, W, labels, g=None, ignore_index: int = -100, reduction:
                       want_dx: bool = True, want_dw: bool = True, piece_bytes: int = 0, dev_status=None):
     """Loss and gradients in one call (two thirds of the tensor work of linear_xent_fwd + linear_xent_bwd), for a loss whose
     gradient is known beforehand: g as in linear_xent_bwd.  Returns (loss, lse, dX, dW)."""
-    X, W, labels, d, ws = _xent_call(X, W, labels, ignore_index, reduction, w_is_cd, piece_bytes, XENT_TRAIN)
+    X, W, labels, d, ws, nbytes = _xent_call(X, W, labels, ignore_index, reduction, w_is_cd, piece_bytes, XENT_TRAIN)
     g = _loss_weight(g, reduction, d.tokens, X.device)
-    lse = torch.empty(d.tokens, dtype=torch.float32, device=X.device)
-    loss = torch.empty((d.tokens,) if reduction == "none" else (), dtype=torch.float32, device=X.device)
-    dX = torch.empty(X.shape, dtype=X.dtype, device=X.device) if want_dx else None
-    dW = torch.empty(W.shape, dtype=W.dtype, device=W.device) if want_dw else None
+    lse = X.new_empty(d.tokens, dtype=torch.float32)
+    loss = X.new_empty((d.tokens,) if reduction == "none" else (), dtype=torch.float32)
+    dX = torch.empty_like(X, memory_format=torch.contiguous_format) if want_dx else None
+    dW = torch.empty_like(W, memory_format=torch.contiguous_format) if want_dw else None
     _check(lib.hdqt_linear_xent_train(C.byref(d), X.data_ptr(), W.data_ptr(), labels.data_ptr(), _ptr(g),
-                                      loss.data_ptr(), lse.data_ptr(), _ptr(dX), _ptr(dW), ws.data_ptr(), ws.numel(),
+                                      loss.data_ptr(), lse.data_ptr(), _ptr(dX), _ptr(dW), ws.data_ptr(), nbytes,
                                       _ptr(dev_status), _stream()), "hdqt_linear_xent_train")
     return loss, lse, dX, dW
