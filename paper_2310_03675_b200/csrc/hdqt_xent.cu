@@ -13,6 +13,7 @@
 #include <math.h>
 
 #include <atomic>
+#include <utility>
 
 #include "hdqt_xent_gemm.cuh"
 
@@ -218,11 +219,26 @@ __global__ void __launch_bounds__(256) xent_stage_kernel(const T* __restrict__ s
   }
 }
 
-// sum of the splits' partial outputs, in order
+// sum of the splits' partial outputs, in order; four elements of the flat [rows, cols] at a time
 template <typename T>
 __global__ void __launch_bounds__(256) xent_join_splits_kernel(const float* __restrict__ part, int splits, int64_t rows,
                                                                int64_t cols, T* __restrict__ out, int64_t ld) {
   const int64_t n = rows * cols;
+  const bool vec = n % 4 == 0 && cols % 4 == 0 && ld % 4 == 0 && (reinterpret_cast<uintptr_t>(out) & (4 * sizeof(T) - 1)) == 0;
+  if (vec) {
+    for (int64_t i = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x); i < n; i += 4 * (int64_t)gridDim.x * 256) {
+      float4 s = *reinterpret_cast<const float4*>(part + i);
+#pragma unroll 4
+      for (int k = 1; k < splits; ++k) {
+        const float4 v = *reinterpret_cast<const float4*>(part + k * n + i);
+        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+      }
+      const float f[4] = {s.x, s.y, s.z, s.w};
+      const int64_t r = i / cols;
+      *reinterpret_cast<Vec<T, 4>*>(out + r * ld + (i - r * cols)) = pack<T>(f);
+    }
+    return;
+  }
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
     float s = part[i];
     for (int k = 1; k < splits; ++k) s += part[k * n + i];
@@ -330,12 +346,24 @@ struct Plan {
 
 constexpr int64_t kPieceBytes = 1ll << 30;
 
-int choose_splits(int64_t kblocks, int64_t per_pair) {
-  // An item longer than half of what a pair has to do in all leaves the others waiting at the end; a split below 16 stages
-  // costs more to join than it saves.
-  const int64_t most = per_pair / 2 > 16 ? per_pair / 2 : 16;
-  const int64_t s = ceil_div(kblocks, most);
-  return (int)(s < 16 ? s : 16);
+// Work items along the contraction of a product of `blocks` output blocks of `kblocks` stages, next to `other` stages of
+// shorter items: the number with the shortest schedule on `pairs` CTA pairs.  A split adds one pass over fp32 partial
+// outputs (8 bytes per element at about 6 TB/s against 0.3 us per stage).
+int choose_splits(int64_t blocks, int64_t kblocks, int64_t elements, int64_t other, int64_t pairs) {
+  int best = 1;
+  double best_time = 0.0;
+  for (int s = 1; s <= 16; ++s) {
+    const int64_t len = ceil_div(kblocks, s), items = blocks * s;
+    if (s > 1 && len < 16) break;
+    const int64_t whole = items / pairs, more = items % pairs;
+    const double mean = (double)(items * len + other) / (double)pairs;
+    const double longest = (double)((whole + (more > 0)) * len);
+    // the pairs with one item fewer fill up with the other product's items
+    const bool filled = other >= (more > 0 ? (pairs - more) * len : 0);
+    const double time = (filled && mean > len ? mean : longest > mean ? longest : mean) + (s > 1 ? (double)elements * s * 8 / 6e12 / 0.3e-6 + 10.0 : 0.0);
+    if (s == 1 || time < best_time) { best = s; best_time = time; }
+  }
+  return best;
 }
 
 hdqt_status_t make_plan(const hdqt_xent_desc_t* d, int kind, Plan* pl) {
@@ -385,13 +413,12 @@ hdqt_status_t make_plan(const hdqt_xent_desc_t* d, int kind, Plan* pl) {
   pl->parts_ld = ceil_div(V, XN) * 2;
   pl->acc_dw = kind == HDQT_XENT_TRAIN && pl->rows_piece < T;
   pl->acc_dx = kind == HDQT_XENT_BWD && pl->cols_piece < V;
-  const int64_t sms = 148;
+  const int64_t pairs = kNumSMsHint / 2;
   const int64_t dx_blocks = ceil_div(pl->rows_piece, XM) * ceil_div(D, XN), dx_k = ceil_div(pl->cols_piece, XK);
   const int64_t dw_blocks = ceil_div(pl->cols_piece, XM) * ceil_div(D, XN), dw_k = ceil_div(pl->rows_piece, XK);
-  const int64_t per_pair = (dx_blocks * dx_k + dw_blocks * dw_k) / (sms / 2);
   const bool whole = !pl->acc_dx && !pl->acc_dw;
-  pl->splits_dx = whole ? choose_splits(dx_k, per_pair) : 1;
-  pl->splits_dw = whole ? choose_splits(dw_k, per_pair) : 1;
+  pl->splits_dx = whole ? choose_splits(dx_blocks, dx_k, pl->rows_piece * D, dw_blocks * dw_k, pairs) : 1;
+  pl->splits_dw = whole ? choose_splits(dw_blocks, dw_k, pl->cols_piece * D, dx_blocks * dx_k, pairs) : 1;
 
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o += up256(bytes); return at; };
@@ -570,18 +597,25 @@ hdqt_status_t gradient_products(const Call& c, int64_t t0, int64_t nt, int64_t v
     ++n;
   }
   if (n == 0) return HDQT_OK;
-  hdqt_status_t st = launch<X_OUT>(p, g, n, c.s);
-  if (st != HDQT_OK) return st;
-  int i = 0;
   auto join = [&](const XProblem& r, void* out, int64_t ld, size_t off) {
     if (r.splits <= 1) return;
-    const int64_t blocks = ceil_div((int64_t)r.M * r.N, 256);
-    const unsigned grid = (unsigned)(blocks < 148 * 16 ? blocks : 148 * 16);
+    const int64_t blocks = ceil_div((int64_t)r.M * r.N, 1024);
+    const unsigned grid = (unsigned)(blocks < 148 * 8 ? blocks : 148 * 8);
     if (bf16) xent_join_splits_kernel<<<grid, 256, 0, c.s>>>(c.at<float>(off), r.splits, r.M, r.N, reinterpret_cast<__nv_bfloat16*>(out), ld);
     else xent_join_splits_kernel<<<grid, 256, 0, c.s>>>(c.at<float>(off), r.splits, r.M, r.N, reinterpret_cast<float*>(out), ld);
   };
-  if (dX) join(p.pr[i++], dX, d.ld_dx, pl.dx_f32);
-  if (dW) join(p.pr[i], dW, d.ld_dw, pl.dw_f32);
+  const XProblem first_problem = p.pr[0], second_problem = p.pr[n - 1];
+  if (n == 2) {
+    if (p.pr[1].kblocks_split > p.pr[0].kblocks_split) {      // the longer items first
+      std::swap(p.pr[0], p.pr[1]);
+      std::swap(g[0], g[1]);
+    }
+    p.extra = p.pr[0].kblocks_split / p.pr[1].kblocks_split;
+  }
+  const hdqt_status_t st = launch<X_OUT>(p, g, n, c.s);
+  if (st != HDQT_OK) return st;
+  if (dX) join(first_problem, dX, d.ld_dx, pl.dx_f32);
+  if (dW) join(second_problem, dW, d.ld_dw, pl.dw_f32);
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy gradients");
 }

@@ -71,6 +71,7 @@ struct XProblem {
 struct XParams {
   XProblem pr[2];
   int32_t num_problems;
+  int32_t extra;                   // see x_item
   int32_t planes;                  // 1 or 3
   int32_t part_iters;
   // statistics and dz epilogues
@@ -95,13 +96,16 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap
       : "memory");
 }
 
-__device__ __forceinline__ void tc_mma_bf16_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
-                                                 uint32_t accumulate) {
+// Descriptors as their two words: along a contraction only the address field of the low word moves.
+__device__ __forceinline__ void tc_mma_bf16_pair(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi,
+                                                 uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+      "mov.b64 a, {%1, %2};\n\t"
+      "mov.b64 b, {%3, %4};\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %5, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
       : "memory");
 }
 
@@ -147,10 +151,25 @@ struct XItem {
   int q;                         // problem
 };
 
-__device__ __forceinline__ XItem x_item(const XParams& p, int i) {
-  XItem t;
-  t.q = 0;
-  if (i >= p.pr[0].items) { t.q = 1; i -= p.pr[0].items; }
+// k-th work item of this pair, or false.  Items of problem 0 (the longer ones) go round the pairs first; the pairs that get one
+// fewer of them take `extra` items of problem 1 in its place, and the rest go round all pairs.
+__device__ __forceinline__ bool x_item(const XParams& p, int pair, int pairs, int k, XItem& t) {
+  const int n0 = p.pr[0].items;
+  const int whole = n0 / pairs, more = n0 - whole * pairs;       // pairs below `more` have one item more
+  const int mine = whole + (pair < more ? 1 : 0);
+  int i;
+  if (k < mine) {
+    t.q = 0;
+    i = pair + k * pairs;
+  } else {
+    if (p.num_problems < 2) return false;
+    t.q = 1;
+    k -= mine;
+    const int low = pairs - more, given = p.extra * low;
+    if (pair >= more && k < p.extra) i = k * low + (pair - more);
+    else i = given + (k - (pair >= more ? p.extra : 0)) * pairs + (pair >= more ? pair - more : low + pair);
+    if (i >= p.pr[1].items) return false;
+  }
   const XProblem& r = p.pr[t.q];
   const int blocks = r.tiles_m * r.tiles_n;
   t.split = i / blocks;
@@ -164,7 +183,7 @@ __device__ __forceinline__ XItem x_item(const XParams& p, int i) {
   t.n = i / rows;
   t.kb0 = t.split * r.kblocks_split;
   t.nkb = min(r.kblocks_split, r.kblocks - t.kb0);
-  return t;
+  return true;
 }
 
 // ---- epilogues: one thread holds 128 consecutive columns of one row ----------------------------------------
@@ -289,14 +308,19 @@ __device__ __forceinline__ void x_out(const XProblem& r, const XItem& t, int row
   }
   if (r.out_bf16) {
     __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(r.out) + at;
-    const bool vec = ((reinterpret_cast<uintptr_t>(o) & 31) == 0);
+    const uintptr_t low = reinterpret_cast<uintptr_t>(o) & 31;      // rows of 16 bytes' multiples alternate between 0 and 16
 #pragma unroll
     for (int j = 0; j < 128; j += 16) {
-      if (vec && j + 16 <= ncols) {
+      if ((low & 15) == 0 && j + 16 <= ncols) {
         uint32_t v[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = pack_bf16(acc[j + 2 * k], acc[j + 2 * k + 1]);
-        st256(o + j, v);
+        if (low == 0) {
+          st256(o + j, v);
+        } else {
+          *reinterpret_cast<uint4*>(o + j) = make_uint4(v[0], v[1], v[2], v[3]);
+          *reinterpret_cast<uint4*>(o + j + 8) = make_uint4(v[4], v[5], v[6], v[7]);
+        }
       } else {
 #pragma unroll
         for (int k = 0; k < 16; ++k)
@@ -305,14 +329,19 @@ __device__ __forceinline__ void x_out(const XProblem& r, const XItem& t, int row
     }
   } else {
     float* o = reinterpret_cast<float*>(r.out) + at;
-    const bool vec = ((reinterpret_cast<uintptr_t>(o) & 31) == 0);
+    const uintptr_t low = reinterpret_cast<uintptr_t>(o) & 31;
 #pragma unroll
     for (int j = 0; j < 128; j += 8) {
-      if (vec && j + 8 <= ncols) {
+      if ((low & 15) == 0 && j + 8 <= ncols) {
         uint32_t v[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = __float_as_uint(acc[j + k]);
-        st256(o + j, v);
+        if (low == 0) {
+          st256(o + j, v);
+        } else {
+          *reinterpret_cast<uint4*>(o + j) = make_uint4(v[0], v[1], v[2], v[3]);
+          *reinterpret_cast<uint4*>(o + j + 4) = make_uint4(v[4], v[5], v[6], v[7]);
+        }
       } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k)
@@ -347,7 +376,6 @@ xent_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_consta
   const uint32_t cta_rank = cluster_ctarank();
   const bool leader = (cta_rank == 0);
   const int pair_id = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
-  const int num_items = p.pr[0].items + (p.num_problems > 1 ? p.pr[1].items : 0);
   const int products = p.planes == 1 ? 1 : 6;
 
   if (threadIdx.x == 0) {
@@ -381,8 +409,8 @@ xent_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_consta
       uint32_t it = 0;                // stages issued so far (for the drain after a timeout)
       uint32_t ps = 0, pe_par = 1u;   // stage slot and the parity its "empty" barrier is waited on with
       bool ok = true;
-      for (int i = pair_id; i < num_items && ok; i += num_pairs) {
-        const XItem t = x_item(p, i);
+      XItem t;
+      for (int i = 0; ok && x_item(p, pair_id, num_pairs, i, t); ++i) {
         const XProblem& r = p.pr[t.q];
         const CUtensorMap* ma = t.q ? &map_a1 : &map_a0;
         const CUtensorMap* mb = t.q ? &map_b1 : &map_b0;
@@ -421,19 +449,24 @@ xent_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_consta
   } else if (warp == 1) {
     // ------------------------------ MMA issuer (leader only) ------------------
     if (lane == 0 && leader) {
+      // The tensor pipe takes one MMA while it works on another, so what this thread does between two MMAs must fit into
+      // one MMA's time: low words of the descriptors by one addition each, one turn of the stage ring unrolled.
       uint32_t s = 0, full_par = 0u;
       int buf_i = 0;             // accumulators filled so far
       bool ok = true;
-      for (int i = pair_id; i < num_items && ok; i += num_pairs) {
-        const XItem t = x_item(p, i);
+      XItem t;
+      for (int i = 0; ok && x_item(p, pair_id, num_pairs, i, t); ++i) {
         const XProblem& r = p.pr[t.q];
         // instruction descriptor: D = f32, A = B = bf16, majors, N = 256, M = 256
         const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)r.a_mn << 15) | ((uint32_t)r.b_mn << 16) |
                                ((uint32_t)(XN >> 3) << 17) | ((uint32_t)(XM >> 4) << 24);
-        const uint64_t da0 = r.a_mn ? make_smem_desc_mn(smem_base, X_OPERAND / 2, 1024) : make_smem_desc(smem_base);
-        const uint64_t db0 = r.b_mn ? make_smem_desc_mn(smem_base + X_OPERAND, X_OPERAND / 2, 1024)
-                                    : make_smem_desc(smem_base + X_OPERAND);
-        const uint64_t ka = r.a_mn ? 2048 >> 4 : 32 >> 4, kb_step = r.b_mn ? 2048 >> 4 : 32 >> 4;   // per 16 k
+        const uint64_t da = r.a_mn ? make_smem_desc_mn(smem_base, X_OPERAND / 2, 1024) : make_smem_desc(smem_base);
+        const uint64_t db = r.b_mn ? make_smem_desc_mn(smem_base + X_OPERAND, X_OPERAND / 2, 1024)
+                                   : make_smem_desc(smem_base + X_OPERAND);
+        const uint32_t ah = (uint32_t)(da >> 32), bh = (uint32_t)(db >> 32);
+        const uint32_t ka = r.a_mn ? 2048 >> 4 : 32 >> 4, kb = r.b_mn ? 2048 >> 4 : 32 >> 4;   // per 16 k
+        const uint32_t a0 = (uint32_t)da, a1 = a0 + ka, a2 = a1 + ka, a3 = a2 + ka;
+        const uint32_t b0 = (uint32_t)db, b1 = b0 + kb, b2 = b1 + kb, b3 = b2 + kb;
         int left = t.nkb * products;
         while (left > 0 && ok) {
           const int n = min(left, p.part_iters);
@@ -442,16 +475,37 @@ xent_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_consta
           if (!mbar_wait(bar_tempty + 8 * buf, (((uint32_t)buf_i >> 1) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
           tc_fence_after();
           const uint32_t d_tmem = tmem_base + buf * XN;
-          for (int k = 0; k < n; ++k) {
+          uint32_t acc = 0u;
+          for (int k = 0; k < n;) {
+            if (s == 0 && k + X_STAGES <= n) {
+#pragma unroll
+              for (int j = 0; j < X_STAGES; ++j) {
+                if (!mbar_try_wait(bar_full + 8 * j, full_par) && !mbar_wait(bar_full + 8 * j, full_par, abort_flag)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t o = (uint32_t)(j * (X_STAGE_BYTES >> 4));
+                tc_mma_bf16_pair(d_tmem, a0 + o, ah, b0 + o, bh, idesc, acc);
+                tc_mma_bf16_pair(d_tmem, a1 + o, ah, b1 + o, bh, idesc, 1u);
+                tc_mma_bf16_pair(d_tmem, a2 + o, ah, b2 + o, bh, idesc, 1u);
+                tc_mma_bf16_pair(d_tmem, a3 + o, ah, b3 + o, bh, idesc, 1u);
+                acc = 1u;
+                tc_commit_pair(bar_empty + 8 * j);
+              }
+              if (!ok) break;
+              full_par ^= 1u;
+              k += X_STAGES;
+              continue;
+            }
             if (!mbar_try_wait(bar_full + 8 * s, full_par) && !mbar_wait(bar_full + 8 * s, full_par, abort_flag)) { ok = false; break; }
             tc_fence_after();
-            const uint64_t o = (uint64_t)(s * (X_STAGE_BYTES >> 4));
-            tc_mma_bf16_pair(d_tmem, da0 + o, db0 + o, idesc, k > 0 ? 1u : 0u);
-            tc_mma_bf16_pair(d_tmem, da0 + o + ka, db0 + o + kb_step, idesc, 1u);
-            tc_mma_bf16_pair(d_tmem, da0 + o + 2 * ka, db0 + o + 2 * kb_step, idesc, 1u);
-            tc_mma_bf16_pair(d_tmem, da0 + o + 3 * ka, db0 + o + 3 * kb_step, idesc, 1u);
+            const uint32_t o = s * (uint32_t)(X_STAGE_BYTES >> 4);
+            tc_mma_bf16_pair(d_tmem, a0 + o, ah, b0 + o, bh, idesc, acc);
+            tc_mma_bf16_pair(d_tmem, a1 + o, ah, b1 + o, bh, idesc, 1u);
+            tc_mma_bf16_pair(d_tmem, a2 + o, ah, b2 + o, bh, idesc, 1u);
+            tc_mma_bf16_pair(d_tmem, a3 + o, ah, b3 + o, bh, idesc, 1u);
+            acc = 1u;
             tc_commit_pair(bar_empty + 8 * s);
             if (++s == X_STAGES) { s = 0; full_par ^= 1u; }
+            ++k;
           }
           if (ok) tc_commit_pair(bar_tfull + 8 * buf);
           ++buf_i;
@@ -465,8 +519,8 @@ xent_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_consta
     const uint32_t tempty = map_to_cta(bar_tempty, 0);      // the leader's barriers, as cluster addresses
     int buf_i = 0;
     bool ok = true;
-    for (int i = pair_id; i < num_items && ok; i += num_pairs) {
-      const XItem t = x_item(p, i);
+    XItem t;
+    for (int i = 0; ok && x_item(p, pair_id, num_pairs, i, t); ++i) {
       const XProblem& r = p.pr[t.q];
       float acc[128];
       bool first = true;
