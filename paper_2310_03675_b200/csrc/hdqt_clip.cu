@@ -130,6 +130,7 @@ __device__ __forceinline__ double block_join(double v) {
 // partials[slot0 + block]: fp64 sum of squares, or the bit pattern of the maximum as a (whole) fp64 number
 template <int N, bool kInf>
 __global__ void __launch_bounds__(kThreads) grad_partial_kernel(const __grid_constant__ Table<N> t, double* __restrict__ partials) {
+  chain_wait();
   Acc<kInf> a;
   for (uint32_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
     const TableEntry& e = t.e[find_entry(t, c)];
@@ -160,6 +161,7 @@ __device__ __forceinline__ float join_partials(const double* __restrict__ partia
 
 template <bool kInf>
 __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const double* __restrict__ partials, int n, float* __restrict__ norm_out) {
+  chain_wait();
   const float norm = join_partials<kInf>(partials, n);
   if (threadIdx.x == 0) *norm_out = norm;
 }
@@ -168,11 +170,14 @@ template <int N, bool kInf>
 __global__ void __launch_bounds__(kThreads)
 grad_scale_kernel(const __grid_constant__ Table<N> t, const double* __restrict__ partials, int n, float max_norm,
                   float* __restrict__ norm_out) {
+  chain_wait();
   const float norm = join_partials<kInf>(partials, n);
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
   float f = max_norm / (norm + 1e-6f);
   if (f > 1.0f) f = 1.0f;      // (a NaN stays)
-  for (uint32_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+  // from the end: what the first pass read last is still in the L2
+  for (uint32_t i = blockIdx.x; i < t.chunks; i += gridDim.x) {
+    const uint32_t c = t.chunks - 1 - i;
     const TableEntry& e = t.e[find_entry(t, c)];
     if (f == 1.0f && e.src == e.dst) continue;
     const bool vec = ((reinterpret_cast<uintptr_t>(e.src) | reinterpret_cast<uintptr_t>(e.dst)) & 15) == 0;
@@ -220,15 +225,17 @@ hdqt_status_t run(const hdqt_tensor_t* tensors, int64_t count, bool clip, float 
   int n_part = 0;
   for (int64_t next = 0; uint32_t chunks = fill_table(tensors, count, &next, &t);) {
     const uint32_t grid = chunks < most ? chunks : most;
-    grad_partial_kernel<N, kInf><<<grid, kThreads, 0, s>>>(t, partials + n_part);
+    if (n_part == 0) grad_partial_kernel<N, kInf><<<grid, kThreads, 0, s>>>(t, partials);
+    else launch_chained(grad_partial_kernel<N, kInf>, grid, kThreads, 0, s, t, partials + n_part);
     n_part += (int)grid;
   }
   if (!clip || n_part == 0) {
-    grad_norm_kernel<kInf><<<1, kThreads, 0, s>>>(partials, n_part, norm_out);
+    if (n_part == 0) grad_norm_kernel<kInf><<<1, kThreads, 0, s>>>(partials, n_part, norm_out);
+    else launch_chained(grad_norm_kernel<kInf>, 1, kThreads, 0, s, partials, n_part, norm_out);
   } else {
     for (int64_t next = 0; uint32_t chunks = fill_table(tensors, count, &next, &t);) {
       const uint32_t grid = chunks < most ? chunks : most;
-      grad_scale_kernel<N, kInf><<<grid, kThreads, 0, s>>>(t, partials, n_part, max_norm, norm_out);
+      launch_chained(grad_scale_kernel<N, kInf>, grid, kThreads, 0, s, t, partials, n_part, max_norm, norm_out);
     }
   }
   const cudaError_t e = cudaGetLastError();

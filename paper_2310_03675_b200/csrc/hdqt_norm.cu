@@ -145,6 +145,7 @@ __device__ __forceinline__ float anchor(const NormParams& p, int64_t b, int g) {
 // chan[b, chunk, c] = (mean - anchor, M2) of the chunk's pixels
 template <typename T, int V>
 __global__ void __launch_bounds__(NT, 3) norm_stats_kernel(const NormParams p) {
+  chain_wait();
   __shared__ float s_mean[NT * V], s_m2[NT * V];
   const Column k = column_of<V>(p);
   const int64_t p0 = (int64_t)blockIdx.x * p.chunk_pixels;
@@ -210,6 +211,7 @@ __device__ __forceinline__ double block_sum(double v) {
 // one block per (image, group): joins the chunks' channel statistics
 template <typename T>
 __global__ void __launch_bounds__(NT) norm_join_stats_kernel(const NormParams p) {
+  chain_wait();
   const int64_t b = blockIdx.x / p.groups;
   const int g = (int)(blockIdx.x - b * p.groups);
   const float2* part = p.chan + b * p.chunks * p.channels + (int64_t)g * p.per_group;
@@ -239,6 +241,7 @@ __global__ void __launch_bounds__(NT) norm_join_stats_kernel(const NormParams p)
 
 template <typename T, int V>
 __global__ void __launch_bounds__(NT, 3) norm_apply_kernel(const NormParams p) {
+  chain_wait();
   const Column k = column_of<V>(p);
   if (!k.live) return;
   const int64_t p0 = (int64_t)blockIdx.x * p.chunk_pixels;
@@ -271,6 +274,7 @@ __global__ void __launch_bounds__(NT, 3) norm_apply_kernel(const NormParams p) {
 // chan[b, chunk, c] = (sum dz, sum dz xhat) of the chunk's pixels
 template <typename T, int V>
 __global__ void __launch_bounds__(NT, 2) norm_bwd_sums_kernel(const NormParams p) {
+  chain_wait();
   __shared__ float s_a[NT * V], s_b[NT * V];
   const Column k = column_of<V>(p);
   const int64_t p0 = (int64_t)blockIdx.x * p.chunk_pixels;
@@ -327,6 +331,7 @@ __global__ void __launch_bounds__(NT, 2) norm_bwd_sums_kernel(const NormParams p
 
 // one block per (image, group): group[b, g] = means of gamma dz and gamma dz xhat
 __global__ void __launch_bounds__(NT) norm_join_sums_kernel(const NormParams p) {
+  chain_wait();
   const int64_t b = blockIdx.x / p.groups;
   const int g = (int)(blockIdx.x - b * p.groups);
   const float2* part = p.chan + b * p.chunks * p.channels + (int64_t)g * p.per_group;
@@ -347,6 +352,7 @@ __global__ void __launch_bounds__(NT) norm_join_sums_kernel(const NormParams p) 
 
 template <typename T, int V>
 __global__ void __launch_bounds__(NT, 2) norm_bwd_apply_kernel(const NormParams p) {
+  chain_wait();
   const Column k = column_of<V>(p);
   if (!k.live) return;
   const int64_t p0 = (int64_t)blockIdx.x * p.chunk_pixels;
@@ -584,6 +590,7 @@ __global__ void __launch_bounds__(NT, 4) norm_fwd_cluster_kernel(const __grid_co
 template <typename T, int V, bool kOne>
 __global__ void __launch_bounds__(NT, 2) norm_bwd_cluster_kernel(const __grid_constant__ NormParams p) {
   extern __shared__ __align__(16) uint8_t smem[];
+  chain_wait();
   const Slab k = slab_of<V>(p);
   using A = Vec<T, V>;
   float2* s_part = reinterpret_cast<float2*>(smem);                // [j][row][column]
@@ -756,6 +763,7 @@ constexpr int kGradChannels = 8;
 __global__ void __launch_bounds__(NT) norm_param_grad_kernel(const float2* __restrict__ part, int64_t parts, int channels,
                                                              void* dgamma, void* dbeta, int32_t param_dtype) {
   __shared__ float2 s[NT / 32][kGradChannels];
+  chain_wait();
   const int lane = threadIdx.x & (kGradChannels - 1), row = threadIdx.x / kGradChannels;
   const int c = blockIdx.x * kGradChannels + lane;
   float a = 0.0f, b = 0.0f;
@@ -1030,8 +1038,8 @@ extern "C" hdqt_status_t hdqt_group_norm_fwd(const hdqt_group_norm_desc_t* d, co
   const dim3 grid = stream_grid(*d, pl);
   return with_type_and_width(d->dtype, vec, [&]<typename T, int V>() {
     norm_stats_kernel<T, V><<<grid, NT, 0, s>>>(p);
-    norm_join_stats_kernel<T><<<(unsigned)(d->batch * d->groups), NT, 0, s>>>(p);
-    norm_apply_kernel<T, V><<<grid, NT, 0, s>>>(p);
+    launch_chained(norm_join_stats_kernel<T>, (unsigned)(d->batch * d->groups), NT, 0, s, p);
+    launch_chained(norm_apply_kernel<T, V>, grid, NT, 0, s, p);
     return last_error("group norm");
   });
 }
@@ -1081,7 +1089,8 @@ extern "C" hdqt_status_t hdqt_group_norm_bwd(const hdqt_group_norm_desc_t* d, co
                                                    : launch_cluster<norm_bwd_cluster_kernel<T, V, false>>(p, dv, d->batch, s);
       if (e != HDQT_OK) return e;
       if (dgamma || dbeta)
-        norm_param_grad_kernel<<<param_blocks, NT, 0, s>>>(chan, d->batch * dv.cluster, (int)d->channels, dgamma, dbeta, d->param_dtype);
+        launch_chained(norm_param_grad_kernel, param_blocks, NT, 0, s, chan, d->batch * dv.cluster, (int)d->channels, dgamma, dbeta,
+                       d->param_dtype);
       return last_error("group norm gradient");
     });
   }
@@ -1089,11 +1098,12 @@ extern "C" hdqt_status_t hdqt_group_norm_bwd(const hdqt_group_norm_desc_t* d, co
   return with_type_and_width(d->dtype, vec, [&]<typename T, int V>() {
     norm_bwd_sums_kernel<T, V><<<grid, NT, 0, s>>>(p);
     if (dx) {
-      norm_join_sums_kernel<<<(unsigned)(d->batch * d->groups), NT, 0, s>>>(p);
-      norm_bwd_apply_kernel<T, V><<<grid, NT, 0, s>>>(p);
+      launch_chained(norm_join_sums_kernel, (unsigned)(d->batch * d->groups), NT, 0, s, p);
+      launch_chained(norm_bwd_apply_kernel<T, V>, grid, NT, 0, s, p);
     }
     if (dgamma || dbeta)
-      norm_param_grad_kernel<<<param_blocks, NT, 0, s>>>(chan, d->batch * pl.chunks, (int)d->channels, dgamma, dbeta, d->param_dtype);
+      launch_chained(norm_param_grad_kernel, param_blocks, NT, 0, s, chan, d->batch * pl.chunks, (int)d->channels, dgamma, dbeta,
+                     d->param_dtype);
     return last_error("group norm gradient");
   });
 }

@@ -98,6 +98,28 @@ __device__ __forceinline__ void store_param(void* p, int32_t dtype, int64_t i, f
   else reinterpret_cast<__half*>(p)[i] = from_f32<__half>(v);
 }
 
+// Programmatic dependent launch: the kernels of one call start while their predecessor runs and wait here for its results, so that
+// launch latency is paid once per call.  The first kernel of a call is launched the ordinary way (behind everything
+// before it); nothing may be read or written ahead of the wait.
+__device__ __forceinline__ void chain_wait() {
+  asm volatile("griddepcontrol.launch_dependents;");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+template <typename... P, typename... A>
+inline void launch_chained(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, A&&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  (void)cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);      // (a failure is left for cudaGetLastError)
+}
+
 inline int dtype_size(int64_t dtype) {   // 0 = unknown type
   return dtype == HDQT_DTYPE_F32 ? 4 : (dtype == HDQT_DTYPE_BF16 || dtype == HDQT_DTYPE_F16) ? 2 : 0;
 }

@@ -16,6 +16,8 @@
 #include <utility>
 
 #include "hdqt_xent_gemm.cuh"
+#include "hdqt_xent_few.cuh"
+#include "hdqt_xent_small.cuh"
 
 namespace hdqt {
 
@@ -32,6 +34,7 @@ xent_labels_kernel(const int64_t* __restrict__ labels, int64_t tokens, int64_t c
                    const float* __restrict__ g, int32_t g_rows, int32_t* __restrict__ label, float* __restrict__ weight,
                    float* __restrict__ scale, int32_t* dev_status) {
   __shared__ int s_kept;
+  chain_wait();
   if (threadIdx.x == 0) s_kept = 0;
   __syncthreads();
   int kept = 0;
@@ -92,6 +95,7 @@ __global__ void __launch_bounds__(kRowThreads) xent_rows_kernel(const float2* __
                                                                 const int32_t* __restrict__ label,
                                                                 const float* __restrict__ label_logit, int64_t rows,
                                                                 float* __restrict__ lse, float* __restrict__ loss) {
+  chain_wait();
   const int64_t row = (int64_t)blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
   if (row >= rows) return;
   const int lane = threadIdx.x & 31;
@@ -112,6 +116,7 @@ __global__ void __launch_bounds__(kRowThreads) xent_rows_kernel(const float2* __
 __global__ void __launch_bounds__(1024) xent_loss_kernel(const float* __restrict__ rows, int64_t n, const float* __restrict__ scale,
                                                          float* __restrict__ loss) {
   __shared__ double s_part[32];
+  chain_wait();
   double s = 0.0;
   for (int64_t i = threadIdx.x; i < n; i += blockDim.x) s += (double)rows[i];
 #pragma unroll
@@ -125,14 +130,15 @@ __global__ void __launch_bounds__(1024) xent_loss_kernel(const float* __restrict
   }
 }
 
-// Training: one block per row joins the row's parts, writes lse and the loss, and turns the row's codes (or fp32
-// logits) into dz = w (softmax - [label]): bf16 in place of the codes, or three bf16 planes.
+// Training: the blocks of a row (blockIdx.y: slices of the classes) join the row's parts, write lse and the loss, and turn
+// the row's codes (or fp32 logits) into dz = w (softmax - [label]): bf16 in place of the codes, or three bf16 planes.
 template <int kPlanes>
 __global__ void __launch_bounds__(kRowThreads)
 xent_dz_kernel(const float2* __restrict__ part, int parts, int64_t parts_ld, const int32_t* __restrict__ label,
                const float* __restrict__ label_logit, const float* __restrict__ weight, int64_t classes, void* z, int64_t ld,
                uint16_t* planes, int64_t plane, float* __restrict__ lse, float* __restrict__ loss) {
   __shared__ float s_m[kRowThreads / 32], s_s[kRowThreads / 32];
+  chain_wait();
   const int64_t row = blockIdx.x;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const float2* pr = part + row * parts_ld;
@@ -148,7 +154,7 @@ xent_dz_kernel(const float2* __restrict__ part, int parts, int64_t parts_ld, con
 #pragma unroll
   for (int w = 1; w < kRowThreads / 32; ++w) v = join(v, MaxSum{s_m[w], s_s[w]});
   const int32_t lab = label[row];
-  if (threadIdx.x == 0) {
+  if (threadIdx.x == 0 && blockIdx.y == 0) {
     const float l = v.m + logf(v.s);
     lse[row] = l;
     loss[row] = row_loss(lab, l, label_logit[row]);
@@ -159,7 +165,7 @@ xent_dz_kernel(const float2* __restrict__ part, int parts, int64_t parts_ld, con
   if (kPlanes == 1) {
     uint4* codes = reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(z) + row * ld);
 #pragma unroll 2
-    for (int j = threadIdx.x; j * 8 < classes; j += kRowThreads) {
+    for (int j = blockIdx.y * kRowThreads + threadIdx.x; j * 8 < classes; j += kRowThreads * gridDim.y) {
       uint4 c = codes[j];
       uint32_t* cw = reinterpret_cast<uint32_t*>(&c);
       const float f = keep ? ex2((pr[j >> 4].x - v.m) * kLog2e) * scale : 0.0f;   // NaN where the row has one
@@ -178,7 +184,7 @@ xent_dz_kernel(const float2* __restrict__ part, int parts, int64_t parts_ld, con
     const float4* logits = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(z) + row * ld);
     uint2* o = reinterpret_cast<uint2*>(planes + row * ld);
 #pragma unroll 2
-    for (int j = threadIdx.x; j * 4 < classes; j += kRowThreads) {
+    for (int j = blockIdx.y * kRowThreads + threadIdx.x; j * 4 < classes; j += kRowThreads * gridDim.y) {
       const float4 q = logits[j];
       float a[4] = {q.x, q.y, q.z, q.w}, p0[4], p1[4], p2[4];
 #pragma unroll
@@ -200,6 +206,7 @@ xent_dz_kernel(const float2* __restrict__ part, int parts, int64_t parts_ld, con
 template <typename T>
 __global__ void __launch_bounds__(256) xent_stage_kernel(const T* __restrict__ src, int64_t ld, int64_t rows, int64_t cols,
                                                          uint16_t* __restrict__ dst, int64_t ld_dst, int64_t plane) {
+  chain_wait();
   const int64_t c = 2 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
   if (c >= cols) return;
   for (int64_t r = blockIdx.y; r < rows; r += gridDim.y) {
@@ -223,6 +230,7 @@ __global__ void __launch_bounds__(256) xent_stage_kernel(const T* __restrict__ s
 template <typename T>
 __global__ void __launch_bounds__(256) xent_join_splits_kernel(const float* __restrict__ part, int splits, int64_t rows,
                                                                int64_t cols, T* __restrict__ out, int64_t ld) {
+  chain_wait();
   const int64_t n = rows * cols;
   const bool vec = n % 4 == 0 && cols % 4 == 0 && ld % 4 == 0 && (reinterpret_cast<uintptr_t>(out) & (4 * sizeof(T) - 1)) == 0;
   if (vec) {
@@ -249,6 +257,7 @@ __global__ void __launch_bounds__(256) xent_join_splits_kernel(const float* __re
 
 template <typename T>
 __global__ void __launch_bounds__(256) xent_zero_kernel(T* out, int64_t rows, int64_t cols, int64_t ld) {
+  chain_wait();
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * cols; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / cols;
     out[r * ld + (i - r * cols)] = from_f32<T>(0.0f);
@@ -303,8 +312,21 @@ XProblem make_problem(const Product& g, int splits) {
   return r;
 }
 
-template <int kEpi>
-hdqt_status_t launch(XParams& p, const Product* g, int n, cudaStream_t s) {
+// attribute of a kernel, per device and for as long as the library is loaded: set at its first launch there
+template <auto kernel>
+cudaError_t allow_smem(int bytes) {
+  static std::atomic<uint64_t> ready{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && (dev > 63 || !((ready.load(std::memory_order_relaxed) >> dev) & 1))) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && dev <= 63) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
+  return e;
+}
+
+template <int kEpi, typename C>
+hdqt_status_t launch(XParams& p, const Product* g, int n, const C& c) {
   CUtensorMap maps[4];
   for (int i = 0; i < n; ++i) {
     if (!make_map(&maps[2 * i], g[i].a, g[i].a_mn) || !make_map(&maps[2 * i + 1], g[i].b, g[i].b_mn)) return HDQT_ERR_CUDA;
@@ -315,16 +337,9 @@ hdqt_status_t launch(XParams& p, const Product* g, int n, cudaStream_t s) {
   if (sms < 2) return HDQT_ERR_CUDA;
   const int items = p.pr[0].items + (n > 1 ? p.pr[1].items : 0);
   const int pairs = items < sms / 2 ? items : sms / 2;
-  // the attribute holds per device for as long as the library is loaded: set at the kernel's first launch there
-  static std::atomic<uint64_t> ready{0};
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e == cudaSuccess && (dev > 63 || !((ready.load(std::memory_order_relaxed) >> dev) & 1))) {
-    e = cudaFuncSetAttribute(xent_gemm_kernel<kEpi>, cudaFuncAttributeMaxDynamicSharedMemorySize, X_SMEM);
-    if (e == cudaSuccess && dev <= 63) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
-  }
+  cudaError_t e = allow_smem<xent_gemm_kernel<kEpi>>(X_SMEM);
   if (e != cudaSuccess) return cuda_failure(e, "cross entropy product");
-  xent_gemm_kernel<kEpi><<<2 * pairs, X_THREADS, X_SMEM, s>>>(maps[0], maps[1], maps[2], maps[3], p);
+  c.run(xent_gemm_kernel<kEpi>, 2 * pairs, X_THREADS, X_SMEM, maps[0], maps[1], maps[2], maps[3], p);
   e = cudaGetLastError();
   return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy product");
 }
@@ -332,6 +347,9 @@ hdqt_status_t launch(XParams& p, const Product* g, int n, cudaStream_t s) {
 // Sizes and workspace of a call.
 struct Plan {
   int planes;
+  int small_rows;                       // > 0: small problem (hdqt_xent_small.cuh), tokens per block
+  size_t small_smem;
+  int few_tokens;                       // > 0: loss of a few tokens (hdqt_xent_few.cuh), tokens a thread accumulates
   bool stage_x, stage_w;
   int64_t ld_xs, ld_ws;                 // of the staged copies
   int64_t w_rows, w_cols;
@@ -345,6 +363,12 @@ struct Plan {
 };
 
 constexpr int64_t kPieceBytes = 1ll << 30;
+
+// Small problems: the rows kernel reads W from the L2 once per block and product, the tensor-core path costs five launches
+// and two pipelines' fill and drain whatever the size.
+constexpr int64_t kSmallTokens = 512, kSmallWeights = 1 << 18, kSmallWork = 1 << 25;
+constexpr size_t kSmallSmem = 100 << 10;
+constexpr int kFewBlocks = 4 * kNumSMsHint;      // most blocks of the few-token kernels
 
 // Work items along the contraction of a product of `blocks` output blocks of `kblocks` stages, next to `other` stages of
 // shorter items: the number with the shortest schedule on `pairs` CTA pairs.  A split adds one pass over fp32 partial
@@ -382,6 +406,23 @@ hdqt_status_t make_plan(const hdqt_xent_desc_t* d, int kind, Plan* pl) {
     return HDQT_ERR_UNSUPPORTED;
   const bool f32 = d->dtype == HDQT_DTYPE_F32;
   pl->planes = f32 ? 3 : 1;
+  pl->small_rows = 0;
+  if (d->tokens > 0 && d->tokens <= kSmallTokens && d->classes * d->features <= kSmallWeights &&
+      d->tokens * d->classes * d->features <= kSmallWork && d->piece_bytes == 0) {
+    int rows = d->tokens <= 2 * kNumSMsHint ? 1 : 2;
+    auto smem = [&](int r) { return sizeof(float) * (size_t)r * (size_t)(d->features + d->classes + kSmallThreads); };
+    if (smem(rows) > kSmallSmem) rows = 1;
+    if (smem(rows) <= kSmallSmem) {
+      pl->small_rows = rows;
+      pl->small_smem = smem(rows);
+    }
+  }
+  pl->few_tokens = 0;
+  if (kind == HDQT_XENT_FWD && pl->small_rows == 0 && d->tokens > 0 && d->tokens <= kFewTokens && d->piece_bytes == 0) {
+    int n = 1;
+    while (n < d->tokens) n *= 2;
+    if (4 * n * d->features <= kFewSmem) pl->few_tokens = n;
+  }
   pl->stage_x = f32 || d->ld_x % 8 != 0;
   pl->stage_w = f32 || d->ld_w % 8 != 0;
   pl->ld_xs = ceil_div(d->features, 8) * 8;
@@ -422,6 +463,18 @@ hdqt_status_t make_plan(const hdqt_xent_desc_t* d, int kind, Plan* pl) {
 
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o += up256(bytes); return at; };
+  if (pl->small_rows > 0) {
+    pl->loss_rows = take(4 * T);
+    pl->dz = kind == HDQT_XENT_FWD ? o : take(4 * T * V);
+    pl->total = o;
+    return HDQT_OK;
+  }
+  if (pl->few_tokens > 0) {
+    pl->label_logit = take(4 * T);
+    pl->part = take(sizeof(float2) * T * kFewBlocks);
+    pl->total = o;
+    return HDQT_OK;
+  }
   pl->label = take(4 * T);
   pl->scale = take(256);
   pl->label_logit = take(4 * T);
@@ -456,8 +509,18 @@ struct Call {
   cudaStream_t s;
   Operand x, w;          // as stored: x [tokens, features], w [w_rows, w_cols]
 
+  mutable bool started = false;
+
   template <typename T>
   T* at(size_t off) const { return reinterpret_cast<T*>(ws + off); }
+
+  // the call's kernels, in order: the first behind everything on the stream, the others chained to it
+  template <typename... P, typename... A>
+  void run(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, A&&... args) const {
+    if (started) launch_chained(kernel, grid, block, smem, s, args...);
+    else kernel<<<grid, block, smem, s>>>(static_cast<P>(args)...);
+    started = true;
+  }
 
   Operand x_rows(int64_t t0, int64_t n) const {
     Operand o = x;
@@ -520,9 +583,9 @@ hdqt_status_t stage(const Call& c, const void* src, int64_t ld, int64_t rows, in
   if (rows == 0) return HDQT_OK;
   const dim3 grid((unsigned)ceil_div(cols, 512), (unsigned)(rows < 16384 ? rows : 16384));
   if (c.d->dtype == HDQT_DTYPE_F32)
-    xent_stage_kernel<<<grid, 256, 0, c.s>>>(reinterpret_cast<const float*>(src), ld, rows, cols, dst, ld_dst, rows * ld_dst);
+    c.run(xent_stage_kernel<float>, grid, 256, 0, reinterpret_cast<const float*>(src), ld, rows, cols, dst, ld_dst, rows * ld_dst);
   else
-    xent_stage_kernel<<<grid, 256, 0, c.s>>>(reinterpret_cast<const __nv_bfloat16*>(src), ld, rows, cols, dst, ld_dst, 0);
+    c.run(xent_stage_kernel<__nv_bfloat16>, grid, 256, 0, reinterpret_cast<const __nv_bfloat16*>(src), ld, rows, cols, dst, ld_dst, 0);
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy operands");
 }
@@ -536,8 +599,7 @@ hdqt_status_t prepare(Call* c, const void* X, const void* W, const int64_t* labe
   if (pl.stage_x) st = stage(*c, X, d.ld_x, d.tokens, d.features, pl.xs, pl.ld_xs, &c->x);
   if (st == HDQT_OK && pl.stage_w) st = stage(*c, W, d.ld_w, pl.w_rows, pl.w_cols, pl.ws, pl.ld_ws, &c->w);
   if (st != HDQT_OK) return st;
-  xent_labels_kernel<<<1, d.tokens > 512 ? 1024 : 256, 0, c->s>>>(
-      labels, d.tokens, d.classes, d.ignore_index, d.reduction == HDQT_REDUCE_MEAN, g, d.reduction == HDQT_REDUCE_NONE,
+  c->run(xent_labels_kernel, 1, d.tokens > 512 ? 1024 : 256, 0, labels, d.tokens, d.classes, d.ignore_index, d.reduction == HDQT_REDUCE_MEAN, g, d.reduction == HDQT_REDUCE_NONE,
       c->at<int32_t>(pl.label), gradients ? c->at<float>(pl.weight) : nullptr, c->at<float>(pl.scale), c->dev_status);
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy labels");
@@ -601,8 +663,8 @@ hdqt_status_t gradient_products(const Call& c, int64_t t0, int64_t nt, int64_t v
     if (r.splits <= 1) return;
     const int64_t blocks = ceil_div((int64_t)r.M * r.N, 1024);
     const unsigned grid = (unsigned)(blocks < 148 * 8 ? blocks : 148 * 8);
-    if (bf16) xent_join_splits_kernel<<<grid, 256, 0, c.s>>>(c.at<float>(off), r.splits, r.M, r.N, reinterpret_cast<__nv_bfloat16*>(out), ld);
-    else xent_join_splits_kernel<<<grid, 256, 0, c.s>>>(c.at<float>(off), r.splits, r.M, r.N, reinterpret_cast<float*>(out), ld);
+    if (bf16) c.run(xent_join_splits_kernel<__nv_bfloat16>, grid, 256, 0, c.at<float>(off), r.splits, r.M, r.N, reinterpret_cast<__nv_bfloat16*>(out), ld);
+    else c.run(xent_join_splits_kernel<float>, grid, 256, 0, c.at<float>(off), r.splits, r.M, r.N, reinterpret_cast<float*>(out), ld);
   };
   const XProblem first_problem = p.pr[0], second_problem = p.pr[n - 1];
   if (n == 2) {
@@ -612,7 +674,7 @@ hdqt_status_t gradient_products(const Call& c, int64_t t0, int64_t nt, int64_t v
     }
     p.extra = p.pr[0].kblocks_split / p.pr[1].kblocks_split;
   }
-  const hdqt_status_t st = launch<X_OUT>(p, g, n, c.s);
+  const hdqt_status_t st = launch<X_OUT>(p, g, n, c);
   if (st != HDQT_OK) return st;
   if (dX) join(first_problem, dX, d.ld_dx, pl.dx_f32);
   if (dW) join(second_problem, dW, d.ld_dw, pl.dw_f32);
@@ -621,8 +683,8 @@ hdqt_status_t gradient_products(const Call& c, int64_t t0, int64_t nt, int64_t v
 }
 
 hdqt_status_t zero_out(const Call& c, void* out, int64_t rows, int64_t cols, int64_t ld) {
-  if (c.d->dtype == HDQT_DTYPE_BF16) xent_zero_kernel<<<148 * 4, 256, 0, c.s>>>(reinterpret_cast<__nv_bfloat16*>(out), rows, cols, ld);
-  else xent_zero_kernel<<<148 * 4, 256, 0, c.s>>>(reinterpret_cast<float*>(out), rows, cols, ld);
+  if (c.d->dtype == HDQT_DTYPE_BF16) c.run(xent_zero_kernel<__nv_bfloat16>, 148 * 4, 256, 0, reinterpret_cast<__nv_bfloat16*>(out), rows, cols, ld);
+  else c.run(xent_zero_kernel<float>, 148 * 4, 256, 0, reinterpret_cast<float*>(out), rows, cols, ld);
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy gradients");
 }
@@ -630,9 +692,117 @@ hdqt_status_t zero_out(const Call& c, void* out, int64_t rows, int64_t cols, int
 // reduced loss from the rows' losses (which are the result themselves without a reduction)
 hdqt_status_t reduce_loss(const Call& c, float* loss) {
   if (c.d->reduction != HDQT_REDUCE_NONE)
-    xent_loss_kernel<<<1, 1024, 0, c.s>>>(c.at<float>(c.pl.loss_rows), c.d->tokens, c.at<float>(c.pl.scale), loss);
+    c.run(xent_loss_kernel, 1, 1024, 0, c.at<float>(c.pl.loss_rows), c.d->tokens, c.at<float>(c.pl.scale), loss);
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy loss");
+}
+
+// A small problem in two launches.  kind as in the plan; lse_in for the backward call.
+template <typename T>
+hdqt_status_t run_small(const Call& c, int kind, const void* X, const void* W, const int64_t* labels, const float* lse_in,
+                        const float* g, float* loss, float* lse, void* dX, void* dW) {
+  const hdqt_xent_desc_t& d = *c.d;
+  const bool none = d.reduction == HDQT_REDUCE_NONE;
+  SmallParams p{};
+  p.x = X;
+  p.w = W;
+  p.labels = labels;
+  p.g = g;
+  p.lse_in = lse_in;
+  p.lse = lse;
+  p.loss_rows = kind == HDQT_XENT_BWD ? nullptr : none ? loss : c.at<float>(c.pl.loss_rows);
+  p.dz = dW ? c.at<float>(c.pl.dz) : nullptr;
+  p.dx = dX;
+  p.dw = dW;
+  p.loss = kind == HDQT_XENT_BWD || none ? nullptr : loss;
+  p.dev_status = c.dev_status;
+  p.ignore = d.ignore_index;
+  p.ld_x = d.ld_x;
+  p.ld_w = d.ld_w;
+  p.ld_dx = d.ld_dx;
+  p.ld_dw = d.ld_dw;
+  p.tokens = (int32_t)d.tokens;
+  p.features = (int32_t)d.features;
+  p.classes = (int32_t)d.classes;
+  p.w_is_cd = d.w_is_cd != 0;
+  p.g_rows = none;
+  p.mean = d.reduction == HDQT_REDUCE_MEAN;
+  const unsigned blocks = (unsigned)ceil_div(d.tokens, c.pl.small_rows);
+  cudaError_t e = c.pl.small_rows == 1 ? allow_smem<xent_small_rows_kernel<T, 1>>((int)kSmallSmem)
+                                       : allow_smem<xent_small_rows_kernel<T, 2>>((int)kSmallSmem);
+  if (e != cudaSuccess) return cuda_failure(e, "cross entropy");
+  if (c.pl.small_rows == 1) c.run(xent_small_rows_kernel<T, 1>, blocks, kSmallThreads, c.pl.small_smem, p);
+  else c.run(xent_small_rows_kernel<T, 2>, blocks, kSmallThreads, c.pl.small_smem, p);
+  if (dW || p.loss) {
+    const dim3 grid((dW ? (unsigned)ceil_div(d.features, 32) : 0) + 1, dW ? (unsigned)ceil_div(d.classes, 32) : 1);
+    c.run(xent_small_grad_kernel<T>, grid, kGradThreads, 0, p);
+  }
+  e = cudaGetLastError();
+  return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy");
+}
+
+template <typename T, int kT, int kV>
+cudaError_t run_few_kernel(const Call& c, const FewParams& p, int* blocks) {
+  const size_t smem = sizeof(float) * kT * (size_t)p.features;
+  const int per_sm = smem > (48 << 10) ? 2 : 4;
+  const int tile = c.d->w_is_cd ? 4 * kFewWarps : 8 * kV;
+  int64_t n = ceil_div(p.classes, tile);
+  *blocks = (int)(n < per_sm * kNumSMsHint ? n : per_sm * kNumSMsHint);
+  // whole rounds: every block the same number of tiles, if that can be had with little fewer blocks
+  const int64_t rounds = ceil_div(n, *blocks);
+  *blocks = (int)ceil_div(n, rounds);
+  cudaError_t e;
+  if (c.d->w_is_cd) {
+    e = allow_smem<xent_few_rows_kernel<T, kT, kV>>(kFewSmem);
+    if (e == cudaSuccess) c.run(xent_few_rows_kernel<T, kT, kV>, *blocks, kFewThreads, smem, p);
+  } else {
+    e = allow_smem<xent_few_columns_kernel<T, kT, kV>>(kFewSmem);
+    if (e == cudaSuccess) c.run(xent_few_columns_kernel<T, kT, kV>, *blocks, kFewThreads, smem, p);
+  }
+  return e;
+}
+
+template <typename T, int kV>
+cudaError_t run_few_tokens(const Call& c, const FewParams& p, int* blocks) {
+  switch (c.pl.few_tokens) {
+    case 1: return run_few_kernel<T, 1, kV>(c, p, blocks);
+    case 2: return run_few_kernel<T, 2, kV>(c, p, blocks);
+    case 4: return run_few_kernel<T, 4, kV>(c, p, blocks);
+    default: return run_few_kernel<T, 8, kV>(c, p, blocks);
+  }
+}
+
+// Loss of a few tokens in two launches.
+hdqt_status_t few(const Call& c, const void* X, const void* W, const int64_t* labels, float* loss, float* lse) {
+  const hdqt_xent_desc_t& d = *c.d;
+  FewParams p{};
+  p.x = X;
+  p.w = W;
+  p.labels = labels;
+  p.part = c.at<float2>(c.pl.part);
+  p.label_logit = c.at<float>(c.pl.label_logit);
+  p.ld_x = d.ld_x;
+  p.ld_w = d.ld_w;
+  p.tokens = (int32_t)d.tokens;
+  p.features = (int32_t)d.features;
+  p.classes = (int32_t)d.classes;
+  const int elem = dtype_size(d.dtype), vec = 16 / elem;
+  const bool wide = (reinterpret_cast<uintptr_t>(W) & 15) == 0 && d.ld_w % vec == 0 && c.pl.w_cols % vec == 0;
+  int blocks = 0;
+  cudaError_t e;
+  if (elem == 2) e = wide ? run_few_tokens<__nv_bfloat16, 8>(c, p, &blocks) : run_few_tokens<__nv_bfloat16, 1>(c, p, &blocks);
+  else e = wide ? run_few_tokens<float, 4>(c, p, &blocks) : run_few_tokens<float, 1>(c, p, &blocks);
+  if (e != cudaSuccess) return cuda_failure(e, "cross entropy of a few tokens");
+  c.run(xent_few_join_kernel, 1, kFewThreads, 0, p.part, blocks, p.label_logit, labels, p.tokens, p.classes, d.ignore_index,
+        d.reduction, lse, loss, c.dev_status);
+  e = cudaGetLastError();
+  return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy of a few tokens");
+}
+
+hdqt_status_t small(const Call& c, int kind, const void* X, const void* W, const int64_t* labels, const float* lse_in,
+                    const float* g, float* loss, float* lse, void* dX, void* dW) {
+  return c.d->dtype == HDQT_DTYPE_BF16 ? run_small<__nv_bfloat16>(c, kind, X, W, labels, lse_in, g, loss, lse, dX, dW)
+                                       : run_small<float>(c, kind, X, W, labels, lse_in, g, loss, lse, dX, dW);
 }
 
 bool outputs_misaligned(const hdqt_xent_desc_t* d, const void* a, const void* b) {
@@ -661,6 +831,8 @@ extern "C" hdqt_status_t hdqt_linear_xent_fwd(const hdqt_xent_desc_t* d, const v
   if (st != HDQT_OK) return st;
   if ((d->tokens > 0 && !lse) || (!loss && (d->tokens > 0 || d->reduction != HDQT_REDUCE_NONE))) return HDQT_ERR_INVALID_ARG;
   if (floats_misaligned(loss, lse, nullptr)) return HDQT_ERR_ALIGNMENT;
+  if (c.pl.small_rows > 0) return small(c, HDQT_XENT_FWD, X, W, labels, nullptr, nullptr, loss, lse, nullptr, nullptr);
+  if (c.pl.few_tokens > 0) return few(c, X, W, labels, loss, lse);
   st = prepare(&c, X, W, labels, nullptr, false);
   if (st != HDQT_OK) return st;
   float* rows = d->reduction == HDQT_REDUCE_NONE ? loss : c.at<float>(c.pl.loss_rows);
@@ -674,10 +846,9 @@ extern "C" hdqt_status_t hdqt_linear_xent_fwd(const hdqt_xent_desc_t* d, const v
     p.part = c.at<float2>(c.pl.part);
     p.parts_ld = c.pl.parts_ld;
     p.label_logit = c.at<float>(c.pl.label_logit) + t0;
-    st = launch<X_STATS>(p, &g, 1, c.s);
+    st = launch<X_STATS>(p, &g, 1, c);
     if (st != HDQT_OK) return st;
-    xent_rows_kernel<<<(unsigned)ceil_div(nt, kRowThreads / 32), kRowThreads, 0, c.s>>>(
-        p.part, (int)p.parts_ld, p.parts_ld, p.label, p.label_logit, nt, lse + t0, rows + t0);
+    c.run(xent_rows_kernel, (unsigned)ceil_div(nt, kRowThreads / 32), kRowThreads, 0, p.part, (int)p.parts_ld, p.parts_ld, p.label, p.label_logit, nt, lse + t0, rows + t0);
   }
   return reduce_loss(c, loss);
 }
@@ -692,6 +863,7 @@ extern "C" hdqt_status_t hdqt_linear_xent_bwd(const hdqt_xent_desc_t* d, const v
   if (floats_misaligned(lse, gr, nullptr) || outputs_misaligned(d, dX, dW)) return HDQT_ERR_ALIGNMENT;
   if (!dX && !dW) return HDQT_OK;
   if (d->tokens == 0) return dW ? zero_out(c, dW, c.pl.w_rows, c.pl.w_cols, d->ld_dw) : HDQT_OK;
+  if (c.pl.small_rows > 0) return small(c, HDQT_XENT_BWD, X, W, labels, lse, gr, nullptr, nullptr, dX, dW);
   st = prepare(&c, X, W, labels, gr, true);
   if (st != HDQT_OK) return st;
   for (int64_t v0 = 0; v0 < d->classes; v0 += c.pl.cols_piece) {
@@ -708,7 +880,7 @@ extern "C" hdqt_status_t hdqt_linear_xent_bwd(const hdqt_xent_desc_t* d, const v
     p.lse = lse;
     p.g = c.at<float>(c.pl.weight);
     p.g_rows = 1;
-    st = launch<X_DZ>(p, &g, 1, c.s);
+    st = launch<X_DZ>(p, &g, 1, c);
     if (st != HDQT_OK) return st;
     st = gradient_products(c, 0, d->tokens, v0, nv, dX, dW, v0 == 0, v0 + nv == d->classes);
     if (st != HDQT_OK) return st;
@@ -726,6 +898,7 @@ extern "C" hdqt_status_t hdqt_linear_xent_train(const hdqt_xent_desc_t* d, const
   if ((d->tokens > 0 && !lse) || (!loss && (d->tokens > 0 || d->reduction != HDQT_REDUCE_NONE))) return HDQT_ERR_INVALID_ARG;
   if (d->tokens > 0 && d->reduction == HDQT_REDUCE_NONE && !gr) return HDQT_ERR_INVALID_ARG;
   if (floats_misaligned(loss, lse, gr) || outputs_misaligned(d, dX, dW)) return HDQT_ERR_ALIGNMENT;
+  if (c.pl.small_rows > 0) return small(c, HDQT_XENT_TRAIN, X, W, labels, nullptr, gr, loss, lse, dX, dW);
   st = prepare(&c, X, W, labels, gr, true);
   if (st != HDQT_OK) return st;
   if (d->tokens == 0) {
@@ -745,14 +918,18 @@ extern "C" hdqt_status_t hdqt_linear_xent_train(const hdqt_xent_desc_t* d, const
     p.label_logit = c.at<float>(c.pl.label_logit) + t0;
     p.z = c.at<void>(c.pl.z);
     p.ld_z = c.pl.ld_z;
-    st = c.pl.planes == 1 ? launch<X_CODES>(p, &g, 1, c.s) : launch<X_LOGITS>(p, &g, 1, c.s);
+    st = c.pl.planes == 1 ? launch<X_CODES>(p, &g, 1, c) : launch<X_LOGITS>(p, &g, 1, c);
     if (st != HDQT_OK) return st;
+    // few rows: slices of the classes fill the machine
+    int64_t slices = ceil_div(4 * kNumSMsHint, nt);
+    const int64_t most = ceil_div(d->classes, 8 * kRowThreads);
+    const dim3 grid((unsigned)nt, (unsigned)(slices < most ? slices : most));
     if (c.pl.planes == 1)
-      xent_dz_kernel<1><<<(unsigned)nt, kRowThreads, 0, c.s>>>(p.part, (int)p.parts_ld, p.parts_ld, p.label, p.label_logit,
+      c.run(xent_dz_kernel<1>, grid, kRowThreads, 0, p.part, (int)p.parts_ld, p.parts_ld, p.label, p.label_logit,
                                                                c.at<float>(c.pl.weight) + t0, d->classes, p.z, c.pl.ld_z,
-                                                               nullptr, 0, lse + t0, rows + t0);
+            static_cast<uint16_t*>(nullptr), 0, lse + t0, rows + t0);
     else
-      xent_dz_kernel<3><<<(unsigned)nt, kRowThreads, 0, c.s>>>(p.part, (int)p.parts_ld, p.parts_ld, p.label, p.label_logit,
+      c.run(xent_dz_kernel<3>, grid, kRowThreads, 0, p.part, (int)p.parts_ld, p.parts_ld, p.label, p.label_logit,
                                                                c.at<float>(c.pl.weight) + t0, d->classes, p.z, c.pl.ld_z,
                                                                c.at<uint16_t>(c.pl.dz), c.pl.rows_piece * c.pl.ld_z,
                                                                lse + t0, rows + t0);

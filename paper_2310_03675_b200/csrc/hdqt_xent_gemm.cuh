@@ -402,6 +402,7 @@ xent_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_consta
   cluster_sync_all();     // the peer's barriers are initialised before anything is signalled across the pair
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
+  chain_wait();           // everything above overlaps the kernel before
 
   if (warp == 0) {
     // ------------------------------ TMA producer (both CTAs) ------------------

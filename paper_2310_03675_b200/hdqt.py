@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import array
 import ctypes as C
+import operator
 import os
 from typing import Optional
 
@@ -484,23 +485,27 @@ def mma_rate_tops(iters: int = 20000, repeats: int = 3, dev_status=None) -> floa
 
 # ---- the rest of a training step: gradient clipping, group norm --------------------------------------
 
+_dtype_of = operator.attrgetter("dtype")
+
+
 def _tensor_table(tensors, out):
     """hdqt_tensor_t[len(tensors)] as a flat int64 array (source, destination, elements, type), and the device.  One pass
     per property: a model has hundreds of tensors, and this is most of the call's host time."""
     n = len(tensors)
-    codes = [DTYPE_CODES.get(t.dtype) for t in tensors]
-    sizes = [t.numel() for t in tensors]
-    at = [t.data_ptr() for t in tensors]
-    devices = {t.get_device() for t in tensors}
-    if None in codes or -1 in devices or not all([t.is_contiguous() for t in tensors]):
+    T = torch.Tensor
+    codes = list(map(DTYPE_CODES.get, map(_dtype_of, tensors)))
+    sizes = list(map(T.numel, tensors))
+    at = list(map(T.data_ptr, tensors))
+    devices = set(map(T.get_device, tensors))
+    if None in codes or -1 in devices or not all(map(T.is_contiguous, tensors)):
         raise ValueError("expected dense fp32, bf16 or fp16 CUDA tensors")
     to = at
     if out is not None:
-        if len(out) != n or [t.numel() for t in out] != sizes or [DTYPE_CODES.get(t.dtype) for t in out] != codes \
-                or not all([t.is_contiguous() for t in out]):
+        if len(out) != n or list(map(T.numel, out)) != sizes or list(map(DTYPE_CODES.get, map(_dtype_of, out))) != codes \
+                or not all(map(T.is_contiguous, out)):
             raise ValueError("out must hold a dense tensor of the type and size of each input")
-        devices.update([t.get_device() for t in out])
-        to = [t.data_ptr() for t in out]
+        devices.update(map(T.get_device, out))
+        to = list(map(T.data_ptr, out))
     if len(devices) > 1:
         raise ValueError("the tensors must be on one device")
     table = array.array("q", bytes(32 * n))

@@ -87,6 +87,10 @@ SHAPES = [    # tokens, features, classes
     (700, 65, 2051),
     (1, 256, 20000),
     (1000, 8, 2),
+    (512, 100, 300),
+    (5, 100, 30001),
+    (8, 2048, 3000),
+    (2, 72, 9000),
 ]
 
 
@@ -121,6 +125,15 @@ def test_all_calls_match_64_bits(case, dtype, w_is_cd):
         close(lse2, want["lse"], "lse (train)")
         close(dx2, want["dx"], "dx (train)")
         close(dw2 if w_is_cd else dw2.t(), want["dw"], "dw (train)")
+        # a stated piece size selects the tensor-core path whatever the size
+        loss3, lse3, dx3, dw3 = hdqt.linear_xent_train(x, ww, labels, g, piece_bytes=1 << 28, **how)
+        close(loss3, want["loss"], "loss (products)")
+        close(lse3, want["lse"], "lse (products)")
+        close(dx3, want["dx"], "dx (products)")
+        close(dw3 if w_is_cd else dw3.t(), want["dw"], "dw (products)")
+        dx4, dw4 = hdqt.linear_xent_bwd(x, ww, labels, lse, g, piece_bytes=1 << 28, **how)
+        close(dx4, want["dx"], "dx (products, bwd)")
+        close(dw4 if w_is_cd else dw4.t(), want["dw"], "dw (products, bwd)")
     hdqt.check_device_status(status)
 
 
@@ -184,17 +197,18 @@ def test_large_logits_and_lowest_values():
 
 @pytest.mark.gpu
 def test_non_finite_inputs_stay_in_their_row():
-    for dtype in ("bf16", "fp32"):
+    for dtype, piece in (("bf16", 0), ("fp32", 0), ("bf16", 1 << 28), ("fp32", 1 << 28)):
         x, w, labels, weights = data(40, 24, 300, dtype, seed=7, ignored=0)
         x[5, 3] = math.nan
         x[9, 2] = math.inf
-        loss, lse, dx, dw = hdqt.linear_xent_train(x, w, labels, weights, reduction="none", w_is_cd=True)
+        how = {"reduction": "none", "w_is_cd": True, "piece_bytes": piece}
+        loss, lse, dx, dw = hdqt.linear_xent_train(x, w, labels, weights, **how)
         bad = torch.zeros(40, dtype=torch.bool, device="cuda")
         bad[5] = bad[9] = True
         assert torch.equal(torch.isnan(loss), bad) and torch.equal(torch.isnan(dx).all(1), bad)
         assert bool(torch.isnan(dw).all())
         labels[5] = labels[9] = -100          # an ignored row takes part in nothing but its own lse
-        loss, lse, dx, dw = hdqt.linear_xent_train(x, w, labels, weights, reduction="none", w_is_cd=True)
+        loss, lse, dx, dw = hdqt.linear_xent_train(x, w, labels, weights, **how)
         assert not bool(torch.isnan(loss).any()) and not bool(torch.isnan(dx).any())
 
 
@@ -202,18 +216,30 @@ def test_non_finite_inputs_stay_in_their_row():
 def test_ignored_invalid_and_missing_tokens():
     x, w, labels, weights = data(50, 32, 90, "bf16", seed=8, ignored=0)
     none = torch.full_like(labels, -100)
-    loss, lse, dx, dw = hdqt.linear_xent_train(x, w, none, w_is_cd=True)
-    assert math.isnan(float(loss)) and not dx.any() and not dw.any()
-    loss, _, dx, dw = hdqt.linear_xent_train(x, w, none, reduction="sum", w_is_cd=True)
-    assert float(loss) == 0.0 and not dx.any() and not dw.any()
+    for piece in (0, 1 << 28):
+        loss, lse, dx, dw = hdqt.linear_xent_train(x, w, none, w_is_cd=True, piece_bytes=piece)
+        assert math.isnan(float(loss)) and not dx.any() and not dw.any()
+        loss, _, dx, dw = hdqt.linear_xent_train(x, w, none, reduction="sum", w_is_cd=True, piece_bytes=piece)
+        assert float(loss) == 0.0 and not dx.any() and not dw.any()
+        status = hdqt.new_status("cuda")
+        bad = labels.clone()
+        bad[7], bad[8] = 90, -1
+        loss, _, dx, dw = hdqt.linear_xent_train(x, w, bad, weights, reduction="none", w_is_cd=True, dev_status=status,
+                                                 piece_bytes=piece)
+        assert torch.equal(torch.isnan(loss).nonzero().flatten().cpu(), torch.tensor([7, 8]))
+        assert not dx[7:9].any() and dx[6].any() and not bool(torch.isnan(dw).any())
+        with pytest.raises(hdqt.HdqtError):
+            hdqt.check_device_status(status)
+    # a few tokens against a large vocabulary
+    x, w, labels, _ = data(4, 64, 9000, "bf16", seed=11, ignored=0)
     status = hdqt.new_status("cuda")
-    bad = labels.clone()
-    bad[7], bad[8] = 90, -1
-    loss, _, dx, dw = hdqt.linear_xent_train(x, w, bad, weights, reduction="none", w_is_cd=True, dev_status=status)
-    assert torch.equal(torch.isnan(loss).nonzero().flatten().cpu(), torch.tensor([7, 8]))
-    assert not dx[7:9].any() and dx[6].any() and not bool(torch.isnan(dw).any())
+    labels[1], labels[2] = -100, 9000
+    loss, lse = hdqt.linear_xent_fwd(x, w, labels, reduction="none", w_is_cd=True, dev_status=status)
+    assert float(loss[1]) == 0.0 and math.isnan(float(loss[2])) and bool(torch.isfinite(loss[[0, 3]]).all())
     with pytest.raises(hdqt.HdqtError):
         hdqt.check_device_status(status)
+    assert math.isnan(float(hdqt.linear_xent_fwd(x, w, torch.full_like(labels, -100), w_is_cd=True)[0]))
+    x, w, labels, weights = data(50, 32, 90, "bf16", seed=8, ignored=0)
     e = torch.empty(0, 32, device="cuda", dtype=torch.bfloat16)
     no = torch.empty(0, device="cuda", dtype=torch.int64)
     loss, lse, dx, dw = hdqt.linear_xent_train(e, w, no, w_is_cd=True)
