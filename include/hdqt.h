@@ -417,6 +417,10 @@ hdqt_status_t hdqt_clip_grad_norm(const hdqt_tensor_t* tensors /*host*/, int64_t
 
 size_t hdqt_grad_norm_workspace_bytes(int64_t count);
 
+/* dst = src * factor[0] (device fp32 scalar), rounded once; with a factor of 1 tensors whose dst equals src are left
+ * untouched: the gradient of a loss that was formed together with the loss, times the gradient that arrives for it. */
+hdqt_status_t hdqt_scale_tensors(const hdqt_tensor_t* tensors /*host*/, int64_t count, const float* factor, void* stream);
+
 /*
  * Group norm with an activation on channels-last activations x[batch, pixels, channels] (the layout of hdqt_conv2d_*;
  * pixels = height * width):

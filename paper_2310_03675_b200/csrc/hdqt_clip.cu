@@ -166,16 +166,10 @@ __global__ void __launch_bounds__(kThreads) grad_norm_kernel(const double* __res
   if (threadIdx.x == 0) *norm_out = norm;
 }
 
-template <int N, bool kInf>
-__global__ void __launch_bounds__(kThreads)
-grad_scale_kernel(const __grid_constant__ Table<N> t, const double* __restrict__ partials, int n, float max_norm,
-                  float* __restrict__ norm_out) {
-  chain_wait();
-  const float norm = join_partials<kInf>(partials, n);
-  if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
-  float f = max_norm / (norm + 1e-6f);
-  if (f > 1.0f) f = 1.0f;      // (a NaN stays)
-  // from the end: what the first pass read last is still in the L2
+// this block's share of dst = src * f
+template <int N>
+__device__ __forceinline__ void scale_table(const Table<N>& t, float f) {
+  // from the end: what a pass over the table read last is still in the L2
   for (uint32_t i = blockIdx.x; i < t.chunks; i += gridDim.x) {
     const uint32_t c = t.chunks - 1 - i;
     const TableEntry& e = t.e[find_entry(t, c)];
@@ -190,6 +184,23 @@ grad_scale_kernel(const __grid_constant__ Table<N> t, const double* __restrict__
     else
       scale_chunk(reinterpret_cast<const __half*>(e.src) + p.at, reinterpret_cast<__half*>(e.dst) + p.at, p.n, vec, f);
   }
+}
+
+template <int N, bool kInf>
+__global__ void __launch_bounds__(kThreads)
+grad_scale_kernel(const __grid_constant__ Table<N> t, const double* __restrict__ partials, int n, float max_norm,
+                  float* __restrict__ norm_out) {
+  chain_wait();
+  const float norm = join_partials<kInf>(partials, n);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
+  float f = max_norm / (norm + 1e-6f);
+  if (f > 1.0f) f = 1.0f;      // (a NaN stays)
+  scale_table(t, f);
+}
+
+template <int N>
+__global__ void __launch_bounds__(kThreads) scale_by_kernel(const __grid_constant__ Table<N> t, const float* __restrict__ factor) {
+  scale_table(t, *factor);
 }
 
 // Fills one launch's table from `tensors` starting at *next; returns the number of chunks (0 = nothing left).
@@ -242,23 +253,44 @@ hdqt_status_t run(const hdqt_tensor_t* tensors, int64_t count, bool clip, float 
   return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "gradient norm");
 }
 
-hdqt_status_t check_and_run(const hdqt_tensor_t* tensors, int64_t count, int32_t norm_type, bool clip, float max_norm,
-                            float* norm_out, void* workspace, size_t workspace_bytes, void* stream) {
-  if (count < 0 || (count > 0 && tensors == nullptr) || !norm_out || !workspace) return HDQT_ERR_INVALID_ARG;
-  if (norm_type != HDQT_NORM_L2 && norm_type != HDQT_NORM_INF) return HDQT_ERR_INVALID_ARG;
-  if (clip && !(max_norm >= 0.0f)) return HDQT_ERR_INVALID_ARG;
-  int64_t used = 0;
+template <int N>
+hdqt_status_t run_scale(const hdqt_tensor_t* tensors, int64_t count, const float* factor, cudaStream_t s) {
+  const int sms = sm_count();
+  if (sms <= 0) return HDQT_ERR_CUDA;
+  const uint32_t most = (uint32_t)(sms * 4 < kMaxBlocks ? sms * 4 : kMaxBlocks);
+  Table<N> t;
+  for (int64_t next = 0; uint32_t chunks = fill_table(tensors, count, &next, &t);)
+    scale_by_kernel<N><<<chunks < most ? chunks : most, kThreads, 0, s>>>(t, factor);
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "scaling");
+}
+
+// the list itself; *used = tensors with elements
+hdqt_status_t check_list(const hdqt_tensor_t* tensors, int64_t count, bool write, int64_t* used) {
+  if (count < 0 || (count > 0 && tensors == nullptr)) return HDQT_ERR_INVALID_ARG;
+  *used = 0;
   for (int64_t i = 0; i < count; ++i) {
     const hdqt_tensor_t& x = tensors[i];
     const int size = dtype_size(x.dtype);
     if (size == 0 || x.numel < 0) return HDQT_ERR_INVALID_ARG;
     if (x.numel == 0) continue;
     if (x.numel > (1ll << 42)) return HDQT_ERR_UNSUPPORTED;
-    if (!x.src || (clip && !x.dst)) return HDQT_ERR_INVALID_ARG;
-    if ((reinterpret_cast<uintptr_t>(x.src) | (clip ? reinterpret_cast<uintptr_t>(x.dst) : 0)) & (uintptr_t)(size - 1))
+    if (!x.src || (write && !x.dst)) return HDQT_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(x.src) | (write ? reinterpret_cast<uintptr_t>(x.dst) : 0)) & (uintptr_t)(size - 1))
       return HDQT_ERR_ALIGNMENT;
-    ++used;
+    ++*used;
   }
+  return HDQT_OK;
+}
+
+hdqt_status_t check_and_run(const hdqt_tensor_t* tensors, int64_t count, int32_t norm_type, bool clip, float max_norm,
+                            float* norm_out, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!norm_out || !workspace) return HDQT_ERR_INVALID_ARG;
+  if (norm_type != HDQT_NORM_L2 && norm_type != HDQT_NORM_INF) return HDQT_ERR_INVALID_ARG;
+  if (clip && !(max_norm >= 0.0f)) return HDQT_ERR_INVALID_ARG;
+  int64_t used = 0;
+  const hdqt_status_t st = check_list(tensors, count, clip, &used);
+  if (st != HDQT_OK) return st;
   if (reinterpret_cast<uintptr_t>(norm_out) & 3) return HDQT_ERR_ALIGNMENT;
   if (reinterpret_cast<uintptr_t>(workspace) & 127) return HDQT_ERR_ALIGNMENT;
   if (workspace_bytes < hdqt_grad_norm_workspace_bytes(count)) return HDQT_ERR_WORKSPACE;
@@ -293,4 +325,14 @@ extern "C" hdqt_status_t hdqt_clip_grad_norm(const hdqt_tensor_t* tensors, int64
                                              float max_norm, float* norm_out, void* workspace, size_t workspace_bytes,
                                              void* stream) {
   return check_and_run(tensors, count, norm_type, true, max_norm, norm_out, workspace, workspace_bytes, stream);
+}
+
+extern "C" hdqt_status_t hdqt_scale_tensors(const hdqt_tensor_t* tensors, int64_t count, const float* factor, void* stream) {
+  if (!factor) return HDQT_ERR_INVALID_ARG;
+  int64_t used = 0;
+  const hdqt_status_t st = check_list(tensors, count, true, &used);
+  if (st != HDQT_OK) return st;
+  if (reinterpret_cast<uintptr_t>(factor) & 3) return HDQT_ERR_ALIGNMENT;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  return used <= 64 ? run_scale<64>(tensors, count, factor, s) : run_scale<kMaxTensors>(tensors, count, factor, s);
 }

@@ -37,7 +37,7 @@ EXPORTED = [
     "hdqt_gemm_i8_workspace_bytes", "hdqt_calibrate_acc_shift", "hdqt_gemm_fwd", "hdqt_gemm_dgrad",
     "hdqt_gemm_wgrad", "hdqt_workspace_bytes", "hdqt_workspace_layout", "hdqt_quantize_hadamard_static",
     "hdqt_selftest_bounded_wait", "hdqt_conv2d_fwd", "hdqt_conv2d_wgrad", "hdqt_selftest_mma_rate",
-    "hdqt_grad_norm", "hdqt_clip_grad_norm", "hdqt_grad_norm_workspace_bytes",
+    "hdqt_grad_norm", "hdqt_clip_grad_norm", "hdqt_grad_norm_workspace_bytes", "hdqt_scale_tensors",
     "hdqt_group_norm_fwd", "hdqt_group_norm_bwd", "hdqt_group_norm_workspace_bytes",
     "hdqt_linear_xent_fwd", "hdqt_linear_xent_bwd", "hdqt_linear_xent_train", "hdqt_linear_xent_workspace_bytes",
 ]
@@ -128,6 +128,8 @@ def _load() -> C.CDLL:
     lib.hdqt_grad_norm.argtypes = [vp, i64, i32, vp, vp, sz, vp]
     lib.hdqt_clip_grad_norm.argtypes = [vp, i64, i32, f32, vp, vp, sz, vp]
     lib.hdqt_grad_norm_workspace_bytes.argtypes = [i64]
+    lib.hdqt_scale_tensors.argtypes = [vp, i64, vp, vp]
+    lib.hdqt_scale_tensors.restype = C.c_int
     lib.hdqt_grad_norm_workspace_bytes.restype = sz
     lib.hdqt_group_norm_fwd.argtypes = [C.POINTER(GroupNormDesc), vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.hdqt_group_norm_bwd.argtypes = [C.POINTER(GroupNormDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
@@ -551,6 +553,17 @@ def clip_grad_norm(tensors, max_norm: float, norm_type: float = 2.0, out=None, d
     _check(lib.hdqt_clip_grad_norm(table.buffer_info()[0], len(tensors), code, max_norm, norm.data_ptr(), ws.data_ptr(),
                                    nbytes, _stream()), "hdqt_clip_grad_norm")
     return norm
+
+
+def scale_tensors(tensors, factor: torch.Tensor, out=None) -> None:
+    """Multiplies dense tensors by an fp32 scalar tensor, in place or into the tensors of `out`; a factor of 1 in place costs
+    one launch and no memory traffic."""
+    tensors = list(tensors)
+    table, dev = _tensor_table(tensors, None if out is None else list(out))
+    if factor.dtype != torch.float32 or factor.numel() != 1 or (dev is not None and factor.device != dev):
+        raise ValueError("factor must be an fp32 scalar on the tensors' device")
+    _check(lib.hdqt_scale_tensors(table.buffer_info()[0], len(tensors), factor.data_ptr(), _stream()),
+           "hdqt_scale_tensors")
 
 
 def _pixel_strides(t: torch.Tensor, name: str):

@@ -1,8 +1,9 @@
 """Thin PyTorch harness over the HDQT GEMM calls: an autograd function for a linear layer whose three
 matrix products (forward, dX, dW) all run through the library, plus the synthetic MLP workload.
 
-Everything that is not a matmul (bias, ReLU, loss, SGD) stays in fp32 torch ops, as in the paper
-(Section 3: only matmul inputs and accumulators are quantized).
+Everything that is not a matmul stays in floating point, as in the paper (Section 3: only matmul inputs and
+accumulators are quantized): bias and ReLU in the forward GEMM's epilogue; group norm with its activation, the cross entropy
+of a linear head and gradient clipping as library operators; batch norm and SGD as torch ops.
 """
 from __future__ import annotations
 
@@ -173,13 +174,15 @@ class GraphedTrainStep:
     once per step (step k rounds with (seed, offset) = (base_step, k)).  Two graphs are recorded and replayed
     alternately, because delayed scaling ping-pongs between two history buffers per tensor.
 
-    `forward(x)` maps the static input batch to logits; `warmup` eager steps run first (they are real training
+    `forward(x)` maps the static input batch to logits, on which torch's cross entropy is taken; `loss(x, labels)`, if
+    given, is the loss instead.  clip_norm: the gradients are clipped to this norm before the update.  `warmup` eager steps run first (they are real training
     steps: optimiser state and workspaces must exist before the recording)."""
 
     def __init__(self, model: torch.nn.Module, opt: torch.optim.Optimizer, x: torch.Tensor, labels: torch.Tensor,
-                 forward=None, base_step: int = 0, warmup: int = 3):
+                 forward=None, base_step: int = 0, warmup: int = 3, loss=None, clip_norm: Optional[float] = None):
         self.model, self.opt = model, opt
         self.forward = forward if forward is not None else model
+        self.loss, self.clip_norm = loss, clip_norm
         dev = x.device
         self.counter = torch.zeros(1, dtype=torch.int32, device=dev)
         for m in model.modules():
@@ -206,8 +209,13 @@ class GraphedTrainStep:
 
     def _body(self):
         self.opt.zero_grad(set_to_none=True)
-        loss = torch.nn.functional.cross_entropy(self.forward(self.x), self.labels)
+        if self.loss is not None:
+            loss = self.loss(self.x, self.labels)
+        else:
+            loss = torch.nn.functional.cross_entropy(self.forward(self.x), self.labels)
         loss.backward()
+        if self.clip_norm is not None:
+            clip_grad_norm_(self.model.parameters(), self.clip_norm)
         self.opt.step()
         self.counter += 1
         return loss
@@ -220,6 +228,108 @@ class GraphedTrainStep:
         self.graphs[i].replay()
         self.steps += 1
         return self.losses[i]
+
+
+# ---- the rest of a training step: normalisation, loss, gradient clipping ------------------------------
+# Section 3 quantizes the inputs and accumulators of matrix products; what lies around them stays in floating point.
+
+class GroupNormFunction(torch.autograd.Function):
+    """act(group norm) of a channels-last tensor x[batch, ..., channels]."""
+
+    @staticmethod
+    def forward(ctx, x, gamma, beta, groups: int, eps: float, act: str):
+        y, mean, rstd = hdqt.group_norm_fwd(x, gamma, beta, groups, eps, act)
+        ctx.save_for_backward(x, gamma, beta, mean, rstd)
+        ctx.meta = (groups, act)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, gamma, beta, mean, rstd = ctx.saved_tensors
+        groups, act = ctx.meta
+        dx, dgamma, dbeta = hdqt.group_norm_bwd(dy, x, gamma, beta, mean, rstd, groups, act,
+                                                want_dx=ctx.needs_input_grad[0],
+                                                want_params=ctx.needs_input_grad[1] or ctx.needs_input_grad[2])
+        return dx, dgamma, dbeta, None, None, None
+
+
+class GroupNormAct(torch.nn.Module):
+    """Group norm with an optional activation ("none", "relu", "silu") of [batch, channels, height, width] tensors held
+    channels last, the layout of HdqtConv2d's activations (no copy; other layouts are brought into it).  No batch
+    statistics: an image's result does not depend on the others of its batch, in training or evaluation."""
+
+    def __init__(self, channels: int, groups: int = 32, act: str = "none", eps: float = 1e-5):
+        super().__init__()
+        self.weight = torch.nn.Parameter(torch.ones(channels))
+        self.bias = torch.nn.Parameter(torch.zeros(channels))
+        self.groups, self.act, self.eps = min(groups, channels), act, eps
+
+    def forward(self, x):
+        y = GroupNormFunction.apply(_nhwc(x), self.weight, self.bias, self.groups, self.eps, self.act)
+        return y.permute(0, 3, 1, 2)
+
+
+class LinearCrossEntropyFunction(torch.autograd.Function):
+    """Softmax cross entropy of x @ w without the logits in memory.  Where the loss is one number its gradients are formed
+    together with it (the logits once instead of twice) and only scaled in the backward pass; per-token losses, and a second
+    backward pass through the same graph, form the logits again."""
+
+    @staticmethod
+    def forward(ctx, x, w, labels, ignore_index: int, reduction: str, w_is_cd: bool):
+        how = {"ignore_index": ignore_index, "reduction": reduction, "w_is_cd": w_is_cd}
+        want_dx, want_dw = ctx.needs_input_grad[:2]
+        ctx.how, ctx.ready = how, None
+        if reduction != "none" and (want_dx or want_dw):
+            loss, lse, dx, dw = hdqt.linear_xent_train(x, w, labels, want_dx=want_dx, want_dw=want_dw, **how)
+            ctx.ready = (dx, dw)
+        else:
+            loss, lse = hdqt.linear_xent_fwd(x, w, labels, **how)
+        ctx.save_for_backward(x, w, labels, lse)
+        return loss
+
+    @staticmethod
+    def backward(ctx, g):
+        want_dx, want_dw = ctx.needs_input_grad[:2]
+        g = g.float()
+        if ctx.ready is not None:
+            dx, dw = ctx.ready
+            ctx.ready = None
+            hdqt.scale_tensors([t for t in (dx, dw) if t is not None], g)
+        else:
+            x, w, labels, lse = ctx.saved_tensors
+            dx, dw = hdqt.linear_xent_bwd(x, w, labels, lse, g, want_dx=want_dx, want_dw=want_dw, **ctx.how)
+        return dx, dw, None, None, None, None
+
+
+def linear_cross_entropy(x, w, labels, bias=None, ignore_index: int = -100, reduction: str = "mean",
+                         w_is_cd: bool = False):
+    """cross_entropy(x @ w + bias, labels) for x [tokens, features] and w [features, classes] (or [classes, features] with
+    w_is_cd), fp32 or bf16, without the logits in memory.  reduction: "mean" over the labels that are not ignore_index,
+    "sum", or "none".  A bias is one more feature whose input is 1 (x and w are copied for it)."""
+    if bias is not None:
+        x = torch.cat([x, x.new_ones((x.shape[0], 1))], 1)
+        w = torch.cat([w, bias[:, None]], 1) if w_is_cd else torch.cat([w, bias[None]], 0)
+    return LinearCrossEntropyFunction.apply(x, w, labels, ignore_index, reduction, w_is_cd)
+
+
+def _dense(t: torch.Tensor) -> torch.Tensor:
+    """The same elements as a contiguous view (a permuted dense tensor keeps its memory)."""
+    if t.is_contiguous():
+        return t
+    order = sorted(range(t.dim()), key=lambda i: -t.stride(i))
+    v = t.permute(order)
+    if not v.is_contiguous():
+        raise ValueError("gradients must be dense")
+    return v
+
+
+def clip_grad_norm_(parameters, max_norm: float, norm_type: float = 2.0) -> torch.Tensor:
+    """Scales the gradients of the parameters in place by min(1, max_norm / (norm + 1e-6)) and returns the norm over all of
+    them (2 or inf); two launches whatever their number, no synchronisation."""
+    if isinstance(parameters, torch.Tensor):
+        parameters = [parameters]
+    grads = [_dense(p.grad) for p in parameters if p.grad is not None]
+    return hdqt.clip_grad_norm(grads, max_norm, norm_type)
 
 
 # ---- convolution as an im2col GEMM -------------------------------------------------------------------
@@ -360,20 +470,32 @@ class HdqtConv2d(torch.nn.Module):
                                         self.implicit)
 
 
+def _norm(kind: str, channels: int, relu: bool):
+    """Normalisation layer: "batch" (torch; its ReLU is applied by the caller) or "group" (one library call, ReLU included)."""
+    if kind == "batch":
+        return torch.nn.BatchNorm2d(channels)
+    if kind == "group":
+        return GroupNormAct(channels, act="relu" if relu else "none")
+    raise ValueError("norm must be 'batch' or 'group'")
+
+
 class _BasicBlock(torch.nn.Module):
-    def __init__(self, cin, cout, stride, ids, quantized, over):
+    def __init__(self, cin, cout, stride, ids, quantized, over, norm="batch"):
         super().__init__()
         self.conv1 = HdqtConv2d(cin, cout, 3, stride, 1, next(ids), quantized, **over)
-        self.bn1 = torch.nn.BatchNorm2d(cout)
+        self.bn1 = _norm(norm, cout, True)
         self.conv2 = HdqtConv2d(cout, cout, 3, 1, 1, next(ids), quantized, **over)
-        self.bn2 = torch.nn.BatchNorm2d(cout)
+        self.bn2 = _norm(norm, cout, False)
         self.shortcut = None
         if stride != 1 or cin != cout:
             self.shortcut = HdqtConv2d(cin, cout, 1, stride, 0, next(ids), quantized, **over)
-            self.bn_sc = torch.nn.BatchNorm2d(cout)
+            self.bn_sc = _norm(norm, cout, False)
+        self.norm = norm
 
     def forward(self, x):
-        y = torch.relu(self.bn1(self.conv1(x)))
+        y = self.bn1(self.conv1(x))
+        if self.norm == "batch":
+            y = torch.relu(y)
         y = self.bn2(self.conv2(y))
         sc = x if self.shortcut is None else self.bn_sc(self.shortcut(x))
         return torch.relu(y + sc)
@@ -382,19 +504,22 @@ class _BasicBlock(torch.nn.Module):
 class ResNet18Width(torch.nn.Module):
     """ResNet-18-width network for 32x32x3 inputs (3x3 stem, four stages of two basic blocks with 64/128/256/512
     channels, global average pool, linear head).  Every convolution and the head go through the HDQT GEMMs;
-    batch norm, ReLU, pooling, loss and the optimiser stay in fp32 torch ops.  `num_outputs` is the size of the
+    normalisation, ReLU, pooling, loss and the optimiser stay in fp32.  norm: "batch" (torch ops) or "group" (GroupNormAct,
+    32 groups: no batch statistics for the replayed classes to disturb).  `num_outputs` is the size of the
     head; `forward(x, n_seen)` uses only the first n_seen output neurons (a head that grows with the classes seen)."""
 
-    def __init__(self, num_outputs: int = 100, quantized: bool = True, widths=(64, 128, 256, 512), **over):
+    def __init__(self, num_outputs: int = 100, quantized: bool = True, widths=(64, 128, 256, 512), norm: str = "batch",
+                 **over):
         super().__init__()
         ids = iter(range(1000))
         self.quantized = quantized
         self.stem = HdqtConv2d(3, widths[0], 3, 1, 1, next(ids), quantized, **over)
-        self.bn = torch.nn.BatchNorm2d(widths[0])
+        self.norm = norm
+        self.bn = _norm(norm, widths[0], True)
         blocks, cin = [], widths[0]
         for i, w in enumerate(widths):
             for j in range(2):
-                blocks.append(_BasicBlock(cin, w, 2 if (i > 0 and j == 0) else 1, ids, quantized, over))
+                blocks.append(_BasicBlock(cin, w, 2 if (i > 0 and j == 0) else 1, ids, quantized, over, norm))
                 cin = w
         self.blocks = torch.nn.ModuleList(blocks)
         self.head = HdqtLinear(cin, num_outputs, layer_id=next(ids), **over)
@@ -404,17 +529,32 @@ class ResNet18Width(torch.nn.Module):
             if isinstance(m, (HdqtConv2d, HdqtLinear)):
                 m.step = step
 
-    def forward(self, x, n_seen: Optional[int] = None):
-        y = torch.relu(self.bn(self.stem(x)))
+    def features(self, x):
+        """The head's input: [batch, widths[-1]]."""
+        y = self.bn(self.stem(x))
+        if self.norm == "batch":
+            y = torch.relu(y)
         for b in self.blocks:
             y = b(y)
-        y = y.mean(dim=(2, 3))
+        return y.mean(dim=(2, 3))
+
+    def _head(self, n_seen: Optional[int]):
         head = self.head
         n = head.weight.shape[1] if n_seen is None else n_seen
-        w = head.weight if n == head.weight.shape[1] else head.weight[:, :n].contiguous()
+        return (head.weight if n == head.weight.shape[1] else head.weight[:, :n].contiguous()), head.bias[:n]
+
+    def loss(self, x, labels, n_seen: Optional[int] = None):
+        """Mean cross entropy with the head in fp32 (not quantized) and without its logits in memory."""
+        w, b = self._head(n_seen)
+        return linear_cross_entropy(self.features(x), w, labels, bias=b)
+
+    def forward(self, x, n_seen: Optional[int] = None):
+        y = self.features(x)
+        w, b = self._head(n_seen)
+        head = self.head
         if self.quantized:
-            return HdqtLinearFunction.apply(y.contiguous(), w, head.bias[:n], False, head.layer_id, head.step, head.over)
-        return y @ w + head.bias[:n]
+            return HdqtLinearFunction.apply(y.contiguous(), w, b, False, head.layer_id, head.step, head.over)
+        return y @ w + b
 
 
 def class_patterns(classes: int, seed: int, device, size: int = 32, waves: int = 4):
@@ -443,11 +583,16 @@ def synthetic_images(labels: torch.Tensor, patterns: torch.Tensor, seed: int, bl
     return (1.0 - blend) * noise + blend * patterns[labels]
 
 
-def cnn_train_step(model: ResNet18Width, opt, x, labels, step: int, n_seen: Optional[int] = None):
+def cnn_train_step(model: ResNet18Width, opt, x, labels, step: int, n_seen: Optional[int] = None,
+                   fused_loss: bool = False, clip_norm: Optional[float] = None):
+    """One training step.  fused_loss: the head and its cross entropy as one operator (ResNet18Width.loss) instead of a
+    quantized head with torch's loss; clip_norm: the gradients are clipped to this norm before the update."""
     model.set_step(step)
     opt.zero_grad(set_to_none=True)
-    loss = torch.nn.functional.cross_entropy(model(x, n_seen), labels)
+    loss = model.loss(x, labels, n_seen) if fused_loss else torch.nn.functional.cross_entropy(model(x, n_seen), labels)
     loss.backward()
+    if clip_norm is not None:
+        clip_grad_norm_(model.parameters(), clip_norm)
     opt.step()
     return loss
 
@@ -455,18 +600,20 @@ def cnn_train_step(model: ResNet18Width, opt, x, labels, step: int, n_seen: Opti
 def class_incremental_run(quantized: bool, device, tasks: int = 5, classes_per_task: int = 20,
                           steps_per_task: int = 1000, batch: int = 128, memory: int = 2000, seed: int = 0,
                           lr: float = 0.05, test_per_class: int = 20, blend: float = 0.2, log=None,
-                          graphed: bool = False, **over):
+                          graphed: bool = False, norm: str = "batch", fused_loss: bool = False,
+                          clip_norm: Optional[float] = None, **over):
     """Plain-replay class-incremental training of the ResNet-18-width model on synthetic classes (paper
     Section 4: tasks arrive one after the other, a bounded memory of exemplars is replayed, the head grows with
     the classes seen; appendix: SGD lr 0.05, momentum 0.9, weight decay 2e-4, memory 2000).  Each batch mixes
     new-task samples and replayed exemplars 1:1.  `blend` is the weight of the class pattern in an image (the rest
     is uniform noise): small enough that the task is not solved trivially.  Returns a dict with the final accuracy over all classes seen,
     the accuracy after each task and the number of steps taken.  graphed=True replays each task's training step from
-    CUDA graphs (recorded anew per task, because the head grows)."""
+    CUDA graphs (recorded anew per task, because the head grows).  norm, fused_loss, clip_norm: see ResNet18Width and
+    cnn_train_step."""
     n_classes = tasks * classes_per_task
     patterns = class_patterns(n_classes, seed, device)
     torch.manual_seed(seed)
-    model = ResNet18Width(n_classes, quantized=quantized, **over).to(device)
+    model = ResNet18Width(n_classes, quantized=quantized, norm=norm, **over).to(device)
     opt = torch.optim.SGD(model.parameters(), lr=lr, momentum=0.9, weight_decay=2e-4)
     g = torch.Generator(device=device)
     g.manual_seed(seed + 1)
@@ -488,12 +635,13 @@ def class_incremental_run(quantized: bool, device, tasks: int = 5, classes_per_t
                 x = torch.cat([x, mem_x[idx]])
                 y = torch.cat([y, mem_y[idx]])
             if not graphed:
-                loss = cnn_train_step(model, opt, x, y, step, n_seen=hi)
+                loss = cnn_train_step(model, opt, x, y, step, n_seen=hi, fused_loss=fused_loss, clip_norm=clip_norm)
                 step += 1
             elif stepper is None:
                 # (its three warm-up steps train on this first batch and count as steps of the task)
                 stepper = GraphedTrainStep(model, opt, x, y, forward=lambda inp, n=hi: model(inp, n),
-                                           base_step=(task + 1) * 1000003)
+                                           base_step=(task + 1) * 1000003, clip_norm=clip_norm,
+                                           loss=(lambda inp, lab, n=hi: model.loss(inp, lab, n)) if fused_loss else None)
                 loss = stepper.losses[0]
                 step += 3
             else:

@@ -118,6 +118,23 @@ def test_same_bits_again_and_on_another_stream():
     assert all(float(a) == float(norm) for a in again)
 
 
+@pytest.mark.gpu
+def test_scaling_by_a_device_scalar():
+    ts = _lists([1, 100, 70_001, 33], ["fp32", "bf16", "fp16", "fp32"], seed=6)
+    for f in (0.37, -3.0, 1.0, 0.0):
+        factor = torch.tensor(f, device="cuda")
+        out = [torch.full_like(t, 5) for t in ts]
+        hdqt.scale_tensors(ts, factor, out=out)
+        want = [(t.float() * factor).to(t.dtype) for t in ts]           # one product, one rounding
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+        inplace = [t.clone() for t in ts]
+        hdqt.scale_tensors(inplace, factor)
+        assert all(torch.equal(a, b) for a, b in zip(inplace, want))
+    hdqt.scale_tensors([], factor)
+    with pytest.raises(ValueError):
+        hdqt.scale_tensors(ts, torch.ones(2, device="cuda"))
+
+
 def test_refusals():
     ok = torch.zeros(4)
     with pytest.raises(ValueError):
@@ -147,3 +164,7 @@ def test_refusals():
     assert call((256, 256, 8, 0), ws_bytes=16) == WS
     assert lib.hdqt_grad_norm(None, 2, 2, 256, 256, 1 << 20, None) == INVALID
     assert lib.hdqt_grad_norm_workspace_bytes(0) > 0
+    table = (C.c_int64 * 4)(256, 256, 8, 0)
+    assert lib.hdqt_scale_tensors(C.addressof(table), 1, None, None) == INVALID
+    assert lib.hdqt_scale_tensors(C.addressof(table), 1, 258, None) == ALIGN
+    assert lib.hdqt_scale_tensors(C.addressof(table), -1, 256, None) == INVALID
