@@ -27,12 +27,12 @@ constexpr int kRowThreads = 256;
 
 // ---- labels ------------------------------------------------------------------------------------------------
 
-// label[t] = class, -1 (ignored) or -2 (outside [0, classes)); scale[0] = 1 / kept rows (mean) or 1;
-// weight[t] = scale[0] times g[t] or g[0] (or 1 without g), the weight of a row's loss.  One block.
+// label[t] = class, -1 (ignored) or -2 (outside [0, classes)); scale[0] = 1 / kept rows (mean) or 1: factor of the reduced
+// loss; scale[1] = scale[0] g (0 if no row is kept): factor of its gradients.  One block.
 __global__ void __launch_bounds__(1024)
 xent_labels_kernel(const int64_t* __restrict__ labels, int64_t tokens, int64_t classes, int64_t ignore, int32_t mean,
-                   const float* __restrict__ g, int32_t g_rows, int32_t* __restrict__ label, float* __restrict__ weight,
-                   float* __restrict__ scale, int32_t* dev_status) {
+                   const float* __restrict__ g, int32_t* __restrict__ label, float* __restrict__ scale,
+                   int32_t* dev_status) {
   __shared__ int s_kept;
   chain_wait();
   if (threadIdx.x == 0) s_kept = 0;
@@ -56,11 +56,10 @@ xent_labels_kernel(const int64_t* __restrict__ labels, int64_t tokens, int64_t c
   }
   if (bad) report_status(dev_status, HDQT_ERR_INVALID_ARG);
   __syncthreads();
-  const float sc = mean ? 1.0f / (float)s_kept : 1.0f;
-  if (threadIdx.x == 0) scale[0] = sc;
-  if (weight != nullptr) {
-#pragma unroll 4
-    for (int64_t t = threadIdx.x; t < tokens; t += blockDim.x) weight[t] = (g != nullptr ? g[g_rows ? t : 0] : 1.0f) * sc;
+  if (threadIdx.x == 0) {
+    const float sc = mean ? 1.0f / (float)s_kept : 1.0f;
+    scale[0] = sc;
+    scale[1] = mean && s_kept == 0 ? 0.0f : sc * (g != nullptr ? *g : 1.0f);
   }
 }
 
@@ -160,7 +159,7 @@ xent_dz_kernel(const float2* __restrict__ part, int parts, int64_t parts_ld, con
     loss[row] = row_loss(lab, l, label_logit[row]);
   }
   const bool keep = lab >= 0;
-  const float w = keep ? weight[row] : 0.0f;
+  const float w = !keep ? 0.0f : weight != nullptr ? weight[row] : 1.0f;
   const float scale = w / v.s;
   if (kPlanes == 1) {
     uint4* codes = reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(z) + row * ld);
@@ -196,6 +195,66 @@ xent_dz_kernel(const float2* __restrict__ part, int parts, int64_t parts_ld, con
       o[j] = make_uint2(pack_bf16(p0[0], p0[1]), pack_bf16(p0[2], p0[3]));
       reinterpret_cast<uint2*>(planes + plane + row * ld)[j] = make_uint2(pack_bf16(p1[0], p1[1]), pack_bf16(p1[2], p1[3]));
       reinterpret_cast<uint2*>(planes + 2 * plane + row * ld)[j] = make_uint2(pack_bf16(p2[0], p2[1]), pack_bf16(p2[2], p2[3]));
+    }
+  }
+}
+
+// Few output blocks: the logits come as fp32 partial products [splits][rows][ld_part].  One block per row sums them in shared
+// memory, forms lse (or takes lse_in) and the loss, and writes dz in 1 or 3 bf16 planes (planes 0: no gradient).
+template <int kPlanes>
+__global__ void __launch_bounds__(kRowThreads)
+xent_softmax_kernel(const float* __restrict__ part, int splits, int64_t rows, int64_t ld_part, int classes,
+                    const int32_t* __restrict__ label, const float* __restrict__ weight, const float* __restrict__ lse_in,
+                    uint16_t* planes, int64_t ld, int64_t plane, float* __restrict__ lse, float* __restrict__ loss) {
+  extern __shared__ float s_z[];
+  __shared__ float s_m[kRowThreads / 32], s_s[kRowThreads / 32];
+  chain_wait();
+  const int64_t row = blockIdx.x;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const float* pr = part + row * ld_part;
+  const int64_t step = rows * ld_part;
+  float m = kLowest;
+#pragma unroll 2
+  for (int j = threadIdx.x; j < classes; j += kRowThreads) {
+    float z = pr[j];
+#pragma unroll 4
+    for (int s = 1; s < splits; ++s) z += pr[s * step + j];
+    s_z[j] = z;
+    m = fmaxf(m, z);
+  }
+  const int32_t lab = label[row];
+  float l;
+  if (lse_in != nullptr) {
+    l = lse_in[row];
+  } else {
+    float s = 0.0f;      // (a thread reads back what it wrote)
+    for (int j = threadIdx.x; j < classes; j += kRowThreads) s += ex2((s_z[j] - m) * kLog2e);
+    MaxSum v = warp_join(MaxSum{m, s});
+    if (lane == 0) { s_m[warp] = v.m; s_s[warp] = v.s; }
+    __syncthreads();
+    v = MaxSum{s_m[0], s_s[0]};
+#pragma unroll
+    for (int w = 1; w < kRowThreads / 32; ++w) v = join(v, MaxSum{s_m[w], s_s[w]});
+    l = v.m + logf(v.s);
+    if (threadIdx.x == 0) {
+      lse[row] = l;
+      loss[row] = row_loss(lab, l, lab >= 0 ? s_z[lab] : 0.0f);
+    }
+  }
+  if (kPlanes == 0) return;
+  const bool keep = lab >= 0;
+  const float w = !keep ? 0.0f : weight != nullptr ? weight[row] : 1.0f;
+  for (int j = threadIdx.x; j < classes; j += kRowThreads) {
+    const float e = keep ? w * (ex2((s_z[j] - l) * kLog2e) - (j == lab ? 1.0f : 0.0f)) : 0.0f;
+    if (kPlanes == 1) {
+      reinterpret_cast<__nv_bfloat16*>(planes)[row * ld + j] = __float2bfloat16_rn(e);
+    } else {
+      float p0, p1, p2;
+      split3(e, p0, p1, p2);
+      __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(planes) + row * ld + j;
+      o[0] = __float2bfloat16_rn(p0);
+      o[plane] = __float2bfloat16_rn(p1);
+      o[2 * plane] = __float2bfloat16_rn(p2);
     }
   }
 }
@@ -356,13 +415,15 @@ struct Plan {
   int64_t rows_piece, cols_piece;       // tokens x classes of a piece
   int64_t ld_z;
   int64_t parts_ld;
-  int splits_dx, splits_dw;
+  int splits_z, splits_dx, splits_dw;   // splits_z > 1: few output blocks, logits as partial products (xent_softmax_kernel)
+  int64_t ld_part;
   bool acc_dx, acc_dw;                  // fp32 sums over several pieces
   // workspace offsets
-  size_t label, scale, label_logit, loss_rows, weight, part, xs, ws, z, dz, dx_f32, dw_f32, total;
+  size_t label, scale, label_logit, loss_rows, part, xs, ws, z, dz, dx_f32, dw_f32, total;
 };
 
 constexpr int64_t kPieceBytes = 1ll << 30;
+constexpr int64_t kSoftmaxClasses = 12000;      // xent_softmax_kernel holds a row of fp32 logits in 48 KB
 
 // Small problems: the rows kernel reads W from the L2 once per block and product, the tensor-core path costs five launches
 // and two pipelines' fill and drain whatever the size.
@@ -370,15 +431,15 @@ constexpr int64_t kSmallTokens = 512, kSmallWeights = 1 << 18, kSmallWork = 1 <<
 constexpr size_t kSmallSmem = 100 << 10;
 constexpr int kFewBlocks = 4 * kNumSMsHint;      // most blocks of the few-token kernels
 
-// Work items along the contraction of a product of `blocks` output blocks of `kblocks` stages, next to `other` stages of
+// Work items along the contraction of a product of `blocks` output blocks of `kblocks` x `products` stages, next to `other` stages of
 // shorter items: the number with the shortest schedule on `pairs` CTA pairs.  A split adds one pass over fp32 partial
 // outputs (8 bytes per element at about 6 TB/s against 0.3 us per stage).
-int choose_splits(int64_t blocks, int64_t kblocks, int64_t elements, int64_t other, int64_t pairs) {
+int choose_splits(int64_t blocks, int64_t kblocks, int64_t products, int64_t elements, int64_t other, int64_t pairs) {
   int best = 1;
   double best_time = 0.0;
   for (int s = 1; s <= 16; ++s) {
-    const int64_t len = ceil_div(kblocks, s), items = blocks * s;
-    if (s > 1 && len < 16) break;
+    const int64_t len = ceil_div(kblocks, s) * products, items = blocks * s;
+    if (s > 1 && (len < 12 || ceil_div(kblocks, s) == ceil_div(kblocks, s - 1))) continue;
     const int64_t whole = items / pairs, more = items % pairs;
     const double mean = (double)(items * len + other) / (double)pairs;
     const double longest = (double)((whole + (more > 0)) * len);
@@ -458,8 +519,13 @@ hdqt_status_t make_plan(const hdqt_xent_desc_t* d, int kind, Plan* pl) {
   const int64_t dx_blocks = ceil_div(pl->rows_piece, XM) * ceil_div(D, XN), dx_k = ceil_div(pl->cols_piece, XK);
   const int64_t dw_blocks = ceil_div(pl->cols_piece, XM) * ceil_div(D, XN), dw_k = ceil_div(pl->rows_piece, XK);
   const bool whole = !pl->acc_dx && !pl->acc_dw;
-  pl->splits_dx = whole ? choose_splits(dx_blocks, dx_k, pl->rows_piece * D, dw_blocks * dw_k, pairs) : 1;
-  pl->splits_dw = whole ? choose_splits(dw_blocks, dw_k, pl->cols_piece * D, dx_blocks * dx_k, pairs) : 1;
+  const int64_t products = f32 ? 6 : 1;
+  pl->splits_dx = whole ? choose_splits(dx_blocks, dx_k, products, pl->rows_piece * D, dw_blocks * dw_k * products, pairs) : 1;
+  pl->splits_dw = whole ? choose_splits(dw_blocks, dw_k, products, pl->cols_piece * D, dx_blocks * dx_k * products, pairs) : 1;
+  pl->splits_z = 1;
+  pl->ld_part = ceil_div(V, 8) * 8;
+  if (pl->rows_piece == T && pl->cols_piece == V && V <= kSoftmaxClasses && d->piece_bytes == 0)
+    pl->splits_z = choose_splits(ceil_div(T, XM) * ceil_div(V, XN), ceil_div(D, XK), products, T * V, 0, pairs);
 
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o += up256(bytes); return at; };
@@ -479,12 +545,14 @@ hdqt_status_t make_plan(const hdqt_xent_desc_t* d, int kind, Plan* pl) {
   pl->scale = take(256);
   pl->label_logit = take(4 * T);
   pl->loss_rows = take(4 * T);
-  pl->weight = take(4 * T);
   pl->part = kind == HDQT_XENT_BWD ? o : take(8 * pl->rows_piece * pl->parts_ld);
   pl->xs = pl->stage_x ? take(2 * pl->planes * T * pl->ld_xs) : o;
   pl->ws = pl->stage_w ? take(2 * pl->planes * pl->w_rows * pl->ld_ws) : o;
   pl->z = pl->dz = o;
-  if (kind == HDQT_XENT_TRAIN) {
+  if (pl->splits_z > 1) {
+    pl->z = take(4 * pl->splits_z * T * pl->ld_part);
+    pl->dz = kind == HDQT_XENT_FWD ? o : take(2 * pl->planes * T * pl->ld_z);
+  } else if (kind == HDQT_XENT_TRAIN) {
     pl->z = take((f32 ? 4 : 2) * pl->rows_piece * pl->ld_z);
     pl->dz = f32 ? take(6 * pl->rows_piece * pl->ld_z) : pl->z;
   } else if (kind == HDQT_XENT_BWD) {
@@ -508,6 +576,8 @@ struct Call {
   int32_t* dev_status;
   cudaStream_t s;
   Operand x, w;          // as stored: x [tokens, features], w [w_rows, w_cols]
+  const float* row_weights = nullptr;   // [tokens]: weights of the rows' losses
+  const float* alpha = nullptr;         // or one weight for all, applied to the gradient products
 
   mutable bool started = false;
 
@@ -590,7 +660,7 @@ hdqt_status_t stage(const Call& c, const void* src, int64_t ld, int64_t rows, in
   return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy operands");
 }
 
-hdqt_status_t prepare(Call* c, const void* X, const void* W, const int64_t* labels, const float* g, bool gradients) {
+hdqt_status_t prepare(Call* c, const void* X, const void* W, const int64_t* labels, const float* g) {
   const hdqt_xent_desc_t& d = *c->d;
   const Plan& pl = c->pl;
   c->x = Operand{X, d.features, d.tokens, d.ld_x, 0, pl.planes};
@@ -599,8 +669,13 @@ hdqt_status_t prepare(Call* c, const void* X, const void* W, const int64_t* labe
   if (pl.stage_x) st = stage(*c, X, d.ld_x, d.tokens, d.features, pl.xs, pl.ld_xs, &c->x);
   if (st == HDQT_OK && pl.stage_w) st = stage(*c, W, d.ld_w, pl.w_rows, pl.w_cols, pl.ws, pl.ld_ws, &c->w);
   if (st != HDQT_OK) return st;
-  c->run(xent_labels_kernel, 1, d.tokens > 512 ? 1024 : 256, 0, labels, d.tokens, d.classes, d.ignore_index, d.reduction == HDQT_REDUCE_MEAN, g, d.reduction == HDQT_REDUCE_NONE,
-      c->at<int32_t>(pl.label), gradients ? c->at<float>(pl.weight) : nullptr, c->at<float>(pl.scale), c->dev_status);
+  // a weight per row goes into dz; one weight for all multiplies the fp32 sums of the gradient products, so that rounding dz
+  // to bf16 never rounds the weight (1 / rows would be off by the same 0.1 % in almost every element)
+  const bool rows = d.reduction == HDQT_REDUCE_NONE;
+  c->row_weights = rows ? g : nullptr;
+  c->alpha = rows ? nullptr : c->at<float>(pl.scale) + 1;
+  c->run(xent_labels_kernel, 1, d.tokens > 512 ? 1024 : 256, 0, labels, d.tokens, d.classes, d.ignore_index,
+         d.reduction == HDQT_REDUCE_MEAN, rows ? nullptr : g, c->at<int32_t>(pl.label), c->at<float>(pl.scale), c->dev_status);
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy labels");
 }
@@ -618,6 +693,7 @@ hdqt_status_t gradient_products(const Call& c, int64_t t0, int64_t nt, int64_t v
   const int64_t D = d.features;
   XParams p;
   fill_common(c, &p);
+  p.alpha = c.alpha;
   Product g[2];
   int n = 0;
   const Operand dz = c.dz(nt, nv);
@@ -805,6 +881,32 @@ hdqt_status_t small(const Call& c, int kind, const void* X, const void* W, const
                                        : run_small<float>(c, kind, X, W, labels, lse_in, g, loss, lse, dX, dW);
 }
 
+// Few output blocks: logits in partial products, then a block per row.  dz (kind != forward) is left for the gradient products.
+hdqt_status_t split_logits(const Call& c, int kind, const float* lse_in, float* loss_rows, float* lse) {
+  const hdqt_xent_desc_t& d = *c.d;
+  const Plan& pl = c.pl;
+  const Product g = logits_product(c, 0, d.tokens, 0, d.classes);
+  XParams p;
+  fill_common(c, &p);
+  p.pr[0] = make_problem(g, pl.splits_z);
+  p.pr[0].out = c.at<float>(pl.z);
+  p.pr[0].ld_out = pl.ld_part;
+  p.pr[0].split_stride = d.tokens * pl.ld_part;
+  const hdqt_status_t st = launch<X_OUT>(p, &g, 1, c);
+  if (st != HDQT_OK) return st;
+  const size_t smem = sizeof(float) * (size_t)d.classes;
+  auto go = [&](auto kernel) {
+    c.run(kernel, (unsigned)d.tokens, kRowThreads, smem, c.at<float>(pl.z), p.pr[0].splits, d.tokens, pl.ld_part,
+          (int)d.classes, c.at<int32_t>(pl.label), c.row_weights, lse_in, c.at<uint16_t>(pl.dz), pl.ld_z,
+          d.tokens * pl.ld_z, lse, loss_rows);
+  };
+  if (kind == HDQT_XENT_FWD) go(xent_softmax_kernel<0>);
+  else if (pl.planes == 1) go(xent_softmax_kernel<1>);
+  else go(xent_softmax_kernel<3>);
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy rows");
+}
+
 bool outputs_misaligned(const hdqt_xent_desc_t* d, const void* a, const void* b) {
   return ((reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) & (uintptr_t)(dtype_size(d->dtype) - 1)) != 0;
 }
@@ -833,9 +935,13 @@ extern "C" hdqt_status_t hdqt_linear_xent_fwd(const hdqt_xent_desc_t* d, const v
   if (floats_misaligned(loss, lse, nullptr)) return HDQT_ERR_ALIGNMENT;
   if (c.pl.small_rows > 0) return small(c, HDQT_XENT_FWD, X, W, labels, nullptr, nullptr, loss, lse, nullptr, nullptr);
   if (c.pl.few_tokens > 0) return few(c, X, W, labels, loss, lse);
-  st = prepare(&c, X, W, labels, nullptr, false);
+  st = prepare(&c, X, W, labels, nullptr);
   if (st != HDQT_OK) return st;
   float* rows = d->reduction == HDQT_REDUCE_NONE ? loss : c.at<float>(c.pl.loss_rows);
+  if (d->tokens > 0 && c.pl.splits_z > 1) {
+    st = split_logits(c, HDQT_XENT_FWD, nullptr, rows, lse);
+    return st == HDQT_OK ? reduce_loss(c, loss) : st;
+  }
   for (int64_t t0 = 0; t0 < d->tokens; t0 += c.pl.rows_piece) {
     const int64_t nt = d->tokens - t0 < c.pl.rows_piece ? d->tokens - t0 : c.pl.rows_piece;
     const Product g = logits_product(c, t0, nt, 0, d->classes);
@@ -864,8 +970,12 @@ extern "C" hdqt_status_t hdqt_linear_xent_bwd(const hdqt_xent_desc_t* d, const v
   if (!dX && !dW) return HDQT_OK;
   if (d->tokens == 0) return dW ? zero_out(c, dW, c.pl.w_rows, c.pl.w_cols, d->ld_dw) : HDQT_OK;
   if (c.pl.small_rows > 0) return small(c, HDQT_XENT_BWD, X, W, labels, lse, gr, nullptr, nullptr, dX, dW);
-  st = prepare(&c, X, W, labels, gr, true);
+  st = prepare(&c, X, W, labels, gr);
   if (st != HDQT_OK) return st;
+  if (c.pl.splits_z > 1) {
+    st = split_logits(c, HDQT_XENT_BWD, lse, nullptr, nullptr);
+    return st == HDQT_OK ? gradient_products(c, 0, d->tokens, 0, d->classes, dX, dW, true, true) : st;
+  }
   for (int64_t v0 = 0; v0 < d->classes; v0 += c.pl.cols_piece) {
     const int64_t nv = d->classes - v0 < c.pl.cols_piece ? d->classes - v0 : c.pl.cols_piece;
     const Product g = logits_product(c, 0, d->tokens, v0, nv);
@@ -878,8 +988,7 @@ extern "C" hdqt_status_t hdqt_linear_xent_bwd(const hdqt_xent_desc_t* d, const v
     p.ld_z = c.pl.ld_z;
     p.plane_z = c.pl.rows_piece * c.pl.ld_z;
     p.lse = lse;
-    p.g = c.at<float>(c.pl.weight);
-    p.g_rows = 1;
+    p.g = c.row_weights;
     st = launch<X_DZ>(p, &g, 1, c);
     if (st != HDQT_OK) return st;
     st = gradient_products(c, 0, d->tokens, v0, nv, dX, dW, v0 == 0, v0 + nv == d->classes);
@@ -899,13 +1008,18 @@ extern "C" hdqt_status_t hdqt_linear_xent_train(const hdqt_xent_desc_t* d, const
   if (d->tokens > 0 && d->reduction == HDQT_REDUCE_NONE && !gr) return HDQT_ERR_INVALID_ARG;
   if (floats_misaligned(loss, lse, gr) || outputs_misaligned(d, dX, dW)) return HDQT_ERR_ALIGNMENT;
   if (c.pl.small_rows > 0) return small(c, HDQT_XENT_TRAIN, X, W, labels, nullptr, gr, loss, lse, dX, dW);
-  st = prepare(&c, X, W, labels, gr, true);
+  st = prepare(&c, X, W, labels, gr);
   if (st != HDQT_OK) return st;
   if (d->tokens == 0) {
     if (dW) st = zero_out(c, dW, c.pl.w_rows, c.pl.w_cols, d->ld_dw);
     return st == HDQT_OK ? reduce_loss(c, loss) : st;
   }
   float* rows = d->reduction == HDQT_REDUCE_NONE ? loss : c.at<float>(c.pl.loss_rows);
+  if (c.pl.splits_z > 1) {
+    st = split_logits(c, HDQT_XENT_TRAIN, nullptr, rows, lse);
+    if (st == HDQT_OK) st = gradient_products(c, 0, d->tokens, 0, d->classes, dX, dW, true, true);
+    return st == HDQT_OK ? reduce_loss(c, loss) : st;
+  }
   for (int64_t t0 = 0; t0 < d->tokens; t0 += c.pl.rows_piece) {
     const int64_t nt = d->tokens - t0 < c.pl.rows_piece ? d->tokens - t0 : c.pl.rows_piece;
     const Product g = logits_product(c, t0, nt, 0, d->classes);
@@ -926,11 +1040,11 @@ extern "C" hdqt_status_t hdqt_linear_xent_train(const hdqt_xent_desc_t* d, const
     const dim3 grid((unsigned)nt, (unsigned)(slices < most ? slices : most));
     if (c.pl.planes == 1)
       c.run(xent_dz_kernel<1>, grid, kRowThreads, 0, p.part, (int)p.parts_ld, p.parts_ld, p.label, p.label_logit,
-                                                               c.at<float>(c.pl.weight) + t0, d->classes, p.z, c.pl.ld_z,
+                                                               c.row_weights ? c.row_weights + t0 : nullptr, d->classes, p.z, c.pl.ld_z,
             static_cast<uint16_t*>(nullptr), 0, lse + t0, rows + t0);
     else
       c.run(xent_dz_kernel<3>, grid, kRowThreads, 0, p.part, (int)p.parts_ld, p.parts_ld, p.label, p.label_logit,
-                                                               c.at<float>(c.pl.weight) + t0, d->classes, p.z, c.pl.ld_z,
+                                                               c.row_weights ? c.row_weights + t0 : nullptr, d->classes, p.z, c.pl.ld_z,
                                                                c.at<uint16_t>(c.pl.dz), c.pl.rows_piece * c.pl.ld_z,
                                                                lse + t0, rows + t0);
     st = gradient_products(c, t0, nt, 0, d->classes, dX, dW, t0 == 0, t0 + nt == d->tokens);

@@ -83,8 +83,8 @@ struct XParams {
   void* z;                         // codes (uint16), logits (fp32) or dz (bf16 planes)
   int64_t ld_z, plane_z;           // elements
   const float* lse;                // [M]
-  const float* g;                  // weight of each row's loss: [M], or one value
-  int32_t g_rows;                  // 0: *g is the weight of every row
+  const float* g;                  // weight of each row's loss, [M]; null: 1
+  const float* alpha;              // X_OUT: the output is this times the product; null: 1
   int32_t* dev_status;
 };
 
@@ -253,7 +253,7 @@ __device__ __forceinline__ void x_dz(const XParams& p, const XProblem& r, int ro
   if (row >= r.M || ncols <= 0) return;
   const int lab_row = __ldg(p.label + row);
   const bool keep = lab_row >= 0;
-  const float lse = p.lse[row], g = p.g[p.g_rows ? row : 0];
+  const float lse = p.lse[row], g = p.g != nullptr ? p.g[row] : 1.0f;
   const int lab = lab_row - p.n0 - col0;
 #pragma unroll
   for (int j = 0; j < 128; ++j) {
@@ -287,9 +287,14 @@ __device__ __forceinline__ void x_dz(const XParams& p, const XProblem& r, int ro
   }
 }
 
-__device__ __forceinline__ void x_out(const XProblem& r, const XItem& t, int row, int col0, float (&acc)[128]) {
+__device__ __forceinline__ void x_out(const XParams& p, const XProblem& r, const XItem& t, int row, int col0, float (&acc)[128]) {
   const int ncols = r.N - col0;
   if (row >= r.M || ncols <= 0) return;
+  if (p.alpha != nullptr) {
+    const float alpha = *p.alpha;
+#pragma unroll
+    for (int j = 0; j < 128; ++j) acc[j] *= alpha;
+  }
   const int64_t at = (int64_t)row * r.ld_out + col0 + t.split * r.split_stride;
   if (r.add != nullptr) {
     const float* a = r.add + (int64_t)row * r.ld_add + col0;
@@ -556,7 +561,7 @@ xent_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_consta
       const int col0 = t.n * XN + half * 128;
       if constexpr (kEpi == X_STATS || kEpi == X_CODES || kEpi == X_LOGITS) x_stats<kEpi>(p, r, t, row, col0, half, acc);
       else if constexpr (kEpi == X_DZ) x_dz(p, r, row, col0, acc);
-      else x_out(r, t, row, col0, acc);
+      else x_out(p, r, t, row, col0, acc);
     }
   }
 
