@@ -261,26 +261,33 @@ xent_softmax_kernel(const float* __restrict__ part, int splits, int64_t rows, in
 
 // ---- operands that cannot be read in place ---------------------------------------------------------------------
 
-// fp32 -> three bf16 planes, or bf16 -> a copy with rows that start on 16 bytes; two columns per thread
-template <typename T>
+// fp32 -> three bf16 planes, or bf16 -> a copy with rows that start on 16 bytes; kV columns per thread (one access where the
+// rows of the source allow it, else element by element), a block walks down the rows
+template <typename T, int kV, bool kWide>
 __global__ void __launch_bounds__(256) xent_stage_kernel(const T* __restrict__ src, int64_t ld, int64_t rows, int64_t cols,
                                                          uint16_t* __restrict__ dst, int64_t ld_dst, int64_t plane) {
   chain_wait();
-  const int64_t c = 2 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
+  const int64_t c = kV * ((int64_t)blockIdx.x * 256 + threadIdx.x);
   if (c >= cols) return;
+#pragma unroll 4
   for (int64_t r = blockIdx.y; r < rows; r += gridDim.y) {
-    const T* s = src + r * ld + c;
-    const float a = to_f32(s[0]), b = c + 1 < cols ? to_f32(s[1]) : 0.0f;
-    uint16_t* d = dst + r * ld_dst + c;
-    if (sizeof(T) == 2) {
-      *reinterpret_cast<uint32_t*>(d) = pack_bf16(a, b);
+    float x[kV];
+    if constexpr (kWide) {
+      unpack(*reinterpret_cast<const Vec<T, kV>*>(src + r * ld + c), x);
     } else {
-      float a0, a1, a2, b0, b1, b2;
-      split3(a, a0, a1, a2);
-      split3(b, b0, b1, b2);
-      *reinterpret_cast<uint32_t*>(d) = pack_bf16(a0, b0);
-      *reinterpret_cast<uint32_t*>(d + plane) = pack_bf16(a1, b1);
-      *reinterpret_cast<uint32_t*>(d + 2 * plane) = pack_bf16(a2, b2);
+#pragma unroll
+      for (int j = 0; j < kV; ++j) x[j] = c + j < cols ? to_f32(src[r * ld + c + j]) : 0.0f;
+    }
+    uint16_t* d = dst + r * ld_dst + c;
+    if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<Vec<__nv_bfloat16, kV>*>(d) = pack<__nv_bfloat16>(x);
+    } else {
+      float p0[kV], p1[kV], p2[kV];
+#pragma unroll
+      for (int j = 0; j < kV; ++j) split3(x[j], p0[j], p1[j], p2[j]);
+      *reinterpret_cast<Vec<__nv_bfloat16, kV>*>(d) = pack<__nv_bfloat16>(p0);
+      *reinterpret_cast<Vec<__nv_bfloat16, kV>*>(d + plane) = pack<__nv_bfloat16>(p1);
+      *reinterpret_cast<Vec<__nv_bfloat16, kV>*>(d + 2 * plane) = pack<__nv_bfloat16>(p2);
     }
   }
 }
@@ -651,11 +658,19 @@ hdqt_status_t stage(const Call& c, const void* src, int64_t ld, int64_t rows, in
   o->ld = ld_dst;
   o->plane = rows * ld_dst;
   if (rows == 0) return HDQT_OK;
-  const dim3 grid((unsigned)ceil_div(cols, 512), (unsigned)(rows < 16384 ? rows : 16384));
-  if (c.d->dtype == HDQT_DTYPE_F32)
-    c.run(xent_stage_kernel<float>, grid, 256, 0, reinterpret_cast<const float*>(src), ld, rows, cols, dst, ld_dst, rows * ld_dst);
-  else
-    c.run(xent_stage_kernel<__nv_bfloat16>, grid, 256, 0, reinterpret_cast<const __nv_bfloat16*>(src), ld, rows, cols, dst, ld_dst, 0);
+  // four rows per thread while that leaves enough blocks
+  const int64_t bx = ceil_div(cols, 1024);
+  int64_t by = ceil_div(rows, 4);
+  if (bx * by < 8 * kNumSMsHint) by = rows;
+  const dim3 grid((unsigned)bx, (unsigned)(by < 65535 ? by : 65535));
+  if (c.d->dtype == HDQT_DTYPE_F32) {
+    const bool wide = (reinterpret_cast<uintptr_t>(src) & 15) == 0 && ld % 4 == 0 && cols % 4 == 0;
+    c.run(wide ? xent_stage_kernel<float, 4, true> : xent_stage_kernel<float, 4, false>, grid, 256, 0,
+          reinterpret_cast<const float*>(src), ld, rows, cols, dst, ld_dst, rows * ld_dst);
+  } else {
+    c.run(xent_stage_kernel<__nv_bfloat16, 4, false>, grid, 256, 0, reinterpret_cast<const __nv_bfloat16*>(src), ld, rows, cols,
+          dst, ld_dst, 0);
+  }
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy operands");
 }

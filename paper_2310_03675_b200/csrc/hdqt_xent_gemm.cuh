@@ -32,7 +32,9 @@ constexpr int X_OPERAND = 128 * 128;                // one operand's bytes per s
 constexpr int X_STAGE_BYTES = 2 * X_OPERAND;
 constexpr int X_EPI_WARPS = 8;
 constexpr int X_THREADS = 32 * (2 + X_EPI_WARPS);
-constexpr int X_SMEM = X_STAGES * X_STAGE_BYTES + 256;
+constexpr int X_BOX = 32 * 33 * 4;                  // per epilogue warp: 32 rows x 32 columns fp32 for the store transpose
+constexpr int X_BOX_OFF = X_STAGES * X_STAGE_BYTES + 256;
+constexpr int X_SMEM = X_BOX_OFF + X_EPI_WARPS * X_BOX;
 constexpr int X_TMEM_COLS = 512;
 static_assert(X_SMEM <= 232448, "exceeds the 227 KB of shared memory a CTA may use");
 
@@ -313,14 +315,14 @@ __device__ __forceinline__ void x_out(const XParams& p, const XProblem& r, const
   }
   if (r.out_bf16) {
     __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(r.out) + at;
-    const uintptr_t low = reinterpret_cast<uintptr_t>(o) & 31;      // rows of 16 bytes' multiples alternate between 0 and 16
+    const bool high = (reinterpret_cast<uintptr_t>(o) & 16) != 0;      // rows of 16 bytes' multiples alternate between 0 and 16
 #pragma unroll
     for (int j = 0; j < 128; j += 16) {
-      if ((low & 15) == 0 && j + 16 <= ncols) {
+      if (j + 16 <= ncols) {
         uint32_t v[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = pack_bf16(acc[j + 2 * k], acc[j + 2 * k + 1]);
-        if (low == 0) {
+        if (!high) {
           st256(o + j, v);
         } else {
           *reinterpret_cast<uint4*>(o + j) = make_uint4(v[0], v[1], v[2], v[3]);
@@ -334,14 +336,14 @@ __device__ __forceinline__ void x_out(const XParams& p, const XProblem& r, const
     }
   } else {
     float* o = reinterpret_cast<float*>(r.out) + at;
-    const uintptr_t low = reinterpret_cast<uintptr_t>(o) & 31;
+    const bool high = (reinterpret_cast<uintptr_t>(o) & 16) != 0;
 #pragma unroll
     for (int j = 0; j < 128; j += 8) {
-      if ((low & 15) == 0 && j + 8 <= ncols) {
+      if (j + 8 <= ncols) {
         uint32_t v[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = __float_as_uint(acc[j + k]);
-        if (low == 0) {
+        if (!high) {
           st256(o + j, v);
         } else {
           *reinterpret_cast<uint4*>(o + j) = make_uint4(v[0], v[1], v[2], v[3]);
@@ -354,6 +356,40 @@ __device__ __forceinline__ void x_out(const XParams& p, const XProblem& r, const
       }
     }
   }
+}
+
+// Output rows that do not all start on 16 bytes: 32 x 32 pieces are turned in shared memory, so that the 32 lanes of a store
+// write neighbouring elements of one row (a store per element and row of its own took 1531 x 1001 x 50257 XXODD us).
+__device__ __forceinline__ void x_out_odd(const XParams& p, const XProblem& r, const XItem& t, int row0, int col0, int lane,
+                                          float* box, float (&acc)[128]) {
+  const float alpha = p.alpha != nullptr ? *p.alpha : 1.0f;
+  const int rows = min(32, r.M - row0);
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const int col = col0 + 32 * c;
+    if (col >= r.N) break;
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 32; ++k) box[lane * 33 + k] = acc[32 * c + k] * alpha;
+    __syncwarp();
+    if (col + lane < r.N) {
+      const int64_t at = (int64_t)row0 * r.ld_out + col + lane + t.split * r.split_stride;
+      const float* a = r.add != nullptr ? r.add + (int64_t)row0 * r.ld_add + col + lane : nullptr;
+#pragma unroll 8
+      for (int i = 0; i < rows; ++i) {
+        float v = box[i * 33 + lane];
+        if (a != nullptr) v += a[i * r.ld_add];
+        if (r.out_bf16) reinterpret_cast<__nv_bfloat16*>(r.out)[at + i * r.ld_out] = __float2bfloat16_rn(v);
+        else reinterpret_cast<float*>(r.out)[at + i * r.ld_out] = v;
+      }
+    }
+  }
+}
+
+// whether every row of the output starts on 16 bytes
+__device__ __forceinline__ bool x_out_even(const XProblem& r) {
+  const int size = r.out_bf16 ? 2 : 4;
+  return ((reinterpret_cast<uintptr_t>(r.out) | (uintptr_t)(r.ld_out * size) | (uintptr_t)(r.split_stride * size)) & 15) == 0;
 }
 
 // Tensor maps: K-major operand {k, rows, planes} with box {64, 128, 1}; MN-major {rows, k, planes} with box {64, 64, 1}
@@ -561,7 +597,8 @@ xent_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_consta
       const int col0 = t.n * XN + half * 128;
       if constexpr (kEpi == X_STATS || kEpi == X_CODES || kEpi == X_LOGITS) x_stats<kEpi>(p, r, t, row, col0, half, acc);
       else if constexpr (kEpi == X_DZ) x_dz(p, r, row, col0, acc);
-      else x_out(p, r, t, row, col0, acc);
+      else if (x_out_even(r)) x_out(p, r, t, row, col0, acc);
+      else x_out_odd(p, r, t, row - lane, col0, lane, reinterpret_cast<float*>(smem_raw + X_BOX_OFF + (warp - 2) * X_BOX), acc);
     }
   }
 
