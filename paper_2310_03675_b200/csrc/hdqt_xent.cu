@@ -201,13 +201,13 @@ xent_dz_kernel(const float2* __restrict__ part, int parts, int64_t parts_ld, con
 
 // Few output blocks: the logits come as fp32 partial products [splits][rows][ld_part].  One block per row sums them in shared
 // memory, forms lse (or takes lse_in) and the loss, and writes dz in 1 or 3 bf16 planes (planes 0: no gradient).
-template <int kPlanes>
-__global__ void __launch_bounds__(kRowThreads)
+template <int kPlanes, int kThreads>
+__global__ void __launch_bounds__(kThreads)
 xent_softmax_kernel(const float* __restrict__ part, int splits, int64_t rows, int64_t ld_part, int classes,
                     const int32_t* __restrict__ label, const float* __restrict__ weight, const float* __restrict__ lse_in,
                     uint16_t* planes, int64_t ld, int64_t plane, float* __restrict__ lse, float* __restrict__ loss) {
   extern __shared__ float s_z[];
-  __shared__ float s_m[kRowThreads / 32], s_s[kRowThreads / 32];
+  __shared__ float s_m[kThreads / 32], s_s[kThreads / 32];
   chain_wait();
   const int64_t row = blockIdx.x;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -215,7 +215,7 @@ xent_softmax_kernel(const float* __restrict__ part, int splits, int64_t rows, in
   const int64_t step = rows * ld_part;
   float m = kLowest;
 #pragma unroll 2
-  for (int j = threadIdx.x; j < classes; j += kRowThreads) {
+  for (int j = threadIdx.x; j < classes; j += kThreads) {
     float z = pr[j];
 #pragma unroll 4
     for (int s = 1; s < splits; ++s) z += pr[s * step + j];
@@ -228,13 +228,13 @@ xent_softmax_kernel(const float* __restrict__ part, int splits, int64_t rows, in
     l = lse_in[row];
   } else {
     float s = 0.0f;      // (a thread reads back what it wrote)
-    for (int j = threadIdx.x; j < classes; j += kRowThreads) s += ex2((s_z[j] - m) * kLog2e);
+    for (int j = threadIdx.x; j < classes; j += kThreads) s += ex2((s_z[j] - m) * kLog2e);
     MaxSum v = warp_join(MaxSum{m, s});
     if (lane == 0) { s_m[warp] = v.m; s_s[warp] = v.s; }
     __syncthreads();
     v = MaxSum{s_m[0], s_s[0]};
 #pragma unroll
-    for (int w = 1; w < kRowThreads / 32; ++w) v = join(v, MaxSum{s_m[w], s_s[w]});
+    for (int w = 1; w < kThreads / 32; ++w) v = join(v, MaxSum{s_m[w], s_s[w]});
     l = v.m + logf(v.s);
     if (threadIdx.x == 0) {
       lse[row] = l;
@@ -244,7 +244,7 @@ xent_softmax_kernel(const float* __restrict__ part, int splits, int64_t rows, in
   if (kPlanes == 0) return;
   const bool keep = lab >= 0;
   const float w = !keep ? 0.0f : weight != nullptr ? weight[row] : 1.0f;
-  for (int j = threadIdx.x; j < classes; j += kRowThreads) {
+  for (int j = threadIdx.x; j < classes; j += kThreads) {
     const float e = keep ? w * (ex2((s_z[j] - l) * kLog2e) - (j == lab ? 1.0f : 0.0f)) : 0.0f;
     if (kPlanes == 1) {
       reinterpret_cast<__nv_bfloat16*>(planes)[row * ld + j] = __float2bfloat16_rn(e);
@@ -416,6 +416,8 @@ struct Plan {
   int small_rows;                       // > 0: small problem (hdqt_xent_small.cuh), tokens per block
   size_t small_smem;
   int few_tokens;                       // > 0: loss of a few tokens (hdqt_xent_few.cuh), tokens a thread accumulates
+  int few_grad;                         // > 0: a few tokens by streamed products, tokens a thread accumulates
+  int few_z_slices, few_dx_slices;
   bool stage_x, stage_w;
   int64_t ld_xs, ld_ws;                 // of the staged copies
   int64_t w_rows, w_cols;
@@ -491,6 +493,13 @@ hdqt_status_t make_plan(const hdqt_xent_desc_t* d, int kind, Plan* pl) {
     while (n < d->tokens) n *= 2;
     if (4 * n * d->features <= kFewSmem) pl->few_tokens = n;
   }
+  // Streamed products, up to where their 3 tokens x |W| fp32 operations pass the time of the tensor-core path with its blocks
+  // of 256 rows (fp32: six products and three planes of W).
+  pl->few_grad = 0;
+  if (pl->small_rows == 0 && pl->few_tokens == 0 && d->tokens > 0 && d->tokens <= (f32 ? 16 : 8) && d->piece_bytes == 0) {
+    pl->few_grad = 1;
+    while (pl->few_grad < d->tokens) pl->few_grad *= 2;
+  }
   pl->stage_x = f32 || d->ld_x % 8 != 0;
   pl->stage_w = f32 || d->ld_w % 8 != 0;
   pl->ld_xs = ceil_div(d->features, 8) * 8;
@@ -545,6 +554,27 @@ hdqt_status_t make_plan(const hdqt_xent_desc_t* d, int kind, Plan* pl) {
   if (pl->few_tokens > 0) {
     pl->label_logit = take(4 * T);
     pl->part = take(sizeof(float2) * T * kFewBlocks);
+    pl->total = o;
+    return HDQT_OK;
+  }
+  if (pl->few_grad > 0) {
+    // slices of the contraction: enough blocks to fill the machine, at least 64 rows or 512 columns each
+    // (threads of four columns on average; a block of 256)
+    const int64_t cols_blocks_v = ceil_div(V, 1024), cols_blocks_d = ceil_div(D, 1024);
+    auto slices = [&](int64_t blocks, int64_t k, int64_t least) {
+      int64_t s = ceil_div(6 * kNumSMsHint, blocks);
+      const int64_t most = ceil_div(k, least);
+      return (int)(s < most ? s : most);
+    };
+    pl->few_z_slices = d->w_is_cd ? slices(ceil_div(V, 16), D, 512) : slices(cols_blocks_v, D, 64);
+    pl->few_dx_slices = d->w_is_cd ? slices(cols_blocks_d, V, 64) : slices(ceil_div(D, 16), V, 512);
+    pl->label = take(4 * T);
+    pl->scale = take(256);
+    pl->loss_rows = take(4 * T);
+    pl->label_logit = take(4 * T);
+    pl->part = take(sizeof(float2) * T * ceil_div(V, kFewSpan));
+    pl->z = take(4 * T * V * pl->few_z_slices);
+    pl->dx_f32 = kind == HDQT_XENT_FWD ? o : take(4 * T * D * pl->few_dx_slices);
     pl->total = o;
     return HDQT_OK;
   }
@@ -658,21 +688,34 @@ hdqt_status_t stage(const Call& c, const void* src, int64_t ld, int64_t rows, in
   o->ld = ld_dst;
   o->plane = rows * ld_dst;
   if (rows == 0) return HDQT_OK;
-  // four rows per thread while that leaves enough blocks
-  const int64_t bx = ceil_div(cols, 1024);
+  // four rows per thread while that leaves enough blocks; fp32 in accesses of four, two or one element as the rows allow
+  const uintptr_t bits = reinterpret_cast<uintptr_t>(src) | (uintptr_t)(ld * 4) | (uintptr_t)(cols * 4);
+  const bool two = c.d->dtype == HDQT_DTYPE_F32 && (bits & 15) != 0 && (bits & 7) == 0;
+  const int64_t bx = ceil_div(cols, two ? 512 : 1024);
   int64_t by = ceil_div(rows, 4);
   if (bx * by < 8 * kNumSMsHint) by = rows;
   const dim3 grid((unsigned)bx, (unsigned)(by < 65535 ? by : 65535));
   if (c.d->dtype == HDQT_DTYPE_F32) {
-    const bool wide = (reinterpret_cast<uintptr_t>(src) & 15) == 0 && ld % 4 == 0 && cols % 4 == 0;
-    c.run(wide ? xent_stage_kernel<float, 4, true> : xent_stage_kernel<float, 4, false>, grid, 256, 0,
-          reinterpret_cast<const float*>(src), ld, rows, cols, dst, ld_dst, rows * ld_dst);
+    c.run((bits & 15) == 0 ? xent_stage_kernel<float, 4, true> : two ? xent_stage_kernel<float, 2, true> : xent_stage_kernel<float, 4, false>,
+          grid, 256, 0, reinterpret_cast<const float*>(src), ld, rows, cols, dst, ld_dst, rows * ld_dst);
   } else {
     c.run(xent_stage_kernel<__nv_bfloat16, 4, false>, grid, 256, 0, reinterpret_cast<const __nv_bfloat16*>(src), ld, rows, cols,
           dst, ld_dst, 0);
   }
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy operands");
+}
+
+void label_rows(Call* c, const int64_t* labels, const float* g) {
+  const hdqt_xent_desc_t& d = *c->d;
+  const Plan& pl = c->pl;
+  // a weight per row goes into dz; one weight for all multiplies the fp32 sums of the gradient products, so that rounding dz
+  // to bf16 never rounds the weight (1 / rows would be off by the same 0.1 % in almost every element)
+  const bool rows = d.reduction == HDQT_REDUCE_NONE;
+  c->row_weights = rows ? g : nullptr;
+  c->alpha = rows ? nullptr : c->at<float>(pl.scale) + 1;
+  c->run(xent_labels_kernel, 1, d.tokens > 512 ? 1024 : 256, 0, labels, d.tokens, d.classes, d.ignore_index,
+         d.reduction == HDQT_REDUCE_MEAN, rows ? nullptr : g, c->at<int32_t>(pl.label), c->at<float>(pl.scale), c->dev_status);
 }
 
 hdqt_status_t prepare(Call* c, const void* X, const void* W, const int64_t* labels, const float* g) {
@@ -684,13 +727,7 @@ hdqt_status_t prepare(Call* c, const void* X, const void* W, const int64_t* labe
   if (pl.stage_x) st = stage(*c, X, d.ld_x, d.tokens, d.features, pl.xs, pl.ld_xs, &c->x);
   if (st == HDQT_OK && pl.stage_w) st = stage(*c, W, d.ld_w, pl.w_rows, pl.w_cols, pl.ws, pl.ld_ws, &c->w);
   if (st != HDQT_OK) return st;
-  // a weight per row goes into dz; one weight for all multiplies the fp32 sums of the gradient products, so that rounding dz
-  // to bf16 never rounds the weight (1 / rows would be off by the same 0.1 % in almost every element)
-  const bool rows = d.reduction == HDQT_REDUCE_NONE;
-  c->row_weights = rows ? g : nullptr;
-  c->alpha = rows ? nullptr : c->at<float>(pl.scale) + 1;
-  c->run(xent_labels_kernel, 1, d.tokens > 512 ? 1024 : 256, 0, labels, d.tokens, d.classes, d.ignore_index,
-         d.reduction == HDQT_REDUCE_MEAN, rows ? nullptr : g, c->at<int32_t>(pl.label), c->at<float>(pl.scale), c->dev_status);
+  label_rows(c, labels, g);
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy labels");
 }
@@ -890,6 +927,130 @@ hdqt_status_t few(const Call& c, const void* X, const void* W, const int64_t* la
   return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy of a few tokens");
 }
 
+template <typename T, int kT, bool kOuter>
+void run_few_columns(const Call& c, const FewProduct& p, int slices, bool wide) {
+  // 16-byte accesses while the sums of so many columns fit into registers, then two elements, or one where rows are odd
+  constexpr int kC = kT <= 8 ? 16 / (int)sizeof(T) : 2;
+  const int groups = (int)ceil_div(p.tokens, kT);
+  auto go = [&](auto kernel, int columns) {
+    const int64_t per_row = ceil_div(p.N, columns);
+    const int threads = per_row < kFewThreads ? (int)ceil_div(per_row, 32) * 32 : kFewThreads;
+    c.run(kernel, dim3((unsigned)(ceil_div(per_row, threads) * groups), slices), threads, 0, p);
+  };
+  if (wide) go(xent_few_columns_product_kernel<T, kT, kC, kOuter>, kC);
+  else go(xent_few_columns_product_kernel<T, kT, 1, kOuter>, 1);
+}
+
+template <typename T, bool kOuter>
+void few_columns_product(const Call& c, FewProduct p, int slices) {
+  p.per_slice = (int32_t)ceil_div(p.K, slices);
+  const int n = c.pl.few_grad;
+  const uintptr_t bits = reinterpret_cast<uintptr_t>(p.m) | (uintptr_t)(p.ld_m * sizeof(T)) | (uintptr_t)(p.N * sizeof(T)) |
+                         (kOuter ? reinterpret_cast<uintptr_t>(p.outer) | (uintptr_t)(p.ld_outer * sizeof(T)) : 0);
+  const bool wide = (bits & (n <= 8 ? 15 : 2 * sizeof(T) - 1)) == 0;
+  switch (n) {
+    case 1: return run_few_columns<T, 1, kOuter>(c, p, slices, wide);
+    case 2: return run_few_columns<T, 2, kOuter>(c, p, slices, wide);
+    case 4: return run_few_columns<T, 4, kOuter>(c, p, slices, wide);
+    case 8: return run_few_columns<T, 8, kOuter>(c, p, slices, wide);
+    default: return run_few_columns<T, 16, kOuter>(c, p, slices, wide);
+  }
+}
+
+template <typename T, int kT>
+void run_few_rows(const Call& c, const FewProduct& p, int slices) {
+  constexpr int kV = 16 / (int)sizeof(T), kN = 4;
+  const dim3 grid((unsigned)(ceil_div(p.N, kN * kFewWarps) * ceil_div(p.tokens, kT)), slices);
+  const bool wide = ((reinterpret_cast<uintptr_t>(p.m) | (uintptr_t)(p.ld_m * sizeof(T)) | (uintptr_t)(p.K * sizeof(T))) & 15) == 0 &&
+                    p.per_slice % kV == 0;
+  if (wide) c.run(xent_few_product_rows_kernel<T, kT, kV>, grid, kFewThreads, 0, p);
+  else c.run(xent_few_product_rows_kernel<T, kT, 1>, grid, kFewThreads, 0, p);
+}
+
+template <typename T>
+void few_rows_product(const Call& c, FewProduct p, int slices) {
+  p.per_slice = (int32_t)(ceil_div(ceil_div(p.K, slices), 8) * 8);
+  switch (c.pl.few_grad) {
+    case 1: return run_few_rows<T, 1>(c, p, slices);
+    case 2: return run_few_rows<T, 2>(c, p, slices);
+    case 4: return run_few_rows<T, 4>(c, p, slices);
+    default: return run_few_rows<T, 8>(c, p, slices);
+  }
+}
+
+// A few tokens by streamed products: logits, softmax, dX and dW (and the reduced loss by the caller).
+template <typename T>
+hdqt_status_t run_few_grad(Call& c, int kind, const void* X, const void* W, const int64_t* labels, const float* lse_in,
+                           const float* g, float* loss_rows, float* lse, void* dX, void* dW) {
+  const hdqt_xent_desc_t& d = *c.d;
+  const Plan& pl = c.pl;
+  const int f32 = d.dtype == HDQT_DTYPE_F32;
+  const int32_t tokens = (int32_t)d.tokens, D = (int32_t)d.features, V = (int32_t)d.classes;
+  label_rows(&c, labels, g);
+  float* z = c.at<float>(pl.z);
+  FewProduct q{};
+  q.in = FewMatrix{X, d.ld_x, f32};
+  q.m = W;
+  q.ld_m = d.ld_w;
+  q.out = z;
+  q.tokens = tokens;
+  q.N = V;
+  q.K = D;
+  if (d.w_is_cd) few_rows_product<T>(c, q, pl.few_z_slices);
+  else few_columns_product<T, false>(c, q, pl.few_z_slices);
+  const bool grads = kind != HDQT_XENT_FWD;
+  const dim3 spans((unsigned)ceil_div(V, kFewSpan), (unsigned)tokens);
+  if (lse_in == nullptr || pl.few_z_slices > 1)
+    c.run(xent_few_stats_kernel, spans, kFewThreads, 0, z, pl.few_z_slices, tokens, V, c.at<int32_t>(pl.label),
+          c.at<float2>(pl.part), c.at<float>(pl.label_logit));
+  c.run(xent_few_softmax_kernel, spans, kFewThreads, 0, z, V, c.at<float2>(pl.part),
+        c.at<int32_t>(pl.label), c.at<float>(pl.label_logit), c.row_weights, c.at<float>(pl.scale) + 1, lse_in, lse, loss_rows,
+        grads ? 1 : 0);
+  if (grads && (dX || dW)) {
+    FewProduct r{};
+    r.in = FewMatrix{z, V, 1};
+    r.b = FewMatrix{X, d.ld_x, f32};
+    r.m = W;
+    r.ld_m = d.ld_w;
+    r.out = dX ? c.at<float>(pl.dx_f32) : nullptr;
+    r.tokens = tokens;
+    r.N = D;
+    r.K = V;
+    if (d.w_is_cd) {             // W [classes, features]: one pass for both
+      r.outer = dW;
+      r.ld_outer = d.ld_dw;
+      if (dW) few_columns_product<T, true>(c, r, pl.few_dx_slices);
+      else few_columns_product<T, false>(c, r, pl.few_dx_slices);
+    } else {
+      if (dX) few_rows_product<T>(c, r, pl.few_dx_slices);
+      if (dW) {
+        FewProduct o{};          // dW [features, classes]
+        o.in = FewMatrix{X, d.ld_x, f32};
+        o.b = FewMatrix{z, V, 1};
+        o.outer = dW;
+        o.ld_outer = d.ld_dw;
+        o.tokens = tokens;
+        o.N = V;
+        o.K = D;
+        few_columns_product<T, true>(c, o, pl.few_z_slices);
+      }
+    }
+    if (dX) {
+      const int64_t total = (int64_t)tokens * D;
+      c.run(xent_few_join_slices_kernel<T>, (unsigned)ceil_div(total, 16), 256, 0, r.out, pl.few_dx_slices, total, D,
+            reinterpret_cast<T*>(dX), d.ld_dx);
+    }
+  }
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy of a few tokens");
+}
+
+hdqt_status_t few_grad(Call& c, int kind, const void* X, const void* W, const int64_t* labels, const float* lse_in,
+                       const float* g, float* loss_rows, float* lse, void* dX, void* dW) {
+  return c.d->dtype == HDQT_DTYPE_BF16 ? run_few_grad<__nv_bfloat16>(c, kind, X, W, labels, lse_in, g, loss_rows, lse, dX, dW)
+                                       : run_few_grad<float>(c, kind, X, W, labels, lse_in, g, loss_rows, lse, dX, dW);
+}
+
 hdqt_status_t small(const Call& c, int kind, const void* X, const void* W, const int64_t* labels, const float* lse_in,
                     const float* g, float* loss, float* lse, void* dX, void* dW) {
   return c.d->dtype == HDQT_DTYPE_BF16 ? run_small<__nv_bfloat16>(c, kind, X, W, labels, lse_in, g, loss, lse, dX, dW)
@@ -910,14 +1071,20 @@ hdqt_status_t split_logits(const Call& c, int kind, const float* lse_in, float* 
   const hdqt_status_t st = launch<X_OUT>(p, &g, 1, c);
   if (st != HDQT_OK) return st;
   const size_t smem = sizeof(float) * (size_t)d.classes;
-  auto go = [&](auto kernel) {
-    c.run(kernel, (unsigned)d.tokens, kRowThreads, smem, c.at<float>(pl.z), p.pr[0].splits, d.tokens, pl.ld_part,
+  auto go = [&](auto kernel, int threads) {
+    c.run(kernel, (unsigned)d.tokens, threads, smem, c.at<float>(pl.z), p.pr[0].splits, d.tokens, pl.ld_part,
           (int)d.classes, c.at<int32_t>(pl.label), c.row_weights, lse_in, c.at<uint16_t>(pl.dz), pl.ld_z,
           d.tokens * pl.ld_z, lse, loss_rows);
   };
-  if (kind == HDQT_XENT_FWD) go(xent_softmax_kernel<0>);
-  else if (pl.planes == 1) go(xent_softmax_kernel<1>);
-  else go(xent_softmax_kernel<3>);
+  if (d.tokens > 2 * kNumSMsHint || d.classes <= 1024) {
+    if (kind == HDQT_XENT_FWD) go(xent_softmax_kernel<0, kRowThreads>, kRowThreads);
+    else if (pl.planes == 1) go(xent_softmax_kernel<1, kRowThreads>, kRowThreads);
+    else go(xent_softmax_kernel<3, kRowThreads>, kRowThreads);
+  } else {                    // few long rows: more threads for each
+    if (kind == HDQT_XENT_FWD) go(xent_softmax_kernel<0, 1024>, 1024);
+    else if (pl.planes == 1) go(xent_softmax_kernel<1, 1024>, 1024);
+    else go(xent_softmax_kernel<3, 1024>, 1024);
+  }
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy rows");
 }
@@ -949,6 +1116,11 @@ extern "C" hdqt_status_t hdqt_linear_xent_fwd(const hdqt_xent_desc_t* d, const v
   if ((d->tokens > 0 && !lse) || (!loss && (d->tokens > 0 || d->reduction != HDQT_REDUCE_NONE))) return HDQT_ERR_INVALID_ARG;
   if (floats_misaligned(loss, lse, nullptr)) return HDQT_ERR_ALIGNMENT;
   if (c.pl.small_rows > 0) return small(c, HDQT_XENT_FWD, X, W, labels, nullptr, nullptr, loss, lse, nullptr, nullptr);
+  if (c.pl.few_grad > 0) {
+    st = few_grad(c, HDQT_XENT_FWD, X, W, labels, nullptr, nullptr, d->reduction == HDQT_REDUCE_NONE ? loss : c.at<float>(c.pl.loss_rows),
+                  lse, nullptr, nullptr);
+    return st == HDQT_OK ? reduce_loss(c, loss) : st;
+  }
   if (c.pl.few_tokens > 0) return few(c, X, W, labels, loss, lse);
   st = prepare(&c, X, W, labels, nullptr);
   if (st != HDQT_OK) return st;
@@ -985,6 +1157,7 @@ extern "C" hdqt_status_t hdqt_linear_xent_bwd(const hdqt_xent_desc_t* d, const v
   if (!dX && !dW) return HDQT_OK;
   if (d->tokens == 0) return dW ? zero_out(c, dW, c.pl.w_rows, c.pl.w_cols, d->ld_dw) : HDQT_OK;
   if (c.pl.small_rows > 0) return small(c, HDQT_XENT_BWD, X, W, labels, lse, gr, nullptr, nullptr, dX, dW);
+  if (c.pl.few_grad > 0) return few_grad(c, HDQT_XENT_BWD, X, W, labels, lse, gr, nullptr, nullptr, dX, dW);
   st = prepare(&c, X, W, labels, gr);
   if (st != HDQT_OK) return st;
   if (c.pl.splits_z > 1) {
@@ -1023,6 +1196,11 @@ extern "C" hdqt_status_t hdqt_linear_xent_train(const hdqt_xent_desc_t* d, const
   if (d->tokens > 0 && d->reduction == HDQT_REDUCE_NONE && !gr) return HDQT_ERR_INVALID_ARG;
   if (floats_misaligned(loss, lse, gr) || outputs_misaligned(d, dX, dW)) return HDQT_ERR_ALIGNMENT;
   if (c.pl.small_rows > 0) return small(c, HDQT_XENT_TRAIN, X, W, labels, nullptr, gr, loss, lse, dX, dW);
+  if (c.pl.few_grad > 0) {
+    st = few_grad(c, HDQT_XENT_TRAIN, X, W, labels, nullptr, gr, d->reduction == HDQT_REDUCE_NONE ? loss : c.at<float>(c.pl.loss_rows),
+                  lse, dX, dW);
+    return st == HDQT_OK ? reduce_loss(c, loss) : st;
+  }
   st = prepare(&c, X, W, labels, gr);
   if (st != HDQT_OK) return st;
   if (d->tokens == 0) {

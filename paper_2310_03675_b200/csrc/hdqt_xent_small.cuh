@@ -38,39 +38,46 @@ struct SmallParams {
 template <typename T>
 __device__ __forceinline__ float ldf(const T* p) { return to_f32(*p); }
 
-// out(r, n) = sum_k in[r][k] M(n, k), M stored [k][n]: a lane per n, the warps share n in tiles of 32 (and k in slices
-// where there are fewer tiles than warps).  red: kSmallThreads * kR floats.  All threads take part.
-template <typename T, int kR, typename F>
+// out(r, n) = sum_k in[r][k] M(n, k), M stored [k][n]: a lane per kV neighbouring n, the warps share n in tiles of 32 kV
+// (and k in slices where there are fewer tiles than warps).  red: kSmallThreads * kR floats.  All threads take part.
+template <typename T, int kR, int kV, typename F>
 __device__ __forceinline__ void rows_by_columns(const float* in, const T* m, int64_t ld, int N, int K, float* red, F&& out) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int tiles = (N + 31) / 32;
-  const int slices = tiles < kSmallWarps ? kSmallWarps / tiles : 1;
+  const int tiles = (N + 32 * kV - 1) / (32 * kV);
+  const int slices = kV == 1 && tiles < kSmallWarps ? kSmallWarps / tiles : 1;
   const int per = (K + slices - 1) / slices;
   const int step = slices > 1 ? tiles : kSmallWarps;
   for (int t0 = 0; t0 < tiles; t0 += step) {         // (one round where the contraction is sliced)
     const int slice = slices > 1 ? warp / tiles : 0;
     const int tile = slices > 1 ? warp - slice * tiles : t0 + warp;
-    const int n = tile * 32 + lane;
-    float acc[kR];
+    const int n = (tile * 32 + lane) * kV;
+    float acc[kR][kV];
 #pragma unroll
-    for (int r = 0; r < kR; ++r) acc[r] = 0.0f;
+    for (int r = 0; r < kR; ++r)
+#pragma unroll
+      for (int j = 0; j < kV; ++j) acc[r][j] = 0.0f;
     const int k1 = min(K, (slice + 1) * per);
-    if (slice < slices && tile < tiles && n < N) {
+    if (slice < slices && tile < tiles && n < N) {   // (kV > 1: N is a multiple of kV)
       const T* p = m + n;
-#pragma unroll 32
+#pragma unroll(kV == 1 ? 32 : 16)
       for (int k = slice * per; k < k1; ++k) {
-        const float v = ldf(p + k * ld);
+        float v[kV];
+        unpack(*reinterpret_cast<const Vec<T, kV>*>(p + k * ld), v);
 #pragma unroll
-        for (int r = 0; r < kR; ++r) acc[r] = fmaf(in[r * K + k], v, acc[r]);
+        for (int r = 0; r < kR; ++r)
+#pragma unroll
+          for (int j = 0; j < kV; ++j) acc[r][j] = fmaf(in[r * K + k], v[j], acc[r][j]);
       }
       if (slices == 1) {
 #pragma unroll
-        for (int r = 0; r < kR; ++r) out(r, n, acc[r]);
+        for (int r = 0; r < kR; ++r)
+#pragma unroll
+          for (int j = 0; j < kV; ++j) out(r, n + j, acc[r][j]);
       }
     }
     if (slices > 1) {
 #pragma unroll
-      for (int r = 0; r < kR; ++r) red[r * kSmallThreads + threadIdx.x] = acc[r];
+      for (int r = 0; r < kR; ++r) red[r * kSmallThreads + threadIdx.x] = acc[r][0];
       __syncthreads();
       if (slice == 0 && n < N) {
 #pragma unroll
@@ -85,10 +92,9 @@ __device__ __forceinline__ void rows_by_columns(const float* in, const T* m, int
   }
 }
 
-// the same with M stored [n][k]: a warp per n (four or eight at a time), lanes along k
-template <typename T, int kR, typename F>
+// the same with M stored [n][k]: a warp per n (kN at a time), lanes along k, kV neighbouring k per access
+template <typename T, int kR, int kV, int kN, typename F>
 __device__ __forceinline__ void rows_by_rows(const float* in, const T* m, int64_t ld, int N, int K, F&& out) {
-  constexpr int kN = kR == 1 ? 8 : 4;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int n0 = warp; n0 < N; n0 += kN * kSmallWarps) {
     const T* p[kN];
@@ -100,16 +106,18 @@ __device__ __forceinline__ void rows_by_rows(const float* in, const T* m, int64_
       for (int r = 0; r < kR; ++r) a[i][r] = 0.0f;
     }
 #pragma unroll 4
-    for (int k = lane; k < K; k += 32) {
-      float v[kN];
+    for (int k = lane * kV; k < K; k += 32 * kV) {   // (kV > 1: K is a multiple of kV)
+      float v[kN][kV];
 #pragma unroll
-      for (int i = 0; i < kN; ++i) v[i] = ldf(p[i] + k);
+      for (int i = 0; i < kN; ++i) unpack(*reinterpret_cast<const Vec<T, kV>*>(p[i] + k), v[i]);
 #pragma unroll
-      for (int r = 0; r < kR; ++r) {
-        const float x = in[r * K + k];
+      for (int r = 0; r < kR; ++r)
 #pragma unroll
-        for (int i = 0; i < kN; ++i) a[i][r] = fmaf(x, v[i], a[i][r]);
-      }
+        for (int j = 0; j < kV; ++j) {
+          const float x = in[r * K + k + j];
+#pragma unroll
+          for (int i = 0; i < kN; ++i) a[i][r] = fmaf(x, v[i][j], a[i][r]);
+        }
     }
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1)
@@ -124,6 +132,21 @@ __device__ __forceinline__ void rows_by_rows(const float* in, const T* m, int64_
       for (int r = 0; r < kR; ++r)
         if (lane == i * kR + r && n0 + i * kSmallWarps < N) out(r, n0 + i * kSmallWarps, a[i][r]);
   }
+}
+
+// by sizes and alignment: as many n per warp as leave work for every warp, four elements per access where rows allow it
+template <typename T, int kR, typename F>
+__device__ __forceinline__ void by_rows(const float* in, const T* m, int64_t ld, int N, int K, F&& out) {
+  const bool wide = ((reinterpret_cast<uintptr_t>(m) | (uintptr_t)(ld * sizeof(T)) | (uintptr_t)(K * sizeof(T))) & (4 * sizeof(T) - 1)) == 0;
+  if (wide) rows_by_rows<T, kR, 4, 2>(in, m, ld, N, K, out);
+  else if (N > 4 * kSmallWarps) rows_by_rows<T, kR, 1, kR == 1 ? 8 : 4>(in, m, ld, N, K, out);
+  else rows_by_rows<T, kR, 1, 2>(in, m, ld, N, K, out);
+}
+template <typename T, int kR, typename F>
+__device__ __forceinline__ void by_columns(const float* in, const T* m, int64_t ld, int N, int K, float* red, F&& out) {
+  const bool wide = ((reinterpret_cast<uintptr_t>(m) | (uintptr_t)(ld * sizeof(T)) | (uintptr_t)(N * sizeof(T))) & (4 * sizeof(T) - 1)) == 0;
+  if (wide && N >= 64 * kSmallWarps) rows_by_columns<T, kR, 4>(in, m, ld, N, K, red, out);
+  else rows_by_columns<T, kR, 1>(in, m, ld, N, K, red, out);
 }
 
 template <typename T, int kR>
@@ -151,8 +174,8 @@ __global__ void __launch_bounds__(kSmallThreads) xent_small_rows_kernel(const __
   kept = __reduce_add_sync(0xFFFFFFFFu, kept);
   if (lane == 0 && kept) atomicAdd(&s_kept, kept);
   auto to_z = [&](int r, int n, float v) { zs[r * V + n] = v; };
-  if (p.w_is_cd) rows_by_rows<T, kR>(xs, w, p.ld_w, V, D, to_z);
-  else rows_by_columns<T, kR>(xs, w, p.ld_w, V, D, red, to_z);
+  if (p.w_is_cd) by_rows<T, kR>(xs, w, p.ld_w, V, D, to_z);
+  else by_columns<T, kR>(xs, w, p.ld_w, V, D, red, to_z);
   __syncthreads();
   const float scale = p.mean ? 1.0f / (float)s_kept : 1.0f;
   if (warp < kR && t0 + warp < p.tokens) {     // a warp per row
@@ -198,8 +221,8 @@ __global__ void __launch_bounds__(kSmallThreads) xent_small_rows_kernel(const __
   auto to_dx = [&](int r, int n, float v) {
     if (t0 + r < p.tokens) dx[(int64_t)(t0 + r) * p.ld_dx + n] = from_f32<T>(v);
   };
-  if (p.w_is_cd) rows_by_columns<T, kR>(zs, w, p.ld_w, D, V, red, to_dx);
-  else rows_by_rows<T, kR>(zs, w, p.ld_w, D, V, to_dx);
+  if (p.w_is_cd) by_columns<T, kR>(zs, w, p.ld_w, D, V, red, to_dx);
+  else by_rows<T, kR>(zs, w, p.ld_w, D, V, to_dx);
 }
 
 // dW[v, d] = sum_t dz[t, v] x[t, d] (stored [classes, features] or transposed), 32 classes x 32 features per block; the
