@@ -424,6 +424,7 @@ struct Plan {
   int64_t rows_piece, cols_piece;       // tokens x classes of a piece
   int64_t ld_z;
   int64_t parts_ld;
+  int splits_dx_alone;                  // of dX where dW is not asked for
   int splits_z, splits_dx, splits_dw;   // splits_z > 1: few output blocks, logits as partial products (xent_softmax_kernel)
   int64_t ld_part;
   bool acc_dx, acc_dw;                  // fp32 sums over several pieces
@@ -440,6 +441,10 @@ constexpr int64_t kSmallTokens = 512, kSmallWeights = 1 << 18, kSmallWork = 1 <<
 constexpr size_t kSmallSmem = 100 << 10;
 constexpr int kFewBlocks = 4 * kNumSMsHint;      // most blocks of the few-token kernels
 
+// An item shorter than this many stages takes as long all the same: its epilogue (256 x 256 outputs) does.
+constexpr int64_t kEpilogueStages = 16;
+int64_t item_cost(int64_t stages) { return stages > kEpilogueStages ? stages : kEpilogueStages; }
+
 // Work items along the contraction of a product of `blocks` output blocks of `kblocks` x `products` stages, next to `other` stages of
 // shorter items: the number with the shortest schedule on `pairs` CTA pairs.  A split adds one pass over fp32 partial
 // outputs (8 bytes per element at about 6 TB/s against 0.3 us per stage).
@@ -447,8 +452,8 @@ int choose_splits(int64_t blocks, int64_t kblocks, int64_t products, int64_t ele
   int best = 1;
   double best_time = 0.0;
   for (int s = 1; s <= 16; ++s) {
-    const int64_t len = ceil_div(kblocks, s) * products, items = blocks * s;
-    if (s > 1 && (len < 12 || ceil_div(kblocks, s) == ceil_div(kblocks, s - 1))) continue;
+    const int64_t len = item_cost(ceil_div(kblocks, s) * products), items = blocks * s;
+    if (s > 1 && (ceil_div(kblocks, s) * products < 12 || ceil_div(kblocks, s) == ceil_div(kblocks, s - 1))) continue;
     const int64_t whole = items / pairs, more = items % pairs;
     const double mean = (double)(items * len + other) / (double)pairs;
     const double longest = (double)((whole + (more > 0)) * len);
@@ -536,8 +541,9 @@ hdqt_status_t make_plan(const hdqt_xent_desc_t* d, int kind, Plan* pl) {
   const int64_t dw_blocks = ceil_div(pl->cols_piece, XM) * ceil_div(D, XN), dw_k = ceil_div(pl->rows_piece, XK);
   const bool whole = !pl->acc_dx && !pl->acc_dw;
   const int64_t products = f32 ? 6 : 1;
-  pl->splits_dx = whole ? choose_splits(dx_blocks, dx_k, products, pl->rows_piece * D, dw_blocks * dw_k * products, pairs) : 1;
-  pl->splits_dw = whole ? choose_splits(dw_blocks, dw_k, products, pl->cols_piece * D, dx_blocks * dx_k * products, pairs) : 1;
+  pl->splits_dx = whole ? choose_splits(dx_blocks, dx_k, products, pl->rows_piece * D, dw_blocks * item_cost(dw_k * products), pairs) : 1;
+  pl->splits_dw = whole ? choose_splits(dw_blocks, dw_k, products, pl->cols_piece * D, dx_blocks * item_cost(dx_k * products), pairs) : 1;
+  pl->splits_dx_alone = whole ? choose_splits(dx_blocks, dx_k, products, pl->rows_piece * D, 0, pairs) : 1;
   pl->splits_z = 1;
   pl->ld_part = ceil_div(V, 8) * 8;
   if (pl->rows_piece == T && pl->cols_piece == V && V <= kSoftmaxClasses && d->piece_bytes == 0)
@@ -597,7 +603,8 @@ hdqt_status_t make_plan(const hdqt_xent_desc_t* d, int kind, Plan* pl) {
   }
   pl->dx_f32 = pl->dw_f32 = o;
   if (kind != HDQT_XENT_FWD) {
-    if (pl->splits_dx > 1) pl->dx_f32 = take(4 * pl->splits_dx * T * D);
+    const int most_dx = pl->splits_dx > pl->splits_dx_alone ? pl->splits_dx : pl->splits_dx_alone;
+    if (most_dx > 1) pl->dx_f32 = take(4 * most_dx * T * D);
     else if (pl->acc_dx && !f32) pl->dx_f32 = take(4 * T * D);
     if (pl->splits_dw > 1) pl->dw_f32 = take(4 * pl->splits_dw * V * D);
     else if (pl->acc_dw && !f32) pl->dw_f32 = take(4 * V * D);
@@ -771,7 +778,7 @@ hdqt_status_t gradient_products(const Call& c, int64_t t0, int64_t nt, int64_t v
   if (dX) {
     // dX[t, d] = sum_v dz[t, v] W[v, d]
     g[n] = Product{dz, c.w_classes(v0, nv), false, d.w_is_cd != 0, nt, D, nv};
-    p.pr[n] = make_problem(g[n], pl.splits_dx);
+    p.pr[n] = make_problem(g[n], dW ? pl.splits_dx : pl.splits_dx_alone);
     target(p.pr[n], dX, d.ld_dx, t0 * d.ld_dx, pl.acc_dx, pl.dx_f32, D);
     ++n;
   }
@@ -800,7 +807,8 @@ hdqt_status_t gradient_products(const Call& c, int64_t t0, int64_t nt, int64_t v
       std::swap(p.pr[0], p.pr[1]);
       std::swap(g[0], g[1]);
     }
-    p.extra = p.pr[0].kblocks_split / p.pr[1].kblocks_split;
+    const int64_t products = pl.planes == 1 ? 1 : 6;
+    p.extra = (int32_t)(item_cost(p.pr[0].kblocks_split * products) / item_cost(p.pr[1].kblocks_split * products));
   }
   const hdqt_status_t st = launch<X_OUT>(p, g, n, c);
   if (st != HDQT_OK) return st;

@@ -123,6 +123,13 @@ __device__ __forceinline__ uint64_t make_smem_desc_mn(uint32_t addr, uint32_t lb
   return d;
 }
 
+// Arrival at the pair leader's barrier for an accumulator that has been read (tcgen05.wait::ld and the fence before it order
+// that).  Not the cluster-scope release of mbar_arrive_cluster: it would also wait for every output store in flight, which
+// made each 256 x 256 block's epilogue 4.7 us long.
+__device__ __forceinline__ void mbar_arrive_read(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+
 // 32 bytes in one access (the address is 32-byte aligned)
 __device__ __forceinline__ void st256(void* p, const uint32_t (&v)[8]) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]),
@@ -364,6 +371,25 @@ __device__ __forceinline__ void x_out_odd(const XParams& p, const XProblem& r, c
                                           float* box, float (&acc)[128]) {
   const float alpha = p.alpha != nullptr ? *p.alpha : 1.0f;
   const int rows = min(32, r.M - row0);
+  if (r.out_bf16 && r.add == nullptr && ((reinterpret_cast<uintptr_t>(r.out) | (uintptr_t)(r.ld_out * 2)) & 3) == 0 && (r.N & 1) == 0) {
+    // rows start on 4 bytes: two neighbouring bf16 per lane, 64 columns at a time
+    uint32_t* pair = reinterpret_cast<uint32_t*>(box);
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int col = col0 + 64 * c;
+      if (col >= r.N) break;
+      __syncwarp();
+#pragma unroll
+      for (int k = 0; k < 32; ++k) pair[lane * 33 + k] = pack_bf16(acc[64 * c + 2 * k] * alpha, acc[64 * c + 2 * k + 1] * alpha);
+      __syncwarp();
+      if (col + 2 * lane < r.N) {
+        uint32_t* o = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(r.out) + (int64_t)row0 * r.ld_out + col + 2 * lane);
+#pragma unroll 8
+        for (int i = 0; i < rows; ++i) o[i * (r.ld_out >> 1)] = pair[i * 33 + lane];
+      }
+    }
+    return;
+  }
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
     const int col = col0 + 32 * c;
@@ -573,15 +599,20 @@ xent_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_consta
         if (!mbar_wait_yield<64>(bar_tfull + 8 * buf, ((uint32_t)buf_i >> 1) & 1u, abort_flag)) { ok = false; break; }
         ++buf_i;
         tc_fence_after();
+        if (first) {                 // all four loads in flight
+          uint32_t v[128];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t v[32];
-          HDQT_TMEM_LD32(lane_addr + buf * XN + c * 32, v);
-          HDQT_TMEM_WAIT32(v);
-          if (first) {
+          for (int c = 0; c < 4; ++c) HDQT_TMEM_LD32(lane_addr + buf * XN + c * 32, (v + c * 32));
 #pragma unroll
-            for (int k = 0; k < 32; ++k) acc[c * 32 + k] = __uint_as_float(v[k]);
-          } else {
+          for (int c = 0; c < 4; ++c) HDQT_TMEM_WAIT32((v + c * 32));
+#pragma unroll
+          for (int k = 0; k < 128; ++k) acc[k] = __uint_as_float(v[k]);
+        } else {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t v[32];
+            HDQT_TMEM_LD32(lane_addr + buf * XN + c * 32, v);
+            HDQT_TMEM_WAIT32(v);
 #pragma unroll
             for (int k = 0; k < 32; ++k) acc[c * 32 + k] += __uint_as_float(v[k]);
           }
@@ -590,7 +621,7 @@ xent_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_consta
         // the accumulator is in registers: hand it back before anything else
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(tempty + 8 * buf);
+        if (lane == 0) mbar_arrive_read(tempty + 8 * buf);
       }
       if (!ok) break;
       const int row = t.m * XM + (int)cta_rank * 128 + quarter * 32 + lane;
