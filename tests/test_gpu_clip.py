@@ -168,3 +168,16 @@ def test_refusals():
     assert lib.hdqt_scale_tensors(C.addressof(table), 1, None, None) == INVALID
     assert lib.hdqt_scale_tensors(C.addressof(table), 1, 258, None) == ALIGN
     assert lib.hdqt_scale_tensors(C.addressof(table), -1, 256, None) == INVALID
+
+
+@pytest.mark.gpu
+def test_offsets_past_32_bits():
+    n = (1 << 31) + 12345
+    big = torch.ones(n, dtype=torch.bfloat16, device="cuda")
+    tail = torch.full((3,), 2.0, device="cuda")
+    norm = hdqt.clip_grad_norm([big, tail], 1.0)
+    want = math.sqrt(n + 12.0)
+    # a thread adds 7100 ones in fp32, exactly
+    assert abs(float(norm) - want) <= 2.0 ** -22 * want
+    f = torch.tensor(1.0 / (want + 1e-6)).to(torch.bfloat16)
+    assert float(big[0]) == float(f) and float(big[-1]) == float(f) and bool((big[1 << 31:] == big[0]).all())

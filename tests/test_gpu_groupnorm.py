@@ -251,3 +251,27 @@ def test_refusals():
     assert lib.hdqt_group_norm_bwd(C.byref(desc()), 256, 256, 256, 256, 256, 256, 256, 258, 256, 256, 1 << 20, None) == ALIGN
     assert lib.hdqt_group_norm_bwd(C.byref(desc()), 256, 256, 256, 256, 256, 256, 256, 256, 256, 256, 8, None) == WS
     assert lib.hdqt_group_norm_workspace_bytes(C.byref(desc(groups=5)), 0) == 0
+
+
+@pytest.mark.gpu
+def test_offsets_past_32_bits():
+    """2.3e9 elements: the last image's groups against 64 bits (statistics of a group: 2^20 x 44 values, summed per thread over at
+    most a few thousand of them: the bounds of the docstring with room for the longer sums)."""
+    b, p, c, groups = 2, 1 << 20, 1100, 25
+    x = torch.empty((b, p, c), dtype=torch.bfloat16, device="cuda")
+    for i in range(b):
+        x[i].normal_(0.5, 1.0)
+    y, mean, rstd = hdqt.group_norm_fwd(x, None, None, groups, EPS, "relu")
+    dx, _, _ = hdqt.group_norm_bwd(x, x, None, None, mean, rstd, groups, "relu", want_params=False)
+    for g in (0, groups - 1):
+        xs = x[1, :, g * 44:(g + 1) * 44].double()
+        mu, rs = xs.mean(), (xs.var(correction=0) + EPS) ** -0.5
+        assert abs(float(mean[1, g]) - float(mu)) < 1e-4 and abs(float(rstd[1, g] / rs) - 1) < 1e-4
+        z = (xs - mu) * rs
+        got = y[1, :, g * 44:(g + 1) * 44].double()
+        assert float((got - z.clamp_min(0)).abs().max()) < 2.0 ** -8 * float(z.max()) + 1e-3
+        dz = torch.where(z > 0, xs, 0.0)
+        want = rs * (dz - dz.mean() - z * (dz * z).mean())
+        far = (dx[1, :, g * 44:(g + 1) * 44].double() - want).abs() > 2.0 ** -8 * want.abs() + 1e-2
+        assert float(far.double().mean()) < 1e-4          # (elements on ReLU's kink)
+        del xs, z, got, dz, want, far

@@ -317,3 +317,39 @@ def test_refusals():
     assert lib.hdqt_linear_xent_train(C.byref(desc(reduction=0)), 256, 256, 256, None, 256, 256, 256, 256, 256, 1 << 30,
                                       None, None) == INVALID
     assert lib.hdqt_linear_xent_workspace_bytes(C.byref(desc()), 3) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens", [3, 20])
+def test_weight_offsets_past_32_bits(tokens):
+    """2.4e9 weights (and as many gradients): classes at both ends of the vocabulary, both ways of storing W."""
+    d, v = 4096, 590_000
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(tokens, d, generator=g, device="cuda").bfloat16()
+    w = torch.empty((v, d), dtype=torch.bfloat16, device="cuda")
+    for a in range(0, v, 59_000):
+        w[a:a + 59_000] = torch.randn(min(59_000, v - a), d, generator=g, device="cuda") * (1.5 / math.sqrt(d))
+    labels = torch.randint(0, v, (tokens,), generator=g, device="cuda")
+    labels[0], labels[1] = v - 1, 0
+    z = torch.cat([x.double() @ w[a:a + 59_000].double().t() for a in range(0, v, 59_000)], 1)
+    lse = torch.logsumexp(z, 1)
+    dz = torch.softmax(z, 1)
+    dz[torch.arange(tokens), labels] -= 1
+    for w_is_cd in (True, False):
+        ww = w if w_is_cd else w.t().contiguous()
+        loss, got_lse, dx, dw = hdqt.linear_xent_train(x, ww, labels, reduction="sum", w_is_cd=w_is_cd)
+        assert float((got_lse.double() - lse).abs().max()) < 1e-4
+        if not w_is_cd:
+            dw = dw.t()
+        for rows in (slice(0, 300), slice(v - 300, v)):
+            want = dz[:, rows].t() @ x.double()
+            far = (dw[rows].double() - want).abs()
+            # dz and the result are rounded to bf16 (2^-8 each), sums of `tokens` terms
+            assert bool((far <= 2.0 ** -6.5 * (dz[:, rows].abs().t() @ x.double().abs()) + 1e-30).all())
+        want = torch.zeros(tokens, d, dtype=torch.float64, device="cuda")
+        size = torch.zeros_like(want)
+        for a in range(0, v, 59_000):
+            want += dz[:, a:a + 59_000] @ w[a:a + 59_000].double()
+            size += dz[:, a:a + 59_000].abs() @ w[a:a + 59_000].double().abs()
+        assert bool(((dx.double() - want).abs() <= 2.0 ** -7.5 * size).all())
+        del ww, dw
