@@ -539,11 +539,17 @@ hdqt_status_t make_plan(const hdqt_xent_desc_t* d, int kind, Plan* pl) {
   const int64_t pairs = kNumSMsHint / 2;
   const int64_t dx_blocks = ceil_div(pl->rows_piece, XM) * ceil_div(D, XN), dx_k = ceil_div(pl->cols_piece, XK);
   const int64_t dw_blocks = ceil_div(pl->cols_piece, XM) * ceil_div(D, XN), dw_k = ceil_div(pl->rows_piece, XK);
-  const bool whole = !pl->acc_dx && !pl->acc_dw;
+  const int64_t pieces = ceil_div(V, pl->cols_piece);
   const int64_t products = f32 ? 6 : 1;
-  pl->splits_dx = whole ? choose_splits(dx_blocks, dx_k, products, pl->rows_piece * D, dw_blocks * item_cost(dw_k * products), pairs) : 1;
-  pl->splits_dw = whole ? choose_splits(dw_blocks, dw_k, products, pl->cols_piece * D, dx_blocks * item_cost(dx_k * products), pairs) : 1;
-  pl->splits_dx_alone = whole ? choose_splits(dx_blocks, dx_k, products, pl->rows_piece * D, 0, pairs) : 1;
+  pl->splits_dx = choose_splits(dx_blocks, dx_k, products, pl->rows_piece * D, dw_blocks * item_cost(dw_k * products), pairs);
+  pl->splits_dw = pl->acc_dw ? 1 : choose_splits(dw_blocks, dw_k, products, pl->cols_piece * D, dx_blocks * item_cost(dx_k * products), pairs);
+  pl->splits_dx_alone = choose_splits(dx_blocks, dx_k, products, pl->rows_piece * D, 0, pairs);
+  if (pl->acc_dx) {
+    // the pieces leave the shares of their splits side by side where there is room for them, and add to one sum otherwise
+    const int64_t most = budget / (4 * pieces * T * D);
+    if (pl->splits_dx > most) pl->splits_dx = most > 1 ? (int)most : 1;
+    if (pl->splits_dx_alone > most) pl->splits_dx_alone = most > 1 ? (int)most : 1;
+  }
   pl->splits_z = 1;
   pl->ld_part = ceil_div(V, 8) * 8;
   if (pl->rows_piece == T && pl->cols_piece == V && V <= kSoftmaxClasses && d->piece_bytes == 0)
@@ -603,10 +609,10 @@ hdqt_status_t make_plan(const hdqt_xent_desc_t* d, int kind, Plan* pl) {
   }
   pl->dx_f32 = pl->dw_f32 = o;
   if (kind != HDQT_XENT_FWD) {
-    const int most_dx = pl->splits_dx > pl->splits_dx_alone ? pl->splits_dx : pl->splits_dx_alone;
-    if (most_dx > 1) pl->dx_f32 = take(4 * most_dx * T * D);
+    const int64_t most_dx = pl->splits_dx > pl->splits_dx_alone ? pl->splits_dx : pl->splits_dx_alone;
+    if (most_dx > 1) pl->dx_f32 = take(4 * pieces * most_dx * pl->rows_piece * D);
     else if (pl->acc_dx && !f32) pl->dx_f32 = take(4 * T * D);
-    if (pl->splits_dw > 1) pl->dw_f32 = take(4 * pl->splits_dw * V * D);
+    if (pl->splits_dw > 1) pl->dw_f32 = take(4 * pl->splits_dw * pl->cols_piece * D);
     else if (pl->acc_dw && !f32) pl->dw_f32 = take(4 * V * D);
   }
   pl->total = o;
@@ -624,6 +630,7 @@ struct Call {
   const float* alpha = nullptr;         // or one weight for all, applied to the gradient products
 
   mutable bool started = false;
+  mutable int dx_shares = 0;            // partial products of dX so far (backward call in pieces)
 
   template <typename T>
   T* at(size_t off) const { return reinterpret_cast<T*>(ws + off); }
@@ -756,15 +763,17 @@ hdqt_status_t gradient_products(const Call& c, int64_t t0, int64_t nt, int64_t v
   Product g[2];
   int n = 0;
   const Operand dz = c.dz(nt, nv);
+  void* dx_rows = dX ? reinterpret_cast<uint8_t*>(dX) + t0 * d.ld_dx * (bf16 ? 2 : 4) : nullptr;
+  void* dw_out = dW ? reinterpret_cast<uint8_t*>(dW) + (d.w_is_cd ? v0 * d.ld_dw : v0) * (bf16 ? 2 : 4) : nullptr;
+  int dx_total = 0;           // shares of dX to be joined
   // where a product goes: partial sums of its splits, the result itself, or fp32 sums over the pieces
-  auto target = [&](XProblem& r, void* out, int64_t ld, int64_t offset, bool acc, size_t f32_off, int64_t f32_ld) {
-    float* f32 = c.at<float>(f32_off);
+  auto target = [&](XProblem& r, void* out, int64_t ld, bool acc, float* f32, int64_t f32_ld) {
     if (r.splits > 1) {
       r.out = f32;
       r.ld_out = f32_ld;
       r.split_stride = (int64_t)r.M * f32_ld;
     } else if (!acc || !bf16) {
-      r.out = reinterpret_cast<uint8_t*>(out) + offset * (bf16 ? 2 : 4);
+      r.out = out;
       r.ld_out = ld;
       r.out_bf16 = bf16;
       if (acc && !first) { r.add = reinterpret_cast<const float*>(r.out); r.ld_add = ld; }
@@ -778,8 +787,19 @@ hdqt_status_t gradient_products(const Call& c, int64_t t0, int64_t nt, int64_t v
   if (dX) {
     // dX[t, d] = sum_v dz[t, v] W[v, d]
     g[n] = Product{dz, c.w_classes(v0, nv), false, d.w_is_cd != 0, nt, D, nv};
-    p.pr[n] = make_problem(g[n], dW ? pl.splits_dx : pl.splits_dx_alone);
-    target(p.pr[n], dX, d.ld_dx, t0 * d.ld_dx, pl.acc_dx, pl.dx_f32, D);
+    const int splits = dW ? pl.splits_dx : pl.splits_dx_alone;
+    p.pr[n] = make_problem(g[n], splits);
+    if (splits > 1) {
+      // (a last piece may be too short for two splits: its share is joined with the others all the same)
+      XProblem& r = p.pr[n];
+      r.out = c.at<float>(pl.dx_f32) + c.dx_shares * nt * D;
+      r.ld_out = D;
+      r.split_stride = nt * D;
+      dx_total = c.dx_shares + r.splits;
+      c.dx_shares = pl.acc_dx ? dx_total : 0;
+    } else {
+      target(p.pr[n], dx_rows, d.ld_dx, pl.acc_dx, c.at<float>(pl.dx_f32), D);
+    }
     ++n;
   }
   if (dW) {
@@ -790,18 +810,17 @@ hdqt_status_t gradient_products(const Call& c, int64_t t0, int64_t nt, int64_t v
       g[n] = Product{c.x_rows(t0, nt), dz, true, true, D, nv, nt};
     }
     p.pr[n] = make_problem(g[n], pl.splits_dw);
-    target(p.pr[n], dW, d.ld_dw, d.w_is_cd ? v0 * d.ld_dw : v0, pl.acc_dw, pl.dw_f32, pl.w_cols);
+    target(p.pr[n], dw_out, d.ld_dw, pl.acc_dw, c.at<float>(pl.dw_f32), d.w_is_cd ? D : nv);
     ++n;
   }
   if (n == 0) return HDQT_OK;
-  auto join = [&](const XProblem& r, void* out, int64_t ld, size_t off) {
-    if (r.splits <= 1) return;
-    const int64_t blocks = ceil_div((int64_t)r.M * r.N, 1024);
+  auto join = [&](int shares, int64_t M, int64_t N, void* out, int64_t ld, size_t off) {
+    const int64_t blocks = ceil_div(M * N, 1024);
     const unsigned grid = (unsigned)(blocks < 148 * 8 ? blocks : 148 * 8);
-    if (bf16) c.run(xent_join_splits_kernel<__nv_bfloat16>, grid, 256, 0, c.at<float>(off), r.splits, r.M, r.N, reinterpret_cast<__nv_bfloat16*>(out), ld);
-    else c.run(xent_join_splits_kernel<float>, grid, 256, 0, c.at<float>(off), r.splits, r.M, r.N, reinterpret_cast<float*>(out), ld);
+    if (bf16) c.run(xent_join_splits_kernel<__nv_bfloat16>, grid, 256, 0, c.at<float>(off), shares, M, N, reinterpret_cast<__nv_bfloat16*>(out), ld);
+    else c.run(xent_join_splits_kernel<float>, grid, 256, 0, c.at<float>(off), shares, M, N, reinterpret_cast<float*>(out), ld);
   };
-  const XProblem first_problem = p.pr[0], second_problem = p.pr[n - 1];
+  const XProblem dw_problem = p.pr[n - 1];      // (if dW is asked for)
   if (n == 2) {
     if (p.pr[1].kblocks_split > p.pr[0].kblocks_split) {      // the longer items first
       std::swap(p.pr[0], p.pr[1]);
@@ -812,8 +831,8 @@ hdqt_status_t gradient_products(const Call& c, int64_t t0, int64_t nt, int64_t v
   }
   const hdqt_status_t st = launch<X_OUT>(p, g, n, c);
   if (st != HDQT_OK) return st;
-  if (dX) join(first_problem, dX, d.ld_dx, pl.dx_f32);
-  if (dW) join(second_problem, dW, d.ld_dw, pl.dw_f32);
+  if (dx_total > 0 && (last || !pl.acc_dx)) join(dx_total, nt, D, dx_rows, d.ld_dx, pl.dx_f32);
+  if (dW && dw_problem.splits > 1) join(dw_problem.splits, dw_problem.M, dw_problem.N, dw_out, d.ld_dw, pl.dw_f32);
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy gradients");
 }

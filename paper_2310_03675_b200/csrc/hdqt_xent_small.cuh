@@ -138,7 +138,8 @@ __device__ __forceinline__ void rows_by_rows(const float* in, const T* m, int64_
 template <typename T, int kR, typename F>
 __device__ __forceinline__ void by_rows(const float* in, const T* m, int64_t ld, int N, int K, F&& out) {
   const bool wide = ((reinterpret_cast<uintptr_t>(m) | (uintptr_t)(ld * sizeof(T)) | (uintptr_t)(K * sizeof(T))) & (4 * sizeof(T) - 1)) == 0;
-  if (wide) rows_by_rows<T, kR, 4, 2>(in, m, ld, N, K, out);
+  if (wide && N > 4 * kSmallWarps) rows_by_rows<T, kR, 4, kR == 1 ? 8 : 4>(in, m, ld, N, K, out);
+  else if (wide) rows_by_rows<T, kR, 4, 2>(in, m, ld, N, K, out);
   else if (N > 4 * kSmallWarps) rows_by_rows<T, kR, 1, kR == 1 ? 8 : 4>(in, m, ld, N, K, out);
   else rows_by_rows<T, kR, 1, 2>(in, m, ld, N, K, out);
 }

@@ -157,6 +157,25 @@ def test_pieces_give_the_same_result(dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_pieces_whose_products_are_split_too(dtype):
+    """Few tokens against many classes: dX has few blocks, so each piece of the vocabulary splits its share of the sum."""
+    for w_is_cd, tokens in ((True, 300), (False, 150)):
+        x, w, labels, weights = data(tokens, 64, 20011, dtype, seed=4)
+        ww = w if w_is_cd else w.t().contiguous()
+        want = reference(x, w, labels, weights, DT[dtype])
+        loss, lse = hdqt.linear_xent_fwd(x, ww, labels, reduction="none", w_is_cd=w_is_cd)
+        how = {"reduction": "none", "w_is_cd": w_is_cd}
+        for classes in (10240, 7000, 20000):
+            piece = tokens * classes * (2 if dtype == "bf16" else 6)
+            dx, dw = hdqt.linear_xent_bwd(x, ww, labels, lse, weights, piece_bytes=piece, **how)
+            close(dx, want["dx"], "dx")
+            close(dw if w_is_cd else dw.t(), want["dw"], "dw")
+            dx, _ = hdqt.linear_xent_bwd(x, ww, labels, lse, weights, piece_bytes=piece, want_dw=False, **how)
+            close(dx, want["dx"], "dx alone")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_strided_rows_odd_addresses_and_partial_gradients(dtype):
     t, d, v = 70, 48, 200
     wide_x, wide_w, labels, weights = data(t, d + 30, v, dtype, seed=5)
