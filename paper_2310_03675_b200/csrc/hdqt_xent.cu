@@ -435,9 +435,40 @@ struct Plan {
 constexpr int64_t kPieceBytes = 1ll << 30;
 constexpr int64_t kSoftmaxClasses = 12000;      // xent_softmax_kernel holds a row of fp32 logits in 48 KB
 
-// Small problems: the rows kernel reads W from the L2 once per block and product, the tensor-core path costs five launches
-// and two pipelines' fill and drain whatever the size.
-constexpr int64_t kSmallTokens = 512, kSmallWeights = 1 << 18, kSmallWork = 1 << 25;
+// Small problems: most tokens, most elements of W and most products of the two launches of hdqt_xent_small.cuh.
+struct SmallLimits {
+  int64_t tokens, weights, work;
+};
+// The rows kernel reads W from the L2 once per token and product and the gradient kernel walks over all tokens, where the
+// tensor-core path costs its launches and its pipelines' fill and drain whatever the size: 25 us on the device (30 us a
+// call) for bf16 gradients, 47 (51) for fp32, 16 (23) and 33 (35) for the loss alone.  Measured (tokens, features, classes; device, both):
+// bf16 gradients 32 x 128 x 64 10 and 20 us, 128 x 512 x 100 27 and 25, 128 x 512 x 300 41 and 27; fp32 gradients 128 x 512 x 100 29 and 47,
+// 256 x 512 x 128 44 and 51, 512 x 512 x 128 63 and 49; bf16 loss from W [classes, features] 64 x 512 x 512 14 and 16, from
+// [features, classes] 25 and 16; fp32 loss 512 x 512 x 128 26 and 33.
+SmallLimits small_limits(bool gradients, bool f32, bool w_is_cd) {
+  if (!gradients) return f32 || w_is_cd ? SmallLimits{512, 1 << 18, 1 << 25} : SmallLimits{512, 1 << 16, 1 << 25};
+  return f32 ? SmallLimits{256, 1 << 18, 1 << 24} : SmallLimits{128, 1 << 16, 1 << 23};
+}
+
+// ... and where the streamed products below would do: 2 x 512 x 512 fp32 loss 27 us here and 8 there, gradients 47 and 23.
+constexpr int64_t kSmallFewWeights = 1 << 16;
+
+// Streamed products: most tokens of a loss in two launches, and of the calls with products written out.  They cost
+// tokens x |W| fp32 operations a product, the tensor-core path the same up to 256 tokens (fp32: six products, and three
+// planes of W to be written first).  2048 x 32000, streamed and tensor-core path, us:
+//   loss, bf16: 1 token 30 and 53, 4 tokens 47 and 47, 8 tokens 84 and 45 (512 x 4000: 14 and 16)
+//   loss, fp32: 8 tokens 91 and 280; 16 tokens 165 and 263, from W [features, classes] 106 and 269
+//   gradients, bf16: 4 tokens 127 and 147, 8 tokens 250 and 145; from W [features, classes] 2 tokens 118 and 149, 4 tokens 167 and 150
+//   gradients, fp32: 8 tokens 215 and 510, 16 tokens 338 and 495, from W [features, classes] 431 and 505
+int64_t few_loss_tokens(bool f32, bool w_is_cd, int64_t weights) {
+  // (fp32 from W [features, classes]: beyond two tokens the products of the next function are faster)
+  if (f32) return w_is_cd ? kFewTokens : 2;
+  return weights <= (1 << 22) ? kFewTokens : 4;
+}
+int64_t few_product_tokens(bool gradients, bool f32, bool w_is_cd) {
+  if (!gradients) return f32 ? (w_is_cd ? 24 : 32) : 0;
+  return f32 ? 16 : w_is_cd ? 4 : 2;
+}
 constexpr size_t kSmallSmem = 100 << 10;
 constexpr int kFewBlocks = 4 * kNumSMsHint;      // most blocks of the few-token kernels
 
@@ -482,9 +513,15 @@ hdqt_status_t make_plan(const hdqt_xent_desc_t* d, int kind, Plan* pl) {
   const bool f32 = d->dtype == HDQT_DTYPE_F32;
   pl->planes = f32 ? 3 : 1;
   pl->small_rows = 0;
-  if (d->tokens > 0 && d->tokens <= kSmallTokens && d->classes * d->features <= kSmallWeights &&
-      d->tokens * d->classes * d->features <= kSmallWork && d->piece_bytes == 0) {
-    int rows = d->tokens <= 2 * kNumSMsHint ? 1 : 2;
+  const bool gradients = kind != HDQT_XENT_FWD, cd = d->w_is_cd != 0;
+  const int64_t weights = d->classes * d->features;
+  const bool any = d->tokens > 0 && d->piece_bytes == 0;      // (a stated piece size selects the tensor-core path)
+  const bool few_loss = any && !gradients && d->tokens <= few_loss_tokens(f32, cd, weights);
+  const bool few_product = any && d->tokens <= few_product_tokens(gradients, f32, cd);
+  const SmallLimits small = small_limits(gradients, f32, cd);
+  const int64_t small_weights = few_loss || few_product ? kSmallFewWeights : small.weights;
+  if (any && d->tokens <= small.tokens && weights <= small_weights && d->tokens * weights <= small.work) {
+    int rows = gradients || d->tokens <= 2 * kNumSMsHint ? 1 : 2;
     auto smem = [&](int r) { return sizeof(float) * (size_t)r * (size_t)(d->features + d->classes + kSmallThreads); };
     if (smem(rows) > kSmallSmem) rows = 1;
     if (smem(rows) <= kSmallSmem) {
@@ -493,17 +530,15 @@ hdqt_status_t make_plan(const hdqt_xent_desc_t* d, int kind, Plan* pl) {
     }
   }
   pl->few_tokens = 0;
-  if (kind == HDQT_XENT_FWD && pl->small_rows == 0 && d->tokens > 0 && d->tokens <= kFewTokens && d->piece_bytes == 0) {
+  if (few_loss && pl->small_rows == 0) {
     int n = 1;
     while (n < d->tokens) n *= 2;
     if (4 * n * d->features <= kFewSmem) pl->few_tokens = n;
   }
-  // Streamed products, up to where their 3 tokens x |W| fp32 operations pass the time of the tensor-core path with its blocks
-  // of 256 rows (fp32: six products and three planes of W).
   pl->few_grad = 0;
-  if (pl->small_rows == 0 && pl->few_tokens == 0 && d->tokens > 0 && d->tokens <= (f32 ? 16 : 8) && d->piece_bytes == 0) {
+  if (few_product && pl->small_rows == 0 && pl->few_tokens == 0) {
     pl->few_grad = 1;
-    while (pl->few_grad < d->tokens) pl->few_grad *= 2;
+    while (pl->few_grad < d->tokens && pl->few_grad < 16) pl->few_grad *= 2;
   }
   pl->stage_x = f32 || d->ld_x % 8 != 0;
   pl->stage_w = f32 || d->ld_w % 8 != 0;
@@ -899,7 +934,7 @@ hdqt_status_t run_small(const Call& c, int kind, const void* X, const void* W, c
 template <typename T, int kT, int kV>
 cudaError_t run_few_kernel(const Call& c, const FewParams& p, int* blocks) {
   const size_t smem = sizeof(float) * kT * (size_t)p.features;
-  const int per_sm = smem > (48 << 10) ? 2 : 4;
+  constexpr int per_sm = 4;
   const int tile = c.d->w_is_cd ? 4 * kFewWarps : 8 * kV;
   int64_t n = ceil_div(p.classes, tile);
   *blocks = (int)(n < per_sm * kNumSMsHint ? n : per_sm * kNumSMsHint);
@@ -910,9 +945,11 @@ cudaError_t run_few_kernel(const Call& c, const FewParams& p, int* blocks) {
   if (c.d->w_is_cd) {
     e = allow_smem<xent_few_rows_kernel<T, kT, kV>>(kFewSmem);
     if (e == cudaSuccess) c.run(xent_few_rows_kernel<T, kT, kV>, *blocks, kFewThreads, smem, p);
-  } else {
+  } else if constexpr (sizeof(T) == 2 || kT <= 2) {            // (few_loss_tokens)
     e = allow_smem<xent_few_columns_kernel<T, kT, kV>>(kFewSmem);
     if (e == cudaSuccess) c.run(xent_few_columns_kernel<T, kT, kV>, *blocks, kFewThreads, smem, p);
+  } else {
+    e = cudaErrorInvalidValue;
   }
   return e;
 }
@@ -975,12 +1012,12 @@ void few_columns_product(const Call& c, FewProduct p, int slices) {
   const uintptr_t bits = reinterpret_cast<uintptr_t>(p.m) | (uintptr_t)(p.ld_m * sizeof(T)) | (uintptr_t)(p.N * sizeof(T)) |
                          (kOuter ? reinterpret_cast<uintptr_t>(p.outer) | (uintptr_t)(p.ld_outer * sizeof(T)) : 0);
   const bool wide = (bits & (n <= 8 ? 15 : 2 * sizeof(T) - 1)) == 0;
-  switch (n) {
-    case 1: return run_few_columns<T, 1, kOuter>(c, p, slices, wide);
-    case 2: return run_few_columns<T, 2, kOuter>(c, p, slices, wide);
-    case 4: return run_few_columns<T, 4, kOuter>(c, p, slices, wide);
-    case 8: return run_few_columns<T, 8, kOuter>(c, p, slices, wide);
-    default: return run_few_columns<T, 16, kOuter>(c, p, slices, wide);
+  if (n == 1) return run_few_columns<T, 1, kOuter>(c, p, slices, wide);
+  if (n == 2) return run_few_columns<T, 2, kOuter>(c, p, slices, wide);
+  if (sizeof(T) == 2 || n == 4) return run_few_columns<T, 4, kOuter>(c, p, slices, wide);
+  if constexpr (sizeof(T) == 4) {                               // (few_product_tokens)
+    if (n == 8) return run_few_columns<T, 8, kOuter>(c, p, slices, wide);
+    return run_few_columns<T, 16, kOuter>(c, p, slices, wide);
   }
 }
 
@@ -997,12 +1034,11 @@ void run_few_rows(const Call& c, const FewProduct& p, int slices) {
 template <typename T>
 void few_rows_product(const Call& c, FewProduct p, int slices) {
   p.per_slice = (int32_t)(ceil_div(ceil_div(p.K, slices), 8) * 8);
-  switch (c.pl.few_grad) {
-    case 1: return run_few_rows<T, 1>(c, p, slices);
-    case 2: return run_few_rows<T, 2>(c, p, slices);
-    case 4: return run_few_rows<T, 4>(c, p, slices);
-    default: return run_few_rows<T, 8>(c, p, slices);
-  }
+  const int n = c.pl.few_grad;
+  if (n == 1) return run_few_rows<T, 1>(c, p, slices);
+  if (n == 2) return run_few_rows<T, 2>(c, p, slices);
+  if (sizeof(T) == 2 || n == 4) return run_few_rows<T, 4>(c, p, slices);
+  if constexpr (sizeof(T) == 4) return run_few_rows<T, 8>(c, p, slices);
 }
 
 // A few tokens by streamed products: logits, softmax, dX and dW (and the reduced loss by the caller).

@@ -366,7 +366,8 @@ __device__ __forceinline__ void x_out(const XParams& p, const XProblem& r, const
 }
 
 // Output rows that do not all start on 16 bytes: 32 x 32 pieces are turned in shared memory, so that the 32 lanes of a store
-// write neighbouring elements of one row (a store per element and row of its own took 1531 x 1001 x 50257 XXODD us).
+// write neighbouring elements of one row (a store per element and row of its own: 3 x 425 x 21344 bf16 loss and gradients 201 us, 96 so;
+// dW [2604, 44400] of 35 tokens 504 us, 262 so).
 __device__ __forceinline__ void x_out_odd(const XParams& p, const XProblem& r, const XItem& t, int row0, int col0, int lane,
                                           float* box, float (&acc)[128]) {
   const float alpha = p.alpha != nullptr ? *p.alpha : 1.0f;

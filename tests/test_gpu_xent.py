@@ -91,6 +91,10 @@ SHAPES = [    # tokens, features, classes
     (5, 100, 30001),
     (8, 2048, 3000),
     (2, 72, 9000),
+    (20, 264, 6001),
+    (32, 100, 7000),
+    (4, 520, 9001),
+    (120, 250, 260),
 ]
 
 
