@@ -471,7 +471,8 @@ size_t hdqt_group_norm_workspace_bytes(const hdqt_group_norm_desc_t* desc /*host
  * X [tokens, features], W [classes, features] (w_is_cd != 0) or [features, classes] (w_is_cd == 0), rows ld_* elements apart,
  * dX and dW in the layout of X and W; bf16 or fp32 (all four the same).  Products are formed on the tensor cores from bf16
  * operands with fp32 sums; an fp32 operand is split into three bf16 planes, which keeps fp32 precision (infinite inputs then
- * give NaN).  For bf16, dz is rounded to bf16 once before the gradient products; dX and dW are rounded once.
+ * give NaN).  Small problems and a few tokens are computed in fp32 arithmetic on the CUDA cores instead.  For bf16, dz is
+ * rounded to bf16 at most once before the gradient products; dX and dW are rounded once.
  * labels: int64 [tokens]; ignore_index rows have loss 0 and gradient 0.  A label outside [0, classes) makes its loss
  * NaN, its gradient 0, and sets HDQT_ERR_INVALID_ARG in *dev_status.
  * reduction: HDQT_REDUCE_NONE loss[tokens]; HDQT_REDUCE_MEAN one value, the mean over the rows that are not ignored (NaN
@@ -482,7 +483,7 @@ size_t hdqt_group_norm_workspace_bytes(const hdqt_group_norm_desc_t* desc /*host
  *           gradient of the loss (NULL = 1).  Works through the vocabulary in pieces.
  *   _train  all of them in one call, for a loss whose gradient's weights are known beforehand: the logits are formed once
  *           and held as 16-bit softmax codes (fp32: as logits) for a piece of the tokens at a time.  g as in _bwd.
- *           Two thirds of _fwd + _bwd's tensor work at the price of a larger workspace.
+ *           Three quarters of _fwd + _bwd's tensor work at the price of a larger workspace.
  *
  * dX or dW may be NULL (not needed).  tokens may be 0 (mean loss NaN, dW = 0).
  * Alignment: bf16 X and W 16 bytes; every other pointer its element's; workspace 256 bytes.  bf16 leading dimensions that are multiples

@@ -764,7 +764,7 @@ def linear_xent_bwd(X, W, labels, lse, g=None, ignore_index: int = -100, reducti
 
 def linear_xent_train(X, W, labels, g=None, ignore_index: int = -100, reduction: str = "mean", w_is_cd: bool = False,
                       want_dx: bool = True, want_dw: bool = True, piece_bytes: int = 0, dev_status=None):
-    """Loss and gradients in one call (two thirds of the tensor work of linear_xent_fwd + linear_xent_bwd), for a loss whose
+    """Loss and gradients in one call (three quarters of the tensor work of linear_xent_fwd + linear_xent_bwd), for a loss whose
     gradient is known beforehand: g as in linear_xent_bwd.  Returns (loss, lse, dX, dW)."""
     X, W, labels, d, ws, nbytes = _xent_call(X, W, labels, ignore_index, reduction, w_is_cd, piece_bytes, XENT_TRAIN)
     g = _loss_weight(g, reduction, d.tokens, X.device)
