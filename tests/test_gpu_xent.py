@@ -95,6 +95,7 @@ SHAPES = [    # tokens, features, classes
     (32, 100, 7000),
     (4, 520, 9001),
     (120, 250, 260),
+    (130, 16500, 300),
 ]
 
 
