@@ -96,6 +96,7 @@ SHAPES = [    # tokens, features, classes
     (4, 520, 9001),
     (120, 250, 260),
     (130, 16500, 300),
+    (2500, 1600, 70),
 ]
 
 
