@@ -233,8 +233,29 @@ class GraphedTrainStep:
 # ---- the rest of a training step: normalisation, loss, gradient clipping ------------------------------
 # Section 3 quantizes the inputs and accumulators of matrix products; what lies around them stays in floating point.
 
+class _FirstOrder(torch.autograd.Function):
+    """The first `count` tensors, which depend on the others in a way that is not recorded: differentiating them raises."""
+
+    @staticmethod
+    def forward(ctx, count: int, *tensors):
+        return tuple(t.clone() for t in tensors[:count])
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("group norm and linear cross entropy have no second derivatives")
+
+
+def _first_order(grads, inputs):
+    """Gradients as a backward pass returns them.  Where that pass is itself recorded (create_graph) a derivative through them is
+    refused rather than taken for zero; torch's once_differentiable would do so only if the incoming gradient needed one."""
+    if not torch.is_grad_enabled():
+        return grads
+    out = iter(_FirstOrder.apply(sum(t is not None for t in grads), *(t for t in grads if t is not None), *inputs))
+    return tuple(None if t is None else next(out) for t in grads)
+
+
 class GroupNormFunction(torch.autograd.Function):
-    """act(group norm) of a channels-last tensor x[batch, ..., channels]."""
+    """act(group norm) of a channels-last tensor x[batch, ..., channels].  First derivatives only."""
 
     @staticmethod
     def forward(ctx, x, gamma, beta, groups: int, eps: float, act: str):
@@ -250,7 +271,7 @@ class GroupNormFunction(torch.autograd.Function):
         dx, dgamma, dbeta = hdqt.group_norm_bwd(dy, x, gamma, beta, mean, rstd, groups, act,
                                                 want_dx=ctx.needs_input_grad[0],
                                                 want_params=ctx.needs_input_grad[1] or ctx.needs_input_grad[2])
-        return dx, dgamma, dbeta, None, None, None
+        return *_first_order((dx, dgamma, dbeta), (dy, x, gamma, beta)), None, None, None
 
 
 class GroupNormAct(torch.nn.Module):
@@ -272,7 +293,7 @@ class GroupNormAct(torch.nn.Module):
 class LinearCrossEntropyFunction(torch.autograd.Function):
     """Softmax cross entropy of x @ w without the logits in memory.  Where the loss is one number its gradients are formed
     together with it (the logits once instead of twice) and only scaled in the backward pass; per-token losses, and a second
-    backward pass through the same graph, form the logits again."""
+    backward pass through the same graph, form the logits again.  First derivatives only."""
 
     @staticmethod
     def forward(ctx, x, w, labels, ignore_index: int, reduction: str, w_is_cd: bool):
@@ -298,6 +319,8 @@ class LinearCrossEntropyFunction(torch.autograd.Function):
         else:
             x, w, labels, lse = ctx.saved_tensors
             dx, dw = hdqt.linear_xent_bwd(x, w, labels, lse, g, want_dx=want_dx, want_dw=want_dw, **ctx.how)
+        if torch.is_grad_enabled():
+            dx, dw = _first_order((dx, dw), (g, *ctx.saved_tensors[:2]))
         return dx, dw, None, None, None, None
 
 

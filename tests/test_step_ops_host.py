@@ -1,0 +1,98 @@
+"""Host side of the step operators (autograd functions, argument checks) on the CPU: the library calls are replaced by plain torch
+where a result is needed, and by a recorder where only the arguments matter.  Nothing is launched."""
+import pytest
+import torch
+
+from paper_2310_03675_b200 import hdqt
+from paper_2310_03675_b200 import nn as hnn
+
+
+@pytest.fixture
+def plain_calls(monkeypatch):
+    """group_norm_* (no activation) and linear_xent_* (mean, sum) as torch formulas on CPU tensors; a list of the loss's calls."""
+    calls = []
+
+    def gn_fwd(x, gamma, beta, groups, eps, act):
+        with torch.no_grad():
+            v = x.flatten(1, -2).unflatten(2, (groups, -1))
+            mean, var = v.mean((1, 3)), v.var((1, 3), correction=0)
+            rstd = (var + eps) ** -0.5
+            xh = (v - mean[:, None, :, None]) * rstd[:, None, :, None]
+            return (xh.flatten(2) * gamma + beta).view(x.shape), mean, rstd
+
+    def gn_bwd(dy, x, gamma, beta, mean, rstd, groups, act, want_dx=True, want_params=True):
+        with torch.enable_grad():
+            xs = [t.detach().requires_grad_(True) for t in (x, gamma, beta)]
+            v = xs[0].flatten(1, -2).unflatten(2, (groups, -1))
+            xh = (v - v.mean((1, 3), keepdim=True)) * (v.var((1, 3), correction=0, keepdim=True) + 1e-5) ** -0.5
+            y = (xh.flatten(2) * xs[1] + xs[2]).view(x.shape)
+            return torch.autograd.grad(y, xs, dy.detach())
+
+    def loss_and_grads(x, w, labels, g, ignore_index, reduction, w_is_cd):
+        with torch.enable_grad():
+            xs = [t.detach().float().requires_grad_(True) for t in (x, w)]
+            z = xs[0] @ (xs[1].t() if w_is_cd else xs[1])
+            loss = torch.nn.functional.cross_entropy(z, labels, ignore_index=ignore_index, reduction=reduction)
+            dx, dw = torch.autograd.grad(loss, xs, torch.ones_like(loss) if g is None else g.detach())
+        return loss.detach(), dx.to(x.dtype), dw.to(w.dtype), torch.logsumexp(z.detach(), 1)
+
+    def xent_fwd(x, w, labels, ignore_index=-100, reduction="mean", w_is_cd=False):
+        calls.append(("fwd", None))
+        z = x.detach().float() @ (w.detach().float().t() if w_is_cd else w.detach().float())
+        return torch.nn.functional.cross_entropy(z, labels, ignore_index=ignore_index, reduction=reduction), torch.logsumexp(z, 1)
+
+    def xent_train(x, w, labels, g=None, ignore_index=-100, reduction="mean", w_is_cd=False, want_dx=True, want_dw=True):
+        calls.append(("train", None if g is None else float(g)))
+        loss, dx, dw, lse = loss_and_grads(x, w, labels, g, ignore_index, reduction, w_is_cd)
+        return loss, lse, dx if want_dx else None, dw if want_dw else None
+
+    def xent_bwd(x, w, labels, lse, g=None, ignore_index=-100, reduction="mean", w_is_cd=False, want_dx=True, want_dw=True):
+        calls.append(("bwd", g if g is None or g.dim() else float(g)))
+        _, dx, dw, _ = loss_and_grads(x, w, labels, g, ignore_index, reduction, w_is_cd)
+        return dx if want_dx else None, dw if want_dw else None
+
+    def scale(tensors, factor, out=None):
+        calls.append(("scale", float(factor)))
+        for t in tensors:
+            t.copy_((t.float() * factor).to(t.dtype))
+
+    for name, f in (("group_norm_fwd", gn_fwd), ("group_norm_bwd", gn_bwd), ("linear_xent_fwd", xent_fwd),
+                    ("linear_xent_train", xent_train), ("linear_xent_bwd", xent_bwd), ("scale_tensors", scale)):
+        monkeypatch.setattr(hdqt, name, f)
+    return calls
+
+
+def test_group_norm_refuses_second_derivatives(plain_calls):
+    torch.manual_seed(0)
+    m = hnn.GroupNormAct(8, groups=2)
+    x = torch.randn(2, 8, 3, 3, requires_grad=True)
+    y = m(x)
+    loss = y.square().mean() + y.pow(3).mean()
+    (dx,) = torch.autograd.grad(loss, x, create_graph=True)
+    ref = torch.nn.functional.group_norm(x, 2, m.weight, m.bias)
+    (want,) = torch.autograd.grad(ref.square().mean() + ref.pow(3).mean(), x)
+    assert torch.allclose(dx, want, atol=1e-5)                   # the gradient itself is there
+    with pytest.raises(RuntimeError, match="second"):
+        (loss + dx.square().sum()).backward()
+    m(x).sum().backward()                                        # first derivatives as before
+    assert x.grad is not None and m.weight.grad is not None
+
+
+@pytest.mark.parametrize("reduction", ["mean", "none"])
+def test_cross_entropy_refuses_second_derivatives(plain_calls, reduction):
+    torch.manual_seed(1)
+    x, w = torch.randn(6, 4, requires_grad=True), torch.randn(4, 5, requires_grad=True)
+    labels = torch.randint(0, 5, (6,))
+    loss = hnn.linear_cross_entropy(x, w, labels, reduction=reduction).sum()
+    dx, dw = torch.autograd.grad(loss, (x, w), create_graph=True)
+    want = torch.autograd.grad(torch.nn.functional.cross_entropy(x @ w, labels, reduction=reduction).sum(), (x, w))
+    assert torch.allclose(dx, want[0], atol=1e-6) and torch.allclose(dw, want[1], atol=1e-6)
+    for d in (dx, dw):
+        with pytest.raises(RuntimeError, match="second"):
+            (loss + d.square().sum()).backward(retain_graph=True)
+    for t in (x, w):                                             # an input that needs no gradient does not lose the refusal
+        other = w if t is x else x
+        out = hnn.linear_cross_entropy(*((t, other.detach()) if t is x else (other.detach(), t)), labels, reduction=reduction)
+        (d,) = torch.autograd.grad(out.sum(), t, create_graph=True)
+        with pytest.raises(RuntimeError, match="second"):
+            d.square().sum().backward()
