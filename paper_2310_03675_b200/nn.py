@@ -291,48 +291,57 @@ class GroupNormAct(torch.nn.Module):
 
 
 class LinearCrossEntropyFunction(torch.autograd.Function):
-    """Softmax cross entropy of x @ w without the logits in memory.  Where the loss is one number its gradients are formed
-    together with it (the logits once instead of twice) and only scaled in the backward pass; per-token losses, and a second
-    backward pass through the same graph, form the logits again.  First derivatives only."""
+    """`scale` times the softmax cross entropy of x @ w.  Where the loss is one number its gradients are formed together with it
+    (the logits once instead of twice) and only scaled in the backward pass; per-token losses, and a second backward pass through
+    the same graph, form the logits again.  First derivatives only.
+
+    bf16 gradients are rounded when they are formed, with `scale` in them.  A factor other than 1 that arrives in the backward pass
+    multiplies the rounded gradients and rounds them once more (powers of two are exact); the second pass through a graph has
+    the factor beforehand and rounds once, so its bits may differ from the first one's."""
 
     @staticmethod
-    def forward(ctx, x, w, labels, ignore_index: int, reduction: str, w_is_cd: bool):
+    def forward(ctx, x, w, labels, ignore_index: int, reduction: str, w_is_cd: bool, scale: float):
         how = {"ignore_index": ignore_index, "reduction": reduction, "w_is_cd": w_is_cd}
         want_dx, want_dw = ctx.needs_input_grad[:2]
-        ctx.how, ctx.ready = how, None
+        ctx.how, ctx.ready, ctx.scale = how, None, scale
         if reduction != "none" and (want_dx or want_dw):
-            loss, lse, dx, dw = hdqt.linear_xent_train(x, w, labels, want_dx=want_dx, want_dw=want_dw, **how)
+            g = None if scale == 1.0 else torch.full((), scale, dtype=torch.float32, device=x.device)
+            loss, lse, dx, dw = hdqt.linear_xent_train(x, w, labels, g, want_dx=want_dx, want_dw=want_dw, **how)
             ctx.ready = (dx, dw)
         else:
             loss, lse = hdqt.linear_xent_fwd(x, w, labels, **how)
         ctx.save_for_backward(x, w, labels, lse)
-        return loss
+        return loss if scale == 1.0 else loss * scale
 
     @staticmethod
     def backward(ctx, g):
         want_dx, want_dw = ctx.needs_input_grad[:2]
-        g = g.float()
+        factor = g.detach().float()
         if ctx.ready is not None:
             dx, dw = ctx.ready
             ctx.ready = None
-            hdqt.scale_tensors([t for t in (dx, dw) if t is not None], g)
+            hdqt.scale_tensors([t for t in (dx, dw) if t is not None], factor)
         else:
             x, w, labels, lse = ctx.saved_tensors
-            dx, dw = hdqt.linear_xent_bwd(x, w, labels, lse, g, want_dx=want_dx, want_dw=want_dw, **ctx.how)
+            if ctx.scale != 1.0:
+                factor = factor * ctx.scale
+            dx, dw = hdqt.linear_xent_bwd(x, w, labels, lse, factor, want_dx=want_dx, want_dw=want_dw, **ctx.how)
         if torch.is_grad_enabled():
             dx, dw = _first_order((dx, dw), (g, *ctx.saved_tensors[:2]))
-        return dx, dw, None, None, None, None
+        return dx, dw, None, None, None, None, None
 
 
 def linear_cross_entropy(x, w, labels, bias=None, ignore_index: int = -100, reduction: str = "mean",
-                         w_is_cd: bool = False):
-    """cross_entropy(x @ w + bias, labels) for x [tokens, features] and w [features, classes] (or [classes, features] with
+                         w_is_cd: bool = False, scale: float = 1.0):
+    """scale * cross_entropy(x @ w + bias, labels) for x [tokens, features] and w [features, classes] (or [classes, features] with
     w_is_cd), fp32 or bf16, without the logits in memory.  reduction: "mean" over the labels that are not ignore_index,
-    "sum", or "none".  A bias is one more feature whose input is 1 (x and w are copied for it)."""
+    "sum", or "none".  A bias is one more feature whose input is 1 (x and w are copied for it).  scale: a factor known
+    beforehand (one over the number of accumulated batches, the loss's weight): bf16 gradients are then rounded once, where
+    multiplying the returned loss rounds them twice."""
     if bias is not None:
         x = torch.cat([x, x.new_ones((x.shape[0], 1))], 1)
         w = torch.cat([w, bias[:, None]], 1) if w_is_cd else torch.cat([w, bias[None]], 0)
-    return LinearCrossEntropyFunction.apply(x, w, labels, ignore_index, reduction, w_is_cd)
+    return LinearCrossEntropyFunction.apply(x, w, labels, ignore_index, reduction, w_is_cd, float(scale))
 
 
 def _dense(t: torch.Tensor) -> torch.Tensor:

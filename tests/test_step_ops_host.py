@@ -96,3 +96,29 @@ def test_cross_entropy_refuses_second_derivatives(plain_calls, reduction):
         (d,) = torch.autograd.grad(out.sum(), t, create_graph=True)
         with pytest.raises(RuntimeError, match="second"):
             d.square().sum().backward()
+
+
+@pytest.mark.parametrize("scale", [1.0, 0.3])
+def test_a_known_factor_of_the_loss_is_rounded_with_the_gradients(plain_calls, scale):
+    """bf16 gradients are rounded once where the factor is stated: it goes into the call that forms them, and what arrives in the
+    backward pass is 1."""
+    torch.manual_seed(2)
+    x = torch.randn(12, 6).bfloat16().requires_grad_(True)
+    w = torch.randn(6, 9).bfloat16().requires_grad_(True)
+    labels = torch.randint(0, 9, (12,))
+    loss = hnn.linear_cross_entropy(x, w, labels, scale=scale)
+    loss.backward(retain_graph=True)
+    assert plain_calls == [("train", None if scale == 1.0 else pytest.approx(scale)), ("scale", 1.0)]
+    xd, wd = x.detach().double().requires_grad_(True), w.detach().double().requires_grad_(True)
+    ref = torch.nn.functional.cross_entropy(xd @ wd, labels) * scale
+    ref.backward()
+    assert abs(loss.item() - ref.item()) < 1e-6
+    first = x.grad.clone(), w.grad.clone()
+    for got, want in zip(first, (xd.grad, wd.grad)):
+        assert bool(((got.double() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-6).all())       # one rounding (fp32 stand-in)
+    loss.backward()                                              # the retained graph: formed again, with the same factor
+    assert plain_calls[-1] == ("bwd", pytest.approx(scale))
+    for got, want in zip((x.grad, w.grad), first):
+        assert torch.equal(got, want * 2)
+    per_token = hnn.linear_cross_entropy(x.detach().float(), w.detach().float().requires_grad_(True), labels, reduction="sum", scale=0.5)
+    assert per_token.item() == pytest.approx(12 * 0.5 * ref.item() / scale, rel=1e-5)
