@@ -167,15 +167,27 @@ def _check(status: int, where: str) -> None:
         raise HdqtError(status, where)
 
 
-# the raw handle of the current stream without a Stream object around it (0.2 us instead of 3 per call)
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-_raw_device = getattr(torch._C, "_cuda_getDevice", None)
+# the raw handle of a device's current stream without a Stream object around it (0.2 us instead of 3 per call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+_raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _stream() -> int:
-    if _raw_stream is not None and _raw_device is not None:
-        return _raw_stream(_raw_device())
-    return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(_raw_device())
+
+
+def _call(name: str, t: torch.Tensor, *args) -> None:
+    """The C entry `name` with `args` and a stream, on t's device: the library launches on the current device, which is made t's
+    for the call where it is another one."""
+    index = t.get_device()
+    if index == _raw_device():
+        status = getattr(lib, name)(*args, _raw_stream(index))
+    elif index < 0:
+        raise ValueError("expected CUDA tensors")
+    else:
+        with torch.cuda.device(index):
+            status = getattr(lib, name)(*args, _raw_stream(index))
+    _check(status, name)
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -224,8 +236,8 @@ def _view_2d(src: torch.Tensor):
 def absmax_hadamard(src: torch.Tensor, had_block: int = 32, dev_status: Optional[torch.Tensor] = None):
     rows, K, ld_row, ld_k = _view_2d(src)
     out = torch.empty(1, dtype=torch.float32, device=src.device)
-    _check(lib.hdqt_absmax_hadamard(src.data_ptr(), rows, K, ld_row, ld_k, had_block, out.data_ptr(),
-                                    _ptr(dev_status), _stream()), "hdqt_absmax_hadamard")
+    _call("hdqt_absmax_hadamard", src, src.data_ptr(), rows, K, ld_row, ld_k, had_block, out.data_ptr(),
+          _ptr(dev_status))
     return out
 
 
@@ -244,9 +256,9 @@ def quantize_hadamard(src: torch.Tensor, had_block: int = 32, bits: int = 4, cli
         ws = torch.empty(lib.hdqt_quantize_workspace_bytes(rows, K, had_block), dtype=torch.uint8, device=src.device)
     else:
         codes, step, norms, ws = out
-    _check(lib.hdqt_quantize_hadamard(src.data_ptr(), rows, K, ld_row, ld_k, had_block, bits, clip, mode, seed, tag,
-                                      _ptr(amax), codes.data_ptr(), step.data_ptr(), _ptr(norms), ws.data_ptr(),
-                                      ws.numel(), _ptr(dev_status), _stream()), "hdqt_quantize_hadamard")
+    _call("hdqt_quantize_hadamard", src, src.data_ptr(), rows, K, ld_row, ld_k, had_block, bits, clip, mode, seed,
+          tag, _ptr(amax), codes.data_ptr(), step.data_ptr(), _ptr(norms), ws.data_ptr(), ws.numel(),
+          _ptr(dev_status))
     return codes, step, norms
 
 
@@ -264,9 +276,8 @@ def quantize_hadamard_static(src: torch.Tensor, codes: torch.Tensor, step: torch
     Operands are limited to rows * K_pad / 32 <= 2 097 152; calls on different streams must not
     overlap (they share the one array)."""
     rows, K, ld_row, ld_k = _view_2d(src)
-    _check(lib.hdqt_quantize_hadamard_static(src.data_ptr(), rows, K, ld_row, ld_k, had_block, bits, clip, mode,
-                                             seed, tag, codes.data_ptr(), step.data_ptr(), _ptr(norms),
-                                             _ptr(dev_status), _stream()), "hdqt_quantize_hadamard_static")
+    _call("hdqt_quantize_hadamard_static", src, src.data_ptr(), rows, K, ld_row, ld_k, had_block, bits, clip, mode,
+          seed, tag, codes.data_ptr(), step.data_ptr(), _ptr(norms), _ptr(dev_status))
     return codes, step, norms
 
 
@@ -292,10 +303,9 @@ def gemm_i8_tiled(Aq: torch.Tensor, Bq: torch.Tensor, step_a: torch.Tensor, step
         elem = 1 if acc_bits <= 8 else 2
         tiles = torch.empty((T, M, N), dtype=torch.int8 if elem == 1 else torch.int16, device=dev)
     ws = torch.empty(max(256, lib.hdqt_gemm_i8_workspace_bytes(M, N, Kp)), dtype=torch.uint8, device=dev)
-    _check(lib.hdqt_gemm_i8_tiled(Aq.data_ptr(), Bq.data_ptr(), step_a.data_ptr(), step_b.data_ptr(), M, N, Kp,
-                                  code_bits, acc_bits, acc_tile, acc_shift, had_block, out.data_ptr(), out.stride(0),
-                                  _ptr(S), _ptr(tiles), elem, _ptr(norms_a), _ptr(norms_b), flags, ws.data_ptr(),
-                                  ws.numel(), _ptr(dev_status), _stream()), "hdqt_gemm_i8_tiled")
+    _call("hdqt_gemm_i8_tiled", Aq, Aq.data_ptr(), Bq.data_ptr(), step_a.data_ptr(), step_b.data_ptr(), M, N, Kp,
+          code_bits, acc_bits, acc_tile, acc_shift, had_block, out.data_ptr(), out.stride(0), _ptr(S), _ptr(tiles),
+          elem, _ptr(norms_a), _ptr(norms_b), flags, ws.data_ptr(), ws.numel(), _ptr(dev_status))
     return out, S, tiles
 
 
@@ -303,8 +313,8 @@ def calibrate_acc_shift(Aq: torch.Tensor, Bq: torch.Tensor, acc_bits: int = 8, a
     M, Kp = Aq.shape
     N = Bq.shape[0]
     out = torch.empty(1, dtype=torch.int32, device=Aq.device)
-    _check(lib.hdqt_calibrate_acc_shift(Aq.data_ptr(), Bq.data_ptr(), M, N, Kp, acc_bits, acc_tile, out.data_ptr(),
-                                        None, 0, None, _stream()), "hdqt_calibrate_acc_shift")
+    _call("hdqt_calibrate_acc_shift", Aq, Aq.data_ptr(), Bq.data_ptr(), M, N, Kp, acc_bits, acc_tile, out.data_ptr(),
+          None, 0, None)
     return out
 
 
@@ -348,9 +358,8 @@ def _w_dims(W: torch.Tensor, w_is_cd: bool):
 def _run(fn_name, desc, a, b, out, Nb, D, C_, w_is_cd, M, N, K, workspace, dev_status):
     if workspace is None:
         workspace = Workspace(desc, M, N, K, a.device)
-    _check(getattr(lib, fn_name)(C.byref(desc), a.data_ptr(), b.data_ptr(), out.data_ptr(), Nb, D, C_,
-                                 1 if w_is_cd else 0, workspace.buf.data_ptr(), workspace.buf.numel(),
-                                 _ptr(dev_status), _stream()), fn_name)
+    _call(fn_name, a, C.byref(desc), a.data_ptr(), b.data_ptr(), out.data_ptr(), Nb, D, C_, 1 if w_is_cd else 0,
+          workspace.buf.data_ptr(), workspace.buf.numel(), _ptr(dev_status))
     return out, workspace
 
 
@@ -426,9 +435,8 @@ def conv2d_fwd(X, W, stride: int = 1, padding: int = 0, desc: Optional[GemmDesc]
         workspace = Workspace(desc, M, N, K, X.device)
     if out is None:
         out = torch.empty((B, Ho, Wo, Cout), dtype=torch.float32, device=X.device)
-    _check(lib.hdqt_conv2d_fwd(C.byref(desc), C.byref(g), X.data_ptr(), W.data_ptr(), out.data_ptr(), Cout,
-                               workspace.buf.data_ptr(), workspace.buf.numel(), _ptr(dev_status), _stream()),
-           "hdqt_conv2d_fwd")
+    _call("hdqt_conv2d_fwd", X, C.byref(desc), C.byref(g), X.data_ptr(), W.data_ptr(), out.data_ptr(), Cout,
+          workspace.buf.data_ptr(), workspace.buf.numel(), _ptr(dev_status))
     return out, workspace
 
 
@@ -464,9 +472,8 @@ def conv2d_wgrad(X, G, kernel, stride: int = 1, padding: int = 0, desc: Optional
         workspace = Workspace(desc, M, N, K, X.device)
     if out is None:
         out = torch.empty((Cout, kh, kw, Cin), dtype=torch.float32, device=X.device)
-    _check(lib.hdqt_conv2d_wgrad(C.byref(desc), C.byref(g), X.data_ptr(), G.data_ptr(), out.data_ptr(), Cout,
-                                 workspace.buf.data_ptr(), workspace.buf.numel(), _ptr(dev_status), _stream()),
-           "hdqt_conv2d_wgrad")
+    _call("hdqt_conv2d_wgrad", X, C.byref(desc), C.byref(g), X.data_ptr(), G.data_ptr(), out.data_ptr(), Cout,
+          workspace.buf.data_ptr(), workspace.buf.numel(), _ptr(dev_status))
     return out, workspace
 
 
@@ -535,8 +542,7 @@ def grad_norm(tensors, norm_type: float = 2.0, device=None) -> torch.Tensor:
     norm = torch.empty((), dtype=torch.float32, device=dev)
     nbytes = lib.hdqt_grad_norm_workspace_bytes(len(tensors))
     ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-    _check(lib.hdqt_grad_norm(table.buffer_info()[0], len(tensors), code, norm.data_ptr(), ws.data_ptr(), nbytes,
-                              _stream()), "hdqt_grad_norm")
+    _call("hdqt_grad_norm", norm, table.buffer_info()[0], len(tensors), code, norm.data_ptr(), ws.data_ptr(), nbytes)
     return norm
 
 
@@ -550,8 +556,8 @@ def clip_grad_norm(tensors, max_norm: float, norm_type: float = 2.0, out=None, d
     norm = torch.empty((), dtype=torch.float32, device=dev)
     nbytes = lib.hdqt_grad_norm_workspace_bytes(len(tensors))
     ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-    _check(lib.hdqt_clip_grad_norm(table.buffer_info()[0], len(tensors), code, max_norm, norm.data_ptr(), ws.data_ptr(),
-                                   nbytes, _stream()), "hdqt_clip_grad_norm")
+    _call("hdqt_clip_grad_norm", norm, table.buffer_info()[0], len(tensors), code, max_norm, norm.data_ptr(),
+          ws.data_ptr(), nbytes)
     return norm
 
 
@@ -562,8 +568,7 @@ def scale_tensors(tensors, factor: torch.Tensor, out=None) -> None:
     table, dev = _tensor_table(tensors, None if out is None else list(out))
     if factor.dtype != torch.float32 or factor.numel() != 1 or (dev is not None and factor.device != dev):
         raise ValueError("factor must be an fp32 scalar on the tensors' device")
-    _check(lib.hdqt_scale_tensors(table.buffer_info()[0], len(tensors), factor.data_ptr(), _stream()),
-           "hdqt_scale_tensors")
+    _call("hdqt_scale_tensors", factor, table.buffer_info()[0], len(tensors), factor.data_ptr())
 
 
 def _pixel_strides(t: torch.Tensor, name: str):
@@ -645,8 +650,8 @@ def group_norm_fwd(x, gamma, beta, groups: int, eps: float = 1e-5, act: str = "n
     stats = x.new_empty((2, d.batch, max(groups, 0)), dtype=torch.float32)
     mean, rstd = stats.unbind(0)
     ws = x.new_empty(nbytes, dtype=torch.uint8)
-    _check(lib.hdqt_group_norm_fwd(C.byref(d), x.data_ptr(), _ptr(gamma), _ptr(beta), y.data_ptr(), mean.data_ptr(),
-                                   rstd.data_ptr(), ws.data_ptr(), nbytes, _stream()), "hdqt_group_norm_fwd")
+    _call("hdqt_group_norm_fwd", x, C.byref(d), x.data_ptr(), _ptr(gamma), _ptr(beta), y.data_ptr(), mean.data_ptr(),
+          rstd.data_ptr(), ws.data_ptr(), nbytes)
     return y, mean, rstd
 
 
@@ -665,9 +670,8 @@ def group_norm_bwd(dy, x, gamma, beta, mean, rstd, groups: int, act: str = "none
     dgamma = torch.empty_like(gamma) if want_params and gamma is not None else None
     dbeta = torch.empty_like(beta) if want_params and beta is not None else None
     ws = x.new_empty(nbytes, dtype=torch.uint8)
-    _check(lib.hdqt_group_norm_bwd(C.byref(d), dy.data_ptr(), x.data_ptr(), _ptr(gamma), _ptr(beta), mean.data_ptr(),
-                                   rstd.data_ptr(), _ptr(dx), _ptr(dgamma), _ptr(dbeta), ws.data_ptr(), nbytes,
-                                   _stream()), "hdqt_group_norm_bwd")
+    _call("hdqt_group_norm_bwd", x, C.byref(d), dy.data_ptr(), x.data_ptr(), _ptr(gamma), _ptr(beta), mean.data_ptr(),
+          rstd.data_ptr(), _ptr(dx), _ptr(dgamma), _ptr(dbeta), ws.data_ptr(), nbytes)
     return dx, dgamma, dbeta
 
 
@@ -739,9 +743,8 @@ def linear_xent_fwd(X, W, labels, ignore_index: int = -100, reduction: str = "me
     X, W, labels, d, ws, nbytes = _xent_call(X, W, labels, ignore_index, reduction, w_is_cd, 0, XENT_FWD)
     lse = X.new_empty(d.tokens, dtype=torch.float32)
     loss = X.new_empty((d.tokens,) if reduction == "none" else (), dtype=torch.float32)
-    _check(lib.hdqt_linear_xent_fwd(C.byref(d), X.data_ptr(), W.data_ptr(), labels.data_ptr(), loss.data_ptr(),
-                                    lse.data_ptr(), ws.data_ptr(), nbytes, _ptr(dev_status), _stream()),
-           "hdqt_linear_xent_fwd")
+    _call("hdqt_linear_xent_fwd", X, C.byref(d), X.data_ptr(), W.data_ptr(), labels.data_ptr(), loss.data_ptr(),
+          lse.data_ptr(), ws.data_ptr(), nbytes, _ptr(dev_status))
     return loss, lse
 
 
@@ -756,9 +759,8 @@ def linear_xent_bwd(X, W, labels, lse, g=None, ignore_index: int = -100, reducti
         raise ValueError("lse must be the dense fp32 [tokens] tensor of the forward call")
     dX = torch.empty_like(X, memory_format=torch.contiguous_format) if want_dx else None
     dW = torch.empty_like(W, memory_format=torch.contiguous_format) if want_dw else None
-    _check(lib.hdqt_linear_xent_bwd(C.byref(d), X.data_ptr(), W.data_ptr(), labels.data_ptr(), lse.data_ptr(), _ptr(g),
-                                    _ptr(dX), _ptr(dW), ws.data_ptr(), nbytes, _ptr(dev_status), _stream()),
-           "hdqt_linear_xent_bwd")
+    _call("hdqt_linear_xent_bwd", X, C.byref(d), X.data_ptr(), W.data_ptr(), labels.data_ptr(), lse.data_ptr(),
+          _ptr(g), _ptr(dX), _ptr(dW), ws.data_ptr(), nbytes, _ptr(dev_status))
     return dX, dW
 
 
@@ -772,7 +774,6 @@ def linear_xent_train(X, W, labels, g=None, ignore_index: int = -100, reduction:
     loss = X.new_empty((d.tokens,) if reduction == "none" else (), dtype=torch.float32)
     dX = torch.empty_like(X, memory_format=torch.contiguous_format) if want_dx else None
     dW = torch.empty_like(W, memory_format=torch.contiguous_format) if want_dw else None
-    _check(lib.hdqt_linear_xent_train(C.byref(d), X.data_ptr(), W.data_ptr(), labels.data_ptr(), _ptr(g),
-                                      loss.data_ptr(), lse.data_ptr(), _ptr(dX), _ptr(dW), ws.data_ptr(), nbytes,
-                                      _ptr(dev_status), _stream()), "hdqt_linear_xent_train")
+    _call("hdqt_linear_xent_train", X, C.byref(d), X.data_ptr(), W.data_ptr(), labels.data_ptr(), _ptr(g),
+          loss.data_ptr(), lse.data_ptr(), _ptr(dX), _ptr(dW), ws.data_ptr(), nbytes, _ptr(dev_status))
     return loss, lse, dX, dW

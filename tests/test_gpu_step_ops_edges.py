@@ -48,3 +48,38 @@ def test_bf16_gradients_through_autograd(tokens, features, classes):
     g = torch.tensor(0.3, device="cuda")
     _, _, dx, dw = hdqt.linear_xent_train(x.detach(), w.detach(), labels, g)
     assert torch.equal(x.grad, dx) and torch.equal(w.grad, dw)               # the bits of the call that rounds once
+
+
+def test_tensors_of_another_device_than_the_current_one(monkeypatch):
+    """With the current device reported as another one every call enters the tensors' own, and gives the same bits."""
+    torch.manual_seed(7)
+    x, w = torch.randn(70, 40, device="cuda"), torch.randn(40, 50, device="cuda")
+    labels = torch.randint(0, 50, (70,), device="cuda")
+    img, dy = torch.randn(2, 3, 3, 16, device="cuda"), torch.randn(2, 3, 3, 16, device="cuda")
+
+    def everything():
+        y, mean, rstd = hdqt.group_norm_fwd(img, None, None, 4)
+        dx = hdqt.group_norm_bwd(dy, img, None, None, mean, rstd, 4)[0]
+        loss, lse = hdqt.linear_xent_fwd(x, w, labels)
+        grads = hdqt.linear_xent_bwd(x, w, labels, lse) + hdqt.linear_xent_train(x, w, labels)
+        clipped = [x.clone()]
+        norm = hdqt.clip_grad_norm(clipped, 1.0)
+        hdqt.scale_tensors(clipped, norm)
+        return y, mean, rstd, dx, loss, lse, *grads, norm, clipped[0], hdqt.grad_norm([x]), hdqt.gemm_fwd(x, w)[0]
+
+    want = everything()
+    entered = []
+    real = torch.cuda.device
+
+    class Guard(real):
+        def __init__(self, index):
+            entered.append(index)
+            super().__init__(index)
+
+    monkeypatch.setattr(hdqt, "_raw_device", lambda: 7)
+    monkeypatch.setattr(torch.cuda, "device", Guard)
+    got = everything()
+    assert len(entered) == 9 and set(entered) == {0}
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    with pytest.raises(ValueError):
+        hdqt.calibrate_acc_shift(torch.zeros(4, 32, dtype=torch.int8), torch.zeros(4, 32, dtype=torch.int8))

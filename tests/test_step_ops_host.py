@@ -122,3 +122,54 @@ def test_a_known_factor_of_the_loss_is_rounded_with_the_gradients(plain_calls, s
         assert torch.equal(got, want * 2)
     per_token = hnn.linear_cross_entropy(x.detach().float(), w.detach().float().requires_grad_(True), labels, reduction="sum", scale=0.5)
     assert per_token.item() == pytest.approx(12 * 0.5 * ref.item() / scale, rel=1e-5)
+
+
+def test_calls_run_on_the_tensors_device(monkeypatch):
+    """A C entry launches on the current device and on the stream it is given: both have to be those of the tensors."""
+    log = []
+
+    class Tensor:
+        def __init__(self, index):
+            self.index = index
+
+        def get_device(self):
+            return self.index
+
+    class Guard:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            log.append(("enter", self.index))
+
+        def __exit__(self, *_):
+            log.append(("exit", self.index))
+
+    class Lib:
+        @staticmethod
+        def hdqt_grad_norm(*args):
+            log.append(args)
+            return 0 if args[0] else 1
+
+        @staticmethod
+        def hdqt_status_string(_):
+            return b"invalid"
+
+    monkeypatch.setattr(hdqt, "lib", Lib)
+    monkeypatch.setattr(hdqt, "_raw_device", lambda: 1)
+    monkeypatch.setattr(hdqt, "_raw_stream", lambda index: 1000 + index)
+    monkeypatch.setattr(torch.cuda, "device", Guard)
+    hdqt._call("hdqt_grad_norm", Tensor(1), 7)
+    assert log == [(7, 1001)]
+    log.clear()
+    hdqt._call("hdqt_grad_norm", Tensor(0), 7)
+    assert log == [("enter", 0), (7, 1000), ("exit", 0)]
+    with pytest.raises(hdqt.HdqtError, match="hdqt_grad_norm"):
+        hdqt._call("hdqt_grad_norm", Tensor(1), 0)
+
+
+def test_no_call_takes_the_current_device_for_the_tensors():
+    """Every launching C entry goes through hdqt._call; only the rate measurement, which has no tensors, names the stream itself."""
+    import inspect
+    direct = [line for line in inspect.getsource(hdqt).splitlines() if "_stream()" in line and "def " not in line]
+    assert len(direct) == 1 and "hdqt_selftest_mma_rate" in direct[0]
