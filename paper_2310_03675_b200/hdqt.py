@@ -194,6 +194,14 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+def _status(t: Optional[torch.Tensor], like: torch.Tensor) -> Optional[int]:
+    if t is None:
+        return None
+    if t.device != like.device or t.dtype != torch.int32 or t.numel() < 1:
+        raise ValueError("dev_status must be an int32 tensor on the operands' device (new_status)")
+    return t.data_ptr()
+
+
 def new_status(device) -> torch.Tensor:
     return torch.zeros(1, dtype=torch.int32, device=device)
 
@@ -662,7 +670,8 @@ def group_norm_bwd(dy, x, gamma, beta, mean, rstd, groups: int, act: str = "none
     if dy.shape != x.shape or dy.dtype != x.dtype or dy.device != x.device:
         raise ValueError("dy must have x's shape, type and device")
     if mean.shape != (d.batch, groups) or mean.shape != rstd.shape or mean.dtype != torch.float32 \
-            or rstd.dtype != torch.float32 or not (mean.is_contiguous() and rstd.is_contiguous()):
+            or rstd.dtype != torch.float32 or not (mean.is_contiguous() and rstd.is_contiguous()) \
+            or mean.device != x.device or rstd.device != x.device:
         raise ValueError("mean and rstd must be the dense fp32 [batch, groups] tensors of the forward call")
     if not dy.is_contiguous():
         dy = dy.contiguous()
@@ -744,7 +753,7 @@ def linear_xent_fwd(X, W, labels, ignore_index: int = -100, reduction: str = "me
     lse = X.new_empty(d.tokens, dtype=torch.float32)
     loss = X.new_empty((d.tokens,) if reduction == "none" else (), dtype=torch.float32)
     _call("hdqt_linear_xent_fwd", X, C.byref(d), X.data_ptr(), W.data_ptr(), labels.data_ptr(), loss.data_ptr(),
-          lse.data_ptr(), ws.data_ptr(), nbytes, _ptr(dev_status))
+          lse.data_ptr(), ws.data_ptr(), nbytes, _status(dev_status, X))
     return loss, lse
 
 
@@ -760,7 +769,7 @@ def linear_xent_bwd(X, W, labels, lse, g=None, ignore_index: int = -100, reducti
     dX = torch.empty_like(X, memory_format=torch.contiguous_format) if want_dx else None
     dW = torch.empty_like(W, memory_format=torch.contiguous_format) if want_dw else None
     _call("hdqt_linear_xent_bwd", X, C.byref(d), X.data_ptr(), W.data_ptr(), labels.data_ptr(), lse.data_ptr(),
-          _ptr(g), _ptr(dX), _ptr(dW), ws.data_ptr(), nbytes, _ptr(dev_status))
+          _ptr(g), _ptr(dX), _ptr(dW), ws.data_ptr(), nbytes, _status(dev_status, X))
     return dX, dW
 
 
@@ -775,5 +784,5 @@ def linear_xent_train(X, W, labels, g=None, ignore_index: int = -100, reduction:
     dX = torch.empty_like(X, memory_format=torch.contiguous_format) if want_dx else None
     dW = torch.empty_like(W, memory_format=torch.contiguous_format) if want_dw else None
     _call("hdqt_linear_xent_train", X, C.byref(d), X.data_ptr(), W.data_ptr(), labels.data_ptr(), _ptr(g),
-          loss.data_ptr(), lse.data_ptr(), _ptr(dX), _ptr(dW), ws.data_ptr(), nbytes, _ptr(dev_status))
+          loss.data_ptr(), lse.data_ptr(), _ptr(dX), _ptr(dW), ws.data_ptr(), nbytes, _status(dev_status, X))
     return loss, lse, dX, dW

@@ -173,3 +173,30 @@ def test_no_call_takes_the_current_device_for_the_tensors():
     import inspect
     direct = [line for line in inspect.getsource(hdqt).splitlines() if "_stream()" in line and "def " not in line]
     assert len(direct) == 1 and "hdqt_selftest_mma_rate" in direct[0]
+
+
+def test_statistics_and_status_words_of_another_device_are_refused(monkeypatch):
+    """Their addresses would be read and written by a kernel that cannot reach them."""
+    launched = []
+    monkeypatch.setattr(hdqt, "_call", lambda name, *args: launched.append(name))
+    d = hdqt.GroupNormDesc(2, 9, 16, 4, 144, 16, 144, 16, 0, 0, 0, 1e-5)
+    monkeypatch.setattr(hdqt, "_group_norm_plan", lambda *args: (d, (256, 256)))
+    x, stat, far = torch.zeros(2, 3, 3, 16), torch.zeros(2, 4), torch.zeros(2, 4, device="meta")
+    for mean, rstd in ((far, stat), (stat, far)):
+        with pytest.raises(ValueError):
+            hdqt.group_norm_bwd(x, x, None, None, mean, rstd, 4)
+    hdqt.group_norm_bwd(x, x, None, None, stat, stat, 4)
+    assert launched == ["hdqt_group_norm_bwd"]
+
+    launched.clear()
+    xd = hdqt.XentDesc(10, 16, 40, 16, 40, 16, 40, -100, 0, 0, 0, 1, 0)
+    X, W, labels, lse = torch.zeros(10, 16), torch.zeros(16, 40), torch.zeros(10, dtype=torch.int64), torch.zeros(10)
+    monkeypatch.setattr(hdqt, "_xent_call", lambda *args: (X, W, labels, xd, torch.zeros(256, dtype=torch.uint8), 256))
+    for status in (torch.zeros(1, dtype=torch.int32, device="meta"), torch.zeros(1), torch.zeros(0, dtype=torch.int32)):
+        for call in (lambda: hdqt.linear_xent_fwd(X, W, labels, dev_status=status),
+                     lambda: hdqt.linear_xent_bwd(X, W, labels, lse, dev_status=status),
+                     lambda: hdqt.linear_xent_train(X, W, labels, dev_status=status)):
+            with pytest.raises(ValueError):
+                call()
+    hdqt.linear_xent_fwd(X, W, labels, dev_status=torch.zeros(1, dtype=torch.int32))
+    assert launched == ["hdqt_linear_xent_fwd"]
