@@ -384,8 +384,9 @@ typedef enum {
 } hdqt_dtype_t;
 
 /* One tensor of a list: `numel` elements of `dtype` (hdqt_dtype_t) at src, read; written to dst, which may equal src
- * but must not overlap any source otherwise.  Elements are dense; the base needs the element's own alignment only
- * (16 bytes, the same for both, selects the vector path).  numel may be 0 (the pointers are then not looked at). */
+ * but must not overlap any other source or destination of the list (HDQT_ERR_INVALID_ARG).  Elements are dense; the base
+ * needs the element's own alignment only (16 bytes, the same for both, selects the vector path).  numel may be 0 (the
+ * pointers are then not looked at). */
 typedef struct hdqt_tensor {
   const void* src;
   void* dst;

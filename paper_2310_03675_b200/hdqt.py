@@ -556,7 +556,8 @@ def grad_norm(tensors, norm_type: float = 2.0, device=None) -> torch.Tensor:
 
 def clip_grad_norm(tensors, max_norm: float, norm_type: float = 2.0, out=None, device=None) -> torch.Tensor:
     """Scales the tensors by min(1, max_norm / (norm + 1e-6)), in place or into the tensors of `out`, and returns the
-    norm they had (see grad_norm).  Nothing synchronises the host; the call can be recorded into a CUDA graph."""
+    norm they had (see grad_norm).  A tensor that is written may not overlap another one of the call.  Nothing synchronises
+    the host; the call can be recorded into a CUDA graph."""
     tensors = list(tensors)
     code = _norm_code(norm_type)
     table, dev = _tensor_table(tensors, None if out is None else list(out))

@@ -200,3 +200,38 @@ def test_statistics_and_status_words_of_another_device_are_refused(monkeypatch):
                 call()
     hdqt.linear_xent_fwd(X, W, labels, dev_status=torch.zeros(1, dtype=torch.int32))
     assert launched == ["hdqt_linear_xent_fwd"]
+
+
+def test_overlapping_tensors_are_refused_where_they_are_written():
+    """Two blocks would read and write the same elements in no fixed order.  Addresses only: the refusal precedes any launch."""
+    import ctypes as C
+    lib, INVALID = hdqt.lib, 1
+
+    def calls(*entries):
+        flat = [v for e in entries for v in e]
+        table = (C.c_int64 * len(flat))(*flat)
+        return (lib.hdqt_clip_grad_norm(C.addressof(table), len(entries), 2, 1.0, 256, 256, 1 << 20, None),
+                lib.hdqt_scale_tensors(C.addressof(table), len(entries), 256, None))
+
+    F32, BF16, A = 0, 1, 1 << 20
+    refused = [
+        [(A, A, 8, F32), (A, A, 8, F32)],                              # the same tensor twice, in place
+        [(A, A, 8, F32), (A + 28, A + 28, 8, F32)],                    # views that share an element
+        [(A, A, 100, F32), (A + 8, A + 8, 2, F32)],                    # one inside the other
+        [(A, A + 4096, 8, F32), (A + 64, A + 4096, 8, F32)],           # one destination for two
+        [(A, A + 16, 8, F32)],                                         # shifted onto its own source
+        [(A, A + 4096, 8, F32), (A + 4096, A + 8192, 8, F32)],         # a destination that another entry reads
+        [(A, A, 8, F32), (A, A + 4096, 8, F32)],                       # scaled in place, and read for another copy
+        [(A + 16 * i, A + 16 * i, 4, F32) for i in range(2000)] + [(A + 16 * 700 + 12, A + 16 * 700 + 12, 1, F32)],
+        [(A, A, 8, BF16), (A + 8, A + 8, 1, F32)],
+    ]
+    for entries in refused:
+        assert calls(*entries) == (INVALID, INVALID), entries[:3]
+    # reading an element twice is no conflict: the norm alone, and copies into places of their own
+    if not torch.cuda.is_available():                                  # (these would run)
+        flat = (C.c_int64 * 8)(A, 0, 8, F32, A, 0, 8, F32)
+        assert lib.hdqt_grad_norm(C.addressof(flat), 2, 2, 256, 256, 1 << 20, None) != INVALID
+        for entries in ([(A, A, 8, F32), (A + 32, A + 32, 8, F32)], [(A, A, 8, F32), (A, A, 0, F32)],
+                        [(A, A + 4096, 8, F32), (A, A + 8192, 8, F32)], [(A, A + 32, 8, F32), (A + 64, A + 96, 8, F32)],
+                        [(A + 16 * i, A + 16 * i, 4, F32) for i in reversed(range(2000))]):
+            assert INVALID not in calls(*entries)
