@@ -335,10 +335,13 @@ def linear_cross_entropy(x, w, labels, bias=None, ignore_index: int = -100, redu
                          w_is_cd: bool = False, scale: float = 1.0):
     """scale * cross_entropy(x @ w + bias, labels) for x [tokens, features] and w [features, classes] (or [classes, features] with
     w_is_cd), fp32 or bf16, without the logits in memory.  reduction: "mean" over the labels that are not ignore_index,
-    "sum", or "none".  A bias is one more feature whose input is 1 (x and w are copied for it).  scale: a factor known
-    beforehand (one over the number of accumulated batches, the loss's weight): bf16 gradients are then rounded once, where
-    multiplying the returned loss rounds them twice."""
+    "sum", or "none".  A bias ([classes], of w's type) is one more feature whose input is 1 (x and w are copied for it).
+    scale: a factor known beforehand (one over the number of accumulated batches, the loss's weight): bf16 gradients are then
+    rounded once, where multiplying the returned loss rounds them twice."""
     if bias is not None:
+        classes = w.shape[0] if w_is_cd else w.shape[-1]
+        if bias.dtype != w.dtype or tuple(bias.shape) != (classes,):
+            raise ValueError(f"bias must be a [{classes}] tensor of w's type")
         x = torch.cat([x, x.new_ones((x.shape[0], 1))], 1)
         w = torch.cat([w, bias[:, None]], 1) if w_is_cd else torch.cat([w, bias[None]], 0)
     return LinearCrossEntropyFunction.apply(x, w, labels, ignore_index, reduction, w_is_cd, float(scale))

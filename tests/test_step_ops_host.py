@@ -235,3 +235,14 @@ def test_overlapping_tensors_are_refused_where_they_are_written():
                         [(A, A + 4096, 8, F32), (A, A + 8192, 8, F32)], [(A, A + 32, 8, F32), (A + 64, A + 96, 8, F32)],
                         [(A + 16 * i, A + 16 * i, 4, F32) for i in reversed(range(2000))]):
             assert INVALID not in calls(*entries)
+
+
+@pytest.mark.parametrize("w_is_cd", [False, True])
+def test_a_bias_of_another_type_or_size_is_named(plain_calls, w_is_cd):
+    x, w = torch.randn(6, 4).bfloat16(), torch.randn((5, 4) if w_is_cd else (4, 5)).bfloat16()
+    labels = torch.randint(0, 5, (6,))
+    for bias in (torch.randn(5), torch.randn(5).half(), torch.randn(4).bfloat16(), torch.randn(5, 1).bfloat16()):
+        with pytest.raises(ValueError, match="bias"):
+            hnn.linear_cross_entropy(x, w, labels, bias=bias, w_is_cd=w_is_cd)
+    got = hnn.linear_cross_entropy(x, w, labels, bias=torch.ones(5).bfloat16(), w_is_cd=w_is_cd)
+    assert float(got) == pytest.approx(float(hnn.linear_cross_entropy(x, w, labels, w_is_cd=w_is_cd)), abs=1e-5)
