@@ -146,9 +146,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// x = p0 + p1 + p2 in bf16, each the rounding of what the ones before leave
+// x = p0 + p1 + p2 in bf16, each the rounding of what the ones before leave.  fp32 values above the largest bf16 value (a mask of
+// the lowest fp32 value) would round to infinity and leave NaN: p0 stops at that value, and the other two still hold the rest.
+constexpr float kBf16Max = 3.38953139e38f;      // 2^128 - 2^120
 __device__ __forceinline__ void split3(float x, float& p0, float& p1, float& p2) {
-  p0 = __bfloat162float(__float2bfloat16_rn(x));
+  p0 = __bfloat162float(__float2bfloat16_rn(fminf(fmaxf(x, -kBf16Max), kBf16Max)));
   p1 = __bfloat162float(__float2bfloat16_rn(x - p0));
   p2 = x - p0 - p1;
 }

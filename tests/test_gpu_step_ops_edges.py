@@ -83,3 +83,39 @@ def test_tensors_of_another_device_than_the_current_one(monkeypatch):
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     with pytest.raises(ValueError):
         hdqt.calibrate_acc_shift(torch.zeros(4, 32, dtype=torch.int8), torch.zeros(4, 32, dtype=torch.int8))
+
+
+def test_fp32_values_above_the_largest_bf16_value():
+    """fp32 operands travel as three bf16 planes; a mask of the lowest fp32 value rounds to -infinity in the first of them.  Classes
+    that no token may take leave loss and gradients those of the other classes; 300 x 32 x 400, O(1) logits.  Tolerances: 32 products
+    of 24 bits, sums of at most 400 terms with 2^-23 dropped at each of 400/16 additions: 1e-5 of the terms' size, which is
+    below 40 for a gradient."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    low = torch.finfo(torch.float32).min
+    x = torch.randn(300, 32, generator=g, device="cuda")
+    w = torch.randn(400, 32, generator=g, device="cuda") * 0.25
+    x[:, 0] = 1.0
+    w[:, 0] = 0.0
+    w[100:, 0] = low
+    labels = torch.randint(0, 100, (300,), generator=g, device="cuda")
+    rows = torch.rand(300, generator=g, device="cuda")
+    xd, wd = x[:, 1:].double(), w[:100, 1:].double()
+    z = xd @ wd.t()
+    lse = torch.logsumexp(z, 1)
+    dz = torch.softmax(z, 1)
+    dz[torch.arange(300), labels] -= 1.0
+    dz *= rows.double()[:, None]
+    for piece in (0, 1 << 28):
+        how = {"reduction": "none", "w_is_cd": True, "piece_bytes": piece}
+        loss, got_lse, dx, dw = hdqt.linear_xent_train(x, w, labels, rows, **how)
+        dx2, dw2 = hdqt.linear_xent_bwd(x, w, labels, got_lse, rows, **how)
+        assert float((got_lse.double() - lse).abs().max()) < 1e-5
+        assert float((loss.double() - (lse - z.gather(1, labels[:, None])[:, 0])).abs().max()) < 1e-5
+        for a, b in ((dx, dw), (dx2, dw2)):
+            assert not b[100:].any()
+            assert float((a[:, 1:].double() - dz @ wd).abs().max()) < 4e-4
+            assert float((b[:100, 1:].double() - dz.t() @ xd).abs().max()) < 4e-4
+    x[5, 3], w[7, 3] = 3.4e38, 0.0                       # a large activation against a class that does not look at it
+    z = x.double()[5] @ w.double()[7]
+    _, got_lse, _, _ = hdqt.linear_xent_train(x, w[7:8].contiguous(), torch.zeros_like(labels), rows, **how)
+    assert abs(float(got_lse[5].double() - z)) < 1e-5
