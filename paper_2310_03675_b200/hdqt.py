@@ -587,6 +587,8 @@ def _pixel_strides(t: torch.Tensor, name: str):
         raise ValueError(f"{name} must be [batch, ..., channels]")
     if st[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"{name} must have its channels contiguous")
+    if 0 in shape[1:-1]:                                       # no pixels: whatever the strides, nothing lies anywhere
+        return 0, shape[-1]
     pixel, step = None, 0
     for size, stride in zip(shape[-2:0:-1], st[-2:0:-1]):      # pixel dimensions, innermost first
         if size == 1:

@@ -119,3 +119,13 @@ def test_fp32_values_above_the_largest_bf16_value():
     z = x.double()[5] @ w.double()[7]
     _, got_lse, _, _ = hdqt.linear_xent_train(x, w[7:8].contiguous(), torch.zeros_like(labels), rows, **how)
     assert abs(float(got_lse[5].double() - z)) < 1e-5
+
+
+@pytest.mark.parametrize("shape", [(2, 3, 0, 8), (2, 0, 0, 8), (0, 3, 0, 8), (3, 0, 8)])
+def test_group_norm_of_images_without_pixels(shape):
+    gamma, beta = torch.ones(8, device="cuda"), torch.zeros(8, device="cuda")
+    x = torch.empty(shape, device="cuda")
+    y, mean, rstd = hdqt.group_norm_fwd(x, gamma, beta, 2)
+    assert y.shape == x.shape and mean.shape == (shape[0], 2) and bool(torch.isnan(mean).all())
+    dx, dgamma, dbeta = hdqt.group_norm_bwd(x, x, gamma, beta, mean, rstd, 2)
+    assert dx.shape == x.shape and not dgamma.any() and not dbeta.any()

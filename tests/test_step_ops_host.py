@@ -246,3 +246,16 @@ def test_a_bias_of_another_type_or_size_is_named(plain_calls, w_is_cd):
             hnn.linear_cross_entropy(x, w, labels, bias=bias, w_is_cd=w_is_cd)
     got = hnn.linear_cross_entropy(x, w, labels, bias=torch.ones(5).bfloat16(), w_is_cd=w_is_cd)
     assert float(got) == pytest.approx(float(hnn.linear_cross_entropy(x, w, labels, w_is_cd=w_is_cd)), abs=1e-5)
+
+
+def test_strides_of_images_without_pixels():
+    """Any order of sizes with a 0 in it is an image without pixels, whatever torch writes down as its strides."""
+    for shape in ((2, 3, 0, 8), (2, 0, 3, 8), (2, 0, 0, 8), (0, 3, 0, 8), (2, 0, 8), (1, 5, 3, 0, 8), (0, 3, 3, 8)):
+        batch, pixel = hdqt._pixel_strides(torch.empty(shape), "x")
+        assert pixel >= 8 and batch >= 0
+    assert hdqt._pixel_strides(torch.empty(2, 5, 3, 8), "x") == (120, 8)
+    assert hdqt._pixel_strides(torch.empty(2, 5, 3, 48)[..., :8], "x") == (720, 48)
+    with pytest.raises(ValueError):
+        hdqt._pixel_strides(torch.empty(2, 5, 3, 8)[:, :, ::2], "x")
+    with pytest.raises(ValueError):
+        hdqt._pixel_strides(torch.empty(2, 8, 3, 0).transpose(1, 3), "x")        # channels still have to be contiguous
