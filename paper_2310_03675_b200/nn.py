@@ -281,9 +281,14 @@ class GroupNormAct(torch.nn.Module):
 
     def __init__(self, channels: int, groups: int = 32, act: str = "none", eps: float = 1e-5):
         super().__init__()
+        groups = min(groups, channels)
+        if groups < 1 or channels % groups != 0:
+            raise ValueError(f"{groups} groups do not divide {channels} channels")
+        if act not in hdqt.ACT_CODES:
+            raise ValueError(f"act must be one of {sorted(hdqt.ACT_CODES)}")
         self.weight = torch.nn.Parameter(torch.ones(channels))
         self.bias = torch.nn.Parameter(torch.zeros(channels))
-        self.groups, self.act, self.eps = min(groups, channels), act, eps
+        self.groups, self.act, self.eps = groups, act, eps
 
     def forward(self, x):
         y = GroupNormFunction.apply(_nhwc(x), self.weight, self.bias, self.groups, self.eps, self.act)

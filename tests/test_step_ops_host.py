@@ -259,3 +259,12 @@ def test_strides_of_images_without_pixels():
         hdqt._pixel_strides(torch.empty(2, 5, 3, 8)[:, :, ::2], "x")
     with pytest.raises(ValueError):
         hdqt._pixel_strides(torch.empty(2, 8, 3, 0).transpose(1, 3), "x")        # channels still have to be contiguous
+
+
+def test_group_norm_module_names_groups_that_do_not_divide_the_channels():
+    for channels, groups in ((48, 32), (8, 3), (8, 0), (8, -2)):
+        with pytest.raises(ValueError, match="groups"):
+            hnn.GroupNormAct(channels, groups=groups)
+    with pytest.raises(ValueError, match="act"):
+        hnn.GroupNormAct(8, groups=2, act="gelu")
+    assert hnn.GroupNormAct(8).groups == 8 and hnn.GroupNormAct(64).groups == 32
