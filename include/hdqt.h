@@ -464,7 +464,7 @@ hdqt_status_t hdqt_group_norm_bwd(const hdqt_group_norm_desc_t* desc /*host*/, c
 size_t hdqt_group_norm_workspace_bytes(const hdqt_group_norm_desc_t* desc /*host*/, int32_t backward);
 
 /*
- * Linear layer + softmax cross entropy over a large vocabulary, without the logits in memory.
+ * Linear layer + softmax cross entropy over a large vocabulary, without the fp32 logits of all tokens in memory.
  *
  *   z[t, v] = sum_d X[t, d] W[v, d],   lse[t] = log sum_v exp z[t, v],   loss[t] = lse[t] - z[t, label[t]]
  *   dz[t, v] = g[t] (exp(z[t, v] - lse[t]) - [v == label[t]]),   dX = dz W,   dW = dz^T X
@@ -473,18 +473,24 @@ size_t hdqt_group_norm_workspace_bytes(const hdqt_group_norm_desc_t* desc /*host
  * dX and dW in the layout of X and W; bf16 or fp32 (all four the same).  Products are formed on the tensor cores from bf16
  * operands with fp32 sums; an fp32 operand is split into three bf16 planes, which keeps fp32 precision (infinite inputs then
  * give NaN).  Small problems and a few tokens are computed in fp32 arithmetic on the CUDA cores instead.  For bf16, dz is
- * rounded to bf16 at most once before the gradient products; dX and dW are rounded once.
+ * rounded to bf16 at most once before the gradient products (with its row's weight in it where every row has one; one
+ * weight for all multiplies the fp32 sums); dX and dW are rounded once.
  * labels: int64 [tokens]; ignore_index rows have loss 0 and gradient 0.  A label outside [0, classes) makes its loss
  * NaN, its gradient 0, and sets HDQT_ERR_INVALID_ARG in *dev_status.
  * reduction: HDQT_REDUCE_NONE loss[tokens]; HDQT_REDUCE_MEAN one value, the mean over the rows that are not ignored (NaN
  * if there are none); HDQT_REDUCE_SUM one value.  lse: [tokens], always written.
  *
- *   _fwd    loss and lse.  The logits exist as 256 x 256 blocks in tensor memory only.
+ *   _fwd    loss and lse.  The logits exist as 256 x 256 blocks in tensor memory only (a few output blocks or tokens: as fp32
+ *           partial products in the workspace).
  *   _bwd    dX and dW from lse, the logits formed again.  g (device fp32): [tokens] for HDQT_REDUCE_NONE, else one value, the
- *           gradient of the loss (NULL = 1).  Works through the vocabulary in pieces.
+ *           gradient of the loss (NULL = 1).  Works through the vocabulary in pieces, dz of a piece in the workspace.  Its
+ *           probabilities exp(z - lse) are as exact as the fp32 lse: |lse| 2^-24 relative.
  *   _train  all of them in one call, for a loss whose gradient's weights are known beforehand: the logits are formed once
- *           and held as 16-bit softmax codes (fp32: as logits) for a piece of the tokens at a time.  g as in _bwd.
+ *           and held for a piece of the tokens at a time, as 16-bit softmax codes that become dz in place (fp32: as logits and
+ *           three planes of dz, 10 bytes).  g as in _bwd.
  *           Three quarters of _fwd + _bwd's tensor work at the price of a larger workspace.
+ * A piece is 1 GiB of that, or what fp32 sums of dX (_bwd) or dW (_train) would take where they are larger; below it all
+ * tokens and classes are one piece (4096 x 2048 x 32000 bf16: 8, 262 and 270 MB; the fp32 logits would be 524 MB).
  *
  * dX or dW may be NULL (not needed).  tokens may be 0 (mean loss NaN, dW = 0).
  * Alignment: bf16 X and W 16 bytes; every other pointer its element's; workspace 256 bytes.  bf16 leading dimensions that are multiples

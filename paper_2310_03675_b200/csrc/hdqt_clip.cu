@@ -8,8 +8,8 @@
 //
 // Bound by HBM: every element is read twice (the factor is known after the last one only) and written once; the scaling pass
 // walks backwards, so that what the first pass left in the L2 is read from there.  400 M elements of mixed types (1.35 GB): 225 us
-// for the norm (6.0 TB/s), 427 us for scaling (6.3 TB/s).  62 tensors with 11 M elements: 26 us on the device, 50 us a call, which is
-// the host's time for filling the table.
+// for the norm (6.0 TB/s), 427 us for scaling (6.3 TB/s).  62 tensors with 11 M elements: 26 us on the device, 53 us a call, which is
+// the host's time for filling the table (and, 1 us of it, for looking for overlaps).
 #include <math.h>
 #include <stdlib.h>
 

@@ -11,7 +11,8 @@
 // pass over the same data (from L1 and L2 up to about 100 MB in flight, from HBM above).  One launch, backward two.
 //
 // Streaming kernels, for groups wider than a block's columns: per-channel partial statistics of a piece of an image, a
-// join per group, and an elementwise pass.
+// join per group, and an elementwise pass.  8 x 64 x 64 x 4160 in two groups, SiLU: bf16 (273 MB) forward 301 us, backward 555
+// (2.7 and 2.5 TB/s of the three and five passes over the data), fp32 410 and 930 us.  The widest accesses spill (48 to 224 bytes).
 //
 // Variance: a thread sums d = x - p and d^2 with p its own first value, so that its M2 = sum d^2 - (sum d)^2 / n never
 // cancels by more than a factor n (p is one of the n values), and thread results are joined by Chan's formula.  Means

@@ -1,4 +1,4 @@
-// Linear layer + softmax cross entropy over a large vocabulary, without the logits in memory.
+// Linear layer + softmax cross entropy over a large vocabulary, without the fp32 logits of all tokens in memory.
 //
 //   z = X W^T,  lse = log sum exp z,  loss = lse - z[label],  dz = g (exp(z - lse) - [label]),  dX = dz W,  dW = dz^T X
 //
@@ -8,8 +8,9 @@
 //
 //   forward  : logits product (statistics) -> rows
 //   training : per piece of the tokens: logits product (statistics + 16-bit codes) -> rows, codes to dz in place ->
-//              dX and dW products in one launch
+//              dX and dW products in one launch (fp32: fp32 logits -> three bf16 planes of dz)
 //   backward : per piece of the vocabulary: logits product (dz from lse) -> dX (fp32 sums over the pieces) and dW
+// A few output blocks or tokens: the logits as fp32 partial products of a split contraction (xent_softmax_kernel, hdqt_xent_few.cuh).
 #include <math.h>
 
 #include <atomic>
@@ -444,7 +445,8 @@ struct SmallLimits {
 // call) for bf16 gradients, 47 (51) for fp32, 16 (23) and 33 (35) for the loss alone.  Measured (tokens, features, classes; device, both):
 // bf16 gradients 32 x 128 x 64 10 and 20 us, 128 x 512 x 100 27 and 25, 128 x 512 x 300 41 and 27; fp32 gradients 128 x 512 x 100 29 and 47,
 // 256 x 512 x 128 44 and 51, 512 x 512 x 128 63 and 49; bf16 loss from W [classes, features] 64 x 512 x 512 14 and 16, from
-// [features, classes] 25 and 16; fp32 loss 512 x 512 x 128 26 and 33.
+// [features, classes] 25 and 16; fp32 loss 512 x 512 x 128 26 and 33.  The limits are set by whole calls; on the device alone the
+// bf16 loss could leave this path earlier (512 x 256 x 256 in a CUDA graph with a cold L2: 22 us here, 18 there).
 SmallLimits small_limits(bool gradients, bool f32, bool w_is_cd) {
   if (!gradients) return f32 || w_is_cd ? SmallLimits{512, 1 << 18, 1 << 25} : SmallLimits{512, 1 << 16, 1 << 25};
   return f32 ? SmallLimits{256, 1 << 18, 1 << 24} : SmallLimits{128, 1 << 16, 1 << 23};

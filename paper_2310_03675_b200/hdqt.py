@@ -750,8 +750,8 @@ def _loss_weight(g, reduction, T, device):
 def linear_xent_fwd(X, W, labels, ignore_index: int = -100, reduction: str = "mean", w_is_cd: bool = False,
                     dev_status=None):
     """Softmax cross entropy of X[tokens, features] times W ([features, classes], or [classes, features] with w_is_cd)
-    against int64 labels; the logits are never stored.  bf16 or fp32.  Returns (loss: scalar, or [tokens] with reduction
-    "none"; lse fp32 [tokens])."""
+    against int64 labels; the logits are not stored but for a few tokens or output blocks.  bf16 or fp32.  Returns (loss:
+    scalar, or [tokens] with reduction "none"; lse fp32 [tokens])."""
     X, W, labels, d, ws, nbytes = _xent_call(X, W, labels, ignore_index, reduction, w_is_cd, 0, XENT_FWD)
     lse = X.new_empty(d.tokens, dtype=torch.float32)
     loss = X.new_empty((d.tokens,) if reduction == "none" else (), dtype=torch.float32)
@@ -779,7 +779,8 @@ def linear_xent_bwd(X, W, labels, lse, g=None, ignore_index: int = -100, reducti
 def linear_xent_train(X, W, labels, g=None, ignore_index: int = -100, reduction: str = "mean", w_is_cd: bool = False,
                       want_dx: bool = True, want_dw: bool = True, piece_bytes: int = 0, dev_status=None):
     """Loss and gradients in one call (three quarters of the tensor work of linear_xent_fwd + linear_xent_bwd), for a loss whose
-    gradient is known beforehand: g as in linear_xent_bwd.  Returns (loss, lse, dX, dW)."""
+    gradient is known beforehand: g as in linear_xent_bwd.  The workspace holds 2 (fp32: 10) bytes per logit of a piece of the
+    tokens.  Returns (loss, lse, dX, dW)."""
     X, W, labels, d, ws, nbytes = _xent_call(X, W, labels, ignore_index, reduction, w_is_cd, piece_bytes, XENT_TRAIN)
     g = _loss_weight(g, reduction, d.tokens, X.device)
     lse = X.new_empty(d.tokens, dtype=torch.float32)

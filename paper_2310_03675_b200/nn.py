@@ -339,8 +339,9 @@ class LinearCrossEntropyFunction(torch.autograd.Function):
 def linear_cross_entropy(x, w, labels, bias=None, ignore_index: int = -100, reduction: str = "mean",
                          w_is_cd: bool = False, scale: float = 1.0):
     """scale * cross_entropy(x @ w + bias, labels) for x [tokens, features] and w [features, classes] (or [classes, features] with
-    w_is_cd), fp32 or bf16, without the logits in memory.  reduction: "mean" over the labels that are not ignore_index,
-    "sum", or "none".  A bias ([classes], of w's type) is one more feature whose input is 1 (x and w are copied for it).
+    w_is_cd), fp32 or bf16.  Where a reduced loss needs gradients the workspace holds a piece of the tokens' softmax, 2 bytes per logit
+    (fp32: 10); otherwise 8 bytes per 128 logits.  reduction: "mean" over the labels that are not ignore_index, "sum", or "none".
+    A bias ([classes], of w's type) is one more feature whose input is 1 (x and w are copied for it).
     scale: a factor known beforehand (one over the number of accumulated batches, the loss's weight): bf16 gradients are then
     rounded once, where multiplying the returned loss rounds them twice."""
     if bias is not None:
@@ -584,7 +585,7 @@ class ResNet18Width(torch.nn.Module):
         return (head.weight if n == head.weight.shape[1] else head.weight[:, :n].contiguous()), head.bias[:n]
 
     def loss(self, x, labels, n_seen: Optional[int] = None):
-        """Mean cross entropy with the head in fp32 (not quantized) and without its logits in memory."""
+        """Mean cross entropy with the head in fp32 (not quantized), as one operator."""
         w, b = self._head(n_seen)
         return linear_cross_entropy(self.features(x), w, labels, bias=b)
 
