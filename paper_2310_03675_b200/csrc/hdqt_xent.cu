@@ -30,15 +30,19 @@ constexpr int kRowThreads = 256;
 
 // label[t] = class, -1 (ignored) or -2 (outside [0, classes)); scale[0] = 1 / kept rows (mean) or 1: factor of the reduced
 // loss; scale[1] = scale[0] g (0 if no row is kept): factor of its gradients.  One block.
+// weights (with unit): a weight per row of the loss.  scale[1] is then their largest finite magnitude (1 if there is none) and
+// unit[t] = weights[t] / scale[1], so that equal weights reach dz as 1.
 __global__ void __launch_bounds__(1024)
 xent_labels_kernel(const int64_t* __restrict__ labels, int64_t tokens, int64_t classes, int64_t ignore, int32_t mean,
                    const float* __restrict__ g, int32_t* __restrict__ label, float* __restrict__ scale,
-                   int32_t* dev_status) {
+                   const float* __restrict__ weights, float* __restrict__ unit, int32_t* dev_status) {
   __shared__ int s_kept;
+  __shared__ uint32_t s_most;
   chain_wait();
-  if (threadIdx.x == 0) s_kept = 0;
+  if (threadIdx.x == 0) { s_kept = 0; s_most = 0u; }
   __syncthreads();
   int kept = 0;
+  uint32_t most = 0u;          // magnitudes order like their bit patterns
   bool bad = false;
 #pragma unroll 4
   for (int64_t t = threadIdx.x; t < tokens; t += blockDim.x) {
@@ -50,6 +54,20 @@ xent_labels_kernel(const int64_t* __restrict__ labels, int64_t tokens, int64_t c
       else { v = -2; bad = true; }
     }
     label[t] = v;
+    if (unit != nullptr && v >= 0) {
+      const uint32_t bits = __float_as_uint(weights[t]) & 0x7FFFFFFFu;
+      if (bits < 0x7F800000u) most = max(most, bits);
+    }
+  }
+  if (unit != nullptr) {
+    most = __reduce_max_sync(0xFFFFFFFFu, most);
+    if ((threadIdx.x & 31) == 0) atomicMax(&s_most, most);
+    __syncthreads();
+    const float s = s_most != 0u ? __uint_as_float(s_most) : 1.0f;
+    for (int64_t t = threadIdx.x; t < tokens; t += blockDim.x) unit[t] = weights[t] / s;
+    if (threadIdx.x == 0) { scale[0] = 1.0f; scale[1] = s; }
+    if (bad) report_status(dev_status, HDQT_ERR_INVALID_ARG);
+    return;
   }
   if (mean) {
     kept = __reduce_add_sync(0xFFFFFFFFu, kept);
@@ -429,8 +447,9 @@ struct Plan {
   int splits_z, splits_dx, splits_dw;   // splits_z > 1: few output blocks, logits as partial products (xent_softmax_kernel)
   int64_t ld_part;
   bool acc_dx, acc_dw;                  // fp32 sums over several pieces
+  bool unit_weights;                    // weights per row go into dz over their largest, which multiplies the fp32 sums
   // workspace offsets
-  size_t label, scale, label_logit, loss_rows, part, xs, ws, z, dz, dx_f32, dw_f32, total;
+  size_t label, scale, unit, label_logit, loss_rows, part, xs, ws, z, dz, dx_f32, dw_f32, total;
 };
 
 constexpr int64_t kPieceBytes = 1ll << 30;
@@ -514,6 +533,7 @@ hdqt_status_t make_plan(const hdqt_xent_desc_t* d, int kind, Plan* pl) {
     return HDQT_ERR_UNSUPPORTED;
   const bool f32 = d->dtype == HDQT_DTYPE_F32;
   pl->planes = f32 ? 3 : 1;
+  pl->unit_weights = false;             // (tensor-core path: set below)
   pl->small_rows = 0;
   const bool gradients = kind != HDQT_XENT_FWD, cd = d->w_is_cd != 0;
   const int64_t weights = d->classes * d->features;
@@ -629,6 +649,8 @@ hdqt_status_t make_plan(const hdqt_xent_desc_t* d, int kind, Plan* pl) {
   }
   pl->label = take(4 * T);
   pl->scale = take(256);
+  pl->unit_weights = !f32 && gradients && d->reduction == HDQT_REDUCE_NONE;
+  pl->unit = pl->unit_weights ? take(4 * T) : o;
   pl->label_logit = take(4 * T);
   pl->loss_rows = take(4 * T);
   pl->part = kind == HDQT_XENT_BWD ? o : take(8 * pl->rows_piece * pl->parts_ld);
@@ -761,12 +783,15 @@ void label_rows(Call* c, const int64_t* labels, const float* g) {
   const hdqt_xent_desc_t& d = *c->d;
   const Plan& pl = c->pl;
   // a weight per row goes into dz; one weight for all multiplies the fp32 sums of the gradient products, so that rounding dz
-  // to bf16 never rounds the weight (1 / rows would be off by the same 0.1 % in almost every element)
+  // to bf16 never rounds the weight (1 / rows would be off by the same 0.1 % in almost every element); of weights per row the
+  // largest does, so that equal ones are as good as one
   const bool rows = d.reduction == HDQT_REDUCE_NONE;
-  c->row_weights = rows ? g : nullptr;
-  c->alpha = rows ? nullptr : c->at<float>(pl.scale) + 1;
+  const bool unit = pl.unit_weights;
+  c->row_weights = unit ? c->at<float>(pl.unit) : rows ? g : nullptr;
+  c->alpha = rows && !unit ? nullptr : c->at<float>(pl.scale) + 1;
   c->run(xent_labels_kernel, 1, d.tokens > 512 ? 1024 : 256, 0, labels, d.tokens, d.classes, d.ignore_index,
-         d.reduction == HDQT_REDUCE_MEAN, rows ? nullptr : g, c->at<int32_t>(pl.label), c->at<float>(pl.scale), c->dev_status);
+         d.reduction == HDQT_REDUCE_MEAN, rows ? nullptr : g, c->at<int32_t>(pl.label), c->at<float>(pl.scale),
+         unit ? g : nullptr, unit ? c->at<float>(pl.unit) : nullptr, c->dev_status);
 }
 
 hdqt_status_t prepare(Call* c, const void* X, const void* W, const int64_t* labels, const float* g) {

@@ -129,3 +129,63 @@ def test_group_norm_of_images_without_pixels(shape):
     assert y.shape == x.shape and mean.shape == (shape[0], 2) and bool(torch.isnan(mean).all())
     dx, dgamma, dbeta = hdqt.group_norm_bwd(x, x, gamma, beta, mean, rstd, 2)
     assert dx.shape == x.shape and not dgamma.any() and not dbeta.any()
+
+
+def rounding_ratio(got, want):
+    """Error of a bf16 result against 64 bits, over what rounding the exact result leaves."""
+    want = want.double()
+    return float((got.double() - want).norm() / (want.bfloat16().double() - want).norm())
+
+
+def weighted_gradients(tokens, features, classes, weights, w_is_cd, seed):
+    """Error ratios of dX and dW, backward and one-call form, bf16 with a weight per row.  Beyond the final rounding there is dz's:
+    at the label p - 1 with p of 1 / classes, a bf16 number to that fraction of an ulp, elsewhere numbers of size p whose roundings
+    add up to 2^-8 / sqrt(classes) of the row.  For 3000 classes and more both together are below a tenth of the final
+    rounding's 2^-8 / sqrt(3) (1 / 2) at the worst, so the ratio is at most 1.1 if the weights themselves are not rounded."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn(tokens, features, generator=g, device="cuda").bfloat16()
+    w = (torch.randn(classes, features, generator=g, device="cuda") / math.sqrt(features)).bfloat16()
+    labels = torch.randint(0, classes, (tokens,), generator=g, device="cuda")
+    dz = torch.softmax(x.double() @ w.double().t(), 1)
+    dz[torch.arange(tokens, device="cuda"), labels] -= 1.0
+    dz *= weights.double()[:, None]
+    ww = w if w_is_cd else w.t().contiguous()
+    how = {"reduction": "none", "w_is_cd": w_is_cd}
+    loss, lse = hdqt.linear_xent_fwd(x, ww, labels, **how)
+    pairs = (hdqt.linear_xent_bwd(x, ww, labels, lse, weights, **how), hdqt.linear_xent_train(x, ww, labels, weights, **how)[2:])
+    return [r for dx, dw in pairs
+            for r in (rounding_ratio(dx, dz @ w.double()), rounding_ratio(dw if w_is_cd else dw.t(), dz.t() @ x.double()))]
+
+
+@pytest.mark.parametrize("w_is_cd", [False, True])
+@pytest.mark.parametrize("tokens,classes", [(600, 3000), (2000, 3001)])
+def test_equal_row_weights_lose_no_bits(tokens, classes, w_is_cd):
+    """What `reduction="none"` and a mean over its losses arrive as.  1 + 2^-8 - 2^-11 lies almost half way between two bf16 numbers."""
+    for value in (1 + 2.0 ** -8 - 2.0 ** -11, -(1 + 2.0 ** -8 - 2.0 ** -11) / tokens):
+        weights = torch.full((tokens,), value, device="cuda")
+        for ratio in weighted_gradients(tokens, 128, classes, weights, w_is_cd, seed=31):
+            assert ratio <= 1.1
+
+
+def test_row_weights_that_are_zero_or_not_finite():
+    g = torch.Generator(device="cuda").manual_seed(32)
+    x = torch.randn(600, 64, generator=g, device="cuda").bfloat16()
+    w = torch.randn(3000, 64, generator=g, device="cuda").bfloat16()
+    labels = torch.randint(0, 3000, (600,), generator=g, device="cuda")
+    labels[10] = -100
+    how = {"reduction": "none", "w_is_cd": True}
+    lse = hdqt.linear_xent_fwd(x, w, labels, **how)[1]
+    for call in (lambda a: hdqt.linear_xent_bwd(x, w, labels, lse, a, **how), lambda a: hdqt.linear_xent_train(x, w, labels, a, **how)[2:]):
+        dx, dw = call(torch.zeros(600, device="cuda"))
+        assert not dx.any() and not dw.any()
+        weights = torch.full((600,), 1e-38, device="cuda")          # the smallest normal numbers
+        dx, dw = call(weights)
+        one, _ = call(torch.ones(600, device="cuda"))
+        assert float((dx.double() * 1e38 - one.double()).norm() / one.double().norm()) < 2.0 ** -6
+        for bad in (math.inf, math.nan):
+            weights = torch.ones(600, device="cuda")
+            weights[7] = weights[10] = bad                           # (row 10 is ignored: its weight is not looked at)
+            dx, dw = call(weights)
+            finite = torch.isfinite(dx).all(1)
+            assert not bool(finite[7]) and bool(finite[:7].all()) and bool(finite[8:].all())
+            assert torch.equal(dx[finite], one[finite]) and not dx[10].any()
