@@ -473,8 +473,8 @@ size_t hdqt_group_norm_workspace_bytes(const hdqt_group_norm_desc_t* desc /*host
  * dX and dW in the layout of X and W; bf16 or fp32 (all four the same).  Products are formed on the tensor cores from bf16
  * operands with fp32 sums; an fp32 operand is split into three bf16 planes, which keeps fp32 precision (infinite inputs then
  * give NaN).  Small problems and a few tokens are computed in fp32 arithmetic on the CUDA cores instead.  For bf16, dz is
- * rounded to bf16 at most once before the gradient products (with its row's weight over the largest one in it; the largest,
- * or one weight for all, multiplies the fp32 sums); dX and dW are rounded once.
+ * rounded to bf16 at most once before the gradient products (one weight for all, or the largest weight of a row, multiplies
+ * the fp32 sums; a row's weight over the largest is in dz, up to 256 tokens in X with 16 bits); dX and dW are rounded once.
  * labels: int64 [tokens]; ignore_index rows have loss 0 and gradient 0.  A label outside [0, classes) makes its loss
  * NaN, its gradient 0, and sets HDQT_ERR_INVALID_ARG in *dev_status.
  * reduction: HDQT_REDUCE_NONE loss[tokens]; HDQT_REDUCE_MEAN one value, the mean over the rows that are not ignored (NaN

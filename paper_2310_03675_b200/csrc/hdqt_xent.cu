@@ -311,6 +311,27 @@ __global__ void __launch_bounds__(256) xent_stage_kernel(const T* __restrict__ s
   }
 }
 
+// bf16 X times the weights of its rows' losses in two planes (16 significant bits), and the weights themselves; a row without a
+// valid label weighs 0 whatever is given for it
+__global__ void __launch_bounds__(256)
+xent_weighted_rows_kernel(const __nv_bfloat16* __restrict__ x, int64_t ld, int64_t cols, const int32_t* __restrict__ label,
+                          const float* __restrict__ g, uint16_t* __restrict__ dst, int64_t ld_dst, int64_t plane,
+                          float* __restrict__ weight) {
+  chain_wait();
+  const int64_t r = blockIdx.y, c = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x);
+  const float w = label[r] >= 0 ? g[r] : 0.0f;
+  if (c == 0) weight[r] = w;
+  if (c >= cols) return;
+  float a[4], p0[4], p1[4], p2[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) a[j] = c + j < cols ? to_f32(x[r * ld + c + j]) : 0.0f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) split3(a[j] * w, p0[j], p1[j], p2[j]);
+  uint16_t* d = dst + r * ld_dst + c;
+  *reinterpret_cast<Vec<__nv_bfloat16, 4>*>(d) = pack<__nv_bfloat16>(p0);
+  *reinterpret_cast<Vec<__nv_bfloat16, 4>*>(d + plane) = pack<__nv_bfloat16>(p1);
+}
+
 // sum of the splits' partial outputs, in order; four elements of the flat [rows, cols] at a time
 template <typename T>
 __global__ void __launch_bounds__(256) xent_join_splits_kernel(const float* __restrict__ part, int splits, int64_t rows,
@@ -393,6 +414,8 @@ XProblem make_problem(const Product& g, int splits) {
   r.splits = (int32_t)ceil_div(r.kblocks, r.kblocks_split);
   r.a_mn = g.a_mn;
   r.b_mn = g.b_mn;
+  r.two = g.a.planes == 2 ? 1 : g.b.planes == 2 ? 2 : 0;
+  r.products = g.a.planes == 3 ? 6 : r.two ? 2 : 1;
   r.items = r.tiles_m * r.tiles_n * r.splits;
   return r;
 }
@@ -447,9 +470,10 @@ struct Plan {
   int splits_z, splits_dx, splits_dw;   // splits_z > 1: few output blocks, logits as partial products (xent_softmax_kernel)
   int64_t ld_part;
   bool acc_dx, acc_dw;                  // fp32 sums over several pieces
-  bool unit_weights;                    // weights per row go into dz over their largest, which multiplies the fp32 sums
+  // weights per row, bf16: in dX's epilogue and in two planes of X (few tokens), or in dz over their largest, which multiplies the sums
+  bool plane_weights, unit_weights;
   // workspace offsets
-  size_t label, scale, unit, label_logit, loss_rows, part, xs, ws, z, dz, dx_f32, dw_f32, total;
+  size_t label, scale, unit, xw, label_logit, loss_rows, part, xs, ws, z, dz, dx_f32, dw_f32, total;
 };
 
 constexpr int64_t kPieceBytes = 1ll << 30;
@@ -495,6 +519,10 @@ constexpr int kFewBlocks = 4 * kNumSMsHint;      // most blocks of the few-token
 
 // An item shorter than this many stages takes as long all the same: its epilogue (256 x 256 outputs) does.
 constexpr int64_t kEpilogueStages = 16;
+// So dW of a few tokens takes X in two planes at next to no cost: backward of 28 x 472 x 121432 bf16 154 us and 152 with the weights in
+// dz, 100 x 2048 x 32000 152 and 148, 300 x 1024 x 50000 160 and 156, but 512 x 2048 x 32000 221 and 190.  Random weights in dz
+// give 1.3 times the error of rounding the exact gradients from a few hundred tokens on, and 1.6 or 2 times with a few.
+constexpr int64_t kPlaneTokens = 4 * XK;
 int64_t item_cost(int64_t stages) { return stages > kEpilogueStages ? stages : kEpilogueStages; }
 
 // Work items along the contraction of a product of `blocks` output blocks of `kblocks` x `products` stages, next to `other` stages of
@@ -533,7 +561,7 @@ hdqt_status_t make_plan(const hdqt_xent_desc_t* d, int kind, Plan* pl) {
     return HDQT_ERR_UNSUPPORTED;
   const bool f32 = d->dtype == HDQT_DTYPE_F32;
   pl->planes = f32 ? 3 : 1;
-  pl->unit_weights = false;             // (tensor-core path: set below)
+  pl->plane_weights = pl->unit_weights = false;       // (tensor-core path: set below)
   pl->small_rows = 0;
   const bool gradients = kind != HDQT_XENT_FWD, cd = d->w_is_cd != 0;
   const int64_t weights = d->classes * d->features;
@@ -649,8 +677,11 @@ hdqt_status_t make_plan(const hdqt_xent_desc_t* d, int kind, Plan* pl) {
   }
   pl->label = take(4 * T);
   pl->scale = take(256);
-  pl->unit_weights = !f32 && gradients && d->reduction == HDQT_REDUCE_NONE;
-  pl->unit = pl->unit_weights ? take(4 * T) : o;
+  const bool row_weights = !f32 && gradients && d->reduction == HDQT_REDUCE_NONE;
+  pl->plane_weights = row_weights && T <= kPlaneTokens;
+  pl->unit_weights = row_weights && T > kPlaneTokens;
+  pl->unit = row_weights ? take(4 * T) : o;
+  pl->xw = pl->plane_weights ? take(2 * 2 * T * pl->ld_xs) : o;
   pl->label_logit = take(4 * T);
   pl->loss_rows = take(4 * T);
   pl->part = kind == HDQT_XENT_BWD ? o : take(8 * pl->rows_piece * pl->parts_ld);
@@ -687,6 +718,7 @@ struct Call {
   Operand x, w;          // as stored: x [tokens, features], w [w_rows, w_cols]
   const float* row_weights = nullptr;   // [tokens]: weights of the rows' losses
   const float* alpha = nullptr;         // or one weight for all, applied to the gradient products
+  const float* row_scale = nullptr;     // [tokens]: weights that dX's epilogue applies, dW's X being weighted X
 
   mutable bool started = false;
   mutable int dx_shares = 0;            // partial products of dX so far (backward call in pieces)
@@ -707,6 +739,11 @@ struct Call {
     o.base = reinterpret_cast<const uint16_t*>(x.base) + t0 * x.ld;
     o.outer = n;
     return o;
+  }
+  // X as dW reads it
+  Operand x_rows_dw(int64_t t0, int64_t n) const {
+    if (!pl.plane_weights) return x_rows(t0, n);
+    return Operand{at<uint16_t>(pl.xw) + t0 * pl.ld_xs, d->features, n, pl.ld_xs, d->tokens * pl.ld_xs, 2};
   }
   // the columns [v0, v0 + n) of the vocabulary
   Operand w_classes(int64_t v0, int64_t n) const {
@@ -787,7 +824,8 @@ void label_rows(Call* c, const int64_t* labels, const float* g) {
   // largest does, so that equal ones are as good as one
   const bool rows = d.reduction == HDQT_REDUCE_NONE;
   const bool unit = pl.unit_weights;
-  c->row_weights = unit ? c->at<float>(pl.unit) : rows ? g : nullptr;
+  c->row_weights = unit ? c->at<float>(pl.unit) : rows && !pl.plane_weights ? g : nullptr;
+  c->row_scale = pl.plane_weights ? c->at<float>(pl.unit) : nullptr;
   c->alpha = rows && !unit ? nullptr : c->at<float>(pl.scale) + 1;
   c->run(xent_labels_kernel, 1, d.tokens > 512 ? 1024 : 256, 0, labels, d.tokens, d.classes, d.ignore_index,
          d.reduction == HDQT_REDUCE_MEAN, rows ? nullptr : g, c->at<int32_t>(pl.label), c->at<float>(pl.scale),
@@ -804,6 +842,10 @@ hdqt_status_t prepare(Call* c, const void* X, const void* W, const int64_t* labe
   if (st == HDQT_OK && pl.stage_w) st = stage(*c, W, d.ld_w, pl.w_rows, pl.w_cols, pl.ws, pl.ld_ws, &c->w);
   if (st != HDQT_OK) return st;
   label_rows(c, labels, g);
+  if (pl.plane_weights && d.tokens > 0)
+    c->run(xent_weighted_rows_kernel, dim3((unsigned)ceil_div(d.features, 1024), (unsigned)d.tokens), 256, 0,
+           reinterpret_cast<const __nv_bfloat16*>(c->x.base), c->x.ld, d.features, c->at<int32_t>(pl.label), g,
+           c->at<uint16_t>(pl.xw), pl.ld_xs, d.tokens * pl.ld_xs, c->at<float>(pl.unit));
   const cudaError_t e = cudaGetLastError();
   return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "cross entropy labels");
 }
@@ -851,6 +893,7 @@ hdqt_status_t gradient_products(const Call& c, int64_t t0, int64_t nt, int64_t v
     g[n] = Product{dz, c.w_classes(v0, nv), false, d.w_is_cd != 0, nt, D, nv};
     const int splits = dW ? pl.splits_dx : pl.splits_dx_alone;
     p.pr[n] = make_problem(g[n], splits);
+    p.pr[n].row_scale = c.row_scale != nullptr ? c.row_scale + t0 : nullptr;
     if (splits > 1) {
       // (a last piece may be too short for two splits: its share is joined with the others all the same)
       XProblem& r = p.pr[n];
@@ -867,9 +910,9 @@ hdqt_status_t gradient_products(const Call& c, int64_t t0, int64_t nt, int64_t v
   if (dW) {
     // dW[v, d] = sum_t dz[t, v] X[t, d], or its transpose
     if (d.w_is_cd) {
-      g[n] = Product{dz, c.x_rows(t0, nt), true, true, nv, D, nt};
+      g[n] = Product{dz, c.x_rows_dw(t0, nt), true, true, nv, D, nt};
     } else {
-      g[n] = Product{c.x_rows(t0, nt), dz, true, true, D, nv, nt};
+      g[n] = Product{c.x_rows_dw(t0, nt), dz, true, true, D, nv, nt};
     }
     p.pr[n] = make_problem(g[n], pl.splits_dw);
     target(p.pr[n], dw_out, d.ld_dw, pl.acc_dw, c.at<float>(pl.dw_f32), d.w_is_cd ? D : nv);
@@ -884,12 +927,12 @@ hdqt_status_t gradient_products(const Call& c, int64_t t0, int64_t nt, int64_t v
   };
   const XProblem dw_problem = p.pr[n - 1];      // (if dW is asked for)
   if (n == 2) {
-    if (p.pr[1].kblocks_split > p.pr[0].kblocks_split) {      // the longer items first
+    auto length = [&](int i) { return (int64_t)p.pr[i].kblocks_split * p.pr[i].products; };
+    if (length(1) > length(0)) {      // the longer items first
       std::swap(p.pr[0], p.pr[1]);
       std::swap(g[0], g[1]);
     }
-    const int64_t products = pl.planes == 1 ? 1 : 6;
-    p.extra = (int32_t)(item_cost(p.pr[0].kblocks_split * products) / item_cost(p.pr[1].kblocks_split * products));
+    p.extra = (int32_t)(item_cost(length(0)) / item_cost(length(1)));
   }
   const hdqt_status_t st = launch<X_OUT>(p, g, n, c);
   if (st != HDQT_OK) return st;

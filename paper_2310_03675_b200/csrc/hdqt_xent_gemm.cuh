@@ -18,6 +18,8 @@
 // additions: a contraction is cut into parts of at most `part_iters` stages, whose sums the epilogue adds up in
 // registers with ordinary fp32 additions.
 //
+// One bf16 operand may come as two planes (X times the rows' weights, 16 significant bits): its product then takes two passes.
+//
 // Bound by the tensor pipe.  4096 x 2048 x 32000 bf16: logits with codes 351 us (1.53 PFLOP/s, pipe 86 % active), dX and dW in
 // one launch 693 us (1.55, 89 %).  2048 x 1024 x 32768 fp32, six products: logits 532 us (1.55, 86 %), dX and dW 1138 us (1.45,
 // 85 %).
@@ -70,8 +72,10 @@ struct XProblem {
   int64_t split_stride;            // elements between the partial outputs of two splits
   const float* add;                // fp32 sums of earlier pieces (may be out itself)
   int64_t ld_add;
+  const float* row_scale;          // [M]: the output row is this times the product (null: XParams::alpha)
   int32_t out_bf16;
-  int32_t pad;
+  int32_t products;                // plane pairs: 1, 6 (fp32) or 2 (one bf16 operand in two planes)
+  int32_t two;                     // which one: 1 = A, 2 = B
 };
 
 struct XParams {
@@ -155,10 +159,10 @@ __device__ __forceinline__ void split3(float x, float& p0, float& p1, float& p2)
   p2 = x - p0 - p1;
 }
 
-// planes of the s-th product of an fp32 contraction, smallest first: (0,2) (2,0) (1,1) (0,1) (1,0) (0,0)
-__device__ __forceinline__ void plane_pair(int planes, int s, int& a, int& b) {
-  a = planes == 1 ? 0 : (int)((0x118u >> (2 * s)) & 3u);
-  b = planes == 1 ? 0 : (int)((0x052u >> (2 * s)) & 3u);
+// planes of the s-th product, smallest first; of an fp32 contraction (0,2) (2,0) (1,1) (0,1) (1,0) (0,0)
+__device__ __forceinline__ void plane_pair(int planes, int two, int s, int& a, int& b) {
+  a = planes > 1 ? (int)((0x118u >> (2 * s)) & 3u) : two == 1 ? 1 - s : 0;
+  b = planes > 1 ? (int)((0x052u >> (2 * s)) & 3u) : two == 2 ? 1 - s : 0;
 }
 
 struct XItem {
@@ -268,8 +272,8 @@ __device__ __forceinline__ void x_stats(const XParams& p, const XProblem& r, con
 // dz but multiplies the fp32 sums (XParams::alpha); a row's largest value, p - 1 at its label, is then close to a bf16 number, and the
 // gradients are as exact as fp32 arithmetic rounded at the end (error against 64 bits 1.7e-3 both, at that size).  Of weights
 // per row the largest is treated like that and the rest, g / largest, multiplied in before the rounding: equal weights cost
-// nothing, random ones give 2.2e-3 against 1.7e-3 at 1531 x 1000 x 50257.  dX's epilogue could take them after the sum, but dW
-// needs them in an operand, where weighted X would be rounded in dz's place.
+// nothing, random ones give 2.2e-3 against 1.7e-3 at 1531 x 1000 x 50257.  Few tokens, whose roundings do not average, keep them
+// out of dz: dX's epilogue multiplies its rows by them, and dW's X is weighted X in two planes (hdqt_xent.cu, kPlaneTokens).
 __device__ __forceinline__ void x_dz(const XParams& p, const XProblem& r, int row, int col0, float (&acc)[128]) {
   const int ncols = r.N - col0;
   if (row >= r.M || ncols <= 0) return;
@@ -312,8 +316,8 @@ __device__ __forceinline__ void x_dz(const XParams& p, const XProblem& r, int ro
 __device__ __forceinline__ void x_out(const XParams& p, const XProblem& r, const XItem& t, int row, int col0, float (&acc)[128]) {
   const int ncols = r.N - col0;
   if (row >= r.M || ncols <= 0) return;
-  if (p.alpha != nullptr) {
-    const float alpha = *p.alpha;
+  if (p.alpha != nullptr || r.row_scale != nullptr) {
+    const float alpha = r.row_scale != nullptr ? r.row_scale[row] : *p.alpha;
 #pragma unroll
     for (int j = 0; j < 128; ++j) acc[j] *= alpha;
   }
@@ -383,8 +387,8 @@ __device__ __forceinline__ void x_out(const XParams& p, const XProblem& r, const
 // row; loss and gradients of 35 x 2604 x 44400 with rows of 4-byte starts: 262 us, and 504).
 __device__ __forceinline__ void x_out_odd(const XParams& p, const XProblem& r, const XItem& t, int row0, int col0, int lane,
                                           float* box, float (&acc)[128]) {
-  const float alpha = p.alpha != nullptr ? *p.alpha : 1.0f;
   const int rows = min(32, r.M - row0);
+  const float alpha = r.row_scale != nullptr ? (lane < rows ? r.row_scale[row0 + lane] : 0.0f) : p.alpha != nullptr ? *p.alpha : 1.0f;
   if (r.out_bf16 && r.add == nullptr && ((reinterpret_cast<uintptr_t>(r.out) | (uintptr_t)(r.ld_out * 2)) & 3) == 0 && (r.N & 1) == 0) {
     // rows start on 4 bytes: two neighbouring bf16 per lane, 64 columns at a time
     uint32_t* pair = reinterpret_cast<uint32_t*>(box);
@@ -439,7 +443,7 @@ __device__ __forceinline__ bool x_out_even(const XProblem& r) {
 // during which the item before has its epilogue (2048 x 1024 x 32768 fp32, loss and gradients: 1970 us, 2100 all in parts of 8).
 constexpr int kHeadStages = 1024;
 __device__ __forceinline__ int x_part(const XParams& p, int left, int nkb) {
-  return left > nkb ? min(left - nkb, kHeadStages) : min(left, p.part_iters);
+  return p.planes > 1 && left > nkb ? min(left - nkb, kHeadStages) : min(left, p.part_iters);
 }
 
 template <int kEpi>
@@ -465,7 +469,6 @@ xent_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_consta
   const uint32_t cta_rank = cluster_ctarank();
   const bool leader = (cta_rank == 0);
   const int pair_id = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
-  const int products = p.planes == 1 ? 1 : 6;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < X_STAGES; ++s) {
@@ -505,9 +508,9 @@ xent_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_consta
         const CUtensorMap* ma = t.q ? &map_a1 : &map_a0;
         const CUtensorMap* mb = t.q ? &map_b1 : &map_b0;
         const int a0 = t.m * XM + (int)cta_rank * 128, b0 = t.n * XN + (int)cta_rank * 128;
-        for (int s = 0; s < products && ok; ++s) {
+        for (int s = 0; s < r.products && ok; ++s) {
           int pa, pb;
-          plane_pair(p.planes, s, pa, pb);
+          plane_pair(p.planes, r.two, s, pa, pb);
           for (int kb = t.kb0; kb < t.kb0 + t.nkb; ++kb, ++it) {
             if (!mbar_try_wait(bar_empty + 8 * ps, pe_par) && !mbar_wait(bar_empty + 8 * ps, pe_par, abort_flag)) { ok = false; break; }
             if (leader) mbar_expect_tx(bar_full + 8 * ps, 2 * X_STAGE_BYTES);   // collects both CTAs' bytes
@@ -557,7 +560,7 @@ xent_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_consta
         const uint32_t ka = r.a_mn ? 2048 >> 4 : 32 >> 4, kb = r.b_mn ? 2048 >> 4 : 32 >> 4;   // per 16 k
         const uint32_t a0 = (uint32_t)da, a1 = a0 + ka, a2 = a1 + ka, a3 = a2 + ka;
         const uint32_t b0 = (uint32_t)db, b1 = b0 + kb, b2 = b1 + kb, b3 = b2 + kb;
-        int left = t.nkb * products;
+        int left = t.nkb * r.products;
         while (left > 0 && ok) {
           const int n = x_part(p, left, t.nkb);
           left -= n;
@@ -614,7 +617,7 @@ xent_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_consta
       const XProblem& r = p.pr[t.q];
       float acc[128];
       bool first = true;
-      int left = t.nkb * products;
+      int left = t.nkb * r.products;
       while (left > 0) {
         left -= x_part(p, left, t.nkb);
         const int buf = buf_i & 1;

@@ -189,3 +189,35 @@ def test_row_weights_that_are_zero_or_not_finite():
             finite = torch.isfinite(dx).all(1)
             assert not bool(finite[7]) and bool(finite[:7].all()) and bool(finite[8:].all())
             assert torch.equal(dx[finite], one[finite]) and not dx[10].any()
+
+
+@pytest.mark.parametrize("w_is_cd", [False, True])
+@pytest.mark.parametrize("tokens,classes", [(9, 9000), (28, 5001), (130, 3000), (256, 3001)])
+def test_row_weights_of_a_few_tokens_lose_no_bits(tokens, classes, w_is_cd):
+    """Few tokens do not average what rounding each one's weight leaves; all but one lie almost half way between bf16 numbers here."""
+    weights = torch.full((tokens,), 0.5 * (1 + 2.0 ** -8 - 2.0 ** -11), device="cuda")
+    weights[0] = 1.0
+    rand = torch.rand(tokens, generator=torch.Generator(device="cuda").manual_seed(33), device="cuda") - 0.5
+    for g in (weights, -3.0 * weights, rand):
+        for ratio in weighted_gradients(tokens, 256, classes, g, w_is_cd, seed=34):
+            assert ratio <= 1.1
+
+
+@pytest.mark.parametrize("w_is_cd", [False, True])
+def test_row_weights_of_a_few_tokens_in_pieces_and_at_odd_sizes(w_is_cd):
+    """Pieces of tokens (one-call form) and of classes (backward), rows that must be copied, ignored rows, non-finite weights of them."""
+    import test_gpu_xent as xe
+    for t, d, v in ((200, 100, 2003), (256, 67, 1025), (40, 1030, 3000), (257, 64, 20011)):
+        x, w, labels, weights = xe.data(t, d, v, "bf16", seed=t)
+        ww = w if w_is_cd else w.t().contiguous()
+        want = xe.reference(x, w, labels, weights, torch.bfloat16)
+        weights[labels == -100] = math.nan                          # not looked at
+        how = {"reduction": "none", "w_is_cd": w_is_cd}
+        lse = hdqt.linear_xent_fwd(x, ww, labels, **how)[1]
+        for piece in (0, 1, 1 << 20):
+            dx, dw = hdqt.linear_xent_bwd(x, ww, labels, lse, weights, piece_bytes=piece, **how)
+            dx2, dw2 = hdqt.linear_xent_train(x, ww, labels, weights, piece_bytes=piece, **how)[2:]
+            only_dx = hdqt.linear_xent_bwd(x, ww, labels, lse, weights, piece_bytes=piece, want_dw=False, **how)[0]
+            only_dw = hdqt.linear_xent_bwd(x, ww, labels, lse, weights, piece_bytes=piece, want_dx=False, **how)[1]
+            for got, name in ((dx, "dx"), (dx2, "dx"), (only_dx, "dx"), (dw, "dw"), (dw2, "dw"), (only_dw, "dw")):
+                xe.close(got if name == "dx" or w_is_cd else got.t(), want[name], name)
