@@ -464,6 +464,87 @@ hdqt_status_t hdqt_group_norm_bwd(const hdqt_group_norm_desc_t* desc /*host*/, c
 size_t hdqt_group_norm_workspace_bytes(const hdqt_group_norm_desc_t* desc /*host*/, int32_t backward);
 
 /*
+ * Layer norm with an activation over the channels of each row of x[rows, channels]:
+ *
+ *   mu, rs = mean and 1/sqrt(variance + eps) of a row,  z = gamma[c] * (x - mu) * rs + beta[c],  y = act(z)
+ *
+ * backward, dz = dy * act'(z) (ReLU's derivative at 0 is 0):
+ *   dgamma[c] = sum dz * xhat,  dbeta[c] = sum dz   over the rows, in a fixed order
+ *   dx = rs * (gamma dz - mean(gamma dz) - xhat * mean(gamma dz * xhat)),   means over the row
+ *
+ * Rows of x start x_row_stride elements apart, those of y, dy, dx y_row_stride (both >= channels; not looked at for a single
+ * row).  16-byte alignment of bases and strides and channels that are multiples of 8 (fp32: 4) select the widest accesses.
+ * gamma, beta (and dgamma, dbeta): [channels] of param_dtype, which is fp32 or x's type; NULL gamma/beta = ones/zeros.
+ * mean, rstd: fp32 [rows], written by the forward call and read by the backward call.  Outputs must not overlap inputs.
+ * rows may be 0: nothing but zero dgamma/dbeta is written then.  channels <= 2^20.
+ * backward: dx, dgamma, dbeta may be NULL (not needed); hdqt_layer_norm_workspace_bytes(desc) bytes, 256-byte aligned.
+ */
+typedef struct hdqt_layer_norm_desc {
+  int64_t rows, channels;
+  int64_t x_row_stride;       /* of x                                                                      */
+  int64_t r_row_stride;       /* of residual (hdqt_dropout_add_layer_norm_fwd only)                        */
+  int64_t y_row_stride;       /* of everything else of that shape                                          */
+  int32_t dtype, param_dtype; /* hdqt_dtype_t */
+  int32_t act;                /* hdqt_act_t   */
+  float eps;                  /* >= 0         */
+  /* dropout (hdqt_dropout_add_layer_norm_* only, see hdqt_dropout_add) */
+  double p;
+  uint64_t seed;
+  const uint32_t* philox_offset;
+  uint32_t tag, reserved /* 0 */;
+} hdqt_layer_norm_desc_t;
+
+hdqt_status_t hdqt_layer_norm_fwd(const hdqt_layer_norm_desc_t* desc /*host*/, const void* x, const void* gamma,
+                                  const void* beta, void* y, float* mean, float* rstd, void* stream);
+
+hdqt_status_t hdqt_layer_norm_bwd(const hdqt_layer_norm_desc_t* desc /*host*/, const void* dy, const void* x,
+                                  const void* gamma, const void* beta, const float* mean, const float* rstd, void* dx,
+                                  void* dgamma, void* dbeta, void* workspace, size_t workspace_bytes, void* stream);
+
+size_t hdqt_layer_norm_workspace_bytes(const hdqt_layer_norm_desc_t* desc /*host*/);
+
+/*
+ * Dropout, added to a residual (NULL = none):
+ *
+ *   y = residual + (u[i] >= T ? x * scale : 0),   T = rint(65536 p),   scale = 65536 / (65536 - T)  (0 for T = 65536)
+ *
+ * u[i]: 16 bits of the library's Philox4x32-10 stream, as the quantizer's stochastic rounding draws them: key = seed, counter =
+ * (g lo, g hi, tag, *philox_offset or 0), g = i / 8, i = row * cols + col whatever the strides; element i % 8 takes the low (even)
+ * or high (odd) half of word (i % 8) / 2.  The mask is never stored: the gradient of x is the same call on dy without a
+ * residual (with the same seed, tag, offset word and sizes), that of the residual is dy.  scale is exact for the probability T / 65536 that
+ * is used (p below 2^-17 drops nothing).  A dropped element is 0 whatever x holds, NaN included.
+ * One fp32 multiplication, one fp32 addition, one rounding to the type.  Row strides as in the layer norm; y must not overlap
+ * x or residual.  Dense tensors (or cols and strides that are multiples of 8) with 16-byte aligned bases select 16-byte accesses.
+ */
+typedef struct hdqt_dropout_desc {
+  int64_t rows, cols;
+  int64_t x_row_stride, r_row_stride, y_row_stride;
+  double p;        /* 0..1 */
+  uint64_t seed;
+  const uint32_t* philox_offset; /* device, NULL = 0: advanced once per replay of a recorded call */
+  uint32_t tag;
+  int32_t dtype;   /* hdqt_dtype_t */
+} hdqt_dropout_desc_t;
+
+hdqt_status_t hdqt_dropout_add(const hdqt_dropout_desc_t* desc /*host*/, const void* x, const void* residual, void* y,
+                               void* stream);
+
+/*
+ * Both on the residual stream in one pass: h = residual + dropout(x), rounded to the type, and y = act(layer norm(h)); formulas,
+ * random numbers and limits as above (residual may be NULL).  The result is that of hdqt_dropout_add followed by
+ * hdqt_layer_norm_fwd on h.  Backward, from h, g = dh + (gradient of the layer norm's input) with dh (NULL = none) the gradient that
+ * arrives for h itself:  dresidual = g,  dx = (u >= T ? g * scale : 0), both rounded once.  dx, dresidual, dgamma, dbeta may be NULL.
+ */
+hdqt_status_t hdqt_dropout_add_layer_norm_fwd(const hdqt_layer_norm_desc_t* desc /*host*/, const void* x,
+                                              const void* residual, const void* gamma, const void* beta, void* h, void* y,
+                                              float* mean, float* rstd, void* stream);
+
+hdqt_status_t hdqt_dropout_add_layer_norm_bwd(const hdqt_layer_norm_desc_t* desc /*host*/, const void* dy, const void* dh,
+                                              const void* h, const void* gamma, const void* beta, const float* mean,
+                                              const float* rstd, void* dx, void* dresidual, void* dgamma, void* dbeta,
+                                              void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Linear layer + softmax cross entropy over a large vocabulary, without the fp32 logits of all tokens in memory.
  *
  *   z[t, v] = sum_d X[t, d] W[v, d],   lse[t] = log sum_v exp z[t, v],   loss[t] = lse[t] - z[t, label[t]]

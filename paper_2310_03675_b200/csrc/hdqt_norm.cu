@@ -59,37 +59,6 @@ struct NormParams {
 __device__ __forceinline__ float gamma_of(const NormParams& p, int c) { return p.gamma ? load_param(p.gamma, p.param_dtype, c) : 1.0f; }
 __device__ __forceinline__ float beta_of(const NormParams& p, int c) { return p.beta ? load_param(p.beta, p.param_dtype, c) : 0.0f; }
 
-// 1 / (1 + exp(-z)); exp overflows to infinity for z < -88, where the reciprocal is the correct 0
-__device__ __forceinline__ float sigmoid(float z) { return rcp(1.0f + ex2(z * -kLog2e)); }
-
-template <int kAct>
-__device__ __forceinline__ float act_fwd(float z) {
-  if constexpr (kAct == HDQT_ACT_RELU) {      // (a NaN stays)
-    float r;
-    asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(z));
-    return r;
-  }
-  if constexpr (kAct == HDQT_ACT_SILU) return z * sigmoid(z);
-  return z;
-}
-// dy * act'(z)
-template <int kAct>
-__device__ __forceinline__ float act_bwd(float dy, float z) {
-  if constexpr (kAct == HDQT_ACT_RELU) return z > 0.0f ? dy : 0.0f;
-  if constexpr (kAct == HDQT_ACT_SILU) {
-    const float s = sigmoid(z);
-    return dy * fmaf(s * (1.0f - s), z, s);
-  }
-  return dy;
-}
-// f<activation>() for the call's activation: the loops inside know it at compile time
-template <typename F>
-__device__ __forceinline__ void with_act(int act, F&& f) {
-  if (act == HDQT_ACT_SILU) f.template operator()<HDQT_ACT_SILU>();
-  else if (act == HDQT_ACT_RELU) f.template operator()<HDQT_ACT_RELU>();
-  else f.template operator()<HDQT_ACT_NONE>();
-}
-
 // Walks i = first, first + step, ... < end in batches whose loads are all issued before the first of them is used:
 // what keeps HBM busy is the number of bytes in flight.
 template <int U, typename L, typename F>
@@ -804,13 +773,6 @@ struct Plan {
   int chunks, chunk_pixels;
 };
 
-// widest access (16 bytes, or down to one element) that `align` (bases and strides in bytes, or-ed together) allows
-int vector_width(int64_t channels, int elem, uintptr_t align) {
-  int v = 16 / elem;
-  while (v > 1 && (channels % v != 0 || (align & (uintptr_t)(v * elem - 1)) != 0)) v >>= 1;
-  return v;
-}
-
 Plan make_plan(const hdqt_group_norm_desc_t& d, int vec) {
   Plan pl;
   pl.vec = vec;
@@ -847,25 +809,6 @@ hdqt_status_t check_desc(const hdqt_group_norm_desc_t* d) {
   return HDQT_OK;
 }
 
-template <typename F>
-hdqt_status_t with_type_and_width(int dtype, int vec, F&& f) {
-  if (dtype == HDQT_DTYPE_F32) {
-    if (vec == 4) return f.template operator()<float, 4>();
-    if (vec == 2) return f.template operator()<float, 2>();
-    return f.template operator()<float, 1>();
-  }
-  if (dtype == HDQT_DTYPE_BF16) {
-    if (vec == 8) return f.template operator()<__nv_bfloat16, 8>();
-    if (vec == 4) return f.template operator()<__nv_bfloat16, 4>();
-    if (vec == 2) return f.template operator()<__nv_bfloat16, 2>();
-    return f.template operator()<__nv_bfloat16, 1>();
-  }
-  if (vec == 8) return f.template operator()<__half, 8>();
-  if (vec == 4) return f.template operator()<__half, 4>();
-  if (vec == 2) return f.template operator()<__half, 2>();
-  return f.template operator()<__half, 1>();
-}
-
 NormParams make_params(const hdqt_group_norm_desc_t& d, const Plan& pl) {
   NormParams p{};
   p.param_dtype = d.param_dtype;
@@ -890,8 +833,6 @@ dim3 stream_grid(const hdqt_group_norm_desc_t& d, const Plan& pl) {
   const int64_t ncol = d.channels / pl.vec;
   return dim3((unsigned)pl.chunks, (unsigned)((ncol + kCols - 1) / kCols), (unsigned)(d.batch < 65535 ? d.batch : 65535));
 }
-
-size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 uintptr_t stride_bits(const hdqt_group_norm_desc_t& d) {
   const int e = dtype_size(d.dtype);
@@ -981,12 +922,14 @@ void set_division(NormParams* p, const hdqt_group_norm_desc_t& d, const Division
   while ((1 << p->cluster_shift) < dv.cluster) ++p->cluster_shift;
 }
 
-hdqt_status_t last_error(const char* what) {
-  const cudaError_t e = cudaGetLastError();
-  return e == cudaSuccess ? HDQT_OK : cuda_failure(e, what);
-}
-
 }  // namespace
+
+void launch_param_grad(const float2* part, int64_t parts, int channels, void* dgamma, void* dbeta, int32_t param_dtype, bool chained,
+                       cudaStream_t s) {
+  const unsigned blocks = (unsigned)((channels + kGradChannels - 1) / kGradChannels);
+  if (chained) launch_chained(norm_param_grad_kernel, blocks, NT, 0, s, part, parts, channels, dgamma, dbeta, param_dtype);
+  else norm_param_grad_kernel<<<blocks, NT, 0, s>>>(part, parts, channels, dgamma, dbeta, param_dtype);
+}
 
 }  // namespace hdqt
 
@@ -1063,10 +1006,9 @@ extern "C" hdqt_status_t hdqt_group_norm_bwd(const hdqt_group_norm_desc_t* d, co
     return HDQT_ERR_ALIGNMENT;
   if (workspace_bytes < hdqt_group_norm_workspace_bytes(d, 1)) return HDQT_ERR_WORKSPACE;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  const unsigned param_blocks = (unsigned)((d->channels + kGradChannels - 1) / kGradChannels);
   float2* chan = reinterpret_cast<float2*>(workspace);
   if (empty) {
-    if (dgamma || dbeta) norm_param_grad_kernel<<<param_blocks, NT, 0, s>>>(chan, 0, (int)d->channels, dgamma, dbeta, d->param_dtype);
+    if (dgamma || dbeta) launch_param_grad(chan, 0, (int)d->channels, dgamma, dbeta, d->param_dtype, false, s);
     return last_error("group norm gradient");
   }
   const int vec = vector_width(d->channels, elem, bases | stride_bits(*d));
@@ -1089,9 +1031,7 @@ extern "C" hdqt_status_t hdqt_group_norm_bwd(const hdqt_group_norm_desc_t* d, co
       const hdqt_status_t e = p.per_group % V == 0 ? launch_cluster<norm_bwd_cluster_kernel<T, V, true>>(p, dv, d->batch, s)
                                                    : launch_cluster<norm_bwd_cluster_kernel<T, V, false>>(p, dv, d->batch, s);
       if (e != HDQT_OK) return e;
-      if (dgamma || dbeta)
-        launch_chained(norm_param_grad_kernel, param_blocks, NT, 0, s, chan, d->batch * dv.cluster, (int)d->channels, dgamma, dbeta,
-                       d->param_dtype);
+      if (dgamma || dbeta) launch_param_grad(chan, d->batch * dv.cluster, (int)d->channels, dgamma, dbeta, d->param_dtype, true, s);
       return last_error("group norm gradient");
     });
   }
@@ -1102,9 +1042,7 @@ extern "C" hdqt_status_t hdqt_group_norm_bwd(const hdqt_group_norm_desc_t* d, co
       launch_chained(norm_join_sums_kernel, (unsigned)(d->batch * d->groups), NT, 0, s, p);
       launch_chained(norm_bwd_apply_kernel<T, V>, grid, NT, 0, s, p);
     }
-    if (dgamma || dbeta)
-      launch_chained(norm_param_grad_kernel, param_blocks, NT, 0, s, chan, d->batch * pl.chunks, (int)d->channels, dgamma, dbeta,
-                     d->param_dtype);
+    if (dgamma || dbeta) launch_param_grad(chan, d->batch * pl.chunks, (int)d->channels, dgamma, dbeta, d->param_dtype, true, s);
     return last_error("group norm gradient");
   });
 }

@@ -120,8 +120,80 @@ inline void launch_chained(void (*kernel)(P...), dim3 grid, dim3 block, size_t s
   (void)cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);      // (a failure is left for cudaGetLastError)
 }
 
+// ---- activations of the normalisation kernels ----
+
+// 1 / (1 + exp(-z)); exp overflows to infinity for z < -88, where the reciprocal is the correct 0
+__device__ __forceinline__ float sigmoid(float z) { return rcp(1.0f + ex2(z * -kLog2e)); }
+
+template <int kAct>
+__device__ __forceinline__ float act_fwd(float z) {
+  if constexpr (kAct == HDQT_ACT_RELU) {      // (a NaN stays)
+    float r;
+    asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(z));
+    return r;
+  }
+  if constexpr (kAct == HDQT_ACT_SILU) return z * sigmoid(z);
+  return z;
+}
+// dy * act'(z)
+template <int kAct>
+__device__ __forceinline__ float act_bwd(float dy, float z) {
+  if constexpr (kAct == HDQT_ACT_RELU) return z > 0.0f ? dy : 0.0f;
+  if constexpr (kAct == HDQT_ACT_SILU) {
+    const float s = sigmoid(z);
+    return dy * fmaf(s * (1.0f - s), z, s);
+  }
+  return dy;
+}
+// f<activation>() for the call's activation: the loops inside know it at compile time
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F&& f) {
+  if (act == HDQT_ACT_SILU) f.template operator()<HDQT_ACT_SILU>();
+  else if (act == HDQT_ACT_RELU) f.template operator()<HDQT_ACT_RELU>();
+  else f.template operator()<HDQT_ACT_NONE>();
+}
+
+// ---- host side ----
+
 inline int dtype_size(int64_t dtype) {   // 0 = unknown type
   return dtype == HDQT_DTYPE_F32 ? 4 : (dtype == HDQT_DTYPE_BF16 || dtype == HDQT_DTYPE_F16) ? 2 : 0;
 }
+
+// widest access (16 bytes, or down to one element) that `align` (bases and strides in bytes, or-ed together) allows
+inline int vector_width(int64_t channels, int elem, uintptr_t align) {
+  int v = 16 / elem;
+  while (v > 1 && (channels % v != 0 || (align & (uintptr_t)(v * elem - 1)) != 0)) v >>= 1;
+  return v;
+}
+
+template <typename F>
+hdqt_status_t with_type_and_width(int dtype, int vec, F&& f) {
+  if (dtype == HDQT_DTYPE_F32) {
+    if (vec == 4) return f.template operator()<float, 4>();
+    if (vec == 2) return f.template operator()<float, 2>();
+    return f.template operator()<float, 1>();
+  }
+  if (dtype == HDQT_DTYPE_BF16) {
+    if (vec == 8) return f.template operator()<__nv_bfloat16, 8>();
+    if (vec == 4) return f.template operator()<__nv_bfloat16, 4>();
+    if (vec == 2) return f.template operator()<__nv_bfloat16, 2>();
+    return f.template operator()<__nv_bfloat16, 1>();
+  }
+  if (vec == 8) return f.template operator()<__half, 8>();
+  if (vec == 4) return f.template operator()<__half, 4>();
+  if (vec == 2) return f.template operator()<__half, 2>();
+  return f.template operator()<__half, 1>();
+}
+
+inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+
+inline hdqt_status_t last_error(const char* what) {
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? HDQT_OK : cuda_failure(e, what);
+}
+
+// dgamma (y) and dbeta (x): sums of the parts [parts, channels] of a backward pass, in a fixed order; NULL = not needed
+void launch_param_grad(const float2* part, int64_t parts, int channels, void* dgamma, void* dbeta, int32_t param_dtype, bool chained,
+                       cudaStream_t s);
 
 }  // namespace hdqt

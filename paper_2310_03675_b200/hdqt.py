@@ -39,6 +39,8 @@ EXPORTED = [
     "hdqt_selftest_bounded_wait", "hdqt_conv2d_fwd", "hdqt_conv2d_wgrad", "hdqt_selftest_mma_rate",
     "hdqt_grad_norm", "hdqt_clip_grad_norm", "hdqt_grad_norm_workspace_bytes", "hdqt_scale_tensors",
     "hdqt_group_norm_fwd", "hdqt_group_norm_bwd", "hdqt_group_norm_workspace_bytes",
+    "hdqt_layer_norm_fwd", "hdqt_layer_norm_bwd", "hdqt_layer_norm_workspace_bytes", "hdqt_dropout_add",
+    "hdqt_dropout_add_layer_norm_fwd", "hdqt_dropout_add_layer_norm_bwd",
     "hdqt_linear_xent_fwd", "hdqt_linear_xent_bwd", "hdqt_linear_xent_train", "hdqt_linear_xent_workspace_bytes",
 ]
 
@@ -68,6 +70,21 @@ class GroupNormDesc(C.Structure):
     _fields_ = [(n, C.c_int64) for n in ("batch", "pixels", "channels", "groups", "x_batch_stride", "x_pixel_stride",
                                          "y_batch_stride", "y_pixel_stride")] + \
                [("dtype", C.c_int32), ("param_dtype", C.c_int32), ("act", C.c_int32), ("eps", C.c_float)]
+
+
+class LayerNormDesc(C.Structure):
+    """Mirror of hdqt_layer_norm_desc_t."""
+    _fields_ = [(n, C.c_int64) for n in ("rows", "channels", "x_row_stride", "r_row_stride", "y_row_stride")] + \
+               [("dtype", C.c_int32), ("param_dtype", C.c_int32), ("act", C.c_int32), ("eps", C.c_float),
+                ("p", C.c_double), ("seed", C.c_uint64), ("philox_offset", C.c_void_p), ("tag", C.c_uint32),
+                ("reserved", C.c_uint32)]
+
+
+class DropoutDesc(C.Structure):
+    """Mirror of hdqt_dropout_desc_t."""
+    _fields_ = [(n, C.c_int64) for n in ("rows", "cols", "x_row_stride", "r_row_stride", "y_row_stride")] + \
+               [("p", C.c_double), ("seed", C.c_uint64), ("philox_offset", C.c_void_p), ("tag", C.c_uint32),
+                ("dtype", C.c_int32)]
 
 
 class XentDesc(C.Structure):
@@ -135,6 +152,17 @@ def _load() -> C.CDLL:
     lib.hdqt_group_norm_bwd.argtypes = [C.POINTER(GroupNormDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.hdqt_group_norm_workspace_bytes.argtypes = [C.POINTER(GroupNormDesc), i32]
     lib.hdqt_group_norm_workspace_bytes.restype = sz
+    lib.hdqt_layer_norm_fwd.argtypes = [C.POINTER(LayerNormDesc), vp, vp, vp, vp, vp, vp, vp]
+    lib.hdqt_layer_norm_bwd.argtypes = [C.POINTER(LayerNormDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.hdqt_layer_norm_workspace_bytes.argtypes = [C.POINTER(LayerNormDesc)]
+    lib.hdqt_layer_norm_workspace_bytes.restype = sz
+    lib.hdqt_dropout_add.argtypes = [C.POINTER(DropoutDesc), vp, vp, vp, vp]
+    lib.hdqt_dropout_add_layer_norm_fwd.argtypes = [C.POINTER(LayerNormDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.hdqt_dropout_add_layer_norm_bwd.argtypes = [C.POINTER(LayerNormDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp,
+                                                    vp, sz, vp]
+    for name in ("hdqt_layer_norm_fwd", "hdqt_layer_norm_bwd", "hdqt_dropout_add", "hdqt_dropout_add_layer_norm_fwd",
+                 "hdqt_dropout_add_layer_norm_bwd"):
+        getattr(lib, name).restype = C.c_int
     lib.hdqt_linear_xent_fwd.argtypes = [C.POINTER(XentDesc), vp, vp, vp, vp, vp, vp, sz, vp, vp]
     lib.hdqt_linear_xent_bwd.argtypes = [C.POINTER(XentDesc), vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp]
     lib.hdqt_linear_xent_train.argtypes = [C.POINTER(XentDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp]
@@ -685,6 +713,208 @@ def group_norm_bwd(dy, x, gamma, beta, mean, rstd, groups: int, act: str = "none
     _call("hdqt_group_norm_bwd", x, C.byref(d), dy.data_ptr(), x.data_ptr(), _ptr(gamma), _ptr(beta), mean.data_ptr(),
           rstd.data_ptr(), _ptr(dx), _ptr(dgamma), _ptr(dbeta), ws.data_ptr(), nbytes)
     return dx, dgamma, dbeta
+
+
+# ---- layer norm, dropout, and both on the residual stream ---------------------------------------------
+
+def _row_stride(t: torch.Tensor, name: str):
+    """Elements between the rows of a [..., channels] tensor whose outer dimensions step evenly (the width itself for one row)."""
+    shape, st = t.shape, t.stride()
+    if not shape:
+        raise ValueError(f"{name} must have at least one dimension")
+    if st[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"{name} must have its last dimension contiguous")
+    row, step = None, 0
+    for size, stride in zip(shape[-2::-1], st[-2::-1]):
+        if size == 0:
+            return shape[-1]
+        if size == 1:
+            continue
+        if row is None:
+            row = stride
+            if row < shape[-1]:
+                raise ValueError(f"the rows of {name} must not overlap")
+        elif stride != step:
+            raise ValueError(f"the rows of {name} must be evenly spaced")
+        step = stride * size
+    return shape[-1] if row is None else row
+
+
+def _row_count(shape) -> int:
+    rows = 1
+    for n in shape[:-1]:
+        rows *= n
+    return rows
+
+
+def _row_operand(t, x, name):
+    """Raises unless t has x's shape, type and device."""
+    if t.shape != x.shape or t.dtype != x.dtype or t.device != x.device:
+        raise ValueError(f"{name} must have x's shape, type and device")
+
+
+def _dropout_args(p, seed, tag, philox_offset, device):
+    p = float(p)
+    if not 0.0 <= p <= 1.0:
+        raise ValueError("p must be a probability")
+    if not 0 <= seed < 1 << 64 or not 0 <= tag < 1 << 32:
+        raise ValueError("seed must fit 64 bits and tag 32 bits, both unsigned")
+    if philox_offset is None:
+        return p, None
+    if philox_offset.dtype != torch.int32 or philox_offset.numel() < 1 or philox_offset.device != device:
+        raise ValueError("philox_offset must be an int32 tensor on x's device")
+    return p, philox_offset.data_ptr()
+
+
+def _layer_norm_desc(x, gamma, beta, eps, act):
+    code = DTYPE_CODES.get(x.dtype)
+    if code is None or not x.is_cuda:
+        raise ValueError("expected an fp32, bf16 or fp16 CUDA tensor")
+    if act not in ACT_CODES:
+        raise ValueError(f"act must be one of {sorted(ACT_CODES)}")
+    stride = _row_stride(x, "x")
+    channels = x.shape[-1]
+    if channels == 0:
+        raise ValueError("x must have at least one channel")
+    pdt = x.dtype
+    for t in (gamma, beta):
+        if t is None:
+            continue
+        if t.shape != (channels,) or not t.is_contiguous():
+            raise ValueError("gamma and beta must be dense [channels] tensors")
+        pdt = t.dtype
+    if gamma is not None and beta is not None and gamma.dtype != beta.dtype:
+        raise ValueError("gamma and beta must have one type")
+    if pdt not in (torch.float32, x.dtype):
+        raise ValueError("gamma and beta must be fp32 or of x's type")
+    rows = _row_count(x.shape)
+    d = LayerNormDesc(rows, channels, stride, channels, channels, code, DTYPE_CODES[pdt], ACT_CODES[act], eps, 0.0, 0, None, 0, 0)
+    return d, max(256, lib.hdqt_layer_norm_workspace_bytes(C.byref(d))), x.shape[:-1]
+
+
+_LAYER_NORM_PLANS = {}     # descriptor, workspace size and shape of the statistics by shapes, strides and types
+
+
+def _layer_norm_plan(x, gamma, beta, eps, act):
+    key = (x.shape, x.stride(), x.dtype, x.is_cuda, eps, act,
+           None if gamma is None else (gamma.shape, gamma.dtype, gamma.is_contiguous()),
+           None if beta is None else (beta.shape, beta.dtype, beta.is_contiguous()))
+    plan = _LAYER_NORM_PLANS.get(key)
+    if plan is None:
+        if len(_LAYER_NORM_PLANS) >= 1024:
+            _LAYER_NORM_PLANS.clear()
+        plan = _LAYER_NORM_PLANS[key] = _layer_norm_desc(x, gamma, beta, eps, act)
+    dev = x.device
+    if (gamma is not None and gamma.device != dev) or (beta is not None and beta.device != dev):
+        raise ValueError("gamma and beta must be on x's device")
+    return plan
+
+
+def _check_stats(mean, rstd, shape, device):
+    if mean.shape != shape or rstd.shape != shape or mean.dtype != torch.float32 or rstd.dtype != torch.float32 \
+            or not (mean.is_contiguous() and rstd.is_contiguous()) or mean.device != device or rstd.device != device:
+        raise ValueError("mean and rstd must be the dense fp32 tensors of the forward call")
+
+
+def layer_norm_fwd(x, gamma, beta, eps: float = 1e-5, act: str = "none"):
+    """act(layer norm) over the last dimension of x[..., channels] (evenly spaced rows: a slice of the channels is fine).
+    gamma, beta: [channels], fp32 or x's type, or None.  act: "none", "relu" or "silu".
+    Returns (y dense, mean fp32 [...], rstd fp32 [...])."""
+    d, _, shape = _layer_norm_plan(x, gamma, beta, eps, act)
+    y = torch.empty_like(x, memory_format=torch.contiguous_format)
+    mean, rstd = x.new_empty(shape, dtype=torch.float32), x.new_empty(shape, dtype=torch.float32)
+    _call("hdqt_layer_norm_fwd", x, C.byref(d), x.data_ptr(), _ptr(gamma), _ptr(beta), y.data_ptr(), mean.data_ptr(),
+          rstd.data_ptr())
+    return y, mean, rstd
+
+
+def layer_norm_bwd(dy, x, gamma, beta, mean, rstd, act: str = "none", want_dx: bool = True, want_params: bool = True):
+    """Gradients of layer_norm_fwd: (dx dense or None, dgamma or None, dbeta or None)."""
+    d, nbytes, shape = _layer_norm_plan(x, gamma, beta, 0.0, act)
+    _row_operand(dy, x, "dy")
+    _check_stats(mean, rstd, shape, x.device)
+    if not dy.is_contiguous():
+        dy = dy.contiguous()
+    dx = torch.empty_like(x, memory_format=torch.contiguous_format) if want_dx else None
+    dgamma = torch.empty_like(gamma) if want_params and gamma is not None else None
+    dbeta = torch.empty_like(beta) if want_params and beta is not None else None
+    ws = x.new_empty(nbytes, dtype=torch.uint8)
+    _call("hdqt_layer_norm_bwd", x, C.byref(d), dy.data_ptr(), x.data_ptr(), _ptr(gamma), _ptr(beta), mean.data_ptr(),
+          rstd.data_ptr(), _ptr(dx), _ptr(dgamma), _ptr(dbeta), ws.data_ptr(), nbytes)
+    return dx, dgamma, dbeta
+
+
+def dropout(x, p: float, seed: int, tag: int = 0, residual=None, philox_offset=None):
+    """residual + dropout(x) (residual None: dropout alone) of x[..., cols], evenly spaced rows, as a dense tensor.  The random
+    numbers are those of (seed, tag, the int32 device word philox_offset or 0) and an element's position in the dense tensor, so
+    that the gradient of x is dropout(dy, p, seed, tag, philox_offset=...); no mask is stored.  Kept elements are divided by the
+    probability 1 - rint(65536 p) / 65536 that is used."""
+    code = DTYPE_CODES.get(x.dtype)
+    if code is None or not x.is_cuda:
+        raise ValueError("expected an fp32, bf16 or fp16 CUDA tensor")
+    p, offset = _dropout_args(p, seed, tag, philox_offset, x.device)
+    shape = x.shape
+    if residual is not None:
+        _row_operand(residual, x, "residual")
+    if x.is_contiguous() and (residual is None or residual.is_contiguous()):
+        n = x.numel()
+        d = DropoutDesc(1, n, n, n, n, p, seed, offset, tag, code)
+    else:
+        cols = shape[-1] if shape else 1
+        d = DropoutDesc(_row_count(shape), cols, _row_stride(x, "x"),
+                        cols if residual is None else _row_stride(residual, "residual"), cols, p, seed, offset, tag, code)
+    y = torch.empty_like(x, memory_format=torch.contiguous_format)
+    _call("hdqt_dropout_add", x, C.byref(d), x.data_ptr(), _ptr(residual), y.data_ptr())
+    return y
+
+
+def dropout_add_layer_norm_fwd(x, residual, gamma, beta, p: float, seed: int, tag: int = 0, eps: float = 1e-5,
+                               act: str = "none", philox_offset=None):
+    """h = residual + dropout(x) (residual may be None) and y = act(layer norm(h)) in one pass over the rows; arguments as in dropout
+    and layer_norm_fwd.  Returns (y, h, mean, rstd), y and h dense."""
+    d, _, shape = _layer_norm_plan(x, gamma, beta, eps, act)
+    p, offset = _dropout_args(p, seed, tag, philox_offset, x.device)
+    d = LayerNormDesc.from_buffer_copy(d)
+    d.p, d.seed, d.tag, d.philox_offset = p, seed, tag, offset
+    if residual is not None:
+        _row_operand(residual, x, "residual")
+        d.r_row_stride = _row_stride(residual, "residual")
+    y = torch.empty_like(x, memory_format=torch.contiguous_format)
+    h = torch.empty_like(x, memory_format=torch.contiguous_format)
+    mean, rstd = x.new_empty(shape, dtype=torch.float32), x.new_empty(shape, dtype=torch.float32)
+    _call("hdqt_dropout_add_layer_norm_fwd", x, C.byref(d), x.data_ptr(), _ptr(residual), _ptr(gamma), _ptr(beta), h.data_ptr(),
+          y.data_ptr(), mean.data_ptr(), rstd.data_ptr())
+    return y, h, mean, rstd
+
+
+def dropout_add_layer_norm_bwd(dy, dh, h, gamma, beta, mean, rstd, p: float, seed: int, tag: int = 0, act: str = "none",
+                               philox_offset=None, want_dx: bool = True, want_residual: bool = True,
+                               want_params: bool = True):
+    """Gradients of dropout_add_layer_norm_fwd from the h it returned (dense); dh: the gradient that arrives for h itself, or None.
+    Returns (dx, dresidual, dgamma, dbeta), None where not wanted.  p, seed, tag, philox_offset as in the forward call (the device
+    word must still hold the value it had then)."""
+    d, nbytes, shape = _layer_norm_plan(h, gamma, beta, 0.0, act)
+    p, offset = _dropout_args(p, seed, tag, philox_offset, h.device)
+    if not h.is_contiguous():
+        raise ValueError("h must be the dense tensor of the forward call")
+    _row_operand(dy, h, "dy")
+    _check_stats(mean, rstd, shape, h.device)
+    if not dy.is_contiguous():
+        dy = dy.contiguous()
+    if dh is not None:
+        _row_operand(dh, h, "dh")
+        if not dh.is_contiguous():
+            dh = dh.contiguous()
+    d = LayerNormDesc.from_buffer_copy(d)
+    d.p, d.seed, d.tag, d.philox_offset = p, seed, tag, offset
+    dx = torch.empty_like(h) if want_dx else None
+    dresidual = torch.empty_like(h) if want_residual else None
+    dgamma = torch.empty_like(gamma) if want_params and gamma is not None else None
+    dbeta = torch.empty_like(beta) if want_params and beta is not None else None
+    ws = h.new_empty(nbytes, dtype=torch.uint8)
+    _call("hdqt_dropout_add_layer_norm_bwd", h, C.byref(d), dy.data_ptr(), _ptr(dh), h.data_ptr(), _ptr(gamma), _ptr(beta),
+          mean.data_ptr(), rstd.data_ptr(), _ptr(dx), _ptr(dresidual), _ptr(dgamma), _ptr(dbeta), ws.data_ptr(), nbytes)
+    return dx, dresidual, dgamma, dbeta
 
 
 # ---- linear layer + softmax cross entropy over a large vocabulary ------------------------------------

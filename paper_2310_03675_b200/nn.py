@@ -2,8 +2,8 @@
 matrix products (forward, dX, dW) all run through the library, plus the synthetic MLP workload.
 
 Everything that is not a matmul stays in floating point, as in the paper (Section 3: only matmul inputs and
-accumulators are quantized): bias and ReLU in the forward GEMM's epilogue; group norm with its activation, the cross entropy
-of a linear head and gradient clipping as library operators; batch norm and SGD as torch ops.
+accumulators are quantized): bias and ReLU in the forward GEMM's epilogue; group and layer norm with their activation, dropout, the
+cross entropy of a linear head and gradient clipping as library operators; batch norm and SGD as torch ops.
 """
 from __future__ import annotations
 
@@ -14,7 +14,7 @@ import torch
 from . import hdqt
 
 # Philox stream tags: 8*layer + 2*gemm_kind + operand, so that no two stochastic roundings of one step
-# share a counter; the step index goes into the seed.
+# share a counter; the step index goes into the seed.  A layer's dropout has tag 8*layer + 6.
 _KIND = {"fwd": 0, "dgrad": 1, "wgrad": 2}
 
 
@@ -120,27 +120,52 @@ class HdqtLinear(torch.nn.Module):
 
 class Mlp(torch.nn.Module):
     """1152 -> 512 -> 256 -> 12 with ReLU (the synthetic sensor-window workload); quantized=False gives
-    the fp32 torch model of the same shape and initialisation for comparison."""
+    the fp32 torch model of the same shape and initialisation for comparison.  norm="layer": layer norm between a hidden layer's
+    product and its ReLU.  dropout: the probability with which hidden values are dropped in training.  residual=True (with
+    norm="layer"): a hidden layer that keeps its width adds its input, relu(layer norm(x + dropout(product)))."""
 
-    def __init__(self, sizes=(1152, 512, 256, 12), quantized: bool = True, **over):
+    def __init__(self, sizes=(1152, 512, 256, 12), quantized: bool = True, norm: Optional[str] = None,
+                 dropout: float = 0.0, residual: bool = False, **over):
         super().__init__()
+        if norm not in (None, "layer"):
+            raise ValueError("norm must be None or 'layer'")
+        if residual and norm is None:
+            raise ValueError("residual=True needs norm='layer'")
         self.quantized = quantized
         self.layers = torch.nn.ModuleList(
             [HdqtLinear(a, b, layer_id=i, **over) for i, (a, b) in enumerate(zip(sizes[:-1], sizes[1:]))])
+        hidden = list(enumerate(zip(sizes[:-2], sizes[1:-1])))
+        self.norms = self.drops = None
+        if norm == "layer":
+            self.norms = torch.nn.ModuleList(
+                [DropoutAddLayerNorm(b, dropout, layer_id=i, act="relu") if residual and a == b else LayerNormAct(b, act="relu")
+                 for i, (a, b) in hidden])
+        if dropout > 0.0:
+            self.drops = torch.nn.ModuleList([Dropout(dropout, layer_id=i) for i, _ in hidden])
 
     def set_step(self, step: int):
-        for l in self.layers:
-            l.step = step
+        for m in self.modules():
+            if isinstance(m, _RANDOM):
+                m.step = step
 
     def forward(self, x):
         for i, l in enumerate(self.layers):
             last = i + 1 == len(self.layers)
+            relu = not last and self.norms is None
             if self.quantized:
-                x = l(x, relu=not last)          # bias and ReLU inside the forward GEMM's epilogue
+                z = l(x, relu=relu)              # bias and ReLU inside the forward GEMM's epilogue
             else:
-                x = x @ l.weight + l.bias
-                if not last:
-                    x = torch.relu(x)
+                z = x @ l.weight + l.bias
+                if relu:
+                    z = torch.relu(z)
+            if not last and self.norms is not None and isinstance(self.norms[i], DropoutAddLayerNorm):
+                x, _ = self.norms[i](z, x)
+                continue
+            if not last and self.norms is not None:
+                z = self.norms[i](z)
+            if not last and self.drops is not None:
+                z = self.drops[i](z)
+            x = z
         return x
 
 
@@ -170,7 +195,7 @@ class GraphedTrainStep:
     step is one graph launch instead of several hundred kernel launches with their host-side cost.
 
     The Philox seed of a recorded call is fixed, so the stochastic roundings of successive replays are told apart
-    on the device: every quantized layer gets `philox_offset` = a device counter that the graph itself increments
+    on the device: every quantized layer and every dropout gets `philox_offset` = a device counter that the graph itself increments
     once per step (step k rounds with (seed, offset) = (base_step, k)).  Two graphs are recorded and replayed
     alternately, because delayed scaling ping-pongs between two history buffers per tensor.
 
@@ -186,7 +211,7 @@ class GraphedTrainStep:
         dev = x.device
         self.counter = torch.zeros(1, dtype=torch.int32, device=dev)
         for m in model.modules():
-            if isinstance(m, (HdqtLinear, HdqtConv2d)):
+            if isinstance(m, _RANDOM):
                 m.over = dict(m.over, philox_offset=self.counter)
                 m.step = base_step
         self.x, self.labels = x.clone(), labels.clone()
@@ -242,7 +267,7 @@ class _FirstOrder(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, *_):
-        raise RuntimeError("group norm and linear cross entropy have no second derivatives")
+        raise RuntimeError("the norms and linear cross entropy have no second derivatives")
 
 
 def _first_order(grads, inputs):
@@ -293,6 +318,139 @@ class GroupNormAct(torch.nn.Module):
     def forward(self, x):
         y = GroupNormFunction.apply(_nhwc(x), self.weight, self.bias, self.groups, self.eps, self.act)
         return y.permute(0, 3, 1, 2)
+
+
+class LayerNormFunction(torch.autograd.Function):
+    """act(layer norm) over the last dimension of x[..., channels].  First derivatives only."""
+
+    @staticmethod
+    def forward(ctx, x, gamma, beta, eps: float, act: str):
+        y, mean, rstd = hdqt.layer_norm_fwd(x, gamma, beta, eps, act)
+        ctx.save_for_backward(x, gamma, beta, mean, rstd)
+        ctx.act = act
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, gamma, beta, mean, rstd = ctx.saved_tensors
+        dx, dgamma, dbeta = hdqt.layer_norm_bwd(dy, x, gamma, beta, mean, rstd, ctx.act, want_dx=ctx.needs_input_grad[0],
+                                                want_params=ctx.needs_input_grad[1] or ctx.needs_input_grad[2])
+        return *_first_order((dx, dgamma, dbeta), (dy, x, gamma, beta)), None, None
+
+
+class LayerNormAct(torch.nn.Module):
+    """Layer norm over the last dimension of [..., features] tensors with an optional activation ("none", "relu", "silu")."""
+
+    def __init__(self, features: int, act: str = "none", eps: float = 1e-5):
+        super().__init__()
+        if act not in hdqt.ACT_CODES:
+            raise ValueError(f"act must be one of {sorted(hdqt.ACT_CODES)}")
+        self.weight = torch.nn.Parameter(torch.ones(features))
+        self.bias = torch.nn.Parameter(torch.zeros(features))
+        self.act, self.eps = act, eps
+
+    def forward(self, x):
+        return LayerNormFunction.apply(x.contiguous(), self.weight, self.bias, self.eps, self.act)
+
+
+class DropoutFunction(torch.autograd.Function):
+    """residual + dropout(x) (residual may be None); the mask is drawn again in the backward pass.  `offset` is the device word of
+    the random stream (or None): changing it between the two passes is an error, which autograd reports."""
+
+    @staticmethod
+    def forward(ctx, x, residual, p: float, seed: int, tag: int, offset):
+        ctx.how = (p, seed, tag)
+        ctx.save_for_backward(offset)
+        return hdqt.dropout(x, p, seed, tag, residual, offset)
+
+    @staticmethod
+    def backward(ctx, dy):
+        offset, = ctx.saved_tensors
+        dx = DropoutFunction.apply(dy.contiguous(), None, *ctx.how, offset) if ctx.needs_input_grad[0] else None
+        return dx, dy if ctx.needs_input_grad[1] else None, None, None, None, None
+
+
+class _RandomLayer(torch.nn.Module):
+    """A layer that drops values: probability and random stream."""
+
+    def __init__(self, p: float, layer_id: int, philox_offset=None):
+        super().__init__()
+        if not 0.0 <= p <= 1.0:
+            raise ValueError("p must be a probability")
+        self.p, self.layer_id = float(p), layer_id
+        self.over = {"philox_offset": philox_offset}
+        self.step = None
+
+    def _stream(self):
+        """(p, seed, tag, device word) of a call: the step where a training loop sets one, else a seed from torch's generator."""
+        if not self.training or self.p == 0.0:
+            return 0.0, 0, 0, None
+        seed = self.step if self.step is not None else int(torch.randint(1 << 62, ()))
+        return self.p, seed, 8 * self.layer_id + 6, self.over["philox_offset"]
+
+
+class Dropout(_RandomLayer):
+    """residual + dropout(x) (residual optional) with a mask from the library's counter-based generator, which is not stored.  Layers
+    of one network need different layer_ids.  step: the seed, advanced by the training loop (train_step, GraphedTrainStep); None
+    (the default) draws a seed from torch's generator at every call."""
+
+    def __init__(self, p: float, layer_id: int = 0, philox_offset=None):
+        super().__init__(p, layer_id, philox_offset)
+
+    def forward(self, x, residual=None):
+        how = self._stream()
+        if how[0] == 0.0 and residual is None:
+            return x
+        return DropoutFunction.apply(x.contiguous(), None if residual is None else residual.contiguous(), *how)
+
+
+class DropoutAddLayerNormFunction(torch.autograd.Function):
+    """(y, h) with h = residual + dropout(x) and y = act(layer norm(h)).  First derivatives only."""
+
+    @staticmethod
+    def forward(ctx, x, residual, gamma, beta, p: float, seed: int, tag: int, offset, eps: float, act: str):
+        y, h, mean, rstd = hdqt.dropout_add_layer_norm_fwd(x, residual, gamma, beta, p, seed, tag, eps, act, offset)
+        ctx.save_for_backward(h, gamma, beta, mean, rstd, offset)
+        ctx.how, ctx.act = (p, seed, tag), act
+        ctx.set_materialize_grads(False)
+        return y, h
+
+    @staticmethod
+    def backward(ctx, dy, dh):
+        h, gamma, beta, mean, rstd, offset = ctx.saved_tensors
+        p, seed, tag = ctx.how
+        want_x, want_r = ctx.needs_input_grad[:2]
+        none = (None,) * 6
+        if dy is None:                   # only the sum was used
+            if dh is None:
+                return None, None, None, None, *none
+            dx = DropoutFunction.apply(dh.contiguous(), None, p, seed, tag, offset) if want_x else None
+            return dx, dh if want_r else None, None, None, *none
+        both = p > 0.0                   # without dropout the two gradients are one tensor
+        dx, dres, dgamma, dbeta = hdqt.dropout_add_layer_norm_bwd(
+            dy, dh, h, gamma, beta, mean, rstd, p, seed, tag, ctx.act, offset, want_dx=want_x and both,
+            want_residual=want_r or (want_x and not both), want_params=ctx.needs_input_grad[2] or ctx.needs_input_grad[3])
+        dx, dres, dgamma, dbeta = _first_order((dx, dres, dgamma, dbeta), (dy, h, gamma, beta) + (() if dh is None else (dh,)))
+        if want_x and not both:
+            dx = dres
+        return dx, dres if want_r else None, dgamma, dbeta, *none
+
+
+class DropoutAddLayerNorm(_RandomLayer):
+    """The end of a residual block: (y, h) with h = residual + dropout(x), the residual stream, and y = act(layer norm(h)), in one
+    pass over the rows.  residual may be None.  layer_id and step: see Dropout."""
+
+    def __init__(self, features: int, p: float, layer_id: int = 0, act: str = "none", eps: float = 1e-5, philox_offset=None):
+        super().__init__(p, layer_id, philox_offset)
+        if act not in hdqt.ACT_CODES:
+            raise ValueError(f"act must be one of {sorted(hdqt.ACT_CODES)}")
+        self.weight = torch.nn.Parameter(torch.ones(features))
+        self.bias = torch.nn.Parameter(torch.zeros(features))
+        self.act, self.eps = act, eps
+
+    def forward(self, x, residual=None):
+        return DropoutAddLayerNormFunction.apply(x.contiguous(), None if residual is None else residual.contiguous(), self.weight,
+                                                 self.bias, *self._stream(), self.eps, self.act)
 
 
 class LinearCrossEntropyFunction(torch.autograd.Function):
@@ -511,6 +669,10 @@ class HdqtConv2d(torch.nn.Module):
                                         self.implicit)
 
 
+# layers with random numbers of their own: a training loop sets their step, a recorded step their device word
+_RANDOM = (HdqtLinear, HdqtConv2d, Dropout, DropoutAddLayerNorm)
+
+
 def _norm(kind: str, channels: int, relu: bool):
     """Normalisation layer: "batch" (torch; its ReLU is applied by the caller) or "group" (one library call, ReLU included)."""
     if kind == "batch":
@@ -567,7 +729,7 @@ class ResNet18Width(torch.nn.Module):
 
     def set_step(self, step: int):
         for m in self.modules():
-            if isinstance(m, (HdqtConv2d, HdqtLinear)):
+            if isinstance(m, _RANDOM):
                 m.step = step
 
     def features(self, x):
