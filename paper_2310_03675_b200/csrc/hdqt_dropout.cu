@@ -23,7 +23,6 @@ struct DropCall {
 template <typename T, bool kLinear>
 __global__ void __launch_bounds__(NT) dropout_vec_kernel(const DropCall p) {
   constexpr int V = 16 / sizeof(T), K = 8 / V;
-  using A = Vec<T, V>;
   const int64_t g = (int64_t)blockIdx.x * NT + threadIdx.x, first = g * 8;
   if (first >= p.n) return;
   int64_t xi = first, ri = first, yi = first;
@@ -37,13 +36,13 @@ __global__ void __launch_bounds__(NT) dropout_vec_kernel(const DropCall p) {
   const T* res = reinterpret_cast<const T*>(p.residual) + ri;
   T* y = reinterpret_cast<T*>(p.y) + yi;
   const bool whole = !kLinear || first + 8 <= p.n;
-  A vx[K], vr[K];
+  Words vx[K], vr[K];
   if (whole) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) vx[k] = *reinterpret_cast<const A*>(x + k * V);
+    for (int k = 0; k < K; ++k) vx[k] = *reinterpret_cast<const Words*>(x + k * V);
     if (p.residual) {
 #pragma unroll
-      for (int k = 0; k < K; ++k) vr[k] = *reinterpret_cast<const A*>(res + k * V);
+      for (int k = 0; k < K; ++k) vr[k] = *reinterpret_cast<const Words*>(res + k * V);
     }
   }
   Philox4 w{};
@@ -52,14 +51,14 @@ __global__ void __launch_bounds__(NT) dropout_vec_kernel(const DropCall p) {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       float f[V], q[V];
-      unpack(vx[k], f);
-      if (p.residual) unpack(vr[k], q);
+      unpack<T>(vx[k], f);
+      if (p.residual) unpack<T>(vr[k], q);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         if (p.d.on) f[j] = drop_keeps(w, k * V + j, p.d.limit) ? __fmul_rn(f[j], p.d.scale) : 0.0f;
         if (p.residual) f[j] = __fadd_rn(q[j], f[j]);
       }
-      *reinterpret_cast<A*>(y + k * V) = pack<T>(f);
+      *reinterpret_cast<Words*>(y + k * V) = pack_words<T>(f);
     }
     return;
   }

@@ -11,6 +11,8 @@
 // blocks' in a fixed order.  Rows too wide for registers are read again from the L2 (the "long" kernels).
 #include <math.h>
 
+#include <atomic>
+
 #include "hdqt_dropout.cuh"
 
 namespace hdqt {
@@ -33,6 +35,7 @@ struct RowParams {
   int32_t param_dtype, act, channels;
   int32_t team;                  // threads of a row: a power of two up to 32, or a multiple of 32
   int32_t params_wide;           // gamma and beta start on 16-byte boundaries
+  int32_t classes;               // rows that are cut at different places (1 = all alike)
   int32_t bits_stride;           // bytes of a team's dropout decisions in shared memory
   int64_t rows, x_rs, r_rs, y_rs;
   float eps;
@@ -69,7 +72,11 @@ __device__ __forceinline__ void load_params(const void* p, const RowParams& q, i
 __device__ __forceinline__ void team_barrier(int team, int size) {
   if (size <= 32) __syncwarp();
   else if (size == (int)blockDim.x) __syncthreads();
-  else asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(size) : "memory");
+  // (constant names: a barrier named by a register makes the block reserve all sixteen, and four such blocks fill an SM)
+  else if (team == 0) asm volatile("bar.sync 1, %0;" ::"r"(size) : "memory");
+  else if (team == 1) asm volatile("bar.sync 2, %0;" ::"r"(size) : "memory");
+  else if (team == 2) asm volatile("bar.sync 3, %0;" ::"r"(size) : "memory");
+  else asm volatile("bar.sync 4, %0;" ::"r"(size) : "memory");
 }
 
 // Sums over the threads of a team; every thread gets them.  s: one slot of N per warp of the block, not in use since the barrier
@@ -121,9 +128,364 @@ __device__ __forceinline__ float dropped(float x, uint32_t bits, int j, float sc
 template <typename T>
 __device__ __forceinline__ float rounded(float v) { return to_f32(from_f32<T>(v)); }
 
-// ---- rows in registers -------------------------------------------------------------------------------------
+// ---- rows in registers, 16-byte accesses ---------------------------------------------------------------------
+//
+// A row is cut at the 16-byte boundaries of memory into chunks of V elements; thread t of a team holds the chunks t, t + team, ...
+// (K of them).  Where the channels are not a multiple of V, rows of a dense tensor start `lead` elements behind a boundary, lead =
+// (row * channels) mod V, which repeats every `classes` rows.  A block keeps to the rows of one class, so that all its rows
+// are cut alike: element j of chunk q is channel q V - lead + j, and a chunk that is shared with a neighbouring row is masked.
+// gamma and beta stand in shared memory in this order, in fp32.
 
-// Element i of thread t: channel ((i / V) * team + t) * V + i % V.
+template <int V>
+struct Cut {
+  int lead, chunks;        // elements in front of the row in its first chunk; chunks of the row
+  uint32_t mask;           // V bits per chunk of this thread: elements that belong to the row
+  __device__ __forceinline__ uint32_t of(int k) const { return (mask >> (k * V)) & ((1u << V) - 1); }
+};
+template <int V, int K>
+__device__ __forceinline__ Cut<V> cut_row(const RowParams& p, int cls, int t, int size) {
+  static_assert(V * K <= 32);
+  Cut<V> u;
+  u.lead = (int)(((int64_t)cls * p.channels) & (V - 1));
+  u.chunks = (u.lead + p.channels + V - 1) / V;
+  u.mask = 0;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int first = (k * size + t) * V - u.lead;          // channel of the chunk's first element
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (first + j >= 0 && first + j < p.channels) u.mask |= 1u << (k * V + j);
+  }
+  return u;
+}
+
+// The chunk at src, with a neighbouring row's elements in it where the mask has gaps.  `edge`: the row's end may be the tensor's, so
+// that a shared chunk is read element by element.
+template <typename T, int V, bool kShift>
+__device__ __forceinline__ Words load_chunk(const T* src, uint32_t mask, bool edge) {
+  Words v{};
+  if (kShift && edge && mask != (1u << V) - 1) {
+    if constexpr (kShift) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+          if ((mask >> i) & 1) v.w[i] = __float_as_uint(src[i]);
+        } else {
+          if ((mask >> (2 * i)) & 1) v.w[i] = reinterpret_cast<const uint16_t*>(src)[2 * i];
+          if ((mask >> (2 * i)) & 2) v.w[i] |= (uint32_t) reinterpret_cast<const uint16_t*>(src)[2 * i + 1] << 16;
+        }
+      }
+    }
+  } else if (mask != 0) {
+    v = *reinterpret_cast<const Words*>(src);
+  }
+  return v;
+}
+template <typename T, int V, bool kShift>
+__device__ __forceinline__ void unpack_chunk(const Words& v, uint32_t mask, float (&f)[V]) {
+  unpack<T>(v, f);
+  if constexpr (kShift) {
+    if (mask != (1u << V) - 1) {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (!((mask >> j) & 1)) f[j] = 0.0f;
+    }
+  }
+}
+template <typename T, int V, bool kShift>
+__device__ __forceinline__ void store_chunk(T* dst, uint32_t mask, const Words& v) {
+  if (mask == (1u << V) - 1) *reinterpret_cast<Words*>(dst) = v;
+  if constexpr (kShift) {
+    if (mask != (1u << V) - 1) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        if ((mask >> j) & 1) {
+          if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t*>(dst)[j] = v.w[j];
+          else reinterpret_cast<uint16_t*>(dst)[j] = (uint16_t)(v.w[j / 2] >> (16 * (j & 1)));
+        }
+      }
+    }
+  }
+}
+
+// gamma or beta in the block's order: four elements of every chunk, then the next four
+template <int V>
+__device__ __forceinline__ void stage_params(const void* src, const RowParams& p, int lead, int slots, float fill, float* s) {
+  for (int i = threadIdx.x; i < slots * V; i += blockDim.x) {
+    const int c = i - lead;
+    const bool in = c >= 0 && c < p.channels;
+    const float v = !in ? 0.0f : src ? load_param(src, p.param_dtype, c) : fill;
+    s[(((i & (V - 1)) >> 2) * slots + i / V) * 4 + (i & 3)] = v;
+  }
+}
+template <int V>
+__device__ __forceinline__ void staged(const float* s, int slots, int q, float (&f)[V]) {
+#pragma unroll
+  for (int i = 0; i < V / 4; ++i) {
+    const float4 v = reinterpret_cast<const float4*>(s)[i * slots + q];
+    f[4 * i] = v.x;
+    f[4 * i + 1] = v.y;
+    f[4 * i + 2] = v.z;
+    f[4 * i + 3] = v.w;
+  }
+}
+
+// random words of chunk number i (of the flattened tensor), its elements the first V
+template <int V>
+__device__ __forceinline__ Philox4 chunk_words(const DropParams& d, uint32_t offset, uint64_t i) {
+  if constexpr (V == 8) return drop_words(d, offset, i);
+  Philox4 w = drop_words(d, offset, i >> 1);
+  if (i & 1) {
+    w.w[0] = w.w[2];
+    w.w[1] = w.w[3];
+  }
+  return w;
+}
+template <int V>
+__device__ __forceinline__ void drop_chunk(const DropParams& d, uint32_t offset, uint64_t i, float (&x)[V]) {
+  const Philox4 w = chunk_words<V>(d, offset, i);
+#pragma unroll
+  for (int j = 0; j < V; ++j) x[j] = drop_keeps(w, j, d.limit) ? __fmul_rn(x[j], d.scale) : 0.0f;
+}
+
+template <typename T, int K, bool kFused, bool kShift>
+__global__ void __launch_bounds__(512) team_fwd_kernel(const RowParams p) {
+  constexpr int V = 16 / sizeof(T);
+  __shared__ float s_sum[2][2][16];
+  extern __shared__ __align__(16) float s_params[];
+  const int size = p.team, teams = blockDim.x / size, team = threadIdx.x / size, t = threadIdx.x - team * size;
+  const int cls = kShift ? blockIdx.x % p.classes : 0;
+  const int64_t step = (int64_t)(gridDim.x / p.classes) * teams * p.classes;
+  int64_t row = (int64_t)(blockIdx.x / p.classes * teams + team) * p.classes + cls;
+  const int64_t ahead = size < 32 ? (int64_t)((threadIdx.x & 31) / size) * p.classes : 0;   // to this warp's first team's row
+  const Cut<V> cut = cut_row<V, K>(p, cls, t, size);
+  const int slots = K * size;
+  float* s_beta = s_params + slots * V;
+
+  Words nx[K], nr[K];      // the next row
+  auto fetch = [&](int64_t r) {
+    const bool live = r < p.rows, edge = r == p.rows - 1;
+    const T* src = reinterpret_cast<const T*>(p.x) + r * p.x_rs - cut.lead;
+    const T* res = reinterpret_cast<const T*>(p.residual) + r * p.r_rs - cut.lead;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const uint32_t m = live ? cut.of(k) : 0;
+      nx[k] = load_chunk<T, V, kShift>(src + (k * size + t) * V, m, edge);
+      if constexpr (kFused) nr[k] = load_chunk<T, V, kShift>(res + (k * size + t) * V, p.residual ? m : 0, edge);
+    }
+  };
+  fetch(row);
+  stage_params<V>(p.gamma, p, cut.lead, slots, 1.0f, s_params);
+  stage_params<V>(p.beta, p, cut.lead, slots, 0.0f, s_beta);
+  __syncthreads();
+  const uint32_t offset = kFused ? drop_offset(p.d) : 0;
+  const float inv_c = 1.0f / (float)p.channels;
+  for (int turn = 0; row - ahead < p.rows; row += step, turn ^= 1) {      // (the same number of turns for all teams of a warp)
+    const bool live = row < p.rows;
+    float x[K][V];
+    float sum[1] = {0.0f};
+    const int64_t at = row * p.y_rs - cut.lead + t * V;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const uint32_t m = live ? cut.of(k) : 0;
+      unpack_chunk<T, V, kShift>(nx[k], m, x[k]);
+      if constexpr (kFused) {
+        if (p.d.on) drop_chunk<V>(p.d, offset, ((uint64_t)row * (uint64_t)p.channels - cut.lead) / V + k * size + t, x[k]);
+        if (p.residual) {
+          float r[V];
+          unpack_chunk<T, V, kShift>(nr[k], m, r);
+#pragma unroll
+          for (int j = 0; j < V; ++j) x[k][j] = __fadd_rn(r[j], x[k][j]);
+        }
+        const Words h = pack_words<T>(x[k]);
+        store_chunk<T, V, kShift>(reinterpret_cast<T*>(p.h) + at + k * size * V, m, h);
+        unpack<T>(h, x[k]);
+      }
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum[0] += x[k][j];
+    }
+    fetch(row + step);
+    team_sum(sum, team, t, size, s_sum[turn][0]);
+    const float mu = sum[0] * inv_c;
+    float m2[1] = {0.0f};
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const uint32_t m = cut.of(k);
+#pragma unroll
+      for (int j = 0; j < V; ++j) x[k][j] -= mu;
+      if (m != (1u << V) - 1) {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+          if (!((m >> j) & 1)) x[k][j] = 0.0f;
+      }
+#pragma unroll
+      for (int j = 0; j < V; ++j) m2[0] = fmaf(x[k][j], x[k][j], m2[0]);
+    }
+    team_sum(m2, team, t, size, s_sum[turn][1]);
+    const float rs = __frsqrt_rn(fmaf(m2[0], inv_c, p.eps));
+    if (t == 0 && live) {
+      p.mean[row] = mu;
+      p.rstd[row] = rs;
+    }
+    with_act(p.act, [&]<int kAct>() {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        float g[V], b[V];
+        staged<V>(s_params, slots, k * size + t, g);
+        staged<V>(s_beta, slots, k * size + t, b);
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[k][j] = act_fwd<kAct>(fmaf(x[k][j] * rs, g[j], b[j]));
+        store_chunk<T, V, kShift>(reinterpret_cast<T*>(p.y) + at + k * size * V, live ? cut.of(k) : 0, pack_words<T>(x[k]));
+      }
+    });
+  }
+}
+
+template <typename T, int K, bool kFused, bool kShift>
+__global__ void __launch_bounds__(512) team_bwd_kernel(const RowParams p) {
+  constexpr int V = 16 / sizeof(T);
+  __shared__ float s_sum[2][32];
+  extern __shared__ __align__(16) float s_params[];
+  const int size = p.team, teams = blockDim.x / size, team = threadIdx.x / size, t = threadIdx.x - team * size;
+  const int cls = kShift ? blockIdx.x % p.classes : 0;
+  const int64_t step = (int64_t)(gridDim.x / p.classes) * teams * p.classes;
+  int64_t row = (int64_t)(blockIdx.x / p.classes * teams + team) * p.classes + cls;
+  const int64_t ahead = size < 32 ? (int64_t)((threadIdx.x & 31) / size) * p.classes : 0;
+  const Cut<V> cut = cut_row<V, K>(p, cls, t, size);
+  const int slots = K * size;
+  float* s_beta = s_params + slots * V;
+
+  Words nx[K], nd[K];      // the next row
+  float nmu = 0.0f, nrs = 0.0f;
+  auto fetch = [&](int64_t r) {
+    const bool live = r < p.rows, edge = r == p.rows - 1;
+    const T* src = reinterpret_cast<const T*>(p.x) + r * p.x_rs - cut.lead;
+    const T* dys = reinterpret_cast<const T*>(p.dy) + r * p.y_rs - cut.lead;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const uint32_t m = live ? cut.of(k) : 0;
+      nx[k] = load_chunk<T, V, kShift>(src + (k * size + t) * V, m, edge);
+      nd[k] = load_chunk<T, V, kShift>(dys + (k * size + t) * V, m, edge);
+    }
+    nmu = live ? p.mean[r] : 0.0f;
+    nrs = live ? p.rstd[r] : 0.0f;
+  };
+  fetch(row);
+  stage_params<V>(p.gamma, p, cut.lead, slots, 1.0f, s_params);
+  if (p.act != HDQT_ACT_NONE) stage_params<V>(p.beta, p, cut.lead, slots, 0.0f, s_beta);
+  __syncthreads();
+  const uint32_t offset = kFused ? drop_offset(p.d) : 0;
+
+  float sum_g[K][V], sum_b[K][V];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum_g[k][j] = sum_b[k][j] = 0.0f;
+  }
+  const float inv_c = 1.0f / (float)p.channels;
+  for (int turn = 0; row - ahead < p.rows; row += step, turn ^= 1) {
+    const bool live = row < p.rows;
+    const int64_t at = row * p.y_rs - cut.lead + t * V;
+    Words vx[K], vh[K];
+    float d[K][V];
+    const float mu = nmu, rs = nrs;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      vx[k] = nx[k];
+      unpack_chunk<T, V, kShift>(nd[k], live ? cut.of(k) : 0, d[k]);
+    }
+    fetch(row + step);
+    if constexpr (kFused) {
+      if (p.dh) {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+          vh[k] = load_chunk<T, V, kShift>(reinterpret_cast<const T*>(p.dh) + at + k * size * V, live ? cut.of(k) : 0, row == p.rows - 1);
+      }
+    }
+    float s[2] = {0.0f, 0.0f};
+    with_act(p.act, [&]<int kAct>() {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        float x[V], g[V], b[V];
+        unpack_chunk<T, V, kShift>(vx[k], cut.of(k), x);
+        staged<V>(s_params, slots, k * size + t, g);
+        if constexpr (kAct != HDQT_ACT_NONE) staged<V>(s_beta, slots, k * size + t, b);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const float xh = (x[j] - mu) * rs;
+          float dz = d[k][j];
+          if constexpr (kAct != HDQT_ACT_NONE) dz = act_bwd<kAct>(dz, fmaf(xh, g[j], b[j]));
+          sum_b[k][j] += dz;
+          sum_g[k][j] = fmaf(dz, xh, sum_g[k][j]);
+          d[k][j] = dz * g[j];
+          s[0] += d[k][j];
+          s[1] = fmaf(d[k][j], xh, s[1]);
+        }
+      }
+    });
+    team_sum(s, team, t, size, s_sum[turn]);
+    const float m1 = s[0] * inv_c, m2 = s[1] * inv_c;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const uint32_t m = live ? cut.of(k) : 0;
+      float x[V], o[V];
+      unpack<T>(vx[k], x);
+#pragma unroll
+      for (int j = 0; j < V; ++j) o[j] = rs * (d[k][j] - m1 - (x[j] - mu) * rs * m2);
+      if constexpr (kFused) {
+        if (p.dh) {
+          float h[V];
+          unpack<T>(vh[k], h);
+#pragma unroll
+          for (int j = 0; j < V; ++j) o[j] += h[j];
+        }
+        if (p.dres) store_chunk<T, V, kShift>(reinterpret_cast<T*>(p.dres) + at + k * size * V, m, pack_words<T>(o));
+        if (p.d.on) drop_chunk<V>(p.d, offset, ((uint64_t)row * (uint64_t)p.channels - cut.lead) / V + k * size + t, o);
+      }
+      if (p.dx) store_chunk<T, V, kShift>(reinterpret_cast<T*>(p.dx) + at + k * size * V, m, pack_words<T>(o));
+    }
+  }
+
+  if (p.part == nullptr) return;
+  // sums of the teams of a warp, then of the block (in shared memory, in the place of gamma and beta), then to this block's part
+  for (int o = size; o < 32; o <<= 1) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        sum_g[k][j] += __shfl_xor_sync(0xFFFFFFFFu, sum_g[k][j], o);
+        sum_b[k][j] += __shfl_xor_sync(0xFFFFFFFFu, sum_b[k][j], o);
+      }
+    }
+  }
+  float2* part = p.part + (int64_t)blockIdx.x * p.channels;
+  const int holders = size <= 32 ? (int)blockDim.x >> 5 : teams;
+  const int holder = size <= 32 ? (int)threadIdx.x >> 5 : team;
+  float2* mine = holders == 1 ? part : reinterpret_cast<float2*>(s_params) + holder * p.channels;
+  if (holders > 1) __syncthreads();
+  if (ahead == 0) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if ((cut.of(k) >> j) & 1) mine[(k * size + t) * V - cut.lead + j] = make_float2(sum_b[k][j], sum_g[k][j]);
+    }
+  }
+  if (holders == 1) return;
+  __syncthreads();
+  for (int c = threadIdx.x; c < p.channels; c += blockDim.x) {
+    float2 a = make_float2(0.0f, 0.0f);
+    for (int i = 0; i < holders; ++i) {
+      const float2 v = reinterpret_cast<const float2*>(s_params)[i * p.channels + c];
+      a.x += v.x;
+      a.y += v.y;
+    }
+    part[c] = a;
+  }
+}
+
+// ---- rows in registers, any strides and addresses: one element per access -------------------------------------
+
 template <typename T, int V, int K, bool kFused>
 __global__ void __launch_bounds__(1024) row_fwd_kernel(const RowParams p) {
   using A = Vec<T, V>;
@@ -581,76 +943,149 @@ int team_size(int channels, int vec, int per_thread) {
   return size;
 }
 
+constexpr int kMostTeam = 512;                   // threads of a row held in registers
+constexpr size_t kMostSmem = 200 * 1024;
+
+// Blocks of a kernel that fit an SM, by the threads of a row (which fix the block and its shared memory).  Looked up once per
+// kernel and row width; the shared memory limit is raised at a kernel's first launch on a device.
 template <auto kernel>
-hdqt_status_t with_smem(size_t smem, const char* what) {
-  if (smem <= 48 * 1024) return HDQT_OK;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  return e == cudaSuccess ? HDQT_OK : cuda_failure(e, what);
+hdqt_status_t blocks_per_sm(int team, int block, size_t smem, int* out) {
+  static std::atomic<uint64_t> ready{0};
+  static std::atomic<int> known[64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && (dev > 63 || !((ready.load(std::memory_order_relaxed) >> dev) & 1))) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem);
+    if (e == cudaSuccess && dev <= 63) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
+  if (e != cudaSuccess) return cuda_failure(e, "layer norm");
+  const int slot = team > 32 ? 6 + team / 32 : __builtin_ctz(team);
+  int n = known[slot].load(std::memory_order_relaxed);
+  if (n == 0) {
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, block, smem);
+    if (e != cudaSuccess) return cuda_failure(e, "layer norm");
+    if (n < 1) n = 1;
+    known[slot].store(n, std::memory_order_relaxed);
+  }
+  *out = n;
+  return HDQT_OK;
 }
 
-template <typename T, int V, bool kFused>
-hdqt_status_t run_fwd(RowParams p, cudaStream_t s) {
-  const int c = p.channels;
-  int e = 8;
-  if (p.rows * team_size(c, V, 8) > 148 * 2048 || team_size(c, V, 8) > 1024) e = 16;
-  if (team_size(c, V, e) > 1024) e = 32;
-  p.team = team_size(c, V, e);
-  if (p.team > 1024) {
-    const unsigned blocks = (unsigned)(p.rows < 2 * kNumSMsHint ? p.rows : 2 * kNumSMsHint);
-    long_fwd_kernel<T, V, kFused><<<blocks, kLongThreads, 0, s>>>(p);
-    return last_error("layer norm");
-  }
-  const int threads = p.team < 128 ? 128 / p.team * p.team : p.team;
-  const int per_block = p.team <= 32 ? threads / p.team : 1;
-  const int block = p.team <= 32 ? threads : p.team;
-  p.bits_stride = V < 8 ? c / 8 + 2 : 0;
-  const size_t smem = kFused ? (size_t)per_block * p.bits_stride : 0;
-  const unsigned blocks = (unsigned)((p.rows + per_block - 1) / per_block);
-  if (e == 8) row_fwd_kernel<T, V, 8 / V, kFused><<<blocks, block, smem, s>>>(p);
-  else if (e == 16) row_fwd_kernel<T, V, 16 / V, kFused><<<blocks, block, smem, s>>>(p);
-  else row_fwd_kernel<T, V, 32 / V, kFused><<<blocks, block, smem, s>>>(p);
+// One launch of a kernel whose teams walk over the rows: as many blocks as the machine holds, at most `most` per SM.
+template <auto kernel>
+hdqt_status_t launch_teams(const RowParams& p, size_t smem, int most, int* blocks, cudaStream_t s) {
+  const int block = p.team < 256 ? 256 / p.team * p.team : p.team, teams = block / p.team;
+  int per_sm = 0;
+  const hdqt_status_t st = blocks_per_sm<kernel>(p.team, block, smem, &per_sm);
+  if (st != HDQT_OK) return st;
+  if (per_sm > most) per_sm = most;
+  const int64_t needed = ((p.rows + p.classes - 1) / p.classes + teams - 1) / teams;       // of each class
+  const int64_t room = (int64_t)per_sm * kNumSMsHint / p.classes;
+  const int64_t n = (needed < room ? needed : room) * p.classes;
+  kernel<<<(unsigned)n, block, smem, s>>>(p);
+  *blocks = (int)n;
   return last_error("layer norm");
 }
 
-template <typename T, int V, int E, bool kFused, int kMaxThreads>
-hdqt_status_t launch_bwd(const RowParams& p, int block, int* parts, cudaStream_t s) {
-  constexpr auto kernel = row_bwd_kernel<T, V, E / V, kFused, kMaxThreads>;
-  const int teams = block / p.team;
-  const int holders = p.team <= 32 ? block / 32 : teams;
-  size_t smem = holders > 1 ? (size_t)holders * p.channels * sizeof(float2) : 0;
-  const size_t bits = kFused ? (size_t)2 * teams * p.bits_stride : 0;
-  if (bits > smem) smem = bits;
-  const hdqt_status_t st = with_smem<kernel>(smem, "layer norm gradient");
-  if (st != HDQT_OK) return st;
-  int per_sm = 0;
-  const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, block, smem);
-  if (e != cudaSuccess) return cuda_failure(e, "layer norm gradient");
-  if (per_sm > kMostParts / kNumSMsHint) per_sm = kMostParts / kNumSMsHint;
-  const int64_t most = (p.rows + teams - 1) / teams;
-  const int64_t blocks = most < (int64_t)per_sm * kNumSMsHint ? most : (int64_t)per_sm * kNumSMsHint;
-  kernel<<<(unsigned)blocks, block, smem, s>>>(p);
-  *parts = (int)blocks;
-  return last_error("layer norm gradient");
+// threads of a row whose chunks are divided K to a thread
+int chunk_team(const RowParams& p, int vec, int k) { return team_size(p.channels + (p.classes > 1 ? vec - 1 : 0), vec, k * vec); }
+
+template <typename T, int K, bool kFused>
+hdqt_status_t fwd_teams(RowParams p, cudaStream_t s) {
+  constexpr int V = 16 / sizeof(T);
+  p.team = chunk_team(p, V, K);
+  const size_t smem = (size_t)2 * K * p.team * V * sizeof(float);
+  int blocks;
+  if (p.classes > 1) return launch_teams<team_fwd_kernel<T, K, kFused, true>>(p, smem, 32, &blocks, s);
+  return launch_teams<team_fwd_kernel<T, K, kFused, false>>(p, smem, 32, &blocks, s);
 }
 
-template <typename T, int V, bool kFused>
-hdqt_status_t run_bwd(RowParams p, int* parts, cudaStream_t s) {
-  const int c = p.channels;
-  constexpr int E = sizeof(T) == 2 ? 16 : 8;
-  p.team = team_size(c, V, E);
-  p.bits_stride = V < 8 ? c / 8 + 2 : 0;
-  if (p.team <= 256) return launch_bwd<T, V, E, kFused, 256>(p, 256 / p.team * p.team, parts, s);
-  if (p.team <= 512) return launch_bwd<T, V, E, kFused, 512>(p, p.team, parts, s);
+template <typename T, bool kFused>
+hdqt_status_t run_fwd(RowParams p, bool wide, cudaStream_t s) {
+  constexpr int V = 16 / sizeof(T), kMost = 32 / V;      // chunks of a thread
+  if (wide && chunk_team(p, V, kMost) <= kMostTeam) {
+    // wider teams where there are too few rows to fill the machine
+    const int64_t chunks = p.rows * ((p.channels + V - 1) / V);
+    if (chunks >= (int64_t)kMost * kNumSMsHint * 768 || chunk_team(p, V, kMost / 2) > kMostTeam) return fwd_teams<T, kMost, kFused>(p, s);
+    if (chunks >= (int64_t)kMost / 2 * kNumSMsHint * 768 || chunk_team(p, V, kMost / 4) > kMostTeam)
+      return fwd_teams<T, kMost / 2, kFused>(p, s);
+    return fwd_teams<T, kMost / 4, kFused>(p, s);
+  }
+  p.classes = 1;
+  p.team = team_size(p.channels, 1, 16);
+  if (p.team <= 1024 && !wide) {
+    const int per_block = p.team <= 32 ? 128 / p.team : 1, block = p.team <= 32 ? 128 : p.team;
+    p.bits_stride = p.channels / 8 + 2;
+    const size_t smem = kFused ? (size_t)per_block * p.bits_stride : 0;
+    row_fwd_kernel<T, 1, 16, kFused><<<(unsigned)((p.rows + per_block - 1) / per_block), block, smem, s>>>(p);
+    return last_error("layer norm");
+  }
   const unsigned blocks = (unsigned)(p.rows < 2 * kNumSMsHint ? p.rows : 2 * kNumSMsHint);
-  if (p.dx || p.dres) long_bwd_kernel<T, V, kFused><<<blocks, kLongThreads, 0, s>>>(p);
+  if (wide && p.channels % V == 0) long_fwd_kernel<T, V, kFused><<<blocks, kLongThreads, 0, s>>>(p);
+  else long_fwd_kernel<T, 1, kFused><<<blocks, kLongThreads, 0, s>>>(p);
+  return last_error("layer norm");
+}
+
+size_t sums_bytes(const RowParams& p) {
+  const int block = p.team < 256 ? 256 / p.team * p.team : p.team, holders = p.team <= 32 ? block / 32 : block / p.team;
+  return holders > 1 ? (size_t)holders * p.channels * sizeof(float2) : 0;
+}
+
+template <typename T, int K, bool kFused>
+hdqt_status_t bwd_teams(RowParams p, int* parts, cudaStream_t s) {
+  constexpr int V = 16 / sizeof(T);
+  p.team = chunk_team(p, V, K);
+  const size_t params = (size_t)2 * K * p.team * V * sizeof(float), sums = sums_bytes(p);
+  const size_t smem = params > sums ? params : sums;
+  if (p.classes > 1) return launch_teams<team_bwd_kernel<T, K, kFused, true>>(p, smem, kMostParts / kNumSMsHint, parts, s);
+  return launch_teams<team_bwd_kernel<T, K, kFused, false>>(p, smem, kMostParts / kNumSMsHint, parts, s);
+}
+
+template <typename T, bool kFused>
+hdqt_status_t run_bwd(RowParams p, bool wide, int* parts, cudaStream_t s) {
+  constexpr int V = 16 / sizeof(T);
+  if (wide && chunk_team(p, V, 2) <= kMostTeam) return bwd_teams<T, 2, kFused>(p, parts, s);
+  p.classes = 1;
+  p.team = team_size(p.channels, 1, 8);
+  if (p.team <= 512 && !wide) {
+    p.bits_stride = p.channels / 8 + 2;
+    const int block = p.team < 256 ? 256 / p.team * p.team : p.team;
+    const size_t bits = kFused ? (size_t)2 * (block / p.team) * p.bits_stride : 0, sums = sums_bytes(p);
+    return launch_teams<row_bwd_kernel<T, 1, 8, kFused, 512>>(p, bits > sums ? bits : sums, kMostParts / kNumSMsHint, parts, s);
+  }
+  const unsigned blocks = (unsigned)(p.rows < 2 * kNumSMsHint ? p.rows : 2 * kNumSMsHint);
+  const bool vector = wide && p.channels % V == 0;
+  if (p.dx || p.dres) {
+    if (vector) long_bwd_kernel<T, V, kFused><<<blocks, kLongThreads, 0, s>>>(p);
+    else long_bwd_kernel<T, 1, kFused><<<blocks, kLongThreads, 0, s>>>(p);
+  }
   if (p.part) {
-    const unsigned columns = (unsigned)((c / V + 255) / 256);
+    const unsigned columns = (unsigned)((p.channels / (vector ? V : 1) + 255) / 256);
     const int64_t want = (8 * kNumSMsHint + columns - 1) / columns;
     const int64_t shares = want < p.rows ? want : p.rows;
     *parts = (int)(shares < kMostParts ? shares : kMostParts);
-    long_param_kernel<T, V><<<dim3(columns, (unsigned)*parts), 256, 0, s>>>(p);
+    if (vector) long_param_kernel<T, V><<<dim3(columns, (unsigned)*parts), 256, 0, s>>>(p);
+    else long_param_kernel<T, 1><<<dim3(columns, (unsigned)*parts), 256, 0, s>>>(p);
   }
   return last_error("layer norm gradient");
+}
+
+// 16-byte accesses: rows of whole chunks on 16-byte boundaries, or dense tensors that start on one (rows cut at the boundaries)
+bool set_classes(RowParams* p, int elem, uintptr_t bases, bool dense, uintptr_t strides) {
+  const int v = 16 / elem;
+  p->classes = 1;
+  if (bases & 15) return false;
+  if (p->channels % v == 0 && (strides & 15) == 0) return true;
+  if (!dense) return false;
+  for (int c = p->channels; (int64_t)c * p->classes % v != 0;) p->classes *= 2;
+  return true;
+}
+
+template <typename F>
+hdqt_status_t with_type(int dtype, F&& f) {
+  if (dtype == HDQT_DTYPE_F32) return f.template operator()<float>();
+  if (dtype == HDQT_DTYPE_BF16) return f.template operator()<__nv_bfloat16>();
+  return f.template operator()<__half>();
 }
 
 hdqt_status_t forward(const hdqt_layer_norm_desc_t* d, bool fused, const void* x, const void* residual, const void* gamma,
@@ -672,9 +1107,10 @@ hdqt_status_t forward(const hdqt_layer_norm_desc_t* d, bool fused, const void* x
   p.y = y;
   if (fused) p.d = make_drop(d->p, d->seed, d->tag, d->philox_offset);
   const uintptr_t strides = d->rows > 1 ? (uintptr_t)((p.x_rs | p.y_rs | (residual ? p.r_rs : 0)) * elem) : 0;
-  const int vec = vector_width(d->channels, elem, bases | strides);
+  const bool dense = d->rows == 1 || (p.x_rs == d->channels && p.y_rs == d->channels && (!residual || p.r_rs == d->channels));
+  const bool wide = set_classes(&p, elem, bases, dense, strides);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  return with_type_and_width(d->dtype, vec, [&]<typename T, int V>() { return fused ? run_fwd<T, V, true>(p, s) : run_fwd<T, V, false>(p, s); });
+  return with_type(d->dtype, [&]<typename T>() { return fused ? run_fwd<T, true>(p, wide, s) : run_fwd<T, false>(p, wide, s); });
 }
 
 hdqt_status_t backward(const hdqt_layer_norm_desc_t* d, bool fused, const void* dy, const void* dh, const void* x, const void* gamma,
@@ -704,9 +1140,10 @@ hdqt_status_t backward(const hdqt_layer_norm_desc_t* d, bool fused, const void* 
     p.part = want_params ? part : nullptr;
     if (fused) p.d = make_drop(d->p, d->seed, d->tag, d->philox_offset);
     const uintptr_t strides = d->rows > 1 ? (uintptr_t)((p.x_rs | p.y_rs) * elem) : 0;
-    const int vec = vector_width(d->channels, elem, bases | strides);
-    const hdqt_status_t e = with_type_and_width(d->dtype, vec, [&]<typename T, int V>() {
-      return fused ? run_bwd<T, V, true>(p, &parts, s) : run_bwd<T, V, false>(p, &parts, s);
+    const bool dense = d->rows == 1 || (p.x_rs == d->channels && p.y_rs == d->channels);
+    const bool wide = set_classes(&p, elem, bases, dense, strides);
+    const hdqt_status_t e = with_type(d->dtype, [&]<typename T>() {
+      return fused ? run_bwd<T, true>(p, wide, &parts, s) : run_bwd<T, false>(p, wide, &parts, s);
     });
     if (e != HDQT_OK) return e;
   }
@@ -722,7 +1159,7 @@ using namespace hdqt;
 
 extern "C" size_t hdqt_layer_norm_workspace_bytes(const hdqt_layer_norm_desc_t* d) {
   if (check_desc(d, false) != HDQT_OK) return 0;
-  const int64_t parts = d->rows < kMostParts ? d->rows : kMostParts;
+  const int64_t parts = d->rows < kMostParts - 7 ? d->rows + 7 : kMostParts;      // (a block of every class, rows or not)
   return align256((size_t)parts * d->channels * sizeof(float2)) + 256;
 }
 

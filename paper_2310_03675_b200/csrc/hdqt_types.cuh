@@ -72,6 +72,39 @@ __device__ __forceinline__ Vec<T, N> pack(const float (&f)[N]) {
   return v;
 }
 
+// Sixteen bytes of elements held as four words.  A Vec of 16-bit elements that lives across a branch or a loop turn is taken apart
+// into eight half-word registers by the compiler, which costs more instructions than the arithmetic on them.
+struct alignas(16) Words {
+  uint32_t w[4];
+};
+template <typename T>
+__device__ __forceinline__ void unpack(const Words& v, float (&f)[16 / sizeof(T)]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      f[i] = __uint_as_float(v.w[i]);
+    } else if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+      f[2 * i] = __uint_as_float(v.w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(v.w[i] & 0xFFFF0000u);
+    } else {
+      const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&v.w[i]));
+      f[2 * i] = t.x;
+      f[2 * i + 1] = t.y;
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ Words pack_words(const float (&f)[16 / sizeof(T)]) {
+  Words v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) v.w[i] = __float_as_uint(f[i]);
+    else if constexpr (std::is_same_v<T, __nv_bfloat16>) *reinterpret_cast<__nv_bfloat162*>(&v.w[i]) = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+    else *reinterpret_cast<__half2*>(&v.w[i]) = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+  }
+  return v;
+}
+
 // hardware approximations (2 units in the last place or better; results below 2^-126 become 0)
 __device__ __forceinline__ float ex2(float x) {
   float r;
