@@ -1,0 +1,698 @@
+// Layer norm with an activation over the rows of a tensor, alone or behind dropout and a residual add: backward.
+//
+// Teams keep the sums of dgamma and dbeta of their columns in registers while they walk over the rows; a block's sums are
+// joined in shared memory and written once, and a second launch adds the blocks' in a fixed order.
+#include "hdqt_rows.cuh"
+
+namespace hdqt {
+
+namespace {
+
+// kKeep: gamma dz stays in registers between the two passes over a row, otherwise it is formed again (wide rows)
+template <typename T, int K, bool kFused, bool kShift, bool kSub, int kThreads, bool kKeep>
+__global__ void __launch_bounds__(kThreads, 1) team_bwd_kernel(const RowParams p) {
+  constexpr int V = 16 / sizeof(T), H = V / 4, kStreams = kFused ? 3 : 2;
+  constexpr uint32_t kStage = kStreams * K * 512;
+  __shared__ __align__(16) float s_sum[4 * kSlots];
+  extern __shared__ __align__(16) char s_dyn[];
+  const Place<T, K, kShift, kSub> me(p);
+  const int n_params = p.act != HDQT_ACT_NONE ? 2 : 1;
+  const char* mine = s_dyn + me.warp * (K * n_params * H * 512) + me.lane * 16;
+  uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_dyn) + params_bytes<T, K>(p.team, n_params) +
+                  (threadIdx.x >> 5) * (p.stages * kStage) + (threadIdx.x & 31) * 16;
+  asm volatile("" : "+r"(ring));
+
+  int64_t x_at = me.offset(p.x_rs, me.row), d_at = me.offset(p.y_rs, me.row), y_at = d_at;
+  uint64_t number = kFused ? me.number(p) : 0;
+  uint32_t next = me.row;
+  auto fetch = [&](uint32_t dst) {
+    if (next < p.rows) {
+      const char* src = reinterpret_cast<const char*>(p.x) + x_at;
+      const char* dys = reinterpret_cast<const char*>(p.dy) + d_at;
+#pragma unroll
+      for (int k = 0; k < K; ++k) me.fetch(dst + k * 512, src, k);
+#pragma unroll
+      for (int k = 0; k < K; ++k) me.fetch(dst + (K + k) * 512, dys, k);
+      if (kFused && p.dh) {
+        const char* dhs = reinterpret_cast<const char*>(p.dh) + d_at;
+#pragma unroll
+        for (int k = 0; k < K; ++k) me.fetch(dst + (2 * K + k) * 512, dhs, k);
+      }
+    }
+    copies_issued();
+    next += p.step;
+    x_at += p.x_step;
+    d_at += p.y_step;
+  };
+  if constexpr (!kShift) {      // what no copy reaches reads as zeros
+    for (int i = 0; i < p.stages * kStreams; ++i) {
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+        if (!me.has(k)) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(ring + (i * K + k) * 512), "r"(0) : "memory");
+    }
+  }
+  for (int i = 0; i < p.stages; ++i) fetch(ring + i * kStage);
+  float nmu = 0.0f, nrs = 0.0f;      // of the next row
+  if (me.row < p.rows) {
+    nmu = p.mean[me.row];
+    nrs = p.rstd[me.row];
+  }
+  stage_params<T, K, kSub>(p.gamma, p, me.lead, n_params, 0, 1.0f, s_dyn);
+  if (n_params == 2) stage_params<T, K, kSub>(p.beta, p, me.lead, 2, 1, 0.0f, s_dyn);
+  for (int i = threadIdx.x; i < 4 * kSlots; i += blockDim.x) s_sum[i] = 0.0f;
+  __syncthreads();
+  float* slots = s_sum + (kSub ? 0 : me.team * ((p.team + 127) >> 7) * 4);
+  const uint32_t offset = kFused ? drop_offset(p.d) : 0;
+
+  float sum_g[K][V], sum_b[K][V];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum_g[k][j] = sum_b[k][j] = 0.0f;
+  }
+  const float inv_c = 1.0f / (float)p.channels;
+  with_act(p.act, [&]<int kAct>() {
+    constexpr int kParams = kAct == HDQT_ACT_NONE ? 1 : 2;
+    uint32_t stage = 0;
+    int turn = 0;
+    for (uint32_t row = me.row; row - me.ahead < p.rows; row += p.step) {
+      const bool live = !kSub || row < p.rows;
+      const float mu = nmu, rs = nrs;
+      if (row + p.step < p.rows) {
+        nmu = p.mean[row + p.step];
+        nrs = p.rstd[row + p.step];
+      }
+      const float shift = -mu * rs;
+      float d[kKeep ? K : 1][V];
+      float s0[2] = {0.0f, 0.0f}, s1[2] = {0.0f, 0.0f};
+      wait_copies(p.stages);
+      // gamma dz of a chunk, and its x; the sums of the first pass
+      auto terms = [&](int k, bool first, float (&x)[V], float (&dg)[V]) {
+        float g[V], xh[V];
+        unpack<T>(shared_words(ring + stage + k * 512), x);
+        unpack<T>(shared_words(ring + stage + (K + k) * 512), dg);
+        me.clear(k, x);
+        me.clear(k, dg);
+        staged<V>(mine, k, kParams, 0, g);
+#pragma unroll
+        for (int j = 0; j < V; j += 2) fma2(xh[j], xh[j + 1], x[j], x[j + 1], rs, rs, shift, shift);
+        if constexpr (kAct != HDQT_ACT_NONE) {
+          float b[V];
+          staged<V>(mine, k, kParams, 1, b);
+#pragma unroll
+          for (int j = 0; j < V; ++j) dg[j] = act_bwd<kAct>(dg[j], fmaf(xh[j], g[j], b[j]));
+        }
+#pragma unroll
+        for (int j = 0; j < V; j += 2) {
+          if (first) {
+            add2(sum_b[k][j], sum_b[k][j + 1], dg[j], dg[j + 1]);
+            fma2(sum_g[k][j], sum_g[k][j + 1], dg[j], dg[j + 1], xh[j], xh[j + 1], sum_g[k][j], sum_g[k][j + 1]);
+          }
+          mul2(dg[j], dg[j + 1], g[j], g[j + 1]);
+          if (first) {
+            add2(s0[0], s0[1], dg[j], dg[j + 1]);
+            fma2(s1[0], s1[1], dg[j], dg[j + 1], xh[j], xh[j + 1], s1[0], s1[1]);
+          }
+        }
+      };
+      if (live) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+          float x[V];
+          terms(k, true, x, d[kKeep ? k : 0]);
+        }
+      }
+      float s[2] = {s0[0] + s0[1], s1[0] + s1[1]};
+      lanes_total<kSub>(s, me.size);
+      if (!kSub && me.size > 32) warps_total(s, me.team + 1, me.size, me.warp, me.lane, slots + turn);
+      // dx = rs d - rs m1 - rs m2 (x rs + shift)
+      const float slope = -rs * rs * (s[1] * inv_c), base = -rs * fmaf(s[1] * inv_c, shift, s[0] * inv_c);
+      if (live) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+          float x[V];
+          if constexpr (kKeep) unpack<T>(shared_words(ring + stage + k * 512), x);
+          else terms(k, false, x, d[0]);
+          float (&o)[V] = d[kKeep ? k : 0];
+#pragma unroll
+          for (int j = 0; j < V; j += 2) {
+            fma2(x[j], x[j + 1], x[j], x[j + 1], slope, slope, base, base);
+            fma2(o[j], o[j + 1], o[j], o[j + 1], rs, rs, x[j], x[j + 1]);
+          }
+          if constexpr (kFused) {
+            if (p.dh) {
+              float h[V];
+              unpack<T>(shared_words(ring + stage + (2 * K + k) * 512), h);
+#pragma unroll
+              for (int j = 0; j < V; j += 2) add2(o[j], o[j + 1], h[j], h[j + 1]);
+            }
+            if (p.dres) store_chunk<T, V, kShift>(reinterpret_cast<char*>(p.dres) + y_at + me.byte(k), me.has(k), me.of(k), me.gaps(k), pack_words<T>(o));
+            if (p.d.on) drop_chunk<V>(p.d, offset, number + me.byte(k) / 16, o);
+          }
+          if (p.dx) store_chunk<T, V, kShift>(reinterpret_cast<char*>(p.dx) + y_at + me.byte(k), me.has(k), me.of(k), me.gaps(k), pack_words<T>(o));
+        }
+      }
+      fetch(ring + stage);                                  // (what was read from the place has been stored)
+      stage = stage + kStage == p.stages * kStage ? 0 : stage + kStage;
+      turn ^= 2 * kSlots;
+      y_at += p.y_step;
+      if (kFused) number += p.chunk_step;
+    }
+  });
+
+  if (p.part == nullptr) return;
+  chain_next();
+  // sums of the teams of a warp, then of the block (in shared memory, over gamma, beta and the ring), then to this block's part
+  if constexpr (kSub) {
+    for (int o = me.size; o < 32; o <<= 1) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          sum_g[k][j] += __shfl_xor_sync(0xFFFFFFFFu, sum_g[k][j], o);
+          sum_b[k][j] += __shfl_xor_sync(0xFFFFFFFFu, sum_b[k][j], o);
+        }
+      }
+    }
+  }
+  // [holder][warp of the team][k][dbeta, dgamma][four elements][lane]
+  const int holder = me.size <= 32 ? (int)threadIdx.x >> 5 : me.team, holders = me.size <= 32 ? (int)blockDim.x >> 5 : me.teams;
+  const int chunks = (kSub ? 32 : me.size) * K;               // chunks of a holder
+  wait_copies(1);
+  __syncthreads();
+  {
+    char* to = s_dyn + holder * (chunks * V * 8) + me.warp * (K * 2 * H * 512) + (threadIdx.x & 31) * 16;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+#pragma unroll
+      for (int i = 0; i < H; ++i) {
+        *reinterpret_cast<float4*>(to + (k * 2 * H + i) * 512) =
+            make_float4(sum_b[k][4 * i], sum_b[k][4 * i + 1], sum_b[k][4 * i + 2], sum_b[k][4 * i + 3]);
+        *reinterpret_cast<float4*>(to + ((k * 2 + 1) * H + i) * 512) =
+            make_float4(sum_g[k][4 * i], sum_g[k][4 * i + 1], sum_g[k][4 * i + 2], sum_g[k][4 * i + 3]);
+      }
+    }
+  }
+  __syncthreads();
+  float2* part = p.part + (int64_t)blockIdx.x * p.channels;
+  for (int i = threadIdx.x; i < chunks * H; i += blockDim.x) {
+    const int lane = i & 31, half = (i >> 5) % H, group = (i >> 5) / H;      // group = warp * K + k
+    const int chunk = kSub ? group * p.team + lane : group * 32 + lane, c = chunk * V + half * 4 - me.lead;
+    if (kSub && lane >= p.team) continue;
+    float4 b = make_float4(0.0f, 0.0f, 0.0f, 0.0f), g = b;
+    const char* from = s_dyn + (group * 2 * H + half) * 512 + lane * 16;
+    for (int n = 0; n < holders; ++n, from += chunks * V * 8) {
+      const float4 u = *reinterpret_cast<const float4*>(from), v = *reinterpret_cast<const float4*>(from + H * 512);
+      b.x += u.x;
+      b.y += u.y;
+      b.z += u.z;
+      b.w += u.w;
+      g.x += v.x;
+      g.y += v.y;
+      g.z += v.z;
+      g.w += v.w;
+    }
+    const float2 pairs[4] = {make_float2(b.x, g.x), make_float2(b.y, g.y), make_float2(b.z, g.z), make_float2(b.w, g.w)};
+    if (!kShift && c < p.channels) {
+      reinterpret_cast<float4*>(part + c)[0] = make_float4(b.x, g.x, b.y, g.y);
+      reinterpret_cast<float4*>(part + c)[1] = make_float4(b.z, g.z, b.w, g.w);
+    } else if (kShift) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (c + j >= 0 && c + j < p.channels) part[c + j] = pairs[j];
+    }
+  }
+}
+
+// ---- few rows: one per block, everything loaded at once --------------------------------------------------------
+
+template <typename T, int K, bool kFused, bool kShift>
+__global__ void __launch_bounds__(1024) once_bwd_kernel(const RowParams p) {
+  constexpr int V = 16 / sizeof(T);
+  __shared__ __align__(16) float s_sum[2 * kSlots];
+  const int64_t row = blockIdx.x;
+  const int lead = kShift ? (int)((row * p.channels) & (V - 1)) : 0;
+  const bool edge = row == p.rows - 1;
+  const char* src = reinterpret_cast<const char*>(p.x) + (row * p.x_rs - lead) * (int64_t)sizeof(T);
+  const int64_t y_at = (row * p.y_rs - lead) * (int64_t)sizeof(T);
+  const char* dys = reinterpret_cast<const char*>(p.dy) + y_at;
+  Words vx[K], vd[K], vh[K];
+  uint32_t mask[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int q = k * blockDim.x + threadIdx.x, c = q * V - lead;
+    mask[k] = kShift ? chunk_mask<V>(p, c) : c < p.channels ? (1u << V) - 1 : 0;
+    vx[k] = load_chunk<T, V, kShift>(src + q * 16, mask[k], edge);
+    vd[k] = load_chunk<T, V, kShift>(dys + q * 16, mask[k], edge);
+    if constexpr (kFused) vh[k] = load_chunk<T, V, kShift>(reinterpret_cast<const char*>(p.dh) + y_at + q * 16, p.dh ? mask[k] : 0, edge);
+  }
+  const float mu = p.mean[row], rs = p.rstd[row], shift = -mu * rs, inv_c = 1.0f / (float)p.channels;
+  if (blockDim.x > 32) {
+    for (int i = threadIdx.x; i < 2 * kSlots; i += blockDim.x) s_sum[i] = 0.0f;
+    __syncthreads();
+  }
+  float d[K][V];
+  float s[2] = {0.0f, 0.0f};
+  float2* part = p.part + row * p.channels;
+  with_act(p.act, [&]<int kAct>() {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c = (k * blockDim.x + threadIdx.x) * V - lead;
+      float x[V], g[V], b[V];
+      if (kShift) {
+        load_params_cut<V>(p.gamma, p, c, 1.0f, g);
+        if constexpr (kAct != HDQT_ACT_NONE) load_params_cut<V>(p.beta, p, c, 0.0f, b);
+      } else if (mask[k]) {
+        load_params<V>(p.gamma, p, c, 1.0f, g);
+        if constexpr (kAct != HDQT_ACT_NONE) load_params<V>(p.beta, p, c, 0.0f, b);
+      }
+      unpack<T>(vx[k], x);
+      unpack<T>(vd[k], d[k]);
+      clear_gaps<V, kShift>(mask[k], x);
+      clear_gaps<V, kShift>(mask[k], d[k]);
+      if (mask[k]) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const float xh = fmaf(x[j], rs, shift);
+          float dz = d[k][j];
+          if constexpr (kAct != HDQT_ACT_NONE) dz = act_bwd<kAct>(dz, fmaf(xh, g[j], b[j]));
+          if (p.part && (!kShift || ((mask[k] >> j) & 1))) part[c + j] = make_float2(dz, dz * xh);
+          d[k][j] = dz * g[j];
+          s[0] += d[k][j];
+          s[1] = fmaf(d[k][j], xh, s[1]);
+        }
+      }
+    }
+  });
+  chain_next();
+  lanes_total<false>(s, 32);
+  if (blockDim.x > 32) warps_total(s, 0, blockDim.x, threadIdx.x >> 5, threadIdx.x & 31, s_sum);
+  const float slope = -rs * rs * (s[1] * inv_c), base = -rs * fmaf(s[1] * inv_c, shift, s[0] * inv_c);
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int q = k * blockDim.x + threadIdx.x;
+    float x[V];
+    unpack<T>(vx[k], x);
+#pragma unroll
+    for (int j = 0; j < V; ++j) d[k][j] = fmaf(d[k][j], rs, fmaf(x[j], slope, base));
+    if constexpr (kFused) {
+      if (p.dh) {
+        float h[V];
+        unpack<T>(vh[k], h);
+#pragma unroll
+        for (int j = 0; j < V; ++j) d[k][j] += h[j];
+      }
+      if (p.dres) store_chunk<T, V, kShift>(reinterpret_cast<char*>(p.dres) + y_at + q * 16, mask[k] != 0, mask[k], true, pack_words<T>(d[k]));
+      if (p.d.on) drop_chunk<V>(p.d, drop_offset(p.d), ((uint64_t)row * (uint64_t)p.channels - lead) / V + q, d[k]);
+    }
+    if (p.dx) store_chunk<T, V, kShift>(reinterpret_cast<char*>(p.dx) + y_at + q * 16, mask[k] != 0, mask[k], true, pack_words<T>(d[k]));
+  }
+}
+
+// ---- any strides and addresses, rows in registers --------------------------------------------------------------
+
+template <typename T, int V, int K, bool kFused, int kMaxThreads>
+__global__ void __launch_bounds__(kMaxThreads) any_bwd_kernel(const RowParams p) {
+  using A = Vec<T, V>;
+  __shared__ float s_sum[2][2 * kMaxThreads / 32];
+  extern __shared__ __align__(16) char s_dyn[];
+  const int size = p.team, teams = blockDim.x / size, team = threadIdx.x / size, t = threadIdx.x - team * size;
+  const int64_t step = (int64_t)gridDim.x * teams;
+  int64_t row = (int64_t)blockIdx.x * teams + team;
+  const int ahead = size < 32 ? (threadIdx.x & 31) / size : 0;      // teams of this warp in front of this one
+
+  A nx[K], nd[K];      // the next row
+  float nmu = 0.0f, nrs = 0.0f;
+  auto fetch = [&](int64_t r) {
+    const bool live = r < p.rows;
+    if (live) {
+      nmu = p.mean[r];
+      nrs = p.rstd[r];
+    } else {
+      nmu = nrs = 0.0f;
+    }
+    const T* src = reinterpret_cast<const T*>(p.x) + r * p.x_rs;
+    const T* dys = reinterpret_cast<const T*>(p.dy) + r * p.y_rs;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c = (k * size + t) * V;
+      nx[k] = A{};
+      nd[k] = A{};
+      if (live && c < p.channels) {
+        nx[k] = *reinterpret_cast<const A*>(src + c);
+        nd[k] = *reinterpret_cast<const A*>(dys + c);
+      }
+    }
+  };
+
+  float sum_g[K][V], sum_b[K][V];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum_g[k][j] = sum_b[k][j] = 0.0f;
+  }
+  const float inv_c = 1.0f / (float)p.channels;
+  int turn = 0;
+  fetch(row);
+  for (; row - ahead < p.rows; row += step, turn ^= 1) {            // (the same number of turns for all teams of a warp)
+    const bool live = row < p.rows;
+    A vx[K], vh[K];
+    float d[K][V];
+    const float mu = nmu, rs = nrs;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      vx[k] = nx[k];
+      unpack(nd[k], d[k]);
+    }
+    fetch(row + step);
+    uint8_t* bits = reinterpret_cast<uint8_t*>(s_dyn) + (turn * teams + team) * p.bits_stride;
+    if constexpr (kFused) {
+      if (p.dh) {
+        const T* dhs = reinterpret_cast<const T*>(p.dh) + row * p.y_rs;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+          const int c = (k * size + t) * V;
+          if (live && c < p.channels) vh[k] = *reinterpret_cast<const A*>(dhs + c);
+        }
+      }
+      if (V < 8 && p.d.on && live) row_bits(p, row, t, size, bits);
+    }
+    float s[2] = {0.0f, 0.0f};
+    with_act(p.act, [&]<int kAct>() {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const int c = (k * size + t) * V;
+        if (c < p.channels) {
+          float x[V], g[V], b[V];
+          unpack(vx[k], x);
+          load_params(p.gamma, p, c, 1.0f, g);
+          if constexpr (kAct != HDQT_ACT_NONE) load_params(p.beta, p, c, 0.0f, b);
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            const float xh = (x[j] - mu) * rs;
+            float dz = d[k][j];
+            if constexpr (kAct != HDQT_ACT_NONE) dz = act_bwd<kAct>(dz, fmaf(xh, g[j], b[j]));
+            sum_b[k][j] += dz;
+            sum_g[k][j] = fmaf(dz, xh, sum_g[k][j]);
+            d[k][j] = dz * g[j];
+            s[0] += d[k][j];
+            s[1] = fmaf(d[k][j], xh, s[1]);
+          }
+        }
+      }
+    });
+    team_sum(s, team, t, size, s_sum[turn]);
+    if (kFused && V < 8 && size <= 32) __syncwarp();
+    const float m1 = s[0] * inv_c, m2 = s[1] * inv_c;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c = (k * size + t) * V;
+      if (live && c < p.channels) {
+        float x[V], o[V];
+        unpack(vx[k], x);
+#pragma unroll
+        for (int j = 0; j < V; ++j) o[j] = rs * (d[k][j] - m1 - (x[j] - mu) * rs * m2);
+        if constexpr (kFused) {
+          if (p.dh) {
+            float h[V];
+            unpack(vh[k], h);
+#pragma unroll
+            for (int j = 0; j < V; ++j) o[j] += h[j];
+          }
+          if (p.dres) *reinterpret_cast<A*>(reinterpret_cast<T*>(p.dres) + row * p.y_rs + c) = pack<T>(o);
+          if (p.d.on) {
+            const uint32_t b = chunk_bits<V>(p, row, c, bits);
+#pragma unroll
+            for (int j = 0; j < V; ++j) o[j] = dropped(o[j], b, j, p.d.scale);
+          }
+        }
+        if (p.dx) *reinterpret_cast<A*>(reinterpret_cast<T*>(p.dx) + row * p.y_rs + c) = pack<T>(o);
+      }
+    }
+  }
+
+  if (p.part == nullptr) return;
+  float2* part = p.part + (int64_t)blockIdx.x * p.channels;
+  // teams of a warp, then those of the block
+  for (int o = size; o < 32; o <<= 1) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        sum_g[k][j] += __shfl_xor_sync(0xFFFFFFFFu, sum_g[k][j], o);
+        sum_b[k][j] += __shfl_xor_sync(0xFFFFFFFFu, sum_b[k][j], o);
+      }
+    }
+  }
+  const int holders = size <= 32 ? (int)blockDim.x >> 5 : teams;
+  const int holder = size <= 32 ? (int)threadIdx.x >> 5 : team;
+  float2* mine = holders == 1 ? part : reinterpret_cast<float2*>(s_dyn) + holder * p.channels;
+  if (holders > 1) __syncthreads();                                 // (the decisions are read, the sums take their place)
+  if (ahead == 0) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c = (k * size + t) * V;
+      if (c < p.channels) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) mine[c + j] = make_float2(sum_b[k][j], sum_g[k][j]);
+      }
+    }
+  }
+  if (holders == 1) return;
+  __syncthreads();
+  for (int c = threadIdx.x; c < p.channels; c += blockDim.x) {
+    float2 a = make_float2(0.0f, 0.0f);
+    for (int i = 0; i < holders; ++i) {
+      const float2 v = reinterpret_cast<const float2*>(s_dyn)[i * p.channels + c];
+      a.x += v.x;
+      a.y += v.y;
+    }
+    part[c] = a;
+  }
+}
+
+// ---- rows of any length, read again from the L2 ----------------------------------------------------------------
+
+// gamma dz of V channels, and xhat
+template <typename T, int V, int kAct>
+__device__ __forceinline__ void long_terms(const RowParams& p, const T* xs, const T* dys, int c, float mu, float rs, float (&xh)[V],
+                                           float (&dz)[V], float (&g)[V]) {
+  unpack(*reinterpret_cast<const Vec<T, V>*>(xs + c), xh);
+  unpack(*reinterpret_cast<const Vec<T, V>*>(dys + c), dz);
+  load_params(p.gamma, p, c, 1.0f, g);
+  float b[V];
+  if constexpr (kAct != HDQT_ACT_NONE) load_params(p.beta, p, c, 0.0f, b);
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    xh[j] = (xh[j] - mu) * rs;
+    if constexpr (kAct != HDQT_ACT_NONE) dz[j] = act_bwd<kAct>(dz[j], fmaf(xh[j], g[j], b[j]));
+  }
+}
+
+template <typename T, int V, bool kFused>
+__global__ void __launch_bounds__(kLongThreads) long_bwd_kernel(const RowParams p) {
+  using A = Vec<T, V>;
+  __shared__ float s_sum[2][64];
+  const int t = threadIdx.x;
+  const uint32_t offset = kFused ? drop_offset(p.d) : 0;
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
+    const T* xs = reinterpret_cast<const T*>(p.x) + row * p.x_rs;
+    const T* dys = reinterpret_cast<const T*>(p.dy) + row * p.y_rs;
+    const float mu = p.mean[row], rs = p.rstd[row];
+    with_act(p.act, [&]<int kAct>() {
+      float s[2] = {0.0f, 0.0f};
+      for (int c = t * V; c < p.channels; c += kLongThreads * V) {
+        float xh[V], dz[V], g[V];
+        long_terms<T, V, kAct>(p, xs, dys, c, mu, rs, xh, dz, g);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          s[0] = fmaf(dz[j], g[j], s[0]);
+          s[1] = fmaf(dz[j] * g[j], xh[j], s[1]);
+        }
+      }
+      team_sum(s, 0, t, kLongThreads, s_sum[turn]);
+      const float m1 = s[0] / (float)p.channels, m2 = s[1] / (float)p.channels;
+      for (int c = t * V; c < p.channels; c += kLongThreads * V) {
+        float xh[V], dz[V], g[V];
+        long_terms<T, V, kAct>(p, xs, dys, c, mu, rs, xh, dz, g);
+        float o[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) o[j] = rs * (dz[j] * g[j] - m1 - xh[j] * m2);
+        if constexpr (kFused) {
+          if (p.dh) {
+            float h[V];
+            unpack(*reinterpret_cast<const A*>(reinterpret_cast<const T*>(p.dh) + row * p.y_rs + c), h);
+#pragma unroll
+            for (int j = 0; j < V; ++j) o[j] += h[j];
+          }
+          if (p.dres) *reinterpret_cast<A*>(reinterpret_cast<T*>(p.dres) + row * p.y_rs + c) = pack<T>(o);
+          if (p.d.on) {
+            const uint64_t i = (uint64_t)row * (uint64_t)p.channels + c;
+            const uint32_t b = drop_bits(p.d, offset, i >> 3) >> (i & 7);
+#pragma unroll
+            for (int j = 0; j < V; ++j) o[j] = dropped(o[j], b, j, p.d.scale);
+          }
+        }
+        if (p.dx) *reinterpret_cast<A*>(reinterpret_cast<T*>(p.dx) + row * p.y_rs + c) = pack<T>(o);
+      }
+    });
+  }
+}
+
+// sums of V columns over a share of the rows
+template <typename T, int V>
+__global__ void __launch_bounds__(256) long_param_kernel(const RowParams p) {
+  const int c = (int)(blockIdx.x * 256 + threadIdx.x) * V;
+  if (c >= p.channels) return;
+  const int64_t first = p.rows * blockIdx.y / gridDim.y, last = p.rows * (blockIdx.y + 1) / gridDim.y;
+  float sum_g[V], sum_b[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) sum_g[j] = sum_b[j] = 0.0f;
+  with_act(p.act, [&]<int kAct>() {
+#pragma unroll 4
+    for (int64_t row = first; row < last; ++row) {
+      float xh[V], dz[V], g[V];
+      long_terms<T, V, kAct>(p, reinterpret_cast<const T*>(p.x) + row * p.x_rs, reinterpret_cast<const T*>(p.dy) + row * p.y_rs, c,
+                             p.mean[row], p.rstd[row], xh, dz, g);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        sum_b[j] += dz[j];
+        sum_g[j] = fmaf(dz[j], xh[j], sum_g[j]);
+      }
+    }
+  });
+#pragma unroll
+  for (int j = 0; j < V; ++j) p.part[(int64_t)blockIdx.y * p.channels + c + j] = make_float2(sum_b[j], sum_g[j]);
+}
+
+// ---- host side -----------------------------------------------------------------------------------------------
+
+template <typename T, int K, bool kFused, bool kSub>
+bool bwd_teams(RowParams p, int* parts, hdqt_status_t* st, cudaStream_t s) {
+  constexpr int V = 16 / sizeof(T), kThreads = K * V == 32 ? 512 : 640;
+  constexpr bool kKeep = K * V <= 16;
+  p.team = team_size(row_chunks(p, V), K);
+  Shape shape;
+  const int params = p.act != HDQT_ACT_NONE ? 2 : 1;
+  if (p.team > kThreads || !shape_of(&p, sizeof(T), K, params, kFused ? 3 : 2, kThreads, true, &shape)) return false;
+  if (p.classes > 1) *st = launch_rows<team_bwd_kernel<T, K, kFused, true, kSub, kThreads, kKeep>>(p, shape, s);
+  else *st = launch_rows<team_bwd_kernel<T, K, kFused, false, kSub, kThreads, kKeep>>(p, shape, s);
+  *parts = shape.blocks;
+  return true;
+}
+
+template <typename T, int K, bool kFused>
+hdqt_status_t bwd_once(const RowParams& p, int* parts, cudaStream_t s) {
+  const int n = (row_chunks(p, 16 / sizeof(T)) + K - 1) / K, threads = (n + 31) / 32 * 32;
+  if (p.classes > 1) once_bwd_kernel<T, K, kFused, true><<<(unsigned)p.rows, threads, 0, s>>>(p);
+  else once_bwd_kernel<T, K, kFused, false><<<(unsigned)p.rows, threads, 0, s>>>(p);
+  *parts = (int)p.rows;
+  return last_error("layer norm gradient");
+}
+
+template <typename T, bool kFused>
+hdqt_status_t run_bwd(RowParams p, bool wide, int* parts, cudaStream_t s) {
+  constexpr int V = 16 / sizeof(T), kMost = 32 / V;
+  if (wide) {
+    hdqt_status_t st = HDQT_OK;
+    const int chunks = row_chunks(p, V);
+    if (p.rows <= kNumSMsHint && chunks <= 2048) return chunks <= 1024 ? bwd_once<T, 1, kFused>(p, parts, s) : bwd_once<T, 2, kFused>(p, parts, s);
+    if (chunks <= 16 * (8 / V)) {
+      if (bwd_teams<T, 8 / V, kFused, true>(p, parts, &st, s)) return st;
+    } else {
+      const int k = kFused && sizeof(T) == 4 ? kMost / 4 : !kFused && sizeof(T) == 2 && chunks >= 512 ? kMost : kMost / 2;
+      if ((k <= kMost / 4 || chunks <= 16 * (kMost / 2)) && bwd_teams<T, kMost / 4, kFused, false>(p, parts, &st, s)) return st;
+      if ((k <= kMost / 2 || chunks <= 16 * kMost) && bwd_teams<T, kMost / 2, kFused, false>(p, parts, &st, s)) return st;
+      if (bwd_teams<T, kMost, kFused, false>(p, parts, &st, s)) return st;
+    }
+  }
+  p.classes = 1;
+  p.team = team_size(p.channels, 8);
+  if (p.team <= 512 && !wide) {
+    p.bits_stride = p.channels / 8 + 2;
+    const int block = p.team < 256 ? 256 / p.team * p.team : p.team, teams = block / p.team;
+    const size_t bits = kFused ? (size_t)2 * teams * p.bits_stride : 0, sums = sums_bytes(p, block, p.channels);
+    const int64_t needed = (p.rows + teams - 1) / teams;
+    *parts = (int)(needed < kMostParts ? needed : kMostParts);
+    return launch_rows<any_bwd_kernel<T, 1, 8, kFused, 512>>(p, Shape{*parts, block, bits > sums ? bits : sums}, s);
+  }
+  const unsigned blocks = (unsigned)(p.rows < 2 * kNumSMsHint ? p.rows : 2 * kNumSMsHint);
+  const bool vector = wide && p.channels % V == 0;
+  if (p.dx || p.dres) {
+    if (vector) long_bwd_kernel<T, V, kFused><<<blocks, kLongThreads, 0, s>>>(p);
+    else long_bwd_kernel<T, 1, kFused><<<blocks, kLongThreads, 0, s>>>(p);
+  }
+  if (p.part) {
+    const unsigned columns = (unsigned)((p.channels / (vector ? V : 1) + 255) / 256);
+    const int64_t want = (8 * kNumSMsHint + columns - 1) / columns;
+    const int64_t shares = want < p.rows ? want : p.rows;
+    *parts = (int)(shares < kMostParts ? shares : kMostParts);
+    if (vector) long_param_kernel<T, V><<<dim3(columns, (unsigned)*parts), 256, 0, s>>>(p);
+    else long_param_kernel<T, 1><<<dim3(columns, (unsigned)*parts), 256, 0, s>>>(p);
+  }
+  return last_error("layer norm gradient");
+}
+
+hdqt_status_t backward(const hdqt_layer_norm_desc_t* d, bool fused, const void* dy, const void* dh, const void* x, const void* gamma,
+                       const void* beta, const float* mean, const float* rstd, void* dx, void* dres, void* dgamma, void* dbeta,
+                       void* workspace, size_t workspace_bytes, void* stream) {
+  const hdqt_status_t st = check_rows_desc(d, fused);
+  if (st != HDQT_OK) return st;
+  if (!workspace || (d->rows > 0 && (!x || !dy || !mean || !rstd))) return HDQT_ERR_INVALID_ARG;
+  const int elem = dtype_size(d->dtype), pelem = dtype_size(d->param_dtype);
+  const uintptr_t bases = bits_of(x) | bits_of(dy) | bits_of(dh) | bits_of(dx) | bits_of(dres);
+  const uintptr_t params = bits_of(gamma) | bits_of(beta) | bits_of(dgamma) | bits_of(dbeta);
+  if ((bases & (uintptr_t)(elem - 1)) || (params & (uintptr_t)(pelem - 1)) || ((bits_of(mean) | bits_of(rstd)) & 3) ||
+      (bits_of(workspace) & 255) || (fused && (bits_of(d->philox_offset) & 3)))
+    return HDQT_ERR_ALIGNMENT;
+  if (workspace_bytes < hdqt_layer_norm_workspace_bytes(d)) return HDQT_ERR_WORKSPACE;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  float2* part = reinterpret_cast<float2*>(workspace);
+  const bool want_params = dgamma || dbeta;
+  int parts = 0;
+  if (d->rows > 0 && (dx || dres || want_params)) {
+    RowParams p = make_row_params(*d, gamma, beta, const_cast<float*>(mean), const_cast<float*>(rstd));
+    p.x = x;
+    p.dy = dy;
+    p.dh = dh;
+    p.dx = dx;
+    p.dres = dres;
+    p.part = want_params ? part : nullptr;
+    if (fused) p.d = make_drop(d->p, d->seed, d->tag, d->philox_offset);
+    const uintptr_t strides = d->rows > 1 ? (uintptr_t)((p.x_rs | p.y_rs) * elem) : 0;
+    const bool dense = d->rows == 1 || (p.x_rs == d->channels && p.y_rs == d->channels);
+    const bool wide = set_classes(&p, elem, bases, dense, strides);
+    const hdqt_status_t e = with_type(d->dtype, [&]<typename T>() {
+      return fused ? run_bwd<T, true>(p, wide, &parts, s) : run_bwd<T, false>(p, wide, &parts, s);
+    });
+    if (e != HDQT_OK) return e;
+  }
+  if (want_params) launch_param_grad(part, parts, (int)d->channels, dgamma, dbeta, d->param_dtype, parts > 0, s);
+  return last_error("layer norm gradient");
+}
+
+}  // namespace
+
+}  // namespace hdqt
+
+using namespace hdqt;
+
+extern "C" size_t hdqt_layer_norm_workspace_bytes(const hdqt_layer_norm_desc_t* d) {
+  if (check_rows_desc(d, false) != HDQT_OK) return 0;
+  const int64_t parts = d->rows < kMostParts - 7 ? d->rows + 7 : kMostParts;      // (a block of every class, rows or not)
+  return align256((size_t)parts * d->channels * sizeof(float2)) + 256;
+}
+
+extern "C" hdqt_status_t hdqt_layer_norm_bwd(const hdqt_layer_norm_desc_t* d, const void* dy, const void* x, const void* gamma,
+                                             const void* beta, const float* mean, const float* rstd, void* dx, void* dgamma,
+                                             void* dbeta, void* workspace, size_t workspace_bytes, void* stream) {
+  return backward(d, false, dy, nullptr, x, gamma, beta, mean, rstd, dx, nullptr, dgamma, dbeta, workspace, workspace_bytes, stream);
+}
+
+extern "C" hdqt_status_t hdqt_dropout_add_layer_norm_bwd(const hdqt_layer_norm_desc_t* d, const void* dy, const void* dh,
+                                                         const void* h, const void* gamma, const void* beta, const float* mean,
+                                                         const float* rstd, void* dx, void* dresidual, void* dgamma, void* dbeta,
+                                                         void* workspace, size_t workspace_bytes, void* stream) {
+  return backward(d, true, dy, dh, h, gamma, beta, mean, rstd, dx, dresidual, dgamma, dbeta, workspace, workspace_bytes, stream);
+}

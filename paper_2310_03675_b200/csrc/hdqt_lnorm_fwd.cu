@@ -1,0 +1,485 @@
+// Layer norm with an activation over the rows of a tensor, alone or behind dropout and a residual add: forward.
+#include "hdqt_rows.cuh"
+
+namespace hdqt {
+
+namespace {
+
+// ---- teams that walk over the rows ---------------------------------------------------------------------------
+
+template <typename T, int K, bool kFused, bool kShift, bool kSub, int kThreads>
+__global__ void __launch_bounds__(kThreads, 1) team_fwd_kernel(const RowParams p) {
+  constexpr int V = 16 / sizeof(T), H = V / 4, kStreams = kFused ? 2 : 1;
+  constexpr uint32_t kStage = kStreams * K * 512;
+  __shared__ __align__(16) float s_sum[4 * kSlots];
+  extern __shared__ __align__(16) char s_dyn[];
+  const Place<T, K, kShift, kSub> me(p);
+  const uint32_t params = params_bytes<T, K>(p.team, 2);
+  const char* mine = s_dyn + me.warp * (K * 2 * H * 512) + me.lane * 16;
+  uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_dyn) + params + (threadIdx.x >> 5) * (p.stages * kStage) + (threadIdx.x & 31) * 16;
+  asm volatile("" : "+r"(ring));
+
+  int64_t x_at = me.offset(p.x_rs, me.row), r_at = kFused ? me.offset(p.r_rs, me.row) : 0, y_at = me.offset(p.y_rs, me.row);
+  uint64_t number = kFused ? me.number(p) : 0;
+  uint32_t next = me.row;
+  auto fetch = [&](uint32_t dst) {
+    if (next < p.rows) {
+      const char* src = reinterpret_cast<const char*>(p.x) + x_at;
+#pragma unroll
+      for (int k = 0; k < K; ++k) me.fetch(dst + k * 512, src, k);
+      if (kFused && p.residual) {
+        const char* res = reinterpret_cast<const char*>(p.residual) + r_at;
+#pragma unroll
+        for (int k = 0; k < K; ++k) me.fetch(dst + (K + k) * 512, res, k);
+      }
+    }
+    copies_issued();
+    next += p.step;
+    x_at += p.x_step;
+    if (kFused) r_at += p.r_step;
+  };
+  if constexpr (!kShift) {      // what no copy reaches reads as zeros
+    for (int i = 0; i < p.stages * kStreams; ++i) {
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+        if (!me.has(k)) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(ring + (i * K + k) * 512), "r"(0) : "memory");
+    }
+  }
+  for (int i = 0; i < p.stages; ++i) fetch(ring + i * kStage);
+  stage_params<T, K, kSub>(p.gamma, p, me.lead, 2, 0, 1.0f, s_dyn);
+  stage_params<T, K, kSub>(p.beta, p, me.lead, 2, 1, 0.0f, s_dyn);
+  for (int i = threadIdx.x; i < 4 * kSlots; i += blockDim.x) s_sum[i] = 0.0f;
+  __syncthreads();
+  float* slots = s_sum + (kSub ? 0 : me.team * ((p.team + 127) >> 7) * 4);
+  const uint32_t offset = kFused ? drop_offset(p.d) : 0;
+  const float inv_c = 1.0f / (float)p.channels;
+  uint32_t stage = 0;
+  int turn = 0;
+  for (uint32_t row = me.row; row - me.ahead < p.rows; row += p.step) {      // (kSub: the same number of turns for all teams of a warp)
+    const bool live = !kSub || row < p.rows;
+    wait_copies(p.stages);
+    float x[K][V];
+    float sum[1] = {0.0f};
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      unpack<T>(shared_words(ring + stage + k * 512), x[k]);
+      me.clear(k, x[k]);
+      if constexpr (kFused) {
+        if (p.d.on) drop_chunk<V>(p.d, offset, number + me.byte(k) / 16, x[k]);
+        if (p.residual) {
+          float r[V];
+          unpack<T>(shared_words(ring + stage + (K + k) * 512), r);
+          me.clear(k, r);
+#pragma unroll
+          for (int j = 0; j < V; j += 2) add2(x[k][j], x[k][j + 1], r[j], r[j + 1]);
+        }
+        const Words h = pack_words<T>(x[k]);
+        store_chunk<T, V, kShift>(reinterpret_cast<char*>(p.h) + y_at + me.byte(k), live && me.has(k), live ? me.of(k) : 0, me.gaps(k), h);
+        unpack<T>(h, x[k]);
+      }
+    }
+    float part[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+#pragma unroll
+      for (int j = 0; j < V; j += 2) add2(part[0], part[1], x[k][j], x[k][j + 1]);
+    }
+    sum[0] = part[0] + part[1];
+    lanes_total<kSub>(sum, me.size);
+    if (!kSub && me.size > 32) warps_total(sum, me.team + 1, me.size, me.warp, me.lane, slots + turn);
+    fetch(ring + stage);                                    // (the sum is there: the place has been read)
+    const float mu = sum[0] * inv_c;
+    part[0] = part[1] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const float center = me.has(k) ? -mu : 0.0f;          // (no chunk: 0 - 0)
+#pragma unroll
+      for (int j = 0; j < V; j += 2) add2(x[k][j], x[k][j + 1], center, center);
+      me.clear(k, x[k]);
+#pragma unroll
+      for (int j = 0; j < V; j += 2) fma2(part[0], part[1], x[k][j], x[k][j + 1], x[k][j], x[k][j + 1], part[0], part[1]);
+    }
+    float m2[1] = {part[0] + part[1]};
+    lanes_total<kSub>(m2, me.size);
+    if (!kSub && me.size > 32) warps_total(m2, me.team + 1, me.size, me.warp, me.lane, slots + kSlots + turn);
+    const float rs = __frsqrt_rn(fmaf(m2[0], inv_c, p.eps));
+    if (me.lane == 0 && me.warp == 0 && live) {
+      p.mean[row] = mu;
+      p.rstd[row] = rs;
+    }
+    char* dst = reinterpret_cast<char*>(p.y) + y_at;
+    with_act(p.act, [&]<int kAct>() {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        float g[V], b[V];
+        staged<V>(mine, k, 2, 0, g);
+        staged<V>(mine, k, 2, 1, b);
+#pragma unroll
+        for (int j = 0; j < V; j += 2) {
+          mul2(x[k][j], x[k][j + 1], rs, rs);
+          fma2(x[k][j], x[k][j + 1], x[k][j], x[k][j + 1], g[j], g[j + 1], b[j], b[j + 1]);
+        }
+        if constexpr (kAct != HDQT_ACT_NONE) {
+#pragma unroll
+          for (int j = 0; j < V; ++j) x[k][j] = act_fwd<kAct>(x[k][j]);
+        }
+        store_chunk<T, V, kShift>(dst + me.byte(k), live && me.has(k), live ? me.of(k) : 0, me.gaps(k), pack_words<T>(x[k]));
+      }
+    });
+    stage = stage + kStage == p.stages * kStage ? 0 : stage + kStage;
+    turn ^= 2 * kSlots;
+    y_at += p.y_step;
+    if (kFused) number += p.chunk_step;
+  }
+}
+
+// ---- few rows: one per block, everything loaded at once --------------------------------------------------------
+
+template <typename T, int K, bool kFused, bool kShift>
+__global__ void __launch_bounds__(1024) once_fwd_kernel(const RowParams p) {
+  constexpr int V = 16 / sizeof(T);
+  __shared__ __align__(16) float s_sum[2 * kSlots];
+  const int64_t row = blockIdx.x;
+  const int lead = kShift ? (int)((row * p.channels) & (V - 1)) : 0;
+  const bool edge = row == p.rows - 1;
+  const char* src = reinterpret_cast<const char*>(p.x) + (row * p.x_rs - lead) * (int64_t)sizeof(T);
+  const char* res = reinterpret_cast<const char*>(p.residual) + (row * p.r_rs - lead) * (int64_t)sizeof(T);
+  const int64_t y_at = (row * p.y_rs - lead) * (int64_t)sizeof(T);
+  Words vx[K], vr[K];
+  uint32_t mask[K];
+  float g[K][V], b[K][V];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int q = k * blockDim.x + threadIdx.x, c = q * V - lead;
+    mask[k] = kShift ? chunk_mask<V>(p, c) : c < p.channels ? (1u << V) - 1 : 0;
+    vx[k] = load_chunk<T, V, kShift>(src + q * 16, mask[k], edge);
+    if constexpr (kFused) vr[k] = load_chunk<T, V, kShift>(res + q * 16, p.residual ? mask[k] : 0, edge);
+  }
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int c = (k * blockDim.x + threadIdx.x) * V - lead;
+    if (kShift) {
+      load_params_cut<V>(p.gamma, p, c, 1.0f, g[k]);
+      load_params_cut<V>(p.beta, p, c, 0.0f, b[k]);
+    } else if (mask[k]) {
+      load_params<V>(p.gamma, p, c, 1.0f, g[k]);
+      load_params<V>(p.beta, p, c, 0.0f, b[k]);
+    }
+  }
+  if (blockDim.x > 32) {
+    for (int i = threadIdx.x; i < 2 * kSlots; i += blockDim.x) s_sum[i] = 0.0f;
+    __syncthreads();
+  }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  float x[K][V];
+  float sum[1] = {0.0f};
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int q = k * blockDim.x + threadIdx.x;
+    unpack<T>(vx[k], x[k]);
+    clear_gaps<V, kShift>(mask[k], x[k]);
+    if constexpr (kFused) {
+      if (p.d.on) drop_chunk<V>(p.d, drop_offset(p.d), ((uint64_t)row * (uint64_t)p.channels - lead) / V + q, x[k]);
+      if (p.residual) {
+        float r[V];
+        unpack<T>(vr[k], r);
+        clear_gaps<V, kShift>(mask[k], r);
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[k][j] = __fadd_rn(r[j], x[k][j]);
+      }
+      const Words h = pack_words<T>(x[k]);
+      store_chunk<T, V, kShift>(reinterpret_cast<char*>(p.h) + y_at + q * 16, mask[k] != 0, mask[k], true, h);
+      unpack<T>(h, x[k]);
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum[0] += x[k][j];
+  }
+  lanes_total<false>(sum, 32);
+  if (blockDim.x > 32) warps_total(sum, 0, blockDim.x, warp, lane, s_sum);
+  const float inv_c = 1.0f / (float)p.channels, mu = sum[0] * inv_c;
+  float m2[1] = {0.0f};
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const float center = mask[k] ? mu : 0.0f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[k][j] -= center;
+    clear_gaps<V, kShift>(mask[k], x[k]);
+#pragma unroll
+    for (int j = 0; j < V; ++j) m2[0] = fmaf(x[k][j], x[k][j], m2[0]);
+  }
+  lanes_total<false>(m2, 32);
+  if (blockDim.x > 32) warps_total(m2, 0, blockDim.x, warp, lane, s_sum + kSlots);
+  const float rs = __frsqrt_rn(fmaf(m2[0], inv_c, p.eps));
+  if (threadIdx.x == 0) {
+    p.mean[row] = mu;
+    p.rstd[row] = rs;
+  }
+  with_act(p.act, [&]<int kAct>() {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) x[k][j] = act_fwd<kAct>(fmaf(x[k][j] * rs, g[k][j], b[k][j]));
+      store_chunk<T, V, kShift>(reinterpret_cast<char*>(p.y) + y_at + (k * blockDim.x + threadIdx.x) * 16, mask[k] != 0, mask[k], true,
+                                pack_words<T>(x[k]));
+    }
+  });
+}
+
+// ---- any strides and addresses, rows in registers --------------------------------------------------------------
+
+template <typename T, int V, int K, bool kFused>
+__global__ void __launch_bounds__(1024) any_fwd_kernel(const RowParams p) {
+  using A = Vec<T, V>;
+  __shared__ float s_sum[2][32];
+  extern __shared__ __align__(16) char s_dyn[];
+  const int size = p.team, team = threadIdx.x / size, t = threadIdx.x - team * size;
+  const int64_t row = (int64_t)blockIdx.x * (blockDim.x / size) + team;
+  const bool live = row < p.rows;
+  uint8_t* bits = reinterpret_cast<uint8_t*>(s_dyn) + team * p.bits_stride;
+
+  A vx[K], vr[K];
+  const T* src = reinterpret_cast<const T*>(p.x) + row * p.x_rs;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int c = (k * size + t) * V;
+    vx[k] = A{};
+    if (live && c < p.channels) vx[k] = *reinterpret_cast<const A*>(src + c);
+  }
+  if constexpr (kFused) {
+    const T* res = reinterpret_cast<const T*>(p.residual) + row * p.r_rs;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c = (k * size + t) * V;
+      vr[k] = A{};
+      if (p.residual && live && c < p.channels) vr[k] = *reinterpret_cast<const A*>(res + c);
+    }
+    if (V < 8 && p.d.on) {
+      if (live) row_bits(p, row, t, size, bits);
+      team_barrier(team, size);
+    }
+  }
+
+  float x[K][V];
+  float sum[1] = {0.0f};
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int c = (k * size + t) * V;
+    unpack(vx[k], x[k]);
+    if constexpr (kFused) {
+      float r[V];
+      unpack(vr[k], r);
+      if (p.d.on && live && c < p.channels) {
+        const uint32_t b = chunk_bits<V>(p, row, c, bits);
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[k][j] = dropped(x[k][j], b, j, p.d.scale);
+      }
+      if (p.residual) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[k][j] = __fadd_rn(r[j], x[k][j]);
+      }
+      const A h = pack<T>(x[k]);
+      if (live && c < p.channels) *reinterpret_cast<A*>(reinterpret_cast<T*>(p.h) + row * p.y_rs + c) = h;
+      unpack(h, x[k]);
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum[0] += x[k][j];
+  }
+  team_sum(sum, team, t, size, s_sum[0]);
+  const float mu = sum[0] / (float)p.channels;
+  float m2[1] = {0.0f};
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    if ((k * size + t) * V < p.channels) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float e = x[k][j] - mu;
+        m2[0] = fmaf(e, e, m2[0]);
+      }
+    }
+  }
+  team_sum(m2, team, t, size, s_sum[1]);
+  const float rs = __frsqrt_rn(m2[0] / (float)p.channels + p.eps);
+  if (!live) return;
+  if (t == 0) {
+    p.mean[row] = mu;
+    p.rstd[row] = rs;
+  }
+  T* dst = reinterpret_cast<T*>(p.y) + row * p.y_rs;
+  with_act(p.act, [&]<int kAct>() {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c = (k * size + t) * V;
+      if (c < p.channels) {
+        float g[V], b[V], o[V];
+        load_params(p.gamma, p, c, 1.0f, g);
+        load_params(p.beta, p, c, 0.0f, b);
+#pragma unroll
+        for (int j = 0; j < V; ++j) o[j] = act_fwd<kAct>(fmaf((x[k][j] - mu) * rs, g[j], b[j]));
+        *reinterpret_cast<A*>(dst + c) = pack<T>(o);
+      }
+    }
+  });
+}
+
+// ---- rows of any length, read again from the L2 ----------------------------------------------------------------
+
+template <typename T, int V, bool kFused>
+__global__ void __launch_bounds__(kLongThreads) long_fwd_kernel(const RowParams p) {
+  using A = Vec<T, V>;
+  __shared__ float s_sum[2][32];
+  const int t = threadIdx.x;
+  const uint32_t offset = kFused ? drop_offset(p.d) : 0;
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+    const T* src = reinterpret_cast<const T*>(p.x) + row * p.x_rs;
+    T* dst = reinterpret_cast<T*>(p.y) + row * p.y_rs;
+    T* hs = kFused ? reinterpret_cast<T*>(p.h) + row * p.y_rs : nullptr;
+    float sum[1] = {0.0f};
+    for (int c = t * V; c < p.channels; c += kLongThreads * V) {
+      float x[V];
+      unpack(*reinterpret_cast<const A*>(src + c), x);
+      if constexpr (kFused) {
+        if (p.d.on) {
+          const uint64_t i = (uint64_t)row * (uint64_t)p.channels + c;
+          const uint32_t b = drop_bits(p.d, offset, i >> 3) >> (i & 7);
+#pragma unroll
+          for (int j = 0; j < V; ++j) x[j] = dropped(x[j], b, j, p.d.scale);
+        }
+        if (p.residual) {
+          float r[V];
+          unpack(*reinterpret_cast<const A*>(reinterpret_cast<const T*>(p.residual) + row * p.r_rs + c), r);
+#pragma unroll
+          for (int j = 0; j < V; ++j) x[j] = __fadd_rn(r[j], x[j]);
+        }
+        const A h = pack<T>(x);
+        *reinterpret_cast<A*>(hs + c) = h;
+        unpack(h, x);
+      }
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum[0] += x[j];
+    }
+    team_sum(sum, 0, t, kLongThreads, s_sum[0]);
+    const float mu = sum[0] / (float)p.channels;
+    const T* in = kFused ? hs : src;                                // (a thread reads back what it has written itself)
+    float m2[1] = {0.0f};
+    for (int c = t * V; c < p.channels; c += kLongThreads * V) {
+      float x[V];
+      unpack(*reinterpret_cast<const A*>(in + c), x);
+#pragma unroll
+      for (int j = 0; j < V; ++j) m2[0] = fmaf(x[j] - mu, x[j] - mu, m2[0]);
+    }
+    team_sum(m2, 0, t, kLongThreads, s_sum[1]);
+    const float rs = __frsqrt_rn(m2[0] / (float)p.channels + p.eps);
+    if (t == 0) {
+      p.mean[row] = mu;
+      p.rstd[row] = rs;
+    }
+    with_act(p.act, [&]<int kAct>() {
+      for (int c = t * V; c < p.channels; c += kLongThreads * V) {
+        float x[V], g[V], b[V];
+        unpack(*reinterpret_cast<const A*>(in + c), x);
+        load_params(p.gamma, p, c, 1.0f, g);
+        load_params(p.beta, p, c, 0.0f, b);
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = act_fwd<kAct>(fmaf((x[j] - mu) * rs, g[j], b[j]));
+        *reinterpret_cast<A*>(dst + c) = pack<T>(x);
+      }
+    });
+  }
+}
+
+// ---- host side -----------------------------------------------------------------------------------------------
+
+template <typename T, int K, bool kFused, bool kSub>
+bool fwd_teams(RowParams p, hdqt_status_t* st, cudaStream_t s) {
+  constexpr int V = 16 / sizeof(T), kThreads = K * V == 32 ? 768 : 1024;
+  p.team = team_size(row_chunks(p, V), K);
+  Shape shape;
+  if (p.team > kThreads || !shape_of(&p, sizeof(T), K, 2, kFused ? 2 : 1, kThreads, false, &shape)) return false;
+  if (p.classes > 1) *st = launch_rows<team_fwd_kernel<T, K, kFused, true, kSub, kThreads>>(p, shape, s);
+  else *st = launch_rows<team_fwd_kernel<T, K, kFused, false, kSub, kThreads>>(p, shape, s);
+  return true;
+}
+
+template <typename T, int K, bool kFused>
+hdqt_status_t fwd_once(const RowParams& p, cudaStream_t s) {
+  const int n = (row_chunks(p, 16 / sizeof(T)) + K - 1) / K, threads = (n + 31) / 32 * 32;
+  if (p.classes > 1) once_fwd_kernel<T, K, kFused, true><<<(unsigned)p.rows, threads, 0, s>>>(p);
+  else once_fwd_kernel<T, K, kFused, false><<<(unsigned)p.rows, threads, 0, s>>>(p);
+  return last_error("layer norm");
+}
+
+template <typename T, bool kFused>
+hdqt_status_t run_fwd(RowParams p, bool wide, cudaStream_t s) {
+  constexpr int V = 16 / sizeof(T), kMost = 32 / V;      // chunks of a thread
+  if (wide) {
+    hdqt_status_t st = HDQT_OK;
+    const int chunks = row_chunks(p, V);
+    const int64_t total = p.rows * chunks;
+    const bool once = total <= (p.classes > 1 ? 100000 : 300000);
+    if (once && chunks <= 2048) return chunks <= 1024 ? fwd_once<T, 1, kFused>(p, s) : fwd_once<T, 2, kFused>(p, s);
+    constexpr int kBest = kFused || sizeof(T) == 4 ? kMost / 2 : kMost;
+    const int k = kFused && sizeof(T) == 4 ? kMost / 4 : kBest;
+    if (chunks <= 16 * (8 / V)) {
+      if (fwd_teams<T, 8 / V, kFused, true>(p, &st, s)) return st;
+    } else {
+      if ((k <= kMost / 4 || chunks <= 16 * (kMost / 2)) && fwd_teams<T, kMost / 4, kFused, false>(p, &st, s)) return st;
+      if ((k <= kMost / 2 || chunks <= 16 * kMost) && fwd_teams<T, kMost / 2, kFused, false>(p, &st, s)) return st;
+      if (fwd_teams<T, kMost, kFused, false>(p, &st, s)) return st;
+    }
+  }
+  p.classes = 1;
+  p.team = team_size(p.channels, 16);
+  if (p.team <= 1024 && !wide) {
+    const int per_block = p.team <= 32 ? 128 / p.team : 1, block = p.team <= 32 ? 128 : p.team;
+    p.bits_stride = p.channels / 8 + 2;
+    const size_t smem = kFused ? (size_t)per_block * p.bits_stride : 0;
+    any_fwd_kernel<T, 1, 16, kFused><<<(unsigned)((p.rows + per_block - 1) / per_block), block, smem, s>>>(p);
+    return last_error("layer norm");
+  }
+  const unsigned blocks = (unsigned)(p.rows < 2 * kNumSMsHint ? p.rows : 2 * kNumSMsHint);
+  if (wide && p.channels % V == 0) long_fwd_kernel<T, V, kFused><<<blocks, kLongThreads, 0, s>>>(p);
+  else long_fwd_kernel<T, 1, kFused><<<blocks, kLongThreads, 0, s>>>(p);
+  return last_error("layer norm");
+}
+
+hdqt_status_t forward(const hdqt_layer_norm_desc_t* d, bool fused, const void* x, const void* residual, const void* gamma,
+                      const void* beta, void* h, void* y, float* mean, float* rstd, void* stream) {
+  const hdqt_status_t st = check_rows_desc(d, fused);
+  if (st != HDQT_OK) return st;
+  if (d->rows == 0) return HDQT_OK;
+  if (!x || !y || !mean || !rstd || (fused && !h)) return HDQT_ERR_INVALID_ARG;
+  if (residual && d->rows > 1 && d->r_row_stride < d->channels) return HDQT_ERR_INVALID_ARG;
+  const int elem = dtype_size(d->dtype), pelem = dtype_size(d->param_dtype);
+  const uintptr_t bases = bits_of(x) | bits_of(residual) | bits_of(h) | bits_of(y);
+  if ((bases & (uintptr_t)(elem - 1)) || ((bits_of(gamma) | bits_of(beta)) & (uintptr_t)(pelem - 1)) ||
+      ((bits_of(mean) | bits_of(rstd)) & 3) || (fused && (bits_of(d->philox_offset) & 3)))
+    return HDQT_ERR_ALIGNMENT;
+  RowParams p = make_row_params(*d, gamma, beta, mean, rstd);
+  p.x = x;
+  p.residual = residual;
+  p.h = h;
+  p.y = y;
+  if (fused) p.d = make_drop(d->p, d->seed, d->tag, d->philox_offset);
+  const uintptr_t strides = d->rows > 1 ? (uintptr_t)((p.x_rs | p.y_rs | (residual ? p.r_rs : 0)) * elem) : 0;
+  const bool dense = d->rows == 1 || (p.x_rs == d->channels && p.y_rs == d->channels && (!residual || p.r_rs == d->channels));
+  const bool wide = set_classes(&p, elem, bases, dense, strides);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  return with_type(d->dtype, [&]<typename T>() { return fused ? run_fwd<T, true>(p, wide, s) : run_fwd<T, false>(p, wide, s); });
+}
+
+}  // namespace
+
+}  // namespace hdqt
+
+using namespace hdqt;
+
+extern "C" hdqt_status_t hdqt_layer_norm_fwd(const hdqt_layer_norm_desc_t* d, const void* x, const void* gamma, const void* beta,
+                                             void* y, float* mean, float* rstd, void* stream) {
+  return forward(d, false, x, nullptr, gamma, beta, nullptr, y, mean, rstd, stream);
+}
+
+extern "C" hdqt_status_t hdqt_dropout_add_layer_norm_fwd(const hdqt_layer_norm_desc_t* d, const void* x, const void* residual,
+                                                         const void* gamma, const void* beta, void* h, void* y, float* mean,
+                                                         float* rstd, void* stream) {
+  return forward(d, true, x, residual, gamma, beta, h, y, mean, rstd, stream);
+}

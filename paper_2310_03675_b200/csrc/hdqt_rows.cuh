@@ -1,0 +1,547 @@
+// Rows of a tensor in registers: what the forward and backward kernels of layer norm (alone, or behind dropout and a residual add)
+// share.
+//
+//   z = gamma (x - mu) rs + beta,  y = act(z);  dz = dy act'(z)
+//   dx = rs (gamma dz - mean(gamma dz) - xhat mean(gamma dz xhat)),  dgamma = sum dz xhat,  dbeta = sum dz
+//
+// Bound by HBM: every input read once, every output written once.  A "team" of threads (part of a warp up to a whole block) holds a
+// row; the mean and then the sum of squared deviations are taken over the same registers (no cancellation however large the
+// mean).  Three kinds of kernels: teams that walk over the rows (team_*), one row per block for few rows (once_*), and any_* for
+// strides and addresses that no 16-byte access fits; rows wider than registers are read again from the L2 (long_*).
+//
+// A row is cut at the 16-byte boundaries of memory into chunks of V elements.  Where the channels are not a multiple of V, rows of a
+// dense tensor start `lead` elements behind a boundary, lead = (row * channels) mod V, which repeats every `classes` rows.  A block
+// keeps to the rows of one class, so that all its rows are cut alike: element j of chunk q is channel q V - lead + j, and a chunk
+// that is shared with a neighbouring row is masked.
+#pragma once
+
+#include <math.h>
+
+#include <atomic>
+
+#include "hdqt_dropout.cuh"
+
+namespace hdqt {
+
+constexpr int kLongThreads = 1024;
+constexpr int kMostParts = 2 * kNumSMsHint;      // blocks that leave sums of dgamma and dbeta
+constexpr int kMostStages = 2;
+constexpr size_t kMostSmem = 224 * 1024;         // dynamic shared memory of an SM's blocks together
+
+struct RowParams {
+  const void* x;                 // x, or h (fused backward)
+  const void* residual;
+  const void* dy;
+  const void* dh;
+  void* y;
+  void* h;
+  void* dx;
+  void* dres;
+  const void* gamma;
+  const void* beta;
+  int32_t param_dtype, act, channels;
+  int32_t team;                  // threads of a row: a power of two below 32, or a multiple of 32
+  int32_t stages;                // rows a team has in flight
+  int32_t classes;               // rows that are cut at different places (1 = all alike)
+  int32_t params_wide;           // gamma and beta start on 16-byte boundaries
+  int32_t bits_stride;           // any_*: bytes of a team's dropout decisions in shared memory
+  int64_t rows, x_rs, r_rs, y_rs;
+  uint32_t step;                 // rows from a team's row to its next
+  int64_t x_step, r_step, y_step, chunk_step;      // the same in bytes of the tensors, and in chunks of a dense tensor
+  float eps;
+  float* mean;
+  float* rstd;
+  float2* part;                  // [blocks, channels] sums of dbeta (x) and dgamma (y)
+  DropParams d;
+};
+
+// ---- pairs of fp32 operations as one instruction ----------------------------------------------------------------
+
+__device__ __forceinline__ void add2(float& a0, float& a1, float b0, float b1) {
+  asm("{\n.reg .b64 a, b;\nmov.b64 a, {%0, %1};\nmov.b64 b, {%2, %3};\nadd.rn.f32x2 a, a, b;\nmov.b64 {%0, %1}, a;\n}"
+      : "+f"(a0), "+f"(a1) : "f"(b0), "f"(b1));
+}
+__device__ __forceinline__ void mul2(float& a0, float& a1, float b0, float b1) {
+  asm("{\n.reg .b64 a, b;\nmov.b64 a, {%0, %1};\nmov.b64 b, {%2, %3};\nmul.rn.f32x2 a, a, b;\nmov.b64 {%0, %1}, a;\n}"
+      : "+f"(a0), "+f"(a1) : "f"(b0), "f"(b1));
+}
+// o = a b + c
+__device__ __forceinline__ void fma2(float& o0, float& o1, float a0, float a1, float b0, float b1, float c0, float c1) {
+  asm("{\n.reg .b64 a, b, c;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\nfma.rn.f32x2 a, a, b, c;\nmov.b64 {%0, %1}, a;\n}"
+      : "=f"(o0), "=f"(o1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1), "f"(c0), "f"(c1));
+}
+
+// ---- gamma and beta ------------------------------------------------------------------------------------------
+
+// V elements of gamma or beta from channel c on
+template <int V>
+__device__ __forceinline__ void load_params(const void* p, const RowParams& q, int c, float fill, float (&f)[V]) {
+  if (p == nullptr) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) f[j] = fill;
+  } else if (!q.params_wide || V == 1) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) f[j] = load_param(p, q.param_dtype, c + j);
+  } else if (q.param_dtype == HDQT_DTYPE_F32) {
+    constexpr int W = V < 4 ? V : 4;
+#pragma unroll
+    for (int j = 0; j < V; j += W) {
+      const Vec<float, W> v = *reinterpret_cast<const Vec<float, W>*>(reinterpret_cast<const float*>(p) + c + j);
+#pragma unroll
+      for (int i = 0; i < W; ++i) f[j + i] = v.v[i];
+    }
+  } else if (q.param_dtype == HDQT_DTYPE_BF16) {
+    unpack(*reinterpret_cast<const Vec<__nv_bfloat16, V>*>(reinterpret_cast<const __nv_bfloat16*>(p) + c), f);
+  } else {
+    unpack(*reinterpret_cast<const Vec<__half, V>*>(reinterpret_cast<const __half*>(p) + c), f);
+  }
+}
+
+// the same from a channel that may lie outside the row: 0 there
+template <int V>
+__device__ __forceinline__ void load_params_cut(const void* p, const RowParams& q, int c, float fill, float (&f)[V]) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    f[j] = 0.0f;
+    if (c + j >= 0 && c + j < q.channels) f[j] = p ? load_param(p, q.param_dtype, c + j) : fill;
+  }
+}
+
+// ---- sums over a team ----------------------------------------------------------------------------------------
+
+__device__ __forceinline__ void team_barrier(int team, int size) {
+  if (size <= 32) __syncwarp();
+  else if (size == (int)blockDim.x) __syncthreads();
+  else asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(size) : "memory");
+}
+
+
+// Sums over the lanes of a warp, or of `size` < 32 lanes (kSub).
+template <bool kSub, int N>
+__device__ __forceinline__ void lanes_total(float (&v)[N], int size) {
+#pragma unroll
+  for (int d = kSub ? 8 : 16; d > 0; d >>= 1) {
+    if (!kSub || d < size) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], d);
+    }
+  }
+}
+// Sums over a team of several warps that have summed up for themselves: a value per warp in the team's slots, which come in fours,
+// hold zeros behind the last warp (cleared before the first call) and are not in use since the barrier before the last one.
+// barrier 0 is the whole block's.
+constexpr int kSlots = 96;          // of a block: four for every team of two to four warps
+template <int N>
+__device__ __forceinline__ void warps_total(float (&v)[N], int barrier, int size, int warp, int lane, float* s) {
+  if (lane == 0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i * kSlots + warp] = v[i];
+  }
+  asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(size) : "memory");
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    float4 a = *reinterpret_cast<const float4*>(s + i * kSlots);
+    for (int q = 4; q * 32 < size; q += 4) {
+      const float4 b = *reinterpret_cast<const float4*>(s + i * kSlots + q);
+      a.x += b.x;
+      a.y += b.y;
+      a.z += b.z;
+      a.w += b.w;
+    }
+    v[i] = (a.x + a.y) + (a.z + a.w);
+  }
+}
+
+// ---- chunks --------------------------------------------------------------------------------------------------
+
+// 16 bytes of shared memory from src, zeros behind the first `bytes`
+__device__ __forceinline__ void copy_async(uint32_t dst, const char* src, uint32_t bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// all but the copies of the last stages - 1 rows have arrived
+__device__ __forceinline__ void wait_copies(int stages) {
+  if (stages == 1) asm volatile("cp.async.wait_group 0;" ::: "memory");
+  else if (stages == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+  else if (stages == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+  else asm volatile("cp.async.wait_group 3;" ::: "memory");
+}
+
+// elements [first, first + V) of a chunk that belong to the row, as bits
+template <int V>
+__device__ __forceinline__ uint32_t chunk_mask(const RowParams& p, int first) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int j = 0; j < V; ++j)
+    if (first + j >= 0 && first + j < p.channels) m |= 1u << j;
+  return m;
+}
+// zeros in the place of a neighbouring row's elements
+template <int V, bool kShift>
+__device__ __forceinline__ void clear_gaps(uint32_t mask, float (&f)[V]) {
+  if constexpr (kShift) {
+    if (mask != (1u << V) - 1) {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (!((mask >> j) & 1)) f[j] = 0.0f;
+    }
+  }
+}
+// `any`: some of the chunk belongs to the row.  `ragged`: a chunk of this warp may have gaps.
+template <typename T, int V, bool kShift>
+__device__ __forceinline__ void store_chunk(char* dst, bool any, uint32_t mask, bool ragged, const Words& v) {
+  if constexpr (!kShift) {
+    if (any) *reinterpret_cast<Words*>(dst) = v;
+  } else {
+    if (mask == (1u << V) - 1) *reinterpret_cast<Words*>(dst) = v;
+    if (ragged && mask != (1u << V) - 1) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        if ((mask >> j) & 1) {
+          if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t*>(dst)[j] = v.w[j];
+          else reinterpret_cast<uint16_t*>(dst)[j] = (uint16_t)(v.w[j / 2] >> (16 * (j & 1)));
+        }
+      }
+    }
+  }
+}
+// The chunk at src, with a neighbouring row's elements in it where the mask has gaps.  `edge`: the row's end may be the tensor's, so
+// that a shared chunk is read element by element.
+template <typename T, int V, bool kShift>
+__device__ __forceinline__ Words load_chunk(const char* src, uint32_t mask, bool edge) {
+  Words v{};
+  if (kShift && edge && mask != (1u << V) - 1) {
+    if constexpr (kShift) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+          if ((mask >> i) & 1) v.w[i] = reinterpret_cast<const uint32_t*>(src)[i];
+        } else {
+          if ((mask >> (2 * i)) & 1) v.w[i] = reinterpret_cast<const uint16_t*>(src)[2 * i];
+          if ((mask >> (2 * i)) & 2) v.w[i] |= (uint32_t) reinterpret_cast<const uint16_t*>(src)[2 * i + 1] << 16;
+        }
+      }
+    }
+  } else if (mask != 0) {
+    v = *reinterpret_cast<const Words*>(src);
+  }
+  return v;
+}
+
+// random words of chunk number i (of the flattened tensor), its elements the first V
+template <int V>
+__device__ __forceinline__ Philox4 chunk_words(const DropParams& d, uint32_t offset, uint64_t i) {
+  if constexpr (V == 8) return drop_words(d, offset, i);
+  Philox4 w = drop_words(d, offset, i >> 1);
+  if (i & 1) {
+    w.w[0] = w.w[2];
+    w.w[1] = w.w[3];
+  }
+  return w;
+}
+template <int V>
+__device__ __forceinline__ void drop_chunk(const DropParams& d, uint32_t offset, uint64_t i, float (&x)[V]) {
+  const Philox4 w = chunk_words<V>(d, offset, i);
+#pragma unroll
+  for (int j = 0; j < V; ++j) x[j] = drop_keeps(w, j, d.limit) ? __fmul_rn(x[j], d.scale) : 0.0f;
+}
+
+// ---- where a thread of a walking team stands -------------------------------------------------------------------
+//
+// A warp of a team holds 32 K consecutive chunks, lane l the chunks l, l + 32, ... of them, so that a thread's places in memory and
+// in shared memory are constants apart.  kSub: a team is part of a warp, lane t holds the chunks t, t + size, ...
+//
+// Every thread copies the chunks of its next rows into places of its own in shared memory (asynchronously, `stages` rows ahead): what
+// is in flight takes no registers, and nobody else has to be waited for.  gamma and beta stand in shared memory in the
+// order of the threads, in fp32.
+
+template <typename T, int K, bool kShift, bool kSub>
+struct Place {
+  static constexpr int V = 16 / sizeof(T), H = V / 4;
+  int size, team, teams, warp, lane;      // threads of a team; this thread's team, warp of the team, lane of the warp or team
+  int lead;
+  int left;                               // bytes from this thread's first chunk to the row's end
+  uint32_t first;                         // bytes from the row's first chunk to this thread's first
+  uint32_t row;
+  uint32_t ahead;                         // kSub: to the row of this warp's first team
+  uint32_t mask;                          // kShift: V bits per chunk, elements that belong to the row
+  uint32_t ragged;                        // kShift: bit k: a lane of this warp shares its chunk k with a neighbouring row
+  __device__ __forceinline__ Place(const RowParams& p) {
+    static_assert(V * K <= 32);
+    size = p.team;
+    teams = blockDim.x / size;
+    if constexpr (kSub) {
+      team = threadIdx.x / size;
+      lane = threadIdx.x - team * size;
+      warp = 0;
+    } else {
+      const int warps = size >> 5, w = threadIdx.x >> 5;
+      team = w / warps;
+      warp = w - team * warps;
+      lane = threadIdx.x & 31;
+    }
+    const uint32_t cls = kShift ? blockIdx.x % p.classes : 0;
+    row = (blockIdx.x / p.classes * teams + team) * p.classes + cls;
+    ahead = kSub ? (threadIdx.x & 31) / size * p.classes : 0;
+    lead = kShift ? (int)(((int64_t)cls * p.channels) & (V - 1)) : 0;
+    first = (uint32_t)(warp * K * 32 + lane) * 16u;
+    left = (p.channels + lead) * (int)sizeof(T) - (int)first;
+    mask = ragged = 0;
+    if constexpr (kShift) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const uint32_t m = chunk_mask<V>(p, (int)((first + byte(k)) / sizeof(T)) - lead);
+        mask |= m << (k * V);
+        if (__any_sync(0xFFFFFFFFu, m != 0 && m != (1u << V) - 1)) ragged |= 1u << k;
+      }
+    }
+    // (kept, not worked out again in every row)
+    asm volatile("" : "+r"(row), "+r"(first), "+r"(left), "+r"(mask), "+r"(ragged));
+  }
+  __device__ __forceinline__ uint32_t byte(int k) const { return kSub ? (uint32_t)(k * size) * 16u : k * 512u; }    // from the first chunk
+  __device__ __forceinline__ bool has(int k) const { return left > (int)byte(k); }
+  __device__ __forceinline__ uint32_t of(int k) const { return (mask >> (k * V)) & ((1u << V) - 1); }
+  __device__ __forceinline__ bool gaps(int k) const { return kShift && ((ragged >> k) & 1); }
+  // zeros in the place of a neighbouring row's elements
+  __device__ __forceinline__ void clear(int k, float (&f)[V]) const {
+    if (gaps(k)) clear_gaps<V, kShift>(of(k), f);
+  }
+  // bytes from base to this thread's first chunk in row r
+  __device__ __forceinline__ int64_t offset(int64_t stride, int64_t r) const { return (r * stride - lead) * (int64_t)sizeof(T) + first; }
+  // number of that chunk in a dense tensor
+  __device__ __forceinline__ uint64_t number(const RowParams& p) const {
+    return ((uint64_t)row * (uint64_t)p.channels - lead) / V + first / 16;
+  }
+  __device__ __forceinline__ void fetch(uint32_t dst, const char* src, int k) const {
+    if constexpr (kShift) copy_async(dst, src + byte(k), (uint32_t)max(0, min(16, left - (int)byte(k))));
+    else if (has(k)) copy_async(dst, src + byte(k), 16);
+  }
+};
+
+// bytes of shared memory of kParams (gamma, beta) in the threads' order
+template <typename T, int K>
+__host__ __device__ constexpr uint32_t params_bytes(int team, int params) {
+  return (uint32_t)((team < 32 ? 32 : team) * K * (16 / (int)sizeof(T)) * 4 * params);
+}
+// One of them, which = 0 or 1 of `params`: [warp][k][which][four elements][lane]
+template <typename T, int K, bool kSub>
+__device__ __forceinline__ void stage_params(const void* src, const RowParams& p, int lead, int params, int which, float fill, char* s) {
+  constexpr int V = 16 / sizeof(T), H = V / 4;
+  const int slots = (kSub ? 32 : p.team) * K;
+  for (int i = threadIdx.x; i < slots * H; i += blockDim.x) {
+    const int half = i % H, slot = i / H, lane = slot & 31, group = slot >> 5;      // group = warp * K + k
+    const int chunk = kSub ? group * p.team + lane : slot;
+    const int c = chunk * V + half * 4 - lead;
+    float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (!kSub || lane < p.team) {
+      if (lead == 0 && c + 4 <= p.channels) load_params<4>(src, p, c, fill, f);
+      else load_params_cut<4>(src, p, c, fill, f);
+    }
+    *reinterpret_cast<float4*>(s + ((group * params + which) * H + half) * 512 + lane * 16) = make_float4(f[0], f[1], f[2], f[3]);
+  }
+}
+// the V of chunk k, from the thread's place (warp and lane) on
+template <int V>
+__device__ __forceinline__ void staged(const char* s, int k, int params, int which, float (&f)[V]) {
+  constexpr int H = V / 4;
+#pragma unroll
+  for (int i = 0; i < H; ++i) {
+    const float4 v = *reinterpret_cast<const float4*>(s + ((k * params + which) * H + i) * 512);
+    f[4 * i] = v.x;
+    f[4 * i + 1] = v.y;
+    f[4 * i + 2] = v.z;
+    f[4 * i + 3] = v.w;
+  }
+}
+
+__device__ __forceinline__ Words shared_words(uint32_t at) {
+  Words v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]) : "r"(at) : "memory");
+  return v;
+}
+
+// ---- any strides and addresses: one element per access --------------------------------------------------------
+
+// Sums over the threads of a team; every thread gets them.  s: one slot of N per warp of the block, not in use since the barrier
+// before the last one.
+template <int N>
+__device__ __forceinline__ void team_sum(float (&v)[N], int team, int t, int size, float* s) {
+  for (int d = (size < 32 ? size : 32) >> 1; d > 0; d >>= 1) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], d);
+  }
+  if (size <= 32) return;
+  const int warps = size >> 5, lane = t & 31;
+  s += team * warps * N;
+  if (lane == 0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[(t >> 5) * N + i] = v[i];
+  }
+  team_barrier(team, size);
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = lane < warps ? s[lane * N + i] : 0.0f;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], d);
+  }
+}
+
+// Dropout decisions of a whole row for accesses narrower than a Philox group of eight: a byte per group in shared memory (visible
+// after the team's next barrier), bit (o & 7) of byte o >> 3 for the element at o = (row * channels) % 8 + channel.
+__device__ __forceinline__ void row_bits(const RowParams& p, int64_t row, int t, int size, uint8_t* bits) {
+  const uint64_t first = (uint64_t)row * (uint64_t)p.channels;
+  const int groups = ((int)(first & 7) + p.channels + 7) >> 3;
+  const uint32_t offset = drop_offset(p.d);
+  for (int k = t; k < groups; k += size) bits[k] = (uint8_t)drop_bits(p.d, offset, (first >> 3) + k);
+}
+// those of the V elements from channel c on
+template <int V>
+__device__ __forceinline__ uint32_t chunk_bits(const RowParams& p, int64_t row, int c, const uint8_t* bits) {
+  if constexpr (V == 8) return drop_bits(p.d, drop_offset(p.d), ((uint64_t)row * (uint64_t)p.channels + c) >> 3);
+  const int o = ((int)((uint64_t)row * (uint64_t)p.channels) & 7) + c;
+  return bits[o >> 3] >> (o & 7);
+}
+
+// x scale where kept, else 0
+__device__ __forceinline__ float dropped(float x, uint32_t bits, int j, float scale) {
+  return (bits >> j) & 1 ? __fmul_rn(x, scale) : 0.0f;
+}
+
+template <typename T>
+__device__ __forceinline__ float rounded(float v) { return to_f32(from_f32<T>(v)); }
+
+
+// ---- host side -----------------------------------------------------------------------------------------------
+
+inline uintptr_t bits_of(const void* p) { return reinterpret_cast<uintptr_t>(p); }
+
+inline hdqt_status_t check_rows_desc(const hdqt_layer_norm_desc_t* d, bool fused) {
+  if (!d) return HDQT_ERR_INVALID_ARG;
+  if (d->rows < 0 || d->channels <= 0 || dtype_size(d->dtype) == 0) return HDQT_ERR_INVALID_ARG;
+  if (d->param_dtype != HDQT_DTYPE_F32 && d->param_dtype != d->dtype) return HDQT_ERR_INVALID_ARG;
+  if (d->act < HDQT_ACT_NONE || d->act > HDQT_ACT_SILU || !(d->eps >= 0.0f)) return HDQT_ERR_INVALID_ARG;
+  if (d->rows > 1 && (d->x_row_stride < d->channels || d->y_row_stride < d->channels)) return HDQT_ERR_INVALID_ARG;
+  if (fused && !valid_probability(d->p)) return HDQT_ERR_INVALID_ARG;
+  if (d->channels > (1 << 20) || d->rows > 0x7FFFFFFFll) return HDQT_ERR_UNSUPPORTED;
+  return HDQT_OK;
+}
+
+inline RowParams make_row_params(const hdqt_layer_norm_desc_t& d, const void* gamma, const void* beta, float* mean, float* rstd) {
+  RowParams p{};
+  p.gamma = gamma;
+  p.beta = beta;
+  p.param_dtype = d.param_dtype;
+  p.act = d.act;
+  p.channels = (int32_t)d.channels;
+  p.params_wide = ((bits_of(gamma) | bits_of(beta)) & 15) == 0;
+  p.rows = d.rows;
+  p.x_rs = d.x_row_stride;
+  p.r_rs = d.r_row_stride;
+  p.y_rs = d.y_row_stride;
+  p.eps = d.eps;
+  p.mean = mean;
+  p.rstd = rstd;
+  return p;
+}
+
+// 16-byte accesses: rows of whole chunks on 16-byte boundaries, or dense tensors that start on one (rows cut at the boundaries)
+inline bool set_classes(RowParams* p, int elem, uintptr_t bases, bool dense, uintptr_t strides) {
+  const int v = 16 / elem;
+  p->classes = 1;
+  if (bases & 15) return false;
+  if (p->channels % v == 0 && (strides & 15) == 0) return true;
+  if (!dense) return false;
+  while ((int64_t)p->channels * p->classes % v != 0) p->classes *= 2;
+  return true;
+}
+
+inline int row_chunks(const RowParams& p, int vec) { return (p.channels + (p.classes > 1 ? vec - 1 : 0) + vec - 1) / vec; }
+
+// threads of a row with k chunks each: a power of two, or whole warps
+inline int team_size(int chunks, int k) {
+  const int n = (chunks + k - 1) / k;
+  if (n > 16) return (n + 31) / 32 * 32;
+  int size = 1;
+  while (size < n) size *= 2;
+  return size;
+}
+
+// the shared memory limit of a kernel, raised at its first launch on a device
+template <auto kernel>
+hdqt_status_t allow_smem() {
+  static std::atomic<uint64_t> ready{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && (dev > 63 || !((ready.load(std::memory_order_relaxed) >> dev) & 1))) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem);
+    if (e == cudaSuccess && dev <= 63) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
+  }
+  return e == cudaSuccess ? HDQT_OK : cuda_failure(e, "layer norm");
+}
+
+// shared memory in which a block's teams (or warps of several teams) leave their sums of dgamma and dbeta
+inline size_t sums_bytes(const RowParams& p, int block, int row_slots) {
+  const int holders = p.team <= 32 ? block / 32 : block / p.team;
+  return (size_t)holders * row_slots * sizeof(float2);
+}
+
+// One block per SM (two where rows come in eight classes, whose number 148 is not a multiple of), as many teams as fit or are of
+// use, as many rows in flight as there is room for.  False: not even one row fits.
+struct Shape {
+  int blocks, threads;
+  size_t smem;
+};
+inline bool shape_of(RowParams* p, int elem, int k, int params, int streams, int most_threads, bool sums, Shape* out) {
+  const int vec = 16 / elem;
+  const int row_slots = (p->team < 32 ? 32 : p->team) * k * vec;
+  const size_t fixed = (size_t)row_slots * 4 * params, per_thread = (size_t)k * 16 * streams;
+  for (int per_sm = p->classes == 8 ? 2 : 1; per_sm > 0; --per_sm) {
+    const size_t room = kMostSmem / per_sm;
+    const int64_t sms = (int64_t)per_sm * kNumSMsHint, useful = (p->rows + sms - 1) / sms;
+    const int group = p->team < 32 ? 32 / p->team : 1;                           // teams of a warp
+    int teams = most_threads / per_sm / p->team;
+    if (teams > useful) teams = (int)useful;
+    teams = (teams + group - 1) / group * group;
+    if (p->team > 32 && teams > 15) teams = 15;                                  // barriers of a block
+    for (; teams > 0; teams -= group) {
+      const int threads = teams * p->team;
+      if (fixed + per_thread * threads > room || (sums && sums_bytes(*p, threads, row_slots) > room)) continue;
+      p->stages = (int)((room - fixed) / (per_thread * threads));
+      if (p->stages > kMostStages) p->stages = kMostStages;
+      out->threads = threads;
+      out->smem = fixed + per_thread * threads * p->stages;
+      if (sums && out->smem < sums_bytes(*p, threads, row_slots)) out->smem = sums_bytes(*p, threads, row_slots);
+      const int64_t needed = ((p->rows + p->classes - 1) / p->classes + teams - 1) / teams;      // blocks of each class
+      const int64_t most_blocks = sms / p->classes;
+      const int64_t n = needed < most_blocks ? needed : most_blocks;
+      out->blocks = (int)(n * p->classes);
+      p->step = (uint32_t)(n * teams * p->classes);
+      p->x_step = (int64_t)p->step * p->x_rs * elem;
+      p->r_step = (int64_t)p->step * p->r_rs * elem;
+      p->y_step = (int64_t)p->step * p->y_rs * elem;
+      p->chunk_step = (int64_t)p->step * p->channels / vec;
+      return true;
+    }
+  }
+  return false;
+}
+
+template <auto kernel>
+hdqt_status_t launch_rows(const RowParams& p, const Shape& shape, cudaStream_t s) {
+  if (shape.smem > 44 * 1024) {      // (48 KB with the static part need no permission)
+    const hdqt_status_t st = allow_smem<kernel>();
+    if (st != HDQT_OK) return st;
+  }
+  kernel<<<(unsigned)shape.blocks, shape.threads, shape.smem, s>>>(p);
+  return last_error("layer norm");
+}
+
+template <typename F>
+hdqt_status_t with_type(int dtype, F&& f) {
+  if (dtype == HDQT_DTYPE_F32) return f.template operator()<float>();
+  if (dtype == HDQT_DTYPE_BF16) return f.template operator()<__nv_bfloat16>();
+  return f.template operator()<__half>();
+}
+
+}  // namespace hdqt

@@ -109,6 +109,9 @@ SHAPES = [
     (1, 1), (3, 1), (1, 8), (5, 7), (2, 33), (37, 30), (3, 4, 12), (1000, 64), (130, 96), (17, 257), (33, 512), (9, 1000),
     (4, 1024), (5, 1531), (1500, 1152), (7, 2048), (300, 2050), (3, 4096), (2, 4100), (700, 4104), (2, 8192), (3, 8200), (2, 10001),
     (2, 16384), (1, 16390), (2, 33000), (2, 40001),
+    # enough rows for teams that walk over several
+    (3001, 7), (5000, 24), (2003, 90), (1999, 128), (1501, 260), (1203, 513), (901, 1001), (700, 1531), (610, 3001), (450, 6001),
+    (401, 8200), (351, 10001), (330, 16384),
 ]
 
 
@@ -157,13 +160,14 @@ def test_fused_with_dropout_and_residual(shape, dtype, param):
         f = factor.double()
         close(dx, (want["dx"][0] * f, want["dx"][1] * f + E * (want["dx"][0] * f).abs()))
         assert not bool(dx[~keep].any())
-        # the parts are the same whatever else is asked for, and the same as the two operators one after the other
+        # the parts are the same whatever else is asked for, and h that of the two operators one after the other
         some = hdqt.dropout_add_layer_norm_bwd(dy, dh, h, gamma, beta, mean, rstd, want_residual=False, want_params=False, **how)
         assert torch.equal(some[0], dx) and some[1] is None and some[2] is None
         two = hdqt.dropout(x, p, seed, tag, res, offset)
         assert torch.equal(two, h)
         y2, mean2, rstd2 = hdqt.layer_norm_fwd(two, gamma, beta, EPS, act)
-        assert torch.equal(y2, y) and torch.equal(mean2, mean) and torch.equal(rstd2, rstd)
+        for got, name in ((y2, "y"), (mean2, "mean"), (rstd2, "rstd")):      # (a row may be divided otherwise: sums in another order)
+            close(got, want[name])
 
 
 @pytest.mark.gpu
