@@ -19,56 +19,64 @@ struct DropCall {
   int64_t x_rs, r_rs, y_rs;
 };
 
-// Eight elements per thread, 16-byte accesses.  kLinear: dense tensors (one row of n elements); otherwise cols % 8 == 0.
-template <typename T, bool kLinear>
+// kGroups times eight elements per thread, 16-byte accesses, all loads ahead of the generator.  kLinear: dense tensors (one row of n
+// elements); otherwise cols % 8 == 0.
+template <typename T, bool kLinear, int kGroups>
 __global__ void __launch_bounds__(NT) dropout_vec_kernel(const DropCall p) {
   constexpr int V = 16 / sizeof(T), K = 8 / V;
-  const int64_t g = (int64_t)blockIdx.x * NT + threadIdx.x, first = g * 8;
-  if (first >= p.n) return;
-  int64_t xi = first, ri = first, yi = first;
-  if constexpr (!kLinear) {
-    const int64_t r = first / p.cols, c = first - r * p.cols;
-    xi = r * p.x_rs + c;
-    ri = r * p.r_rs + c;
-    yi = r * p.y_rs + c;
-  }
-  const T* x = reinterpret_cast<const T*>(p.x) + xi;
-  const T* res = reinterpret_cast<const T*>(p.residual) + ri;
-  T* y = reinterpret_cast<T*>(p.y) + yi;
-  const bool whole = !kLinear || first + 8 <= p.n;
-  Words vx[K], vr[K];
-  if (whole) {
+  const uint32_t offset = p.d.on ? drop_offset(p.d) : 0;
+  int64_t g[kGroups], yi[kGroups];
+  Words vx[kGroups][K], vr[kGroups][K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) vx[k] = *reinterpret_cast<const Words*>(x + k * V);
-    if (p.residual) {
-#pragma unroll
-      for (int k = 0; k < K; ++k) vr[k] = *reinterpret_cast<const Words*>(res + k * V);
+  for (int u = 0; u < kGroups; ++u) {
+    g[u] = ((int64_t)blockIdx.x * kGroups + u) * NT + threadIdx.x;
+    const int64_t first = g[u] * 8;
+    int64_t xi = first, ri = first;
+    yi[u] = first;
+    if constexpr (!kLinear) {
+      const int64_t r = first / p.cols, c = first - r * p.cols;
+      xi = r * p.x_rs + c;
+      ri = r * p.r_rs + c;
+      yi[u] = r * p.y_rs + c;
     }
-  }
-  Philox4 w{};
-  if (p.d.on) w = drop_words(p.d, drop_offset(p.d), (uint64_t)g);
-  if (whole) {
+    if (first + 8 <= p.n) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      float f[V], q[V];
-      unpack<T>(vx[k], f);
-      if (p.residual) unpack<T>(vr[k], q);
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        if (p.d.on) f[j] = drop_keeps(w, k * V + j, p.d.limit) ? __fmul_rn(f[j], p.d.scale) : 0.0f;
-        if (p.residual) f[j] = __fadd_rn(q[j], f[j]);
+      for (int k = 0; k < K; ++k) {
+        vx[u][k] = *reinterpret_cast<const Words*>(reinterpret_cast<const T*>(p.x) + xi + k * V);
+        if (p.residual) vr[u][k] = *reinterpret_cast<const Words*>(reinterpret_cast<const T*>(p.residual) + ri + k * V);
       }
-      *reinterpret_cast<Words*>(y + k * V) = pack_words<T>(f);
     }
-    return;
   }
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {      // the last elements of a tensor
-    if (first + j >= p.n) break;
-    float f = to_f32(x[j]);
-    if (p.d.on) f = drop_keeps(w, j, p.d.limit) ? __fmul_rn(f, p.d.scale) : 0.0f;
-    if (p.residual) f = __fadd_rn(to_f32(res[j]), f);
-    y[j] = from_f32<T>(f);
+  for (int u = 0; u < kGroups; ++u) {
+    const int64_t first = g[u] * 8;
+    if (first >= p.n) return;
+    Philox4 w{};
+    if (p.d.on) w = drop_words(p.d, offset, (uint64_t)g[u]);
+    T* y = reinterpret_cast<T*>(p.y) + yi[u];
+    if (first + 8 <= p.n) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        float f[V], q[V];
+        unpack<T>(vx[u][k], f);
+        if (p.residual) unpack<T>(vr[u][k], q);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          if (p.d.on) f[j] = drop_keeps(w, k * V + j, p.d.limit) ? __fmul_rn(f[j], p.d.scale) : 0.0f;
+          if (p.residual) f[j] = __fadd_rn(q[j], f[j]);
+        }
+        *reinterpret_cast<Words*>(y + k * V) = pack_words<T>(f);
+      }
+    } else {      // the last elements of a dense tensor
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (first + j >= p.n) break;
+        float f = to_f32(reinterpret_cast<const T*>(p.x)[first + j]);
+        if (p.d.on) f = drop_keeps(w, j, p.d.limit) ? __fmul_rn(f, p.d.scale) : 0.0f;
+        if (p.residual) f = __fadd_rn(to_f32(reinterpret_cast<const T*>(p.residual)[first + j]), f);
+        y[j] = from_f32<T>(f);
+      }
+    }
   }
 }
 
@@ -92,9 +100,11 @@ __global__ void __launch_bounds__(NT) dropout_any_kernel(const DropCall p) {
 
 template <typename T>
 void launch_dropout(const DropCall& p, bool linear, bool wide, cudaStream_t s) {
-  const unsigned blocks = (unsigned)(((p.n + 7) / 8 + NT - 1) / NT);
-  if (wide && linear) dropout_vec_kernel<T, true><<<blocks, NT, 0, s>>>(p);
-  else if (wide) dropout_vec_kernel<T, false><<<blocks, NT, 0, s>>>(p);
+  constexpr int kGroups = sizeof(T) == 2 ? 2 : 1;      // 32 bytes of every tensor per thread
+  const int64_t groups = (p.n + 7) / 8;
+  const unsigned blocks = (unsigned)((groups + NT - 1) / NT), fewer = (unsigned)((groups + kGroups * NT - 1) / (kGroups * NT));
+  if (wide && linear) dropout_vec_kernel<T, true, kGroups><<<fewer, NT, 0, s>>>(p);
+  else if (wide) dropout_vec_kernel<T, false, kGroups><<<fewer, NT, 0, s>>>(p);
   else dropout_any_kernel<T><<<blocks, NT, 0, s>>>(p);
 }
 

@@ -224,13 +224,115 @@ __global__ void __launch_bounds__(kThreads, 1) team_bwd_kernel(const RowParams p
   }
 }
 
-// ---- few rows: one per block, everything loaded at once --------------------------------------------------------
+// ---- few rows: a block per row, everything loaded at once, and blocks that read a few columns of all rows again (from the L2)
+// for dgamma and dbeta, which need nothing of the rows' sums: one launch and no workspace ---------------------------
+
+constexpr int kColumnFloats = 32 * 64;       // shared memory of a block that sums up columns
+
+template <int kAct>
+__device__ __forceinline__ void column_terms(float x, float dy, float mu, float rs, float g, float b, float& sum_g, float& sum_b) {
+  const float xh = fmaf(x, rs, -mu * rs);
+  float dz = dy;
+  if constexpr (kAct != HDQT_ACT_NONE) dz = act_bwd<kAct>(dz, fmaf(xh, g, b));
+  sum_b += dz;
+  sum_g = fmaf(dz, xh, sum_g);
+}
+
+// four chunks of all rows: lane l takes chunk l % 4 of the rows l / 4, ...
+template <typename T>
+__device__ __forceinline__ void chunk_columns(const RowParams& p, int block, float* s) {
+  constexpr int V = 16 / sizeof(T);
+  const int q = threadIdx.x & 3, c = (block * 4 + q) * V, lanes = blockDim.x >> 2;
+  float sum_g[V], sum_b[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) sum_g[j] = sum_b[j] = 0.0f;
+  if (c < p.channels) {
+    with_act(p.act, [&]<int kAct>() {
+      float g[V], b[V];
+      if constexpr (kAct != HDQT_ACT_NONE) {
+        load_params<V>(p.gamma, p, c, 1.0f, g);
+        load_params<V>(p.beta, p, c, 0.0f, b);
+      }
+#pragma unroll 4
+      for (int64_t row = threadIdx.x >> 2; row < p.rows; row += lanes) {
+        float x[V], d[V];
+        unpack<T>(*reinterpret_cast<const Words*>(reinterpret_cast<const T*>(p.x) + row * p.x_rs + c), x);
+        unpack<T>(*reinterpret_cast<const Words*>(reinterpret_cast<const T*>(p.dy) + row * p.y_rs + c), d);
+        const float mu = p.mean[row], rs = p.rstd[row];
+#pragma unroll
+        for (int j = 0; j < V; ++j) column_terms<kAct>(x[j], d[j], mu, rs, kAct ? g[j] : 0.0f, kAct ? b[j] : 0.0f, sum_g[j], sum_b[j]);
+      }
+    });
+  }
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) {
+      sum_g[j] += __shfl_xor_sync(0xFFFFFFFFu, sum_g[j], o);
+      sum_b[j] += __shfl_xor_sync(0xFFFFFFFFu, sum_b[j], o);
+    }
+  }
+  if ((threadIdx.x & 31) < 4) {
+    float* to = s + (threadIdx.x >> 5) * 64 + q * V;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      to[j] = sum_b[j];
+      to[32 + j] = sum_g[j];
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    const int i = threadIdx.x & 31, at = block * 4 * V + i;
+    float sum = 0.0f;
+    for (int w = 0; w < (int)blockDim.x >> 5; ++w) sum += s[w * 64 + threadIdx.x];
+    void* to = threadIdx.x < 32 ? p.dbeta : p.dgamma;
+    if (i < 4 * V && at < p.channels && to) store_param(to, p.param_dtype, at, sum);
+  }
+}
+
+// 32 columns of all rows, one element per access
+template <typename T>
+__device__ __forceinline__ void element_columns(const RowParams& p, int block, float* s) {
+  const int lane = threadIdx.x & 31, c = block * 32 + lane, warps = blockDim.x >> 5;
+  float sum_g = 0.0f, sum_b = 0.0f;
+  if (c < p.channels) {
+    with_act(p.act, [&]<int kAct>() {
+      const float g = kAct != HDQT_ACT_NONE && p.gamma ? load_param(p.gamma, p.param_dtype, c) : 1.0f;
+      const float b = kAct != HDQT_ACT_NONE && p.beta ? load_param(p.beta, p.param_dtype, c) : 0.0f;
+#pragma unroll 8
+      for (int64_t row = threadIdx.x >> 5; row < p.rows; row += warps)
+        column_terms<kAct>(to_f32(reinterpret_cast<const T*>(p.x)[row * p.x_rs + c]), to_f32(reinterpret_cast<const T*>(p.dy)[row * p.y_rs + c]),
+                           p.mean[row], p.rstd[row], g, b, sum_g, sum_b);
+    });
+  }
+  s[(threadIdx.x >> 5) * 64 + lane] = sum_b;
+  s[(threadIdx.x >> 5) * 64 + 32 + lane] = sum_g;
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    float sum = 0.0f;
+    for (int w = 0; w < warps; ++w) sum += s[w * 64 + threadIdx.x];
+    void* to = threadIdx.x < 32 ? p.dbeta : p.dgamma;
+    if (c < p.channels && to) store_param(to, p.param_dtype, c, sum);
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(512) columns_kernel(const RowParams p) {
+  __shared__ float s_columns[kColumnFloats];
+  element_columns<T>(p, blockIdx.x, s_columns);
+}
 
 template <typename T, int K, bool kFused, bool kShift>
 __global__ void __launch_bounds__(1024) once_bwd_kernel(const RowParams p) {
   constexpr int V = 16 / sizeof(T);
   __shared__ __align__(16) float s_sum[2 * kSlots];
-  const int64_t row = blockIdx.x;
+  __shared__ float s_columns[kColumnFloats];
+  if ((int)blockIdx.x < p.column_blocks) {
+    if constexpr (kShift) element_columns<T>(p, blockIdx.x, s_columns);
+    else chunk_columns<T>(p, blockIdx.x, s_columns);
+    return;
+  }
+  const int64_t row = blockIdx.x - p.column_blocks;
   const int lead = kShift ? (int)((row * p.channels) & (V - 1)) : 0;
   const bool edge = row == p.rows - 1;
   const char* src = reinterpret_cast<const char*>(p.x) + (row * p.x_rs - lead) * (int64_t)sizeof(T);
@@ -253,7 +355,6 @@ __global__ void __launch_bounds__(1024) once_bwd_kernel(const RowParams p) {
   }
   float d[K][V];
   float s[2] = {0.0f, 0.0f};
-  float2* part = p.part + row * p.channels;
   with_act(p.act, [&]<int kAct>() {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -276,7 +377,6 @@ __global__ void __launch_bounds__(1024) once_bwd_kernel(const RowParams p) {
           const float xh = fmaf(x[j], rs, shift);
           float dz = d[k][j];
           if constexpr (kAct != HDQT_ACT_NONE) dz = act_bwd<kAct>(dz, fmaf(xh, g[j], b[j]));
-          if (p.part && (!kShift || ((mask[k] >> j) & 1))) part[c + j] = make_float2(dz, dz * xh);
           d[k][j] = dz * g[j];
           s[0] += d[k][j];
           s[1] = fmaf(d[k][j], xh, s[1]);
@@ -284,7 +384,6 @@ __global__ void __launch_bounds__(1024) once_bwd_kernel(const RowParams p) {
       }
     }
   });
-  chain_next();
   lanes_total<false>(s, 32);
   if (blockDim.x > 32) warps_total(s, 0, blockDim.x, threadIdx.x >> 5, threadIdx.x & 31, s_sum);
   const float slope = -rs * rs * (s[1] * inv_c), base = -rs * fmaf(s[1] * inv_c, shift, s[0] * inv_c);
@@ -583,21 +682,30 @@ bool bwd_teams(RowParams p, int* parts, hdqt_status_t* st, cudaStream_t s) {
 }
 
 template <typename T, int K, bool kFused>
-hdqt_status_t bwd_once(const RowParams& p, int* parts, cudaStream_t s) {
-  const int n = (row_chunks(p, 16 / sizeof(T)) + K - 1) / K, threads = (n + 31) / 32 * 32;
-  if (p.classes > 1) once_bwd_kernel<T, K, kFused, true><<<(unsigned)p.rows, threads, 0, s>>>(p);
-  else once_bwd_kernel<T, K, kFused, false><<<(unsigned)p.rows, threads, 0, s>>>(p);
-  *parts = (int)p.rows;
+hdqt_status_t bwd_once(RowParams p, bool params, cudaStream_t s) {
+  constexpr int V = 16 / sizeof(T);
+  const int n = (row_chunks(p, V) + K - 1) / K, threads = n <= 256 ? 256 : (n + 31) / 32 * 32;
+  const int columns = p.classes > 1 ? 32 : 4 * V;
+  p.column_blocks = params ? (p.channels + columns - 1) / columns : 0;
+  const unsigned blocks = p.column_blocks + (p.dx || p.dres ? (unsigned)p.rows : 0);
+  if (p.classes > 1) once_bwd_kernel<T, K, kFused, true><<<blocks, threads, 0, s>>>(p);
+  else once_bwd_kernel<T, K, kFused, false><<<blocks, threads, 0, s>>>(p);
   return last_error("layer norm gradient");
 }
 
+bool few_rows(const hdqt_layer_norm_desc_t& d) { return d.rows <= kFewRows && d.channels <= kFewChannels; }
+
 template <typename T, bool kFused>
-hdqt_status_t run_bwd(RowParams p, bool wide, int* parts, cudaStream_t s) {
+hdqt_status_t run_bwd(RowParams p, bool wide, bool few, bool params, int* parts, cudaStream_t s) {
   constexpr int V = 16 / sizeof(T), kMost = 32 / V;
+  const int chunks = row_chunks(p, V);
+  if (few && wide) return chunks <= 1024 ? bwd_once<T, 1, kFused>(p, params, s) : bwd_once<T, 2, kFused>(p, params, s);
+  if (few && params) {
+    columns_kernel<T><<<(unsigned)((p.channels + 31) / 32), 512, 0, s>>>(p);
+    if (!p.dx && !p.dres) return last_error("layer norm gradient");
+  }
   if (wide) {
     hdqt_status_t st = HDQT_OK;
-    const int chunks = row_chunks(p, V);
-    if (p.rows <= kNumSMsHint && chunks <= 2048) return chunks <= 1024 ? bwd_once<T, 1, kFused>(p, parts, s) : bwd_once<T, 2, kFused>(p, parts, s);
     if (chunks <= 16 * (8 / V)) {
       if (bwd_teams<T, 8 / V, kFused, true>(p, parts, &st, s)) return st;
     } else {
@@ -639,7 +747,8 @@ hdqt_status_t backward(const hdqt_layer_norm_desc_t* d, bool fused, const void* 
                        void* workspace, size_t workspace_bytes, void* stream) {
   const hdqt_status_t st = check_rows_desc(d, fused);
   if (st != HDQT_OK) return st;
-  if (!workspace || (d->rows > 0 && (!x || !dy || !mean || !rstd))) return HDQT_ERR_INVALID_ARG;
+  const bool few = few_rows(*d);
+  if ((!workspace && !few) || (d->rows > 0 && (!x || !dy || !mean || !rstd))) return HDQT_ERR_INVALID_ARG;
   const int elem = dtype_size(d->dtype), pelem = dtype_size(d->param_dtype);
   const uintptr_t bases = bits_of(x) | bits_of(dy) | bits_of(dh) | bits_of(dx) | bits_of(dres);
   const uintptr_t params = bits_of(gamma) | bits_of(beta) | bits_of(dgamma) | bits_of(dbeta);
@@ -658,17 +767,19 @@ hdqt_status_t backward(const hdqt_layer_norm_desc_t* d, bool fused, const void* 
     p.dh = dh;
     p.dx = dx;
     p.dres = dres;
-    p.part = want_params ? part : nullptr;
+    p.part = want_params && !few ? part : nullptr;
+    p.dgamma = dgamma;
+    p.dbeta = dbeta;
     if (fused) p.d = make_drop(d->p, d->seed, d->tag, d->philox_offset);
     const uintptr_t strides = d->rows > 1 ? (uintptr_t)((p.x_rs | p.y_rs) * elem) : 0;
     const bool dense = d->rows == 1 || (p.x_rs == d->channels && p.y_rs == d->channels);
     const bool wide = set_classes(&p, elem, bases, dense, strides);
     const hdqt_status_t e = with_type(d->dtype, [&]<typename T>() {
-      return fused ? run_bwd<T, true>(p, wide, &parts, s) : run_bwd<T, false>(p, wide, &parts, s);
+      return fused ? run_bwd<T, true>(p, wide, few, want_params, &parts, s) : run_bwd<T, false>(p, wide, few, want_params, &parts, s);
     });
     if (e != HDQT_OK) return e;
   }
-  if (want_params) launch_param_grad(part, parts, (int)d->channels, dgamma, dbeta, d->param_dtype, parts > 0, s);
+  if (want_params && (d->rows == 0 || !few)) launch_param_grad(part, parts, (int)d->channels, dgamma, dbeta, d->param_dtype, parts > 0, s);
   return last_error("layer norm gradient");
 }
 
@@ -679,9 +790,9 @@ hdqt_status_t backward(const hdqt_layer_norm_desc_t* d, bool fused, const void* 
 using namespace hdqt;
 
 extern "C" size_t hdqt_layer_norm_workspace_bytes(const hdqt_layer_norm_desc_t* d) {
-  if (check_rows_desc(d, false) != HDQT_OK) return 0;
+  if (check_rows_desc(d, false) != HDQT_OK || few_rows(*d)) return 0;
   const int64_t parts = d->rows < kMostParts - 7 ? d->rows + 7 : kMostParts;      // (a block of every class, rows or not)
-  return align256((size_t)parts * d->channels * sizeof(float2)) + 256;
+  return align256((size_t)parts * d->channels * sizeof(float2));
 }
 
 extern "C" hdqt_status_t hdqt_layer_norm_bwd(const hdqt_layer_norm_desc_t* d, const void* dy, const void* x, const void* gamma,

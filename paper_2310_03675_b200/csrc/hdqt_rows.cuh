@@ -25,6 +25,8 @@ namespace hdqt {
 
 constexpr int kLongThreads = 1024;
 constexpr int kMostParts = 2 * kNumSMsHint;      // blocks that leave sums of dgamma and dbeta
+// "Few rows" need no workspace: every block either takes a row or sums up some columns of all rows.
+constexpr int kFewRows = 2 * kNumSMsHint, kFewChannels = 8192;
 constexpr int kMostStages = 2;
 constexpr size_t kMostSmem = 224 * 1024;         // dynamic shared memory of an SM's blocks together
 
@@ -52,6 +54,9 @@ struct RowParams {
   float* mean;
   float* rstd;
   float2* part;                  // [blocks, channels] sums of dbeta (x) and dgamma (y)
+  void* dgamma;                  // few rows: written at once
+  void* dbeta;
+  int32_t column_blocks;         // few rows: blocks that sum up columns
   DropParams d;
 };
 

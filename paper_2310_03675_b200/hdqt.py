@@ -789,7 +789,7 @@ def _layer_norm_desc(x, gamma, beta, eps, act):
         raise ValueError("gamma and beta must be fp32 or of x's type")
     rows = _row_count(x.shape)
     d = LayerNormDesc(rows, channels, stride, channels, channels, code, DTYPE_CODES[pdt], ACT_CODES[act], eps, 0.0, 0, None, 0, 0)
-    return d, max(256, lib.hdqt_layer_norm_workspace_bytes(C.byref(d))), x.shape[:-1]
+    return d, lib.hdqt_layer_norm_workspace_bytes(C.byref(d)), tuple(x.shape[:-1])
 
 
 _LAYER_NORM_PLANS = {}     # descriptor, workspace size and shape of the statistics by shapes, strides and types
@@ -822,7 +822,8 @@ def layer_norm_fwd(x, gamma, beta, eps: float = 1e-5, act: str = "none"):
     Returns (y dense, mean fp32 [...], rstd fp32 [...])."""
     d, _, shape = _layer_norm_plan(x, gamma, beta, eps, act)
     y = torch.empty_like(x, memory_format=torch.contiguous_format)
-    mean, rstd = x.new_empty(shape, dtype=torch.float32), x.new_empty(shape, dtype=torch.float32)
+    dev = x.device
+    mean, rstd = torch.empty(shape, dtype=torch.float32, device=dev), torch.empty(shape, dtype=torch.float32, device=dev)
     _call("hdqt_layer_norm_fwd", x, C.byref(d), x.data_ptr(), _ptr(gamma), _ptr(beta), y.data_ptr(), mean.data_ptr(),
           rstd.data_ptr())
     return y, mean, rstd
@@ -838,9 +839,9 @@ def layer_norm_bwd(dy, x, gamma, beta, mean, rstd, act: str = "none", want_dx: b
     dx = torch.empty_like(x, memory_format=torch.contiguous_format) if want_dx else None
     dgamma = torch.empty_like(gamma) if want_params and gamma is not None else None
     dbeta = torch.empty_like(beta) if want_params and beta is not None else None
-    ws = x.new_empty(nbytes, dtype=torch.uint8)
+    ws = x.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
     _call("hdqt_layer_norm_bwd", x, C.byref(d), dy.data_ptr(), x.data_ptr(), _ptr(gamma), _ptr(beta), mean.data_ptr(),
-          rstd.data_ptr(), _ptr(dx), _ptr(dgamma), _ptr(dbeta), ws.data_ptr(), nbytes)
+          rstd.data_ptr(), _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(ws), nbytes)
     return dx, dgamma, dbeta
 
 
@@ -881,7 +882,8 @@ def dropout_add_layer_norm_fwd(x, residual, gamma, beta, p: float, seed: int, ta
         d.r_row_stride = _row_stride(residual, "residual")
     y = torch.empty_like(x, memory_format=torch.contiguous_format)
     h = torch.empty_like(x, memory_format=torch.contiguous_format)
-    mean, rstd = x.new_empty(shape, dtype=torch.float32), x.new_empty(shape, dtype=torch.float32)
+    dev = x.device
+    mean, rstd = torch.empty(shape, dtype=torch.float32, device=dev), torch.empty(shape, dtype=torch.float32, device=dev)
     _call("hdqt_dropout_add_layer_norm_fwd", x, C.byref(d), x.data_ptr(), _ptr(residual), _ptr(gamma), _ptr(beta), h.data_ptr(),
           y.data_ptr(), mean.data_ptr(), rstd.data_ptr())
     return y, h, mean, rstd
@@ -911,9 +913,9 @@ def dropout_add_layer_norm_bwd(dy, dh, h, gamma, beta, mean, rstd, p: float, see
     dresidual = torch.empty_like(h) if want_residual else None
     dgamma = torch.empty_like(gamma) if want_params and gamma is not None else None
     dbeta = torch.empty_like(beta) if want_params and beta is not None else None
-    ws = h.new_empty(nbytes, dtype=torch.uint8)
+    ws = h.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
     _call("hdqt_dropout_add_layer_norm_bwd", h, C.byref(d), dy.data_ptr(), _ptr(dh), h.data_ptr(), _ptr(gamma), _ptr(beta),
-          mean.data_ptr(), rstd.data_ptr(), _ptr(dx), _ptr(dresidual), _ptr(dgamma), _ptr(dbeta), ws.data_ptr(), nbytes)
+          mean.data_ptr(), rstd.data_ptr(), _ptr(dx), _ptr(dresidual), _ptr(dgamma), _ptr(dbeta), _ptr(ws), nbytes)
     return dx, dresidual, dgamma, dbeta
 
 

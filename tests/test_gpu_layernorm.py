@@ -427,8 +427,10 @@ def test_refusals():
     def bwd(d, dy=256, dx=256, ws=256, ws_bytes=1 << 20):
         return lib.hdqt_layer_norm_bwd(C.byref(d), dy, 256, 256, 256, 256, 256, dx, 256, 256, ws, ws_bytes, None)
 
-    assert bwd(desc(), dy=None) == INVALID and bwd(desc(), ws=None) == INVALID and bwd(desc(), dx=258) == ALIGN
-    assert bwd(desc(), ws=384 + 8) == ALIGN and bwd(desc(), ws_bytes=8) == WS
+    many = desc(rows=1000)                                                     # (few rows need no workspace)
+    assert lib.hdqt_layer_norm_workspace_bytes(C.byref(desc())) == 0 < lib.hdqt_layer_norm_workspace_bytes(C.byref(many))
+    assert bwd(desc(), dy=None) == INVALID and bwd(many, ws=None) == INVALID and bwd(desc(), dx=258) == ALIGN
+    assert bwd(many, ws=384 + 8) == ALIGN and bwd(many, ws_bytes=8) == WS
     assert lib.hdqt_dropout_add_layer_norm_bwd(C.byref(desc(p=2.0)), *[256] * 12, 1 << 20, None) == INVALID
-    assert lib.hdqt_dropout_add_layer_norm_bwd(C.byref(desc()), *[256] * 12, 8, None) == WS
+    assert lib.hdqt_dropout_add_layer_norm_bwd(C.byref(many), *[256] * 12, 8, None) == WS
     assert lib.hdqt_dropout_add_layer_norm_bwd(C.byref(desc()), 256, 258, *[256] * 10, 1 << 20, None) == ALIGN
