@@ -21,16 +21,17 @@ struct DropCall {
 
 // kGroups times eight elements per thread, 16-byte accesses, all loads ahead of the generator.  kLinear: dense tensors (one row of n
 // elements); otherwise cols % 8 == 0.
-template <typename T, bool kLinear, int kGroups>
+template <typename T, bool kLinear, bool kResidual, int kGroups>
 __global__ void __launch_bounds__(NT) dropout_vec_kernel(const DropCall p) {
   constexpr int V = 16 / sizeof(T), K = 8 / V;
-  const uint32_t offset = p.d.on ? drop_offset(p.d) : 0;
-  int64_t g[kGroups], yi[kGroups];
+  const uint32_t offset = drop_offset(p.d);
+  uint64_t g[kGroups];
+  int64_t yi[kGroups];
   Words vx[kGroups][K], vr[kGroups][K];
 #pragma unroll
   for (int u = 0; u < kGroups; ++u) {
-    g[u] = ((int64_t)blockIdx.x * kGroups + u) * NT + threadIdx.x;
-    const int64_t first = g[u] * 8;
+    g[u] = ((uint64_t)blockIdx.x * kGroups + u) * NT + threadIdx.x;
+    const int64_t first = (int64_t)g[u] * 8;
     int64_t xi = first, ri = first;
     yi[u] = first;
     if constexpr (!kLinear) {
@@ -43,27 +44,32 @@ __global__ void __launch_bounds__(NT) dropout_vec_kernel(const DropCall p) {
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         vx[u][k] = *reinterpret_cast<const Words*>(reinterpret_cast<const T*>(p.x) + xi + k * V);
-        if (p.residual) vr[u][k] = *reinterpret_cast<const Words*>(reinterpret_cast<const T*>(p.residual) + ri + k * V);
+        if (kResidual) vr[u][k] = *reinterpret_cast<const Words*>(reinterpret_cast<const T*>(p.residual) + ri + k * V);
       }
     }
   }
+  Philox4 words[kGroups];
+  drop_words(p.d, offset, g, words);
+  const uint32_t limit = p.d.limit;
+  const bool all = !p.d.on;      // nothing is dropped
 #pragma unroll
   for (int u = 0; u < kGroups; ++u) {
-    const int64_t first = g[u] * 8;
+    const int64_t first = (int64_t)g[u] * 8;
     if (first >= p.n) return;
-    Philox4 w{};
-    if (p.d.on) w = drop_words(p.d, offset, (uint64_t)g[u]);
+    const Philox4& w = words[u];
     T* y = reinterpret_cast<T*>(p.y) + yi[u];
     if (first + 8 <= p.n) {
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         float f[V], q[V];
         unpack<T>(vx[u][k], f);
-        if (p.residual) unpack<T>(vr[u][k], q);
+        if (kResidual) unpack<T>(vr[u][k], q);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          if (p.d.on) f[j] = drop_keeps(w, k * V + j, p.d.limit) ? __fmul_rn(f[j], p.d.scale) : 0.0f;
-          if (p.residual) f[j] = __fadd_rn(q[j], f[j]);
+        for (int j = 0; j < V; j += 2) {
+          mul2(f[j], f[j + 1], p.d.scale, p.d.scale);
+          f[j] = drop_keeps(w, k * V + j, limit) || all ? f[j] : 0.0f;
+          f[j + 1] = drop_keeps(w, k * V + j + 1, limit) || all ? f[j + 1] : 0.0f;
+          if (kResidual) add2(f[j], f[j + 1], q[j], q[j + 1]);
         }
         *reinterpret_cast<Words*>(y + k * V) = pack_words<T>(f);
       }
@@ -72,8 +78,8 @@ __global__ void __launch_bounds__(NT) dropout_vec_kernel(const DropCall p) {
       for (int j = 0; j < 8; ++j) {
         if (first + j >= p.n) break;
         float f = to_f32(reinterpret_cast<const T*>(p.x)[first + j]);
-        if (p.d.on) f = drop_keeps(w, j, p.d.limit) ? __fmul_rn(f, p.d.scale) : 0.0f;
-        if (p.residual) f = __fadd_rn(to_f32(reinterpret_cast<const T*>(p.residual)[first + j]), f);
+        f = drop_keeps(w, j, limit) || all ? __fmul_rn(f, p.d.scale) : 0.0f;
+        if (kResidual) f = __fadd_rn(to_f32(reinterpret_cast<const T*>(p.residual)[first + j]), f);
         y[j] = from_f32<T>(f);
       }
     }
@@ -98,14 +104,18 @@ __global__ void __launch_bounds__(NT) dropout_any_kernel(const DropCall p) {
   }
 }
 
+template <typename T, bool kLinear>
+void launch_vec(const DropCall& p, cudaStream_t s) {
+  constexpr int kGroups = sizeof(T) == 2 ? 2 : 1;      // 32 bytes of every tensor per thread
+  const unsigned blocks = (unsigned)(((p.n + 7) / 8 + kGroups * NT - 1) / (kGroups * NT));
+  if (p.residual) dropout_vec_kernel<T, kLinear, true, kGroups><<<blocks, NT, 0, s>>>(p);
+  else dropout_vec_kernel<T, kLinear, false, kGroups><<<blocks, NT, 0, s>>>(p);
+}
 template <typename T>
 void launch_dropout(const DropCall& p, bool linear, bool wide, cudaStream_t s) {
-  constexpr int kGroups = sizeof(T) == 2 ? 2 : 1;      // 32 bytes of every tensor per thread
-  const int64_t groups = (p.n + 7) / 8;
-  const unsigned blocks = (unsigned)((groups + NT - 1) / NT), fewer = (unsigned)((groups + kGroups * NT - 1) / (kGroups * NT));
-  if (wide && linear) dropout_vec_kernel<T, true, kGroups><<<fewer, NT, 0, s>>>(p);
-  else if (wide) dropout_vec_kernel<T, false, kGroups><<<fewer, NT, 0, s>>>(p);
-  else dropout_any_kernel<T><<<blocks, NT, 0, s>>>(p);
+  if (wide && linear) launch_vec<T, true>(p, s);
+  else if (wide) launch_vec<T, false>(p, s);
+  else dropout_any_kernel<T><<<(unsigned)(((p.n + 7) / 8 + NT - 1) / NT), NT, 0, s>>>(p);
 }
 
 }  // namespace

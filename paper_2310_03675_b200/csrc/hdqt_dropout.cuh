@@ -36,6 +36,30 @@ __device__ __forceinline__ uint32_t drop_offset(const DropParams& d) { return d.
 __device__ __forceinline__ Philox4 drop_words(const DropParams& d, uint32_t offset, uint64_t g) {
   return philox4x32_10((uint32_t)g, (uint32_t)(g >> 32), d.tag, offset, d.keys);
 }
+// those of several groups at once, so that a round's keys are fetched once for all
+template <int N>
+__device__ __forceinline__ void drop_words(const DropParams& d, uint32_t offset, const uint64_t (&g)[N], Philox4 (&w)[N]) {
+  constexpr uint32_t M0 = 0xD2511F53u, M1 = 0xCD9E8D57u;
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    w[u].w[0] = (uint32_t)g[u];
+    w[u].w[1] = (uint32_t)(g[u] >> 32);
+    w[u].w[2] = d.tag;
+    w[u].w[3] = offset;
+  }
+#pragma unroll
+  for (int r = 0; r < 10; ++r) {
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      uint32_t(&c)[4] = w[u].w;
+      const uint32_t hi0 = __umulhi(M0, c[0]), lo0 = M0 * c[0], hi1 = __umulhi(M1, c[2]), lo1 = M1 * c[2];
+      c[0] = hi1 ^ c[1] ^ d.keys.k[r][0];
+      c[1] = lo1;
+      c[2] = hi0 ^ c[3] ^ d.keys.k[r][1];
+      c[3] = lo0;
+    }
+  }
+}
 __device__ __forceinline__ bool drop_keeps(const Philox4& r, int j, uint32_t limit) {
   return (j & 1 ? r.w[j >> 1] : r.w[j >> 1] << 16) > limit;
 }

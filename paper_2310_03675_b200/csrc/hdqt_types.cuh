@@ -105,6 +105,24 @@ __device__ __forceinline__ Words pack_words(const float (&f)[16 / sizeof(T)]) {
   return v;
 }
 
+// ---- pairs of fp32 operations as one instruction ----------------------------------------------------------------
+
+__device__ __forceinline__ void add2(float& a0, float& a1, float b0, float b1) {
+  asm("{\n.reg .b64 a, b;\nmov.b64 a, {%0, %1};\nmov.b64 b, {%2, %3};\nadd.rn.f32x2 a, a, b;\nmov.b64 {%0, %1}, a;\n}"
+      : "+f"(a0), "+f"(a1) : "f"(b0), "f"(b1));
+}
+__device__ __forceinline__ void mul2(float& a0, float& a1, float b0, float b1) {
+  asm("{\n.reg .b64 a, b;\nmov.b64 a, {%0, %1};\nmov.b64 b, {%2, %3};\nmul.rn.f32x2 a, a, b;\nmov.b64 {%0, %1}, a;\n}"
+      : "+f"(a0), "+f"(a1) : "f"(b0), "f"(b1));
+}
+// o = a b + c
+__device__ __forceinline__ void fma2(float& o0, float& o1, float a0, float a1, float b0, float b1, float c0, float c1) {
+  asm("{\n.reg .b64 a, b, c;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\nfma.rn.f32x2 a, a, b, c;\nmov.b64 {%0, %1}, a;\n}"
+      : "=f"(o0), "=f"(o1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1), "f"(c0), "f"(c1));
+}
+
+// ---- activations and what they are made of ----
+
 // hardware approximations (2 units in the last place or better; results below 2^-126 become 0)
 __device__ __forceinline__ float ex2(float x) {
   float r;
@@ -154,8 +172,6 @@ inline void launch_chained(void (*kernel)(P...), dim3 grid, dim3 block, size_t s
   cfg.numAttrs = 1;
   (void)cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);      // (a failure is left for cudaGetLastError)
 }
-
-// ---- activations of the normalisation kernels ----
 
 // 1 / (1 + exp(-z)); exp overflows to infinity for z < -88, where the reciprocal is the correct 0
 __device__ __forceinline__ float sigmoid(float z) { return rcp(1.0f + ex2(z * -kLog2e)); }
