@@ -57,8 +57,7 @@ __global__ void __launch_bounds__(kThreads, 1) team_bwd_kernel(const RowParams p
     nmu = p.mean[me.row];
     nrs = p.rstd[me.row];
   }
-  stage_params<T, K, kSub>(p.gamma, p, me.lead, n_params, 0, 1.0f, s_dyn);
-  if (n_params == 2) stage_params<T, K, kSub>(p.beta, p, me.lead, 2, 1, 0.0f, s_dyn);
+  stage_params<T, K, kSub>(p, me.lead, n_params, s_dyn);
   for (int i = threadIdx.x; i < 4 * kSlots; i += blockDim.x) s_sum[i] = 0.0f;
   __syncthreads();
   float* slots = s_sum + (kSub ? 0 : me.team * ((p.team + 127) >> 7) * 4);

@@ -87,12 +87,22 @@ __device__ __forceinline__ void load_params(const void* p, const RowParams& q, i
 }
 
 // the same from a channel that may lie outside the row: 0 there
+template <typename P, int V>
+__device__ __forceinline__ void load_cut(const void* p, const RowParams& q, int c, float (&f)[V]) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) f[j] = c + j >= 0 && c + j < q.channels ? to_f32(reinterpret_cast<const P*>(p)[c + j]) : 0.0f;
+}
 template <int V>
 __device__ __forceinline__ void load_params_cut(const void* p, const RowParams& q, int c, float fill, float (&f)[V]) {
+  if (p == nullptr) {
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    f[j] = 0.0f;
-    if (c + j >= 0 && c + j < q.channels) f[j] = p ? load_param(p, q.param_dtype, c + j) : fill;
+    for (int j = 0; j < V; ++j) f[j] = c + j >= 0 && c + j < q.channels ? fill : 0.0f;
+  } else if (q.param_dtype == HDQT_DTYPE_F32) {
+    load_cut<float>(p, q, c, f);
+  } else if (q.param_dtype == HDQT_DTYPE_BF16) {
+    load_cut<__nv_bfloat16>(p, q, c, f);
+  } else {
+    load_cut<__half>(p, q, c, f);
   }
 }
 
@@ -312,21 +322,29 @@ template <typename T, int K>
 __host__ __device__ constexpr uint32_t params_bytes(int team, int params) {
   return (uint32_t)((team < 32 ? 32 : team) * K * (16 / (int)sizeof(T)) * 4 * params);
 }
-// One of them, which = 0 or 1 of `params`: [warp][k][which][four elements][lane]
+// gamma, and beta if params == 2: [warp][k][which][four elements][lane]
 template <typename T, int K, bool kSub>
-__device__ __forceinline__ void stage_params(const void* src, const RowParams& p, int lead, int params, int which, float fill, char* s) {
+__device__ __forceinline__ void stage_params(const RowParams& p, int lead, int params, char* s) {
   constexpr int V = 16 / sizeof(T), H = V / 4;
-  const int slots = (kSub ? 32 : p.team) * K;
-  for (int i = threadIdx.x; i < slots * H; i += blockDim.x) {
+  const int items = (kSub ? 32 : p.team) * K * H;
+#pragma unroll 2
+  for (int i = threadIdx.x; i < items; i += blockDim.x) {
     const int half = i % H, slot = i / H, lane = slot & 31, group = slot >> 5;      // group = warp * K + k
     const int chunk = kSub ? group * p.team + lane : slot;
     const int c = chunk * V + half * 4 - lead;
-    float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    float g[4] = {0.0f, 0.0f, 0.0f, 0.0f}, b[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (!kSub || lane < p.team) {
-      if (lead == 0 && c + 4 <= p.channels) load_params<4>(src, p, c, fill, f);
-      else load_params_cut<4>(src, p, c, fill, f);
+      if (lead == 0 && c + 4 <= p.channels) {
+        load_params<4>(p.gamma, p, c, 1.0f, g);
+        if (params == 2) load_params<4>(p.beta, p, c, 0.0f, b);
+      } else if (c + 4 > 0 && c < p.channels) {
+        load_params_cut<4>(p.gamma, p, c, 1.0f, g);
+        if (params == 2) load_params_cut<4>(p.beta, p, c, 0.0f, b);
+      }
     }
-    *reinterpret_cast<float4*>(s + ((group * params + which) * H + half) * 512 + lane * 16) = make_float4(f[0], f[1], f[2], f[3]);
+    char* to = s + (group * params * H + half) * 512 + lane * 16;
+    *reinterpret_cast<float4*>(to) = make_float4(g[0], g[1], g[2], g[3]);
+    if (params == 2) *reinterpret_cast<float4*>(to + H * 512) = make_float4(b[0], b[1], b[2], b[3]);
   }
 }
 // the V of chunk k, from the thread's place (warp and lane) on
