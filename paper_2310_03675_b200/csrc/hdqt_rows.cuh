@@ -295,7 +295,7 @@ struct Place {
       }
     }
     // (kept, not worked out again in every row)
-    asm volatile("" : "+r"(row), "+r"(first), "+r"(left), "+r"(mask), "+r"(ragged));
+    asm volatile("" : "+r"(row), "+r"(first), "+r"(left), "+r"(mask));
   }
   __device__ __forceinline__ uint32_t byte(int k) const { return kSub ? (uint32_t)(k * size) * 16u : k * 512u; }    // from the first chunk
   __device__ __forceinline__ bool has(int k) const { return left > (int)byte(k); }
@@ -303,7 +303,11 @@ struct Place {
   __device__ __forceinline__ bool gaps(int k) const { return kShift && ((ragged >> k) & 1); }
   // zeros in the place of a neighbouring row's elements
   __device__ __forceinline__ void clear(int k, float (&f)[V]) const {
-    if (gaps(k)) clear_gaps<V, kShift>(of(k), f);
+    if (gaps(k)) {
+      const uint32_t m = of(k);
+#pragma unroll
+      for (int j = 0; j < V; ++j) f[j] = (m >> j) & 1 ? f[j] : 0.0f;
+    }
   }
   // bytes from base to this thread's first chunk in row r
   __device__ __forceinline__ int64_t offset(int64_t stride, int64_t r) const { return (r * stride - lead) * (int64_t)sizeof(T) + first; }
@@ -493,20 +497,20 @@ inline size_t sums_bytes(const RowParams& p, int block, int row_slots) {
   return (size_t)holders * row_slots * sizeof(float2);
 }
 
-// One block per SM (two where rows come in eight classes, whose number 148 is not a multiple of), as many teams as fit or are of
-// use, as many rows in flight as there is room for.  False: not even one row fits.
+// One block per SM, or two where rows come in eight classes (148 is not a multiple of eight, 296 is) and that makes for more threads:
+// as many teams as fit or are of use, as many rows in flight as there is room for.  False: not even one row fits.
 struct Shape {
   int blocks, threads;
   size_t smem;
 };
 inline bool shape_of(RowParams* p, int elem, int k, int params, int streams, int most_threads, bool sums, Shape* out) {
-  const int vec = 16 / elem;
-  const int row_slots = (p->team < 32 ? 32 : p->team) * k * vec;
+  const int vec = 16 / elem, row_slots = (p->team < 32 ? 32 : p->team) * k * vec;
   const size_t fixed = (size_t)row_slots * 4 * params, per_thread = (size_t)k * 16 * streams;
-  for (int per_sm = p->classes == 8 ? 2 : 1; per_sm > 0; --per_sm) {
+  const int group = p->team < 32 ? 32 / p->team : 1;                             // teams of a warp
+  int64_t most_total = 0;
+  for (int per_sm = 1; per_sm <= (p->classes == 8 ? 2 : 1); ++per_sm) {
     const size_t room = kMostSmem / per_sm;
     const int64_t sms = (int64_t)per_sm * kNumSMsHint, useful = (p->rows + sms - 1) / sms;
-    const int group = p->team < 32 ? 32 / p->team : 1;                           // teams of a warp
     int teams = most_threads / per_sm / p->team;
     if (teams > useful) teams = (int)useful;
     teams = (teams + group - 1) / group * group;
@@ -514,24 +518,25 @@ inline bool shape_of(RowParams* p, int elem, int k, int params, int streams, int
     for (; teams > 0; teams -= group) {
       const int threads = teams * p->team;
       if (fixed + per_thread * threads > room || (sums && sums_bytes(*p, threads, row_slots) > room)) continue;
+      const int64_t needed = ((p->rows + p->classes - 1) / p->classes + teams - 1) / teams;      // blocks of each class
+      const int64_t most_blocks = sms / p->classes, n = needed < most_blocks ? needed : most_blocks;
+      if (n * p->classes * threads <= most_total) break;
+      most_total = n * p->classes * threads;
       p->stages = (int)((room - fixed) / (per_thread * threads));
       if (p->stages > kMostStages) p->stages = kMostStages;
       out->threads = threads;
       out->smem = fixed + per_thread * threads * p->stages;
       if (sums && out->smem < sums_bytes(*p, threads, row_slots)) out->smem = sums_bytes(*p, threads, row_slots);
-      const int64_t needed = ((p->rows + p->classes - 1) / p->classes + teams - 1) / teams;      // blocks of each class
-      const int64_t most_blocks = sms / p->classes;
-      const int64_t n = needed < most_blocks ? needed : most_blocks;
       out->blocks = (int)(n * p->classes);
       p->step = (uint32_t)(n * teams * p->classes);
-      p->x_step = (int64_t)p->step * p->x_rs * elem;
-      p->r_step = (int64_t)p->step * p->r_rs * elem;
-      p->y_step = (int64_t)p->step * p->y_rs * elem;
-      p->chunk_step = (int64_t)p->step * p->channels / vec;
-      return true;
+      break;
     }
   }
-  return false;
+  p->x_step = (int64_t)p->step * p->x_rs * elem;
+  p->r_step = (int64_t)p->step * p->r_rs * elem;
+  p->y_step = (int64_t)p->step * p->y_rs * elem;
+  p->chunk_step = (int64_t)p->step * p->channels / vec;
+  return most_total > 0;
 }
 
 template <auto kernel>
