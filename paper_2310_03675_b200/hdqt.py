@@ -719,9 +719,12 @@ def group_norm_bwd(dy, x, gamma, beta, mean, rstd, groups: int, act: str = "none
 
 def _row_stride(t: torch.Tensor, name: str):
     """Elements between the rows of a [..., channels] tensor whose outer dimensions step evenly (the width itself for one row)."""
-    shape, st = t.shape, t.stride()
+    shape = t.shape
     if not shape:
         raise ValueError(f"{name} must have at least one dimension")
+    if t.is_contiguous():
+        return shape[-1]
+    st = t.stride()
     if st[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"{name} must have its last dimension contiguous")
     row, step = None, 0
@@ -749,11 +752,11 @@ def _row_count(shape) -> int:
 
 def _row_operand(t, x, name):
     """Raises unless t has x's shape, type and device."""
-    if t.shape != x.shape or t.dtype != x.dtype or t.device != x.device:
+    if t.shape != x.shape or t.dtype is not x.dtype or t.get_device() != x.get_device():
         raise ValueError(f"{name} must have x's shape, type and device")
 
 
-def _dropout_args(p, seed, tag, philox_offset, device):
+def _dropout_args(p, seed, tag, philox_offset, index):
     p = float(p)
     if not 0.0 <= p <= 1.0:
         raise ValueError("p must be a probability")
@@ -761,7 +764,7 @@ def _dropout_args(p, seed, tag, philox_offset, device):
         raise ValueError("seed must fit 64 bits and tag 32 bits, both unsigned")
     if philox_offset is None:
         return p, None
-    if philox_offset.dtype != torch.int32 or philox_offset.numel() < 1 or philox_offset.device != device:
+    if philox_offset.dtype is not torch.int32 or philox_offset.numel() < 1 or philox_offset.get_device() != index:
         raise ValueError("philox_offset must be an int32 tensor on x's device")
     return p, philox_offset.data_ptr()
 
@@ -796,24 +799,26 @@ _LAYER_NORM_PLANS = {}     # descriptor, workspace size and shape of the statist
 
 
 def _layer_norm_plan(x, gamma, beta, eps, act):
-    key = (x.shape, x.stride(), x.dtype, x.is_cuda, eps, act,
-           None if gamma is None else (gamma.shape, gamma.dtype, gamma.is_contiguous()),
-           None if beta is None else (beta.shape, beta.dtype, beta.is_contiguous()))
+    key = (x.shape, x.stride(), x.dtype, eps, act, None if gamma is None else (gamma.shape, gamma.stride(), gamma.dtype),
+           None if beta is None else (beta.shape, beta.stride(), beta.dtype))
     plan = _LAYER_NORM_PLANS.get(key)
     if plan is None:
+        plan = _layer_norm_desc(x, gamma, beta, eps, act)
         if len(_LAYER_NORM_PLANS) >= 1024:
             _LAYER_NORM_PLANS.clear()
-        plan = _LAYER_NORM_PLANS[key] = _layer_norm_desc(x, gamma, beta, eps, act)
-    dev = x.device
-    if (gamma is not None and gamma.device != dev) or (beta is not None and beta.device != dev):
+        _LAYER_NORM_PLANS[key] = plan
+    index = x.get_device()
+    if index < 0:
+        raise ValueError("expected CUDA tensors")
+    if (gamma is not None and gamma.get_device() != index) or (beta is not None and beta.get_device() != index):
         raise ValueError("gamma and beta must be on x's device")
     return plan
 
 
-def _check_stats(mean, rstd, shape, device):
-    if mean.shape != shape or rstd.shape != shape or mean.dtype != torch.float32 or rstd.dtype != torch.float32 \
-            or not (mean.is_contiguous() and rstd.is_contiguous()) or mean.device != device or rstd.device != device:
-        raise ValueError("mean and rstd must be the dense fp32 tensors of the forward call")
+def _check_stats(mean, rstd, shape, index):
+    for t in (mean, rstd):
+        if t.shape != shape or t.dtype is not torch.float32 or not t.is_contiguous() or t.get_device() != index:
+            raise ValueError("mean and rstd must be the dense fp32 tensors of the forward call")
 
 
 def layer_norm_fwd(x, gamma, beta, eps: float = 1e-5, act: str = "none"):
@@ -833,7 +838,7 @@ def layer_norm_bwd(dy, x, gamma, beta, mean, rstd, act: str = "none", want_dx: b
     """Gradients of layer_norm_fwd: (dx dense or None, dgamma or None, dbeta or None)."""
     d, nbytes, shape = _layer_norm_plan(x, gamma, beta, 0.0, act)
     _row_operand(dy, x, "dy")
-    _check_stats(mean, rstd, shape, x.device)
+    _check_stats(mean, rstd, shape, x.get_device())
     if not dy.is_contiguous():
         dy = dy.contiguous()
     dx = torch.empty_like(x, memory_format=torch.contiguous_format) if want_dx else None
@@ -853,7 +858,7 @@ def dropout(x, p: float, seed: int, tag: int = 0, residual=None, philox_offset=N
     code = DTYPE_CODES.get(x.dtype)
     if code is None or not x.is_cuda:
         raise ValueError("expected an fp32, bf16 or fp16 CUDA tensor")
-    p, offset = _dropout_args(p, seed, tag, philox_offset, x.device)
+    p, offset = _dropout_args(p, seed, tag, philox_offset, x.get_device())
     shape = x.shape
     if residual is not None:
         _row_operand(residual, x, "residual")
@@ -874,8 +879,8 @@ def dropout_add_layer_norm_fwd(x, residual, gamma, beta, p: float, seed: int, ta
     """h = residual + dropout(x) (residual may be None) and y = act(layer norm(h)) in one pass over the rows; arguments as in dropout
     and layer_norm_fwd.  Returns (y, h, mean, rstd), y and h dense."""
     d, _, shape = _layer_norm_plan(x, gamma, beta, eps, act)
-    p, offset = _dropout_args(p, seed, tag, philox_offset, x.device)
-    d = LayerNormDesc.from_buffer_copy(d)
+    p, offset = _dropout_args(p, seed, tag, philox_offset, x.get_device())
+    d = LayerNormDesc.from_buffer_copy(d)      # (a call of its own: plans are shared)
     d.p, d.seed, d.tag, d.philox_offset = p, seed, tag, offset
     if residual is not None:
         _row_operand(residual, x, "residual")
@@ -896,11 +901,11 @@ def dropout_add_layer_norm_bwd(dy, dh, h, gamma, beta, mean, rstd, p: float, see
     Returns (dx, dresidual, dgamma, dbeta), None where not wanted.  p, seed, tag, philox_offset as in the forward call (the device
     word must still hold the value it had then)."""
     d, nbytes, shape = _layer_norm_plan(h, gamma, beta, 0.0, act)
-    p, offset = _dropout_args(p, seed, tag, philox_offset, h.device)
+    p, offset = _dropout_args(p, seed, tag, philox_offset, h.get_device())
     if not h.is_contiguous():
         raise ValueError("h must be the dense tensor of the forward call")
     _row_operand(dy, h, "dy")
-    _check_stats(mean, rstd, shape, h.device)
+    _check_stats(mean, rstd, shape, h.get_device())
     if not dy.is_contiguous():
         dy = dy.contiguous()
     if dh is not None:
