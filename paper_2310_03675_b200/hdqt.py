@@ -821,14 +821,20 @@ def _check_stats(mean, rstd, shape, index):
             raise ValueError("mean and rstd must be the dense fp32 tensors of the forward call")
 
 
+def _new_stats(shape, device):
+    if not shape:      # one row
+        return torch.empty((), dtype=torch.float32, device=device), torch.empty((), dtype=torch.float32, device=device)
+    # (sizes as single arguments: a tuple takes torch another microsecond)
+    return torch.empty(*shape, dtype=torch.float32, device=device), torch.empty(*shape, dtype=torch.float32, device=device)
+
+
 def layer_norm_fwd(x, gamma, beta, eps: float = 1e-5, act: str = "none"):
     """act(layer norm) over the last dimension of x[..., channels] (evenly spaced rows: a slice of the channels is fine).
     gamma, beta: [channels], fp32 or x's type, or None.  act: "none", "relu" or "silu".
     Returns (y dense, mean fp32 [...], rstd fp32 [...])."""
     d, _, shape = _layer_norm_plan(x, gamma, beta, eps, act)
     y = torch.empty_like(x, memory_format=torch.contiguous_format)
-    dev = x.device
-    mean, rstd = torch.empty(shape, dtype=torch.float32, device=dev), torch.empty(shape, dtype=torch.float32, device=dev)
+    mean, rstd = _new_stats(shape, x.device)
     _call("hdqt_layer_norm_fwd", x, C.byref(d), x.data_ptr(), _ptr(gamma), _ptr(beta), y.data_ptr(), mean.data_ptr(),
           rstd.data_ptr())
     return y, mean, rstd
@@ -887,8 +893,7 @@ def dropout_add_layer_norm_fwd(x, residual, gamma, beta, p: float, seed: int, ta
         d.r_row_stride = _row_stride(residual, "residual")
     y = torch.empty_like(x, memory_format=torch.contiguous_format)
     h = torch.empty_like(x, memory_format=torch.contiguous_format)
-    dev = x.device
-    mean, rstd = torch.empty(shape, dtype=torch.float32, device=dev), torch.empty(shape, dtype=torch.float32, device=dev)
+    mean, rstd = _new_stats(shape, x.device)
     _call("hdqt_dropout_add_layer_norm_fwd", x, C.byref(d), x.data_ptr(), _ptr(residual), _ptr(gamma), _ptr(beta), h.data_ptr(),
           y.data_ptr(), mean.data_ptr(), rstd.data_ptr())
     return y, h, mean, rstd
