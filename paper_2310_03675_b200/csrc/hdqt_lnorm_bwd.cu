@@ -667,13 +667,14 @@ __global__ void __launch_bounds__(256) long_param_kernel(const RowParams p) {
 // ---- host side -----------------------------------------------------------------------------------------------
 
 template <typename T, int K, bool kFused, bool kSub>
-bool bwd_teams(RowParams p, int* parts, hdqt_status_t* st, cudaStream_t s) {
+bool bwd_teams(RowParams p, int threads, int* parts, hdqt_status_t* st, cudaStream_t s) {
   constexpr int V = 16 / sizeof(T), kThreads = K * V == 32 ? 512 : 640;
   constexpr bool kKeep = K * V <= 16;
   p.team = team_size(row_chunks(p, V), K);
   Shape shape;
   const int params = p.act != HDQT_ACT_NONE ? 2 : 1;
-  if (p.team > kThreads || !shape_of(&p, sizeof(T), K, params, kFused ? 3 : 2, kThreads, true, &shape)) return false;
+  if (threads < p.team || threads > kThreads) threads = kThreads;
+  if (p.team > threads || !shape_of(&p, sizeof(T), K, params, kFused ? 3 : 2, threads, true, &shape)) return false;
   if (p.classes > 1) *st = launch_rows<team_bwd_kernel<T, K, kFused, true, kSub, kThreads, kKeep>>(p, shape, s);
   else *st = launch_rows<team_bwd_kernel<T, K, kFused, false, kSub, kThreads, kKeep>>(p, shape, s);
   *parts = shape.blocks;
@@ -705,13 +706,31 @@ hdqt_status_t run_bwd(RowParams p, bool wide, bool few, bool params, int* parts,
   }
   if (wide) {
     hdqt_status_t st = HDQT_OK;
-    if (chunks <= 16 * (8 / V)) {
-      if (bwd_teams<T, 8 / V, kFused, true>(p, parts, &st, s)) return st;
+    // Elements per thread, 8, 16 or 32 (which form gamma dz twice instead of keeping it):
+    const int64_t total = p.rows * chunks;
+    const bool cheap = p.act != HDQT_ACT_SILU;
+    int k, threads = kFused ? 512 : 640;                // (65536 x 1024 bf16 with dropout: 111 us with 512 threads, 125 with 640)
+    if (sizeof(T) == 4) {
+      // fp32: 8192 x 4096 72.6 us with 16, 76.5 with 8; 2048 x 2048 15.4 and 14.7, 20000 x 333 29 and 22; with dropout 8
+      k = !kFused && p.classes == 1 && chunks >= 512 && total >= 4000000 ? kMost / 2 : kMost / 4;
+      if (k == kMost / 2) threads = 512;
+    } else if (p.classes > 1) {
+      // cut rows: 20000 x 1001 bf16 30.8 us with 32, 34.4 with 8 (SiLU: 46.7 and 39.4), 47 with 16, which spill
+      k = cheap && chunks >= 96 && (!kFused || total >= 2000000) ? kMost : kMost / 4;
+    } else if (kFused) {
+      // 8192 x 8192 116 us with 32, 126 with 16; 16384 x 4096 130 and 117
+      k = cheap && chunks >= 1024 ? kMost : kMost / 2;
     } else {
-      const int k = kFused && sizeof(T) == 4 ? kMost / 4 : !kFused && sizeof(T) == 2 && chunks >= 512 ? kMost : kMost / 2;
-      if ((k <= kMost / 4 || chunks <= 16 * (kMost / 2)) && bwd_teams<T, kMost / 4, kFused, false>(p, parts, &st, s)) return st;
-      if ((k <= kMost / 2 || chunks <= 16 * kMost) && bwd_teams<T, kMost / 2, kFused, false>(p, parts, &st, s)) return st;
-      if (bwd_teams<T, kMost, kFused, false>(p, parts, &st, s)) return st;
+      // 16384 x 4096 72.6 us with 32, 81 with 16; 60000 x 768 51.5 and 54.5; 4096 x 2048 19.1 and 16.7
+      k = cheap && (chunks >= 512 || (chunks >= 96 && total >= 4000000)) ? kMost : kMost / 2;
+      if (chunks >= 256 && cheap) threads = 512;
+    }
+    if (chunks <= 16 * (8 / V)) {
+      if (bwd_teams<T, 8 / V, kFused, true>(p, 640, parts, &st, s)) return st;
+    } else {
+      if ((k <= kMost / 4 || chunks <= 16 * (kMost / 2)) && bwd_teams<T, kMost / 4, kFused, false>(p, threads, parts, &st, s)) return st;
+      if ((k <= kMost / 2 || chunks <= 16 * kMost) && bwd_teams<T, kMost / 2, kFused, false>(p, threads, parts, &st, s)) return st;
+      if (bwd_teams<T, kMost, kFused, false>(p, 512, parts, &st, s)) return st;
     }
   }
   p.classes = 1;

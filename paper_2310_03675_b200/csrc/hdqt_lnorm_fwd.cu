@@ -389,11 +389,12 @@ __global__ void __launch_bounds__(kLongThreads) long_fwd_kernel(const RowParams 
 // ---- host side -----------------------------------------------------------------------------------------------
 
 template <typename T, int K, bool kFused, bool kSub>
-bool fwd_teams(RowParams p, hdqt_status_t* st, cudaStream_t s) {
+bool fwd_teams(RowParams p, int threads, hdqt_status_t* st, cudaStream_t s) {
   constexpr int V = 16 / sizeof(T), kThreads = K * V == 32 ? 768 : 1024;
   p.team = team_size(row_chunks(p, V), K);
   Shape shape;
-  if (p.team > kThreads || !shape_of(&p, sizeof(T), K, 2, kFused ? 2 : 1, kThreads, false, &shape)) return false;
+  if (threads < p.team || threads > kThreads) threads = kThreads;
+  if (p.team > threads || !shape_of(&p, sizeof(T), K, 2, kFused ? 2 : 1, threads, false, &shape)) return false;
   if (p.classes > 1) *st = launch_rows<team_fwd_kernel<T, K, kFused, true, kSub, kThreads>>(p, shape, s);
   else *st = launch_rows<team_fwd_kernel<T, K, kFused, false, kSub, kThreads>>(p, shape, s);
   return true;
@@ -413,17 +414,22 @@ hdqt_status_t run_fwd(RowParams p, bool wide, cudaStream_t s) {
   if (wide) {
     hdqt_status_t st = HDQT_OK;
     const int chunks = row_chunks(p, V);
+    // One block per row, nothing staged, up to 5 MB (600 x 4096 bf16 6.4 us, walking teams 6.9; 4096 x 2048 bf16 13.4 against 11.6).  Cut
+    // rows load gamma and beta element by element, which pays for few of them only (5003 x 1531 fp16: 25.7 against 12.4 us).
     const int64_t total = p.rows * chunks;
-    const bool once = total <= (p.classes > 1 ? 100000 : 300000);
-    if (once && chunks <= 2048) return chunks <= 1024 ? fwd_once<T, 1, kFused>(p, s) : fwd_once<T, 2, kFused>(p, s);
-    constexpr int kBest = kFused || sizeof(T) == 4 ? kMost / 2 : kMost;
-    const int k = kFused && sizeof(T) == 4 ? kMost / 4 : kBest;
+    if (total <= (p.classes > 1 ? 100000 : 300000) && chunks <= 2048) return chunks <= 1024 ? fwd_once<T, 1, kFused>(p, s) : fwd_once<T, 2, kFused>(p, s);
+    // Elements per thread: many take less of the row's fixed work each, few leave more warps.  Without dropout 32 (fp32: 16): 16384 x 4096
+    // bf16 50.6 us against 54.6 with 16; with it 16 (fp32: 8): 91 against 97, but cut rows 32 (20000 x 1001 fp16: 40.6 against 46.2).
+    int k = kMost, threads = 768;
+    if (kFused ? p.classes == 1 || sizeof(T) == 4 : sizeof(T) == 4) k = kFused && sizeof(T) == 4 ? kMost / 4 : kMost / 2;
+    // (65536 x 1024 bf16 with dropout: 88 us with 768 threads, 101 with 1024; 8192 x 8192: 121 and 98)
+    if (kFused && chunks >= 512) threads = 1024;
     if (chunks <= 16 * (8 / V)) {
-      if (fwd_teams<T, 8 / V, kFused, true>(p, &st, s)) return st;
+      if (fwd_teams<T, 8 / V, kFused, true>(p, 1024, &st, s)) return st;
     } else {
-      if ((k <= kMost / 4 || chunks <= 16 * (kMost / 2)) && fwd_teams<T, kMost / 4, kFused, false>(p, &st, s)) return st;
-      if ((k <= kMost / 2 || chunks <= 16 * kMost) && fwd_teams<T, kMost / 2, kFused, false>(p, &st, s)) return st;
-      if (fwd_teams<T, kMost, kFused, false>(p, &st, s)) return st;
+      if ((k <= kMost / 4 || chunks <= 16 * (kMost / 2)) && fwd_teams<T, kMost / 4, kFused, false>(p, 1024, &st, s)) return st;
+      if ((k <= kMost / 2 || chunks <= 16 * kMost) && fwd_teams<T, kMost / 2, kFused, false>(p, threads, &st, s)) return st;
+      if (fwd_teams<T, kMost, kFused, false>(p, 768, &st, s)) return st;
     }
   }
   p.classes = 1;

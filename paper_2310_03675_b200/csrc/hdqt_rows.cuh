@@ -25,8 +25,9 @@ namespace hdqt {
 
 constexpr int kLongThreads = 1024;
 constexpr int kMostParts = 2 * kNumSMsHint;      // blocks that leave sums of dgamma and dbeta
-// "Few rows" need no workspace: every block either takes a row or sums up some columns of all rows.
-constexpr int kFewRows = 2 * kNumSMsHint, kFewChannels = 8192;
+// "Few rows" need no workspace: every block either takes a row or sums up some columns of all rows.  (1024 threads hold 2048 chunks of
+// a row, which 8000 channels never pass, however they are cut.)
+constexpr int kFewRows = 2 * kNumSMsHint, kFewChannels = 8000;
 constexpr int kMostStages = 2;
 constexpr size_t kMostSmem = 224 * 1024;         // dynamic shared memory of an SM's blocks together
 

@@ -108,10 +108,10 @@ def scale_of(p):
 SHAPES = [
     (40,), (1, 1), (3, 1), (1, 8), (5, 7), (2, 33), (37, 30), (3, 4, 12), (1000, 64), (130, 96), (17, 257), (33, 512), (9, 1000),
     (4, 1024), (5, 1531), (1500, 1152), (7, 2048), (300, 2050), (3, 4096), (2, 4100), (700, 4104), (2, 8192), (3, 8200), (2, 10001),
-    (2, 16384), (1, 16390), (2, 33000), (2, 40001),
+    (3, 7999), (2, 8000), (2, 8191), (2, 16384), (1, 16390), (2, 33000), (2, 40001),
     # enough rows for teams that walk over several
     (3001, 7), (5000, 24), (2003, 90), (1999, 128), (1501, 260), (1203, 513), (901, 1001), (700, 1531), (610, 3001), (450, 6001),
-    (401, 8200), (351, 10001), (330, 16384),
+    (401, 8200), (351, 10001), (330, 16384), (300, 16383), (296, 777), (297, 1000),
 ]
 
 
