@@ -388,15 +388,21 @@ __global__ void __launch_bounds__(kLongThreads) long_fwd_kernel(const RowParams 
 
 // ---- host side -----------------------------------------------------------------------------------------------
 
-template <typename T, int K, bool kFused, bool kSub>
+// kCut: rows may be cut (classes > 1)
+template <typename T, int K, bool kFused, bool kSub, bool kCut = true>
 bool fwd_teams(RowParams p, int threads, hdqt_status_t* st, cudaStream_t s) {
   constexpr int V = 16 / sizeof(T), kThreads = K * V == 32 ? 768 : 1024;
   p.team = team_size(row_chunks(p, V), K);
   Shape shape;
   if (threads < p.team || threads > kThreads) threads = kThreads;
   if (p.team > threads || !shape_of(&p, sizeof(T), K, 2, kFused ? 2 : 1, threads, false, &shape)) return false;
-  if (p.classes > 1) *st = launch_rows<team_fwd_kernel<T, K, kFused, true, kSub, kThreads>>(p, shape, s);
-  else *st = launch_rows<team_fwd_kernel<T, K, kFused, false, kSub, kThreads>>(p, shape, s);
+  if constexpr (kCut) {
+    if (p.classes > 1) {
+      *st = launch_rows<team_fwd_kernel<T, K, kFused, true, kSub, kThreads>>(p, shape, s);
+      return true;
+    }
+  }
+  *st = launch_rows<team_fwd_kernel<T, K, kFused, false, kSub, kThreads>>(p, shape, s);
   return true;
 }
 
@@ -424,6 +430,13 @@ hdqt_status_t run_fwd(RowParams p, bool wide, cudaStream_t s) {
     if (kFused ? p.classes == 1 || sizeof(T) == 4 : sizeof(T) == 4) k = kFused && sizeof(T) == 4 ? kMost / 4 : kMost / 2;
     // (65536 x 1024 bf16 with dropout: 88 us with 768 threads, 101 with 1024; 8192 x 8192: 121 and 98)
     if (kFused && chunks >= 512) threads = 1024;
+    // Part of a warp per row, 8 elements per thread, or 16 where those are not mostly idle: 500000 x 64 bf16 25.0 us against 30.2, 200000 x 96 fp32 28.1 and 29.2;
+    // with dropout and for cut rows 8 were faster.
+    if constexpr (!kFused) {
+      if (p.classes == 1 && chunks >= (V == 8 ? 8 : 20) && chunks <= 16 * (16 / V) &&
+          fwd_teams<T, 16 / V, false, true, false>(p, 1024, &st, s))
+        return st;
+    }
     if (chunks <= 16 * (8 / V)) {
       if (fwd_teams<T, 8 / V, kFused, true>(p, 1024, &st, s)) return st;
     } else {

@@ -110,7 +110,7 @@ SHAPES = [
     (4, 1024), (5, 1531), (1500, 1152), (7, 2048), (300, 2050), (3, 4096), (2, 4100), (700, 4104), (2, 8192), (3, 8200), (2, 10001),
     (3, 7999), (2, 8000), (2, 8191), (2, 16384), (1, 16390), (2, 33000), (2, 40001),
     # enough rows for teams that walk over several
-    (3001, 7), (5000, 24), (2003, 90), (1999, 128), (1501, 260), (1203, 513), (901, 1001), (700, 1531), (610, 3001), (450, 6001),
+    (3001, 7), (5000, 24), (2003, 90), (1999, 128), (1700, 256), (1501, 260), (1203, 513), (901, 1001), (700, 1531), (610, 3001), (450, 6001),
     (401, 8200), (351, 10001), (330, 16384), (300, 16383), (296, 777), (297, 1000),
 ]
 
