@@ -409,8 +409,9 @@ __global__ void __launch_bounds__(1024) once_bwd_kernel(const RowParams p) {
 
 // ---- any strides and addresses, rows in registers --------------------------------------------------------------
 
-template <typename T, int V, int K, bool kFused, int kMaxThreads>
+template <typename T, int K, bool kFused, int kMaxThreads>
 __global__ void __launch_bounds__(kMaxThreads) any_bwd_kernel(const RowParams p) {
+  constexpr int V = 1;
   using A = Vec<T, V>;
   __shared__ float s_sum[2][2 * kMaxThreads / 32];
   extern __shared__ __align__(16) char s_dyn[];
@@ -473,7 +474,7 @@ __global__ void __launch_bounds__(kMaxThreads) any_bwd_kernel(const RowParams p)
           if (live && c < p.channels) vh[k] = *reinterpret_cast<const A*>(dhs + c);
         }
       }
-      if (V < 8 && p.d.on && live) row_bits(p, row, t, size, bits);
+      if (p.d.on && live) row_bits(p, row, t, size, bits);
     }
     float s[2] = {0.0f, 0.0f};
     with_act(p.act, [&]<int kAct>() {
@@ -500,7 +501,7 @@ __global__ void __launch_bounds__(kMaxThreads) any_bwd_kernel(const RowParams p)
       }
     });
     team_sum(s, team, t, size, s_sum[turn]);
-    if (kFused && V < 8 && size <= 32) __syncwarp();
+    if (kFused && size <= 32) __syncwarp();
     const float m1 = s[0] * inv_c, m2 = s[1] * inv_c;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -519,7 +520,7 @@ __global__ void __launch_bounds__(kMaxThreads) any_bwd_kernel(const RowParams p)
           }
           if (p.dres) *reinterpret_cast<A*>(reinterpret_cast<T*>(p.dres) + row * p.y_rs + c) = pack<T>(o);
           if (p.d.on) {
-            const uint32_t b = chunk_bits<V>(p, row, c, bits);
+            const uint32_t b = element_bit(p, row, c, bits);
 #pragma unroll
             for (int j = 0; j < V; ++j) o[j] = dropped(o[j], b, j, p.d.scale);
           }
@@ -755,7 +756,7 @@ hdqt_status_t run_bwd(RowParams p, bool wide, bool few, bool params, int* parts,
     const size_t bits = kFused ? (size_t)2 * teams * p.bits_stride : 0, sums = sums_bytes(p, block, p.channels);
     const int64_t needed = (p.rows + teams - 1) / teams;
     *parts = (int)(needed < kMostParts ? needed : kMostParts);
-    return launch_rows<any_bwd_kernel<T, 1, 8, kFused, 512>>(p, Shape{*parts, block, bits > sums ? bits : sums}, s);
+    return launch_rows<any_bwd_kernel<T, 8, kFused, 512>>(p, Shape{*parts, block, bits > sums ? bits : sums}, s);
   }
   const unsigned blocks = (unsigned)(p.rows < 2 * kNumSMsHint ? p.rows : 2 * kNumSMsHint);
   const bool vector = wide && p.channels % V == 0;

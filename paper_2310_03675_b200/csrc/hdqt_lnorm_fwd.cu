@@ -226,8 +226,9 @@ __global__ void __launch_bounds__(1024) once_fwd_kernel(const RowParams p) {
 
 // ---- any strides and addresses, rows in registers --------------------------------------------------------------
 
-template <typename T, int V, int K, bool kFused>
+template <typename T, int K, bool kFused>
 __global__ void __launch_bounds__(1024) any_fwd_kernel(const RowParams p) {
+  constexpr int V = 1;
   using A = Vec<T, V>;
   __shared__ float s_sum[2][32];
   extern __shared__ __align__(16) char s_dyn[];
@@ -252,7 +253,7 @@ __global__ void __launch_bounds__(1024) any_fwd_kernel(const RowParams p) {
       vr[k] = A{};
       if (p.residual && live && c < p.channels) vr[k] = *reinterpret_cast<const A*>(res + c);
     }
-    if (V < 8 && p.d.on) {
+    if (p.d.on) {
       if (live) row_bits(p, row, t, size, bits);
       team_barrier(team, size);
     }
@@ -268,7 +269,7 @@ __global__ void __launch_bounds__(1024) any_fwd_kernel(const RowParams p) {
       float r[V];
       unpack(vr[k], r);
       if (p.d.on && live && c < p.channels) {
-        const uint32_t b = chunk_bits<V>(p, row, c, bits);
+        const uint32_t b = element_bit(p, row, c, bits);
 #pragma unroll
         for (int j = 0; j < V; ++j) x[k][j] = dropped(x[k][j], b, j, p.d.scale);
       }
@@ -451,7 +452,7 @@ hdqt_status_t run_fwd(RowParams p, bool wide, cudaStream_t s) {
     const int per_block = p.team <= 32 ? 128 / p.team : 1, block = p.team <= 32 ? 128 : p.team;
     p.bits_stride = p.channels / 8 + 2;
     const size_t smem = kFused ? (size_t)per_block * p.bits_stride : 0;
-    any_fwd_kernel<T, 1, 16, kFused><<<(unsigned)((p.rows + per_block - 1) / per_block), block, smem, s>>>(p);
+    any_fwd_kernel<T, 16, kFused><<<(unsigned)((p.rows + per_block - 1) / per_block), block, smem, s>>>(p);
     return last_error("layer norm");
   }
   const unsigned blocks = (unsigned)(p.rows < 2 * kNumSMsHint ? p.rows : 2 * kNumSMsHint);

@@ -115,7 +115,6 @@ __device__ __forceinline__ void team_barrier(int team, int size) {
   else asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(size) : "memory");
 }
 
-
 // Sums over the lanes of a warp, or of `size` < 32 lanes (kSub).
 template <bool kSub, int N>
 __device__ __forceinline__ void lanes_total(float (&v)[N], int size) {
@@ -399,18 +398,15 @@ __device__ __forceinline__ void team_sum(float (&v)[N], int team, int t, int siz
   }
 }
 
-// Dropout decisions of a whole row for accesses narrower than a Philox group of eight: a byte per group in shared memory (visible
-// after the team's next barrier), bit (o & 7) of byte o >> 3 for the element at o = (row * channels) % 8 + channel.
+// Dropout decisions of a whole row: a byte per Philox group of eight in shared memory (visible after the team's next barrier), bit
+// (o & 7) of byte o >> 3 for the element at o = (row * channels) % 8 + channel.
 __device__ __forceinline__ void row_bits(const RowParams& p, int64_t row, int t, int size, uint8_t* bits) {
   const uint64_t first = (uint64_t)row * (uint64_t)p.channels;
   const int groups = ((int)(first & 7) + p.channels + 7) >> 3;
   const uint32_t offset = drop_offset(p.d);
   for (int k = t; k < groups; k += size) bits[k] = (uint8_t)drop_bits(p.d, offset, (first >> 3) + k);
 }
-// those of the V elements from channel c on
-template <int V>
-__device__ __forceinline__ uint32_t chunk_bits(const RowParams& p, int64_t row, int c, const uint8_t* bits) {
-  if constexpr (V == 8) return drop_bits(p.d, drop_offset(p.d), ((uint64_t)row * (uint64_t)p.channels + c) >> 3);
+__device__ __forceinline__ uint32_t element_bit(const RowParams& p, int64_t row, int c, const uint8_t* bits) {
   const int o = ((int)((uint64_t)row * (uint64_t)p.channels) & 7) + c;
   return bits[o >> 3] >> (o & 7);
 }

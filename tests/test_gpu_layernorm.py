@@ -203,6 +203,37 @@ def test_slices_odd_addresses_and_missing_parameters(dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("lo,hi", [(8, 104), (16, 72), (0, 200), (1, 34), (3, 200), (5, 101), (64, 65)])
+def test_many_rows_of_wider_tensors(dtype, lo, hi):
+    """Rows apart in memory, at 16-byte boundaries and elsewhere, more of them than blocks."""
+    wide, gamma, beta, dy = inputs((1700, 200), dtype, "fp32", seed=hi)
+    other = inputs((1700, 248), dtype, "fp32", seed=hi + 1)[0]
+    x, d, r = wide[:, lo:hi], dy[:, lo:hi], other[:, lo:hi]
+    g, b = gamma[lo:hi], beta[lo:hi]
+    want = reference(x, g, b, "silu", d)
+    y, mean, rstd = hdqt.layer_norm_fwd(x, g, b, EPS, "silu")
+    for got, name in ((y, "y"), (mean, "mean"), (rstd, "rstd")):
+        close(got, want[name])
+    for got, name in zip(hdqt.layer_norm_bwd(d, x, g, b, mean, rstd, "silu"), ("dx", "dgamma", "dbeta")):
+        close(got, want[name])
+    y, h, mean, rstd = hdqt.dropout_add_layer_norm_fwd(x, r, g, b, 0.3, 8, eps=EPS)
+    keep = kept(h.numel(), 0.3, 8).cuda().view(h.shape)
+    assert torch.equal(h, (r.float() + torch.where(keep, x.float() * torch.tensor(scale_of(0.3), device="cuda"), 0.0)).to(x.dtype))
+    close(y, reference(h, g, b, "none")["y"])
+    # h, dy and dx at addresses that no 16-byte access fits, all in one call
+    if hi - lo > 1:
+        n = h.numel()
+        odd = lambda t: torch.empty(n + 1, dtype=t.dtype, device="cuda")[1:].view(t.shape).copy_(t)  # noqa: E731
+        ho, do = odd(h), odd(d)
+        want = reference(h, g, b, "none", d)
+        dx, dres, dgamma, dbeta = hdqt.dropout_add_layer_norm_bwd(do, None, ho, g, b, mean, rstd, 0.3, 8)
+        for got, name in ((dres, "dx"), (dgamma, "dgamma"), (dbeta, "dbeta")):
+            close(got, want[name])
+        assert not bool(dx[~keep].any()) and torch.equal(dx != 0, keep & (dres != 0))
+
+
+@pytest.mark.gpu
 def test_large_mean_constant_rows_and_outliers():
     x, gamma, beta, dy = inputs((20, 1000), "fp32", "fp32", seed=3)
     x = x + 1000.0

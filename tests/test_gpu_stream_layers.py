@@ -136,7 +136,7 @@ def test_recorded_steps_equal_eager_steps_and_drop_anew():
         if graphed:
             step = hnn.GraphedTrainStep(model, opt, x, labels, base_step=3, clip_norm=1.0)
             word = step.counter
-            losses = [float(step(x, labels)) for _ in range(5)]
+            losses = [float(step(x, labels).detach()) for _ in range(5)]
             assert int(word) == 8
         else:
             word = torch.zeros(1, dtype=torch.int32, device="cuda")
