@@ -429,6 +429,8 @@ hdqt_status_t run_fwd(RowParams p, bool wide, cudaStream_t s) {
     // bf16 50.6 us against 54.6 with 16; with it 16 (fp32: 8): 91 against 97, but cut rows 32 (20000 x 1001 fp16: 40.6 against 46.2).
     int k = kMost, threads = 768;
     if (kFused ? p.classes == 1 || sizeof(T) == 4 : sizeof(T) == 4) k = kFused && sizeof(T) == 4 ? kMost / 4 : kMost / 2;
+    // (8192 x 16384 bf16 134 us with 16, 140 with 32: one row at a time is all that an SM holds)
+    if (chunks > 1536 && p.classes == 1 && k > kMost / 2) k = kMost / 2;
     // (65536 x 1024 bf16 with dropout: 88 us with 768 threads, 101 with 1024; 8192 x 8192: 121 and 98)
     if (kFused && chunks >= 512) threads = 1024;
     // Part of a warp per row, 8 elements per thread, or 16 where those are not mostly idle: 500000 x 64 bf16 25.0 us against 30.2, 200000 x 96 fp32 28.1 and 29.2;
