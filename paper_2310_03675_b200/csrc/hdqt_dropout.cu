@@ -1,7 +1,8 @@
 // Dropout, added to a residual: y = residual + (u >= T ? x scale : 0), u 16 bits of Philox4x32-10 per element.
 //
 // One Philox call serves eight consecutive elements (of the flattened tensor), which is one 16-byte access of a 16-bit type and two
-// of fp32.  Bound by HBM: x and residual read once, y written once; the generator costs about 6 instructions per element.
+// of fp32.  Bound by HBM: x and residual read once, y written once.  32768 x 4096 bf16: 81 us (6.6 TB/s, what a copy reaches), with a
+// residual 116 us (6.9); 14 instructions per element, six of them the generator's, fill 65 % of the issue slots.
 #include "hdqt_dropout.cuh"
 
 namespace hdqt {
