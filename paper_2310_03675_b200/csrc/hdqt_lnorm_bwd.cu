@@ -707,6 +707,12 @@ hdqt_status_t bwd_once(RowParams p, bool params, cudaStream_t s) {
 
 bool few_rows(const hdqt_layer_norm_desc_t& d) { return d.rows <= kFewRows && d.channels <= kFewChannels; }
 
+// shares of the rows whose columns long_param_kernel sums up, with `columns` blocks next to each other: about eight blocks per SM
+int long_shares(int64_t rows, int64_t columns) {
+  const int64_t want = (8 * kNumSMsHint + columns - 1) / columns, shares = want < rows ? want : rows;
+  return (int)(shares < kMostParts ? shares : kMostParts);
+}
+
 template <typename T, bool kFused>
 hdqt_status_t run_bwd(RowParams p, bool wide, bool few, bool params, int* parts, cudaStream_t s) {
   constexpr int V = 16 / sizeof(T), kMost = 32 / V;
@@ -770,9 +776,7 @@ hdqt_status_t run_bwd(RowParams p, bool wide, bool few, bool params, int* parts,
   }
   if (p.part) {
     const unsigned columns = (unsigned)((p.channels / (vector ? V : 1) + 255) / 256);
-    const int64_t want = (8 * kNumSMsHint + columns - 1) / columns;
-    const int64_t shares = want < p.rows ? want : p.rows;
-    *parts = (int)(shares < kMostParts ? shares : kMostParts);
+    *parts = long_shares(p.rows, columns);
     if (vector) long_param_kernel<T, V><<<dim3(columns, (unsigned)*parts), 256, 0, s>>>(p);
     else long_param_kernel<T, 1><<<dim3(columns, (unsigned)*parts), 256, 0, s>>>(p);
   }
@@ -828,7 +832,10 @@ using namespace hdqt;
 
 extern "C" size_t hdqt_layer_norm_workspace_bytes(const hdqt_layer_norm_desc_t* d) {
   if (check_rows_desc(d, false) != HDQT_OK || few_rows(*d)) return 0;
-  const int64_t parts = d->rows < kMostParts - 7 ? d->rows + 7 : kMostParts;      // (a block of every class, rows or not)
+  int64_t parts = d->rows < kMostParts - 7 ? d->rows + 7 : kMostParts;            // (a block of every class, rows or not)
+  if (d->channels > kMostTeamChannels) {                                          // (the widest access makes for the most shares)
+    parts = long_shares(d->rows, (d->channels / 8 + 255) / 256);
+  }
   return align256((size_t)parts * d->channels * sizeof(float2));
 }
 

@@ -25,10 +25,11 @@ namespace hdqt {
 
 constexpr int kLongThreads = 1024;
 constexpr int kMostParts = 2 * kNumSMsHint;      // blocks that leave sums of dgamma and dbeta
+constexpr int kMostTeamChannels = 512 * 32;      // of a row in registers, backward
 // "Few rows" need no workspace: every block either takes a row or sums up some columns of all rows.  (1024 threads hold 2048 chunks of
 // a row, which 8000 channels never pass, however they are cut.)
 constexpr int kFewRows = 2 * kNumSMsHint, kFewChannels = 8000;
-constexpr int kMostStages = 2;
+constexpr int kMostStages = 2;                   // rows a team has in flight (more gained nothing)
 constexpr size_t kMostSmem = 224 * 1024;         // dynamic shared memory of an SM's blocks together
 
 struct RowParams {
@@ -44,7 +45,7 @@ struct RowParams {
   const void* beta;
   int32_t param_dtype, act, channels;
   int32_t team;                  // threads of a row: a power of two below 32, or a multiple of 32
-  int32_t stages;                // rows a team has in flight
+  int32_t stages;                // rows a team has in flight, 1 or 2
   int32_t classes;               // rows that are cut at different places (1 = all alike)
   int32_t params_wide;           // gamma and beta start on 16-byte boundaries
   int32_t bits_stride;           // any_*: bytes of a team's dropout decisions in shared memory
@@ -161,9 +162,7 @@ __device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_
 // all but the copies of the last stages - 1 rows have arrived
 __device__ __forceinline__ void wait_copies(int stages) {
   if (stages == 1) asm volatile("cp.async.wait_group 0;" ::: "memory");
-  else if (stages == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
-  else if (stages == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
-  else asm volatile("cp.async.wait_group 3;" ::: "memory");
+  else asm volatile("cp.async.wait_group 1;" ::: "memory");
 }
 
 // elements [first, first + V) of a chunk that belong to the row, as bits
@@ -416,8 +415,6 @@ __device__ __forceinline__ float dropped(float x, uint32_t bits, int j, float sc
   return (bits >> j) & 1 ? __fmul_rn(x, scale) : 0.0f;
 }
 
-template <typename T>
-__device__ __forceinline__ float rounded(float v) { return to_f32(from_f32<T>(v)); }
 
 
 // ---- host side -----------------------------------------------------------------------------------------------

@@ -25,8 +25,8 @@ E = 2.0 ** -24
 EPS = 1e-5
 
 
-def reference(x, gamma, beta, act, dy=None, dh=None, eps=EPS):
-    """64-bit forward and backward over the last dimension, with the error bounds of the docstring."""
+def reference(x, gamma, beta, act, dy=None, dh=None, eps=EPS, terms=96):
+    """64-bit forward and backward over the last dimension, with the error bounds of the docstring (`terms` in the place of 96)."""
     c = x.shape[-1]
     xd = x.double()
     g = torch.ones(c, dtype=torch.float64, device=x.device) if gamma is None else gamma.double()
@@ -37,13 +37,13 @@ def reference(x, gamma, beta, act, dy=None, dh=None, eps=EPS):
     xh = (xd - mu) * rs
     z = xh * g + b
     size = mean(xd.abs()) + xd.abs()
-    exh = 96 * E * rs * size
+    exh = terms * E * rs * size
     ez = g.abs() * exh + 8 * E * (b.abs() + z.abs())
     sig = torch.sigmoid(z)
     y = {"none": z, "relu": z.clamp_min(0), "silu": z * sig}[act]
     out = {"y": (y, ez * 1.2 + (2.0 ** -20 * z.abs() if act == "silu" else 0)),
-           "mean": (mu[..., 0], 96 * E * mean(xd.abs())[..., 0]),
-           "rstd": (rs[..., 0], (rs * 96 * E * (1 + rs * mean(xd.abs())))[..., 0]),
+           "mean": (mu[..., 0], terms * E * mean(xd.abs())[..., 0]),
+           "rstd": (rs[..., 0], (rs * terms * E * (1 + rs * mean(xd.abs())))[..., 0]),
            "z_margin": float((z.abs() / (ez + 1e-30)).min()) if z.numel() else 2.0}
     if dy is not None:
         d = dy.double()
@@ -52,8 +52,8 @@ def reference(x, gamma, beta, act, dy=None, dh=None, eps=EPS):
         dz, edz = d * slope, d.abs() * (eslope + 4 * E)
         dg, edg = dz * g, edz * g.abs()
         m1, m2 = mean(dg), mean(dg * xh)
-        em1 = mean(edg) + 192 * E * mean(dg.abs())
-        em2 = mean(edg * xh.abs() + dg.abs() * exh) + 192 * E * mean((dg * xh).abs())
+        em1 = mean(edg) + 2 * terms * E * mean(dg.abs())
+        em2 = mean(edg * xh.abs() + dg.abs() * exh) + 2 * terms * E * mean((dg * xh).abs())
         dx = rs * (dg - m1 - xh * m2)
         edx = rs * (edg + em1 + xh.abs() * em2 + exh * m2.abs() + 16 * E * (dg.abs() + m1.abs() + (xh * m2).abs())) + dx.abs() * 128 * E
         if dh is not None:
@@ -302,6 +302,28 @@ def test_non_finite_values_stay_in_their_row():
     clean = hdqt.dropout_add_layer_norm_fwd(x, None, gamma, beta, 0.5, 11)
     dirty = hdqt.dropout_add_layer_norm_fwd(torch.where(keep, x, math.nan), None, gamma, beta, 0.5, 11)
     assert all(torch.equal(a, b) for a, b in zip(clean, dirty))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_the_longest_rows(dtype):
+    """2^20 channels: 1024 terms per thread and 10 additions behind them in a sum, so 1100 e in the place of 96 e."""
+    x, gamma, beta, dy = inputs((3, 1 << 20), dtype, "fp32", seed=2)
+    res = inputs((3, 1 << 20), dtype, "fp32", seed=3)[0]
+    want = reference(x, gamma, beta, "none", dy, terms=1100)
+    y, mean, rstd = hdqt.layer_norm_fwd(x, gamma, beta, EPS)
+    for got, name in ((y, "y"), (mean, "mean"), (rstd, "rstd")):
+        close(got, want[name])
+    for got, name in zip(hdqt.layer_norm_bwd(dy, x, gamma, beta, mean, rstd), ("dx", "dgamma", "dbeta")):
+        close(got, want[name])
+    y, h, mean, rstd = hdqt.dropout_add_layer_norm_fwd(x, res, gamma, beta, 0.5, 3, eps=EPS)
+    want = reference(h, gamma, beta, "none", dy, res, terms=1100)
+    close(y, want["y"])
+    dx, dres, dgamma, dbeta = hdqt.dropout_add_layer_norm_bwd(dy, res, h, gamma, beta, mean, rstd, 0.5, 3)
+    for got, name in ((dres, "dx"), (dgamma, "dgamma"), (dbeta, "dbeta")):
+        close(got, want[name])
+    assert torch.equal(h, hdqt.dropout(x, 0.5, 3, residual=res))
+    assert torch.equal(dx != 0, (hdqt.dropout(torch.ones_like(x), 0.5, 3) != 0) & (dres != 0))
 
 
 @pytest.mark.gpu
