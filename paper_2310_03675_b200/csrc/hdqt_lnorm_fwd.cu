@@ -138,11 +138,14 @@ __global__ void __launch_bounds__(kThreads, 1) team_fwd_kernel(const RowParams p
 }
 
 // ---- few rows: one per block, everything loaded at once --------------------------------------------------------
+// The mean is summed in 64 bits, which costs nothing here: next to values that nearly cancel an fp32 sum of one row can be off by
+// a few parts in 10^6 of the mean (over many rows such errors average out, and the walking teams sum in fp32).
 
 template <typename T, int K, bool kFused, bool kShift>
 __global__ void __launch_bounds__(1024) once_fwd_kernel(const RowParams p) {
   constexpr int V = 16 / sizeof(T);
-  __shared__ __align__(16) float s_sum[2 * kSlots];
+  __shared__ __align__(16) float s_sum[kSlots];
+  __shared__ double s_mean[32];
   const int64_t row = blockIdx.x;
   const int lead = kShift ? (int)((row * p.channels) & (V - 1)) : 0;
   const bool edge = row == p.rows - 1;
@@ -171,12 +174,11 @@ __global__ void __launch_bounds__(1024) once_fwd_kernel(const RowParams p) {
     }
   }
   if (blockDim.x > 32) {
-    for (int i = threadIdx.x; i < 2 * kSlots; i += blockDim.x) s_sum[i] = 0.0f;
-    __syncthreads();
+    for (int i = threadIdx.x; i < kSlots; i += blockDim.x) s_sum[i] = 0.0f;
   }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   float x[K][V];
-  float sum[1] = {0.0f};
+  double sum = 0.0;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const int q = k * blockDim.x + threadIdx.x;
@@ -196,11 +198,9 @@ __global__ void __launch_bounds__(1024) once_fwd_kernel(const RowParams p) {
       unpack<T>(h, x[k]);
     }
 #pragma unroll
-    for (int j = 0; j < V; ++j) sum[0] += x[k][j];
+    for (int j = 0; j < V; ++j) sum += (double)x[k][j];
   }
-  lanes_total<false>(sum, 32);
-  if (blockDim.x > 32) warps_total(sum, 0, blockDim.x, warp, lane, s_sum);
-  const float inv_c = 1.0f / (float)p.channels, mu = sum[0] * inv_c;
+  const float mu = (float)(block_total(sum, s_mean) * p.inv_channels), inv_c = (float)p.inv_channels;
   float m2[1] = {0.0f};
 #pragma unroll
   for (int k = 0; k < K; ++k) {
@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(1024) once_fwd_kernel(const RowParams p) {
     for (int j = 0; j < V; ++j) m2[0] = fmaf(x[k][j], x[k][j], m2[0]);
   }
   lanes_total<false>(m2, 32);
-  if (blockDim.x > 32) warps_total(m2, 0, blockDim.x, warp, lane, s_sum + kSlots);
+  if (blockDim.x > 32) warps_total(m2, 0, blockDim.x, warp, lane, s_sum);      // (the slots were cleared ahead of the mean's barrier)
   const float rs = __frsqrt_rn(fmaf(m2[0], inv_c, p.eps));
   if (threadIdx.x == 0) {
     p.mean[row] = mu;
@@ -429,7 +429,13 @@ hdqt_status_t run_fwd(RowParams p, bool wide, cudaStream_t s) {
     // One block per row, nothing staged, up to 5 MB (600 x 4096 bf16 6.4 us, walking teams 6.9; 4096 x 2048 bf16 13.4 against 11.6).  Cut
     // rows load gamma and beta element by element, which pays for few of them only (5003 x 1531 fp16: 25.7 against 12.4 us).
     const int64_t total = p.rows * chunks;
-    if (total <= (p.classes > 1 ? 100000 : 300000) && chunks <= 2048) return chunks <= 1024 ? fwd_once<T, 1, kFused>(p, s) : fwd_once<T, 2, kFused>(p, s);
+    if (total <= (p.classes > 1 ? 100000 : 300000)) {
+      if (chunks <= 1024) return fwd_once<T, 1, kFused>(p, s);
+      if (chunks <= 2048) return fwd_once<T, 2, kFused>(p, s);
+      if constexpr (sizeof(T) == 4) {
+        if (chunks <= 4096) return fwd_once<T, 4, kFused>(p, s);
+      }
+    }
     // Elements per thread: many take less of the row's fixed work each, few leave more warps.  Without dropout 32 (fp32: 16): 16384 x 4096
     // bf16 50.6 us against 54.6 with 16; with it 16 (fp32: 8): 91 against 97, but cut rows 32 (20000 x 1001 fp16: 40.6 against 46.2).
     int k = kMost, threads = 768;

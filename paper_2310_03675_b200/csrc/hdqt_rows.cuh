@@ -53,6 +53,7 @@ struct RowParams {
   uint32_t step;                 // rows from a team's row to its next
   int64_t x_step, r_step, y_step, chunk_step;      // the same in bytes of the tensors, and in chunks of a dense tensor
   float eps;
+  double inv_channels;
   float* mean;
   float* rstd;
   float2* part;                  // [blocks, channels] sums of dbeta (x) and dgamma (y)
@@ -150,6 +151,20 @@ __device__ __forceinline__ void warps_total(float (&v)[N], int barrier, int size
     }
     v[i] = (a.x + a.y) + (a.z + a.w);
   }
+}
+
+// Sum over a block in 64 bits, every thread gets it; s: a value per warp.
+__device__ __forceinline__ double block_total(double v, double* s) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+  const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
+  if (warps == 1) return v;
+  if (lane == 0) s[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = lane < warps ? s[lane] : 0.0;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+  return v;
 }
 
 // ---- chunks --------------------------------------------------------------------------------------------------
@@ -445,6 +460,7 @@ inline RowParams make_row_params(const hdqt_layer_norm_desc_t& d, const void* ga
   p.r_rs = d.r_row_stride;
   p.y_rs = d.y_row_stride;
   p.eps = d.eps;
+  p.inv_channels = 1.0 / (double)d.channels;
   p.mean = mean;
   p.rstd = rstd;
   return p;

@@ -256,6 +256,17 @@ def test_large_mean_constant_rows_and_outliers():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("c", [40, 2024, 4099, 16384])
+def test_mean_of_a_few_rows_that_nearly_cancel(c):
+    """Summed in 64 bits and rounded once: e |mean|, and 2^-50 of the values' size for the 64-bit sum itself."""
+    x = inputs((3, c), "fp32", "fp32", seed=c, offset=0.0)[0]
+    x = x - x.mean(1, keepdim=True) + 1e-6
+    for mean in (hdqt.layer_norm_fwd(x, None, None, EPS)[1], hdqt.dropout_add_layer_norm_fwd(x, None, None, None, 0.0, 1)[2]):
+        want = x.double().mean(1)
+        assert bool(((mean.double() - want).abs() <= E * want.abs() + 2.0 ** -50 * x.abs().double().mean(1)).all())
+
+
+@pytest.mark.gpu
 def test_gradients_match_differences():
     """<grad, v> against (L(+h v) - L(-h v)) / 2h with h = 2^-5 and L formed in 64 bits from the call's outputs: the
     third-derivative term is h^2/6 = 1.6e-4 times O(1), the rounding of L e sqrt(n) |y| / h = 1e-4 of |v||c|."""
