@@ -680,10 +680,11 @@ bool bwd_teams(RowParams p, int threads, int* parts, hdqt_status_t* st, cudaStre
   Shape shape;
   const int params = p.act != HDQT_ACT_NONE ? 2 : 1;
   if (threads < p.team || threads > kThreads) threads = kThreads;
+  if (K * V == 16 && p.classes > 1 && threads > 512) threads = 512;      // (128 registers: cut rows spill with 96)
   if (p.team > threads || !shape_of(&p, sizeof(T), K, params, kFused ? 3 : 2, threads, true, &shape)) return false;
   if constexpr (kCut) {
     if (p.classes > 1) {
-      *st = launch_rows<team_bwd_kernel<T, K, kFused, true, kSub, kThreads, kKeep>>(p, shape, s);
+      *st = launch_rows<team_bwd_kernel<T, K, kFused, true, kSub, K * V == 16 ? 512 : kThreads, kKeep>>(p, shape, s);
       *parts = shape.blocks;
       return true;
     }
@@ -728,13 +729,14 @@ hdqt_status_t run_bwd(RowParams p, bool wide, bool few, bool params, int* parts,
     const int64_t total = p.rows * chunks;
     const bool cheap = p.act != HDQT_ACT_SILU;
     int k, threads = kFused ? 512 : 640;                // (65536 x 1024 bf16 with dropout: 111 us with 512 threads, 125 with 640)
-    if (sizeof(T) == 4) {
-      // fp32: 8192 x 4096 72.6 us with 16, 76.5 with 8; 2048 x 2048 15.4 and 14.7, 20000 x 333 29 and 22; with dropout 8
-      k = !kFused && p.classes == 1 && chunks >= 512 && total >= 4000000 ? kMost / 2 : kMost / 4;
+    if (p.classes > 1) {
+      // cut rows: 16, 20000 x 1001 bf16 30.2 us (8: 34.3, 32: 31.0), SiLU 35.8 (39.6, 47), with dropout 45.3 (51.6, 54); 8000 x 4099 56 with 32,
+      // 75 with 16.  fp32: 20000 x 333 20.8 us with 16, 22.3 with 8; with dropout 6000 x 777 26.5 and 25.3
+      k = !kFused && sizeof(T) == 2 && chunks >= 512 ? kMost : kFused && sizeof(T) == 4 ? kMost / 4 : kMost / 2;
+    } else if (sizeof(T) == 4) {
+      // fp32: 8192 x 4096 72.6 us with 16, 76.5 with 8; 2048 x 2048 15.4 and 14.7; with dropout 8
+      k = !kFused && chunks >= 512 && total >= 4000000 ? kMost / 2 : kMost / 4;
       if (k == kMost / 2) threads = 512;
-    } else if (p.classes > 1) {
-      // cut rows: 20000 x 1001 bf16 30.8 us with 32, 34.4 with 8 (SiLU: 46.7 and 39.4), 47 with 16, which spill
-      k = cheap && chunks >= 96 && (!kFused || total >= 2000000) ? kMost : kMost / 4;
     } else if (kFused) {
       // 8192 x 8192 116 us with 32, 126 with 16; 16384 x 4096 130 and 117
       k = cheap && chunks >= 1024 ? kMost : kMost / 2;
