@@ -674,7 +674,8 @@ __global__ void __launch_bounds__(256) long_param_kernel(const RowParams p) {
 // kCut: rows may be cut (classes > 1)
 template <typename T, int K, bool kFused, bool kSub, bool kCut = true>
 bool bwd_teams(RowParams p, int threads, int* parts, hdqt_status_t* st, cudaStream_t s) {
-  constexpr int V = 16 / sizeof(T), kThreads = K * V == 32 ? 512 : 640;
+  // (96 registers where that spills nothing)
+  constexpr int V = 16 / sizeof(T), kThreads = K * V == 32 || (K * V == 16 && !kSub && (kFused || sizeof(T) == 4)) ? 512 : 640;
   constexpr bool kKeep = K * V <= 16;
   p.team = team_size(row_chunks(p, V), K);
   Shape shape;

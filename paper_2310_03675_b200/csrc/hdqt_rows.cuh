@@ -293,8 +293,12 @@ struct Place {
       warp = w - team * warps;
       lane = threadIdx.x & 31;
     }
-    const uint32_t cls = kShift ? blockIdx.x % p.classes : 0;
-    row = (blockIdx.x / p.classes * teams + team) * p.classes + cls;
+    // the rows of a turn go round the blocks, so that those of the last turn are spread over all of them (kSub: the teams of a warp
+    // take neighbouring rows)
+    const uint32_t cls = kShift ? blockIdx.x % p.classes : 0, block = blockIdx.x / p.classes, blocks = gridDim.x / p.classes;
+    if constexpr (kSub) row = ((threadIdx.x >> 5) * blocks + block) * (32 / size) + (threadIdx.x & 31) / size;
+    else row = team * blocks + block;
+    row = row * p.classes + cls;
     ahead = kSub ? (threadIdx.x & 31) / size * p.classes : 0;
     lead = kShift ? (int)(((int64_t)cls * p.channels) & (V - 1)) : 0;
     first = (uint32_t)(warp * K * 32 + lane) * 16u;
