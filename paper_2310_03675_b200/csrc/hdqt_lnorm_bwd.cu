@@ -9,7 +9,7 @@ namespace hdqt {
 namespace {
 
 // 32768 x 8192 bf16 265 us (6.1 TB/s) and 8 us for the sums of dgamma and dbeta, 16384 x 4096 bf16 67 + 5; 16384 x 4096 bf16 with dropout and
-// residual 117 us (5.7 TB/s).  The sums take 2 of a thread's registers per element, which sets how many elements it can have: with 16
+// residual 113 us (5.9 TB/s).  The sums take 2 of a thread's registers per element, which sets how many elements it can have: with 16
 // gamma dz is kept between the two passes, with 32 (128 registers, 16 warps per SM) it is formed again from shared memory.
 //
 // kKeep: gamma dz stays in registers between the two passes over a row, otherwise it is formed again (wide rows)

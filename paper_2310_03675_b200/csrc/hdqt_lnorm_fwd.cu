@@ -8,8 +8,8 @@ namespace {
 // ---- teams that walk over the rows ---------------------------------------------------------------------------
 //
 // One block per SM; per row and warp of 1024 elements about 380 instructions, of which 100 are paired arithmetic.  Bound by HBM where rows
-// are many: 32768 x 8192 bf16 194 us (5.5 TB/s), 8192 x 4096 fp32 45 us (5.9), 16384 x 4096 bf16 with dropout and residual 90 us (6.0);
-// by some 4 us of launch and first loads below a few MB (4096 x 2048 bf16 11.6 us).  What keeps the first from the copy's rate is the
+// are many: 32768 x 8192 bf16 196 us (5.5 TB/s), 8192 x 4096 fp32 46 us (5.8), 16384 x 4096 bf16 with dropout and residual 89 us (6.0);
+// by some 4 us of launch and first loads below a few MB (4096 x 2048 bf16 10.6 us).  What keeps the first from the copy's rate is the
 // latency of two sums per row with three rows at work per SM, and gamma and beta from shared memory (half of its traffic).
 
 template <typename T, int K, bool kFused, bool kShift, bool kSub, int kThreads>
@@ -426,7 +426,7 @@ hdqt_status_t run_fwd(RowParams p, bool wide, cudaStream_t s) {
   if (wide) {
     hdqt_status_t st = HDQT_OK;
     const int chunks = row_chunks(p, V);
-    // One block per row, nothing staged, up to 5 MB (600 x 4096 bf16 6.4 us, walking teams 6.9; 4096 x 2048 bf16 13.4 against 11.6).  Cut
+    // One block per row, nothing staged, up to 5 MB (600 x 4096 bf16 6.4 us, walking teams 6.9; 4096 x 2048 bf16 13.4 against 10.6).  Cut
     // rows load gamma and beta element by element, which pays for few of them only (5003 x 1531 fp16: 25.7 against 12.4 us).
     const int64_t total = p.rows * chunks;
     if (total <= (p.classes > 1 ? 100000 : 300000)) {
