@@ -16,7 +16,7 @@ template <typename T, int K, bool kFused, bool kShift, bool kSub, int kThreads>
 __global__ void __launch_bounds__(kThreads, 1) team_fwd_kernel(const RowParams p) {
   constexpr int V = 16 / sizeof(T), H = V / 4, kStreams = kFused ? 2 : 1;
   constexpr uint32_t kStage = kStreams * K * 512;
-  __shared__ __align__(16) float s_sum[4 * kSlots];
+  __shared__ __align__(16) float s_sum[5 * kSlots];
   extern __shared__ __align__(16) char s_dyn[];
   const Place<T, K, kShift, kSub> me(p);
   const uint32_t params = params_bytes<T, K>(p.team, 2);
@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(kThreads, 1) team_fwd_kernel(const RowParams p
   }
   for (int i = 0; i < p.stages; ++i) fetch(ring + i * kStage);
   stage_params<T, K, kSub>(p, me.lead, 2, s_dyn);
-  for (int i = threadIdx.x; i < 4 * kSlots; i += blockDim.x) s_sum[i] = 0.0f;
+  for (int i = threadIdx.x; i < 5 * kSlots; i += blockDim.x) s_sum[i] = 0.0f;
   __syncthreads();
   float* slots = s_sum + (kSub ? 0 : me.team * ((p.team + 127) >> 7) * 4);
   const uint32_t offset = kFused ? drop_offset(p.d) : 0;
@@ -63,7 +63,6 @@ __global__ void __launch_bounds__(kThreads, 1) team_fwd_kernel(const RowParams p
     const bool live = !kSub || row < p.rows;
     wait_copies(p.stages);
     float x[K][V];
-    float sum[1] = {0.0f};
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       unpack<T>(shared_words(ring + stage + k * 512), x[k]);
@@ -82,31 +81,42 @@ __global__ void __launch_bounds__(kThreads, 1) team_fwd_kernel(const RowParams p
         unpack<T>(h, x[k]);
       }
     }
-    float part[2] = {0.0f, 0.0f};
+    float part[2] = {0.0f, 0.0f}, square[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int k = 0; k < K; ++k) {
 #pragma unroll
-      for (int j = 0; j < V; j += 2) add2(part[0], part[1], x[k][j], x[k][j + 1]);
+      for (int j = 0; j < V; j += 2) {
+        add2(part[0], part[1], x[k][j], x[k][j + 1]);
+        fma2(square[0], square[1], x[k][j], x[k][j + 1], x[k][j], x[k][j + 1], square[0], square[1]);
+      }
     }
-    sum[0] = part[0] + part[1];
+    float sum[2] = {part[0] + part[1], square[0] + square[1]};
     lanes_total<kSub>(sum, me.size);
     if (!kSub && me.size > 32) warps_total(sum, me.team + 1, me.size, me.warp, me.lane, slots + turn);
-    fetch(ring + stage);                                    // (the sum is there: the place has been read)
+    fetch(ring + stage);                                    // (the sums are there: the place has been read)
     const float mu = sum[0] * inv_c;
-    part[0] = part[1] = 0.0f;
+    float var = fmaf(-mu, mu, sum[1] * inv_c);
+    // A mean above the spread would cost the difference of the two sums its digits: the deviations are squared then.
+    const bool again = !(mu * mu <= var && var < INFINITY);
+    float center = 0.0f;                                    // what has been taken off x
+    if (kSub ? __any_sync(0xFFFFFFFFu, again) : again) {
+      center = again ? mu : 0.0f;
+      part[0] = part[1] = 0.0f;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const float center = me.has(k) ? -mu : 0.0f;          // (no chunk: 0 - 0)
+      for (int k = 0; k < K; ++k) {
+        const float c = me.has(k) ? -center : 0.0f;         // (no chunk: 0 - 0)
 #pragma unroll
-      for (int j = 0; j < V; j += 2) add2(x[k][j], x[k][j + 1], center, center);
-      me.clear(k, x[k]);
+        for (int j = 0; j < V; j += 2) add2(x[k][j], x[k][j + 1], c, c);
+        me.clear(k, x[k]);
 #pragma unroll
-      for (int j = 0; j < V; j += 2) fma2(part[0], part[1], x[k][j], x[k][j + 1], x[k][j], x[k][j + 1], part[0], part[1]);
+        for (int j = 0; j < V; j += 2) fma2(part[0], part[1], x[k][j], x[k][j + 1], x[k][j], x[k][j + 1], part[0], part[1]);
+      }
+      float m2[1] = {part[0] + part[1]};
+      lanes_total<kSub>(m2, me.size);
+      if (!kSub && me.size > 32) warps_total(m2, me.team + 1, me.size, me.warp, me.lane, slots + 4 * kSlots);
+      if (again) var = m2[0] * inv_c;
     }
-    float m2[1] = {part[0] + part[1]};
-    lanes_total<kSub>(m2, me.size);
-    if (!kSub && me.size > 32) warps_total(m2, me.team + 1, me.size, me.warp, me.lane, slots + kSlots + turn);
-    const float rs = __frsqrt_rn(fmaf(m2[0], inv_c, p.eps));
+    const float rs = __frsqrt_rn(var + p.eps), shift = (center - mu) * rs;
     if (me.lane == 0 && me.warp == 0 && live) {
       p.mean[row] = mu;
       p.rstd[row] = rs;
@@ -120,7 +130,7 @@ __global__ void __launch_bounds__(kThreads, 1) team_fwd_kernel(const RowParams p
         staged<V>(mine, k, 2, 1, b);
 #pragma unroll
         for (int j = 0; j < V; j += 2) {
-          mul2(x[k][j], x[k][j + 1], rs, rs);
+          fma2(x[k][j], x[k][j + 1], x[k][j], x[k][j + 1], rs, rs, shift, shift);
           fma2(x[k][j], x[k][j + 1], x[k][j], x[k][j + 1], g[j], g[j + 1], b[j], b[j + 1]);
         }
         if constexpr (kAct != HDQT_ACT_NONE) {
