@@ -446,14 +446,24 @@ hdqt_status_t run_fwd(RowParams p, bool wide, cudaStream_t s) {
         if (chunks <= 4096) return fwd_once<T, 4, kFused>(p, s);
       }
     }
-    // Elements per thread: many take less of the row's fixed work each, few leave more warps.  Without dropout 32 (fp32: 16): 16384 x 4096
-    // bf16 50.6 us against 54.6 with 16; with it 16 (fp32: 8): 91 against 97, but cut rows 32 (20000 x 1001 fp16: 40.6 against 46.2).
+    // Elements per thread (many take less of the row's fixed work each, few leave more warps) and threads of a block:
     int k = kMost, threads = 768;
-    if (kFused ? p.classes == 1 || sizeof(T) == 4 : sizeof(T) == 4) k = kFused && sizeof(T) == 4 ? kMost / 4 : kMost / 2;
-    // (8192 x 16384 bf16 134 us with 16, 140 with 32: one row at a time is all that an SM holds)
-    if (chunks > 1536 && p.classes == 1 && k > kMost / 2) k = kMost / 2;
-    // (65536 x 1024 bf16 with dropout: 88 us with 768 threads, 101 with 1024; 8192 x 8192: 121 and 98)
-    if (kFused && chunks >= 512) threads = 1024;
+    if (!kFused && sizeof(T) == 2) {
+      // 32: 16384 x 4096 bf16 45.3 us with 640 threads, 47.9 with 768; 32768 x 8192 (teams of 256) 185 and 165
+      if (chunks <= 640) threads = 640;
+    } else if (!kFused) {
+      // fp32: 8192 x 4096 45.4 us with 8, 51.3 with 16; 4096 x 16384 94 with 8, 90 with 32
+      if (chunks <= 2048) k = kMost / 4, threads = 1024;
+    } else if (sizeof(T) == 4) {
+      // fp32 with dropout: 8, 8192 x 4096 90 us with 640 threads, 101 with 1024
+      k = kMost / 4, threads = 640;
+    } else if (p.classes > 1) {
+      // cut rows with dropout: 20000 x 1001 fp16 37.6 us with 32, 44 with 16
+      threads = 640;
+    } else if (chunks <= 1024) {
+      // 16-bit with dropout: 16, 65536 x 1024 88 us with 640 threads, 97 with 768; 16384 x 4096 88 with 768, 93 with 1024; 8192 x 8192 91 with 1024
+      k = kMost / 2, threads = chunks <= 256 ? 640 : chunks <= 768 ? 768 : 1024;
+    }
     // Part of a warp per row, 8 elements per thread, or 16 where those are not mostly idle: 500000 x 64 bf16 25.0 us against 30.2, 200000 x 96 fp32 28.1 and 29.2;
     // with dropout and for cut rows 8 were faster.
     if constexpr (!kFused) {
@@ -464,9 +474,9 @@ hdqt_status_t run_fwd(RowParams p, bool wide, cudaStream_t s) {
     if (chunks <= 16 * (8 / V)) {
       if (fwd_teams<T, 8 / V, kFused, true>(p, 1024, &st, s)) return st;
     } else {
-      if ((k <= kMost / 4 || chunks <= 16 * (kMost / 2)) && fwd_teams<T, kMost / 4, kFused, false>(p, 1024, &st, s)) return st;
+      if ((k <= kMost / 4 || chunks <= 16 * (kMost / 2)) && fwd_teams<T, kMost / 4, kFused, false>(p, threads, &st, s)) return st;
       if ((k <= kMost / 2 || chunks <= 16 * kMost) && fwd_teams<T, kMost / 2, kFused, false>(p, threads, &st, s)) return st;
-      if (fwd_teams<T, kMost, kFused, false>(p, 768, &st, s)) return st;
+      if (fwd_teams<T, kMost, kFused, false>(p, threads, &st, s)) return st;
     }
   }
   p.classes = 1;

@@ -256,6 +256,34 @@ def test_large_mean_constant_rows_and_outliers():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("c", [7, 24, 64, 96, 600, 1001, 4096])
+def test_means_above_the_spread_among_others(c):
+    """Rows far from zero, constant ones, ones whose squares overflow and ordinary ones, in one call with more rows than blocks; the
+    bounds of the docstring hold for each, and no row's result depends on its neighbours."""
+    rows = max(3000, 12000000 // c // 8)
+    x, gamma, beta, dy = inputs((rows, c), "fp32", "fp32", seed=c)
+    plain = x.clone()
+    x[1::5] += 1000.0
+    x[2::5] = 3.0
+    x[3::15] = 3e19 + 1e17 * x[3::15]
+    x[4::15] *= 1e-25
+    want = reference(x, gamma, beta, "none", dy)
+    y, mean, rstd = hdqt.layer_norm_fwd(x, gamma, beta, EPS)
+    keep = torch.ones(rows, dtype=torch.bool, device="cuda")
+    keep[2::5] = False                          # (a constant row: the rounding of its mean over sqrt(eps), and no more)
+    for got, name in ((y, "y"), (mean, "mean"), (rstd, "rstd")):
+        close(got[keep], tuple(t[keep] for t in want[name]))
+    assert float((mean[2::5] - 3).abs().max()) <= 52 * E * 3
+    assert float((y[2::5] - beta).abs().max()) <= 1.5 * (52 * E * 3 * EPS ** -0.5 + E)
+    dx = hdqt.layer_norm_bwd(dy, x, gamma, beta, mean, rstd)[0]
+    close(dx[keep], tuple(t[keep] for t in want["dx"]))
+    y2, mean2, rstd2 = hdqt.layer_norm_fwd(plain, gamma, beta, EPS)
+    assert torch.equal(y[0::5], y2[0::5]) and torch.equal(mean[0::5], mean2[0::5]) and torch.equal(rstd[0::5], rstd2[0::5])
+    h = hdqt.dropout_add_layer_norm_fwd(x, None, gamma, beta, 0.0, 1, eps=EPS)
+    close(h[0][keep], tuple(t[keep] for t in want["y"]))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("c", [40, 2024, 4099, 16384])
 def test_mean_of_a_few_rows_that_nearly_cancel(c):
     """Summed in 64 bits and rounded once: e |mean|, and 2^-50 of the values' size for the 64-bit sum itself."""
