@@ -7,10 +7,10 @@ namespace {
 
 // ---- teams that walk over the rows ---------------------------------------------------------------------------
 //
-// One block per SM; per row and warp of 1024 elements about 380 instructions, of which 100 are paired arithmetic.  Bound by HBM where rows
-// are many: 32768 x 8192 bf16 196 us (5.5 TB/s), 8192 x 4096 fp32 46 us (5.8), 16384 x 4096 bf16 with dropout and residual 89 us (6.0);
-// by some 4 us of launch and first loads below a few MB (4096 x 2048 bf16 10.6 us).  What keeps the first from the copy's rate is the
-// latency of two sums per row with three rows at work per SM, and gamma and beta from shared memory (half of its traffic).
+// One block per SM.  Bound by HBM where rows are many: 32768 x 8192 bf16 165 us (6.5 TB/s), 8192 x 4096 fp32 46 us (5.9), 16384 x 4096 bf16
+// with dropout and residual 88 us (6.1); by some 4 us of launch and first loads below a few MB (4096 x 2048 bf16 9.9 us).  x and x^2 are
+// summed at once: one exchange over a team per row instead of two, one after the other (196 us); where a mean above the spread would
+// cost that its digits, the deviations are squared as well (test of both sides in the loop).
 
 template <typename T, int K, bool kFused, bool kShift, bool kSub, int kThreads>
 __global__ void __launch_bounds__(kThreads, 1) team_fwd_kernel(const RowParams p) {
