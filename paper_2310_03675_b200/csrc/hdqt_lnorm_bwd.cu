@@ -746,8 +746,8 @@ hdqt_status_t run_bwd(RowParams p, bool wide, bool few, bool params, int* parts,
       k = cheap && (chunks >= 512 || (chunks >= 96 && total >= 4000000)) ? kMost : kMost / 2;
       if (chunks >= 256 && cheap) threads = 512;
     }
-    // Part of a warp per row, 8 elements per thread, or 16 where those are not mostly idle: 500000 x 64 bf16 39.4 us against 43.3, 200000 x 96 fp32 43.5 and 44.2;
-    // with dropout and for cut rows 8 were faster.
+    // Part of a warp per row, 8 elements per thread, or 16 where those are not mostly idle: 500000 x 64 bf16 39.4 us against 43.3, 200000 x 96
+    // fp32 43.5 and 44.2; with dropout and for cut rows 8 were faster.
     if constexpr (!kFused) {
       if (p.classes == 1 && chunks >= (V == 8 ? 8 : 20) && chunks <= 16 * (16 / V) &&
           bwd_teams<T, 16 / V, false, true, false>(p, 512, parts, &st, s))

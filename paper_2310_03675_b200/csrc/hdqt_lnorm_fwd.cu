@@ -10,7 +10,7 @@ namespace {
 // One block per SM.  Bound by HBM where rows are many: 32768 x 8192 bf16 165 us (6.5 TB/s), 8192 x 4096 fp32 46 us (5.9), 16384 x 4096 bf16
 // with dropout and residual 88 us (6.1); by some 4 us of launch and first loads below a few MB (4096 x 2048 bf16 9.9 us).  x and x^2 are
 // summed at once: one exchange over a team per row instead of two, one after the other (196 us); where a mean above the spread would
-// cost that its digits, the deviations are squared as well (test of both sides in the loop).
+// cost that its digits, the deviations from it are squared as well.
 
 template <typename T, int K, bool kFused, bool kShift, bool kSub, int kThreads>
 __global__ void __launch_bounds__(kThreads, 1) team_fwd_kernel(const RowParams p) {
@@ -464,8 +464,8 @@ hdqt_status_t run_fwd(RowParams p, bool wide, cudaStream_t s) {
       // 16-bit with dropout: 16, 65536 x 1024 88 us with 640 threads, 97 with 768; 16384 x 4096 88 with 768, 93 with 1024; 8192 x 8192 91 with 1024
       k = kMost / 2, threads = chunks <= 256 ? 640 : chunks <= 768 ? 768 : 1024;
     }
-    // Part of a warp per row, 8 elements per thread, or 16 where those are not mostly idle: 500000 x 64 bf16 25.0 us against 30.2, 200000 x 96 fp32 28.1 and 29.2;
-    // with dropout and for cut rows 8 were faster.
+    // Part of a warp per row, 8 elements per thread, or 16 where those are not mostly idle: 500000 x 64 bf16 25.0 us against 30.2, 200000 x 96
+    // fp32 28.1 and 29.2; with dropout and for cut rows 8 were faster.
     if constexpr (!kFused) {
       if (p.classes == 1 && chunks >= (V == 8 ? 8 : 20) && chunks <= 16 * (16 / V) &&
           fwd_teams<T, 16 / V, false, true, false>(p, 1024, &st, s))

@@ -5,8 +5,9 @@
 //   dx = rs (gamma dz - mean(gamma dz) - xhat mean(gamma dz xhat)),  dgamma = sum dz xhat,  dbeta = sum dz
 //
 // Bound by HBM: every input read once, every output written once.  A "team" of threads (part of a warp up to a whole block) holds a
-// row, so that its mean and spread are taken over registers.  Three kinds of kernels: teams that walk over the rows (team_*), one row per block for few rows (once_*), and any_* for
-// strides and addresses that no 16-byte access fits; rows wider than registers are read again from the L2 (long_*).
+// row, so that its mean and spread are taken over registers.  Three kinds of kernels: teams that walk over the rows (team_*), one row
+// per block for few rows (once_*), and any_* for strides and addresses that no 16-byte access fits; rows wider than registers are
+// read again from the L2 (long_*).
 //
 // A row is cut at the 16-byte boundaries of memory into chunks of V elements.  Where the channels are not a multiple of V, rows of a
 // dense tensor start `lead` elements behind a boundary, lead = (row * channels) mod V, which repeats every `classes` rows.  A block
